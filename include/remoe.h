@@ -58,7 +58,8 @@ enum {
                                 the streams and events do not guarantee; see remoe_last_cuda_error() */
 };
 
-enum { REMOE_F32 = 0, REMOE_BF16 = 1, REMOE_FP8_E4M3 = 2, REMOE_INT4_G32 = 3 };
+enum { REMOE_F32 = 0, REMOE_BF16 = 1, REMOE_FP8_E4M3 = 2, REMOE_INT4_G32 = 3,
+       REMOE_F16 = 4 /* rows of logits only */ };
 enum { REMOE_POLICY_LRU = 0, REMOE_POLICY_FIFO = 1, REMOE_POLICY_LFU = 2 };
 
 /* Shape of the stack.  Sec. 3.1: N_r routed experts, Top-K; shared experts always active. */
@@ -327,6 +328,98 @@ int remoe_expert_ffn_static(int32_t hidden, int32_t weight_dtype, int32_t n_expe
                             const void* const* expert_blocks_dev, const int32_t* inter,
                             const float* scales, const float* hidden_in_dev, float* hidden_out_dev,
                             void* cuda_stream);
+
+/*
+ * Operators on rows of logits.  A decode step's hidden states end in rows of logits, a router's rows are logits over
+ * its experts, and the rerouting bonus, the low-precision stores and a fine-tuned router all move them: these calls say
+ * what the model answers (log probabilities, entropy, top alternatives), how far it has moved from a teacher
+ * (divergence from recorded top log probabilities) and give the gradients of both (the paper's objective, Eq. 3, is a
+ * cross-entropy plus an anchor to the frozen model).  The paper ships no such kernels; definitions are given here.
+ *
+ * Common to the four calls
+ *   - Stateless: no stack, no allocation, no workspace, nothing kept between calls, one kernel launch on `cuda_stream`; calls
+ *     on any streams may overlap, and a call may be captured into a CUDA graph.  Results are bit-for-bit the same on
+ *     every run.  The first capture on a device should follow one plain call there (kernels are loaded lazily).
+ *   - Rows: logits_dev holds n_rows rows of `vocab` elements, `row_stride` elements apart (>= vocab; a row may start at any
+ *     element address, 16-byte aligned rows are fastest).  dtype REMOE_F32, REMOE_BF16 or REMOE_F16.  Everything is computed in
+ *     float32 or wider and rounded once.  1 <= vocab <= REMOE_ROWS_MAX_VOCAB; n_rows = 0 does nothing.  p below is
+ *     softmax(inv_temperature * row), inv_temperature finite and > 0.
+ *   - The device is the one that logits_dev lies on (it need not be current; the stream and all other pointers belong to it).
+ *   - -inf is a masked element (probability 0, gradient 0).  A row of -inf alone has no distribution: its log probabilities
+ *     are -inf, its entropy, losses and gradients 0.  The type's lowest value is an ordinary value (a row of it is
+ *     uniform).  A row that holds a NaN or +inf gives NaN wherever its values enter.
+ *   - A gradient may be written in place (d_logits_dev == logits_dev with the same stride); other overlap of outputs with
+ *     inputs or one another is not allowed.  What lies between rows is left as it was.
+ *   Errors: ARG (null or misaligned pointers, sizes, strides, rows in host memory), UNSUPPORTED (FP8 or 4-bit rows, vocab or
+ *   top_k beyond the limits below, more blocks than a grid holds), CUDA.
+ */
+#define REMOE_ROWS_MAX_VOCAB 1048576
+#define REMOE_ROWS_MAX_TOP 256
+
+/*
+ * Log probabilities of given tokens, entropy and top alternatives.
+ *   tokens       [n_rows] int32 or NULL; -1 = the row has no token (its log probability reads 0)
+ *   logprob      [n_rows] float32 or NULL: ln p_token.  Exact also where p is nearly one.  A token outside [0, vocab)
+ *                other than -1 gives NaN.
+ *   entropy      [n_rows] float32 or NULL: -sum p ln p
+ *   top_ids      [n_rows, top_k] int32, top_logprob [n_rows, top_k] float32: the top_k <= min(vocab, REMOE_ROWS_MAX_TOP) largest by
+ *                descending logit, equal logits by ascending id (-0 equals +0).  top_k = 0: both may be NULL.  A row with a
+ *                NaN or +inf reads -1 and NaN.
+ *   row_stats    [n_rows, 4] float32 or NULL, kept for the backward call: largest logit m, ln Z = ln sum exp(inv_temperature *
+ *                (x - m)), entropy, log probability (so the row's log-sum-exp is inv_temperature * m + ln Z)
+ */
+int remoe_token_logprobs(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits_dev, int64_t row_stride,
+                         float inv_temperature, const int32_t* tokens_dev, int32_t top_k, float* logprob_dev,
+                         float* entropy_dev, int32_t* top_ids_dev, float* top_logprob_dev, float* row_stats_dev,
+                         void* cuda_stream);
+
+/*
+ * Gradient of sum_t grad_logprob[t] * logprob[t] + grad_entropy[t] * entropy[t] with respect to the logits, from the same
+ * logits, tokens and temperature and the row_stats of the forward call.  Either of grad_logprob and grad_entropy ([n_rows]
+ * float32) may be NULL (= 0).  A row whose two gradients are 0 (grad_logprob counts as 0 where the token is -1) is
+ * not read: its gradient is 0 whatever it holds.  top_logprob carries no gradient.
+ *   d_logits     [n_rows, vocab] of dtype, rows d_row_stride elements apart
+ */
+int remoe_token_logprobs_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits_dev,
+                                  int64_t row_stride, float inv_temperature, const int32_t* tokens_dev,
+                                  const float* row_stats_dev, const float* grad_logprob_dev,
+                                  const float* grad_entropy_dev, void* d_logits_dev, int64_t d_row_stride,
+                                  void* cuda_stream);
+
+/*
+ * Divergence from a teacher that is known by its top log probabilities (top_ids and top_logprob of
+ * remoe_token_logprobs, taken at the same temperature), and its gradient in the same call where it is asked for.
+ *   teacher_ids       [n_rows, n_top] int32, 1 <= n_top <= min(vocab, REMOE_ROWS_MAX_TOP); -1 = unused entry.  An id may occur
+ *                     more than once: each entry adds its own term, the element's q is their sum.
+ *   teacher_logprobs  [n_rows, n_top] float32, < +inf; -inf = probability 0
+ *   tail = 0:  q = softmax of the row's values (any shift), loss = sum q (ln q - ln p) over the list
+ *   tail = 1:  q = exp of the values, and all that is not listed is one more class: with q_r = max(0, 1 - sum q) and p_r = the
+ *              student's probability outside the list, loss gains q_r (ln q_r - ln p_r).  The term is left out where the student has
+ *              no live element outside the list.
+ *   row_weight        [n_rows] float32 or NULL (= 1): weight of the row in the gradient (not in loss).  0 leaves the row out: it is
+ *                     not looked at, loss and gradient are 0 (padding of a batch).
+ *   loss              [n_rows] float32 or NULL; 0 for rows without a usable entry and rows of -inf alone; +inf where the student
+ *                     masks a token that the teacher allows (the gradient stays finite)
+ *   row_stats         [n_rows, 8] float32 or NULL, for the backward call: m, ln Z (as above), the same two of the elements outside the
+ *                     list, p_r - q_r, ln of the list's sum (tail = 0), 1 if the row takes part, unused
+ *   d_logits          [n_rows, vocab] of dtype or NULL: gradient of sum_t row_weight[t] * loss[t]
+ * A row with an id outside [-1, vocab), or a NaN or +inf among its values, gives NaN.
+ */
+int remoe_distill_topk(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits_dev, int64_t row_stride,
+                       float inv_temperature, int32_t n_top, const int32_t* teacher_ids_dev,
+                       const float* teacher_logprobs_dev, int32_t tail, const float* row_weight_dev, float* loss_dev,
+                       float* row_stats_dev, void* d_logits_dev, int64_t d_row_stride, void* cuda_stream);
+
+/*
+ * The gradient alone, of sum_t grad_loss[t] * loss[t], from the row_stats of a forward call with the same logits, list and
+ * temperature: for losses whose weight is known only after the forward pass.  With weights known before, one
+ * call of remoe_distill_topk with d_logits reads the logits once less.  grad_loss [n_rows] float32; 0 leaves the row out.
+ */
+int remoe_distill_topk_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits_dev,
+                                int64_t row_stride, float inv_temperature, int32_t n_top,
+                                const int32_t* teacher_ids_dev, const float* teacher_logprobs_dev,
+                                const float* row_stats_dev, const float* grad_loss_dev, void* d_logits_dev,
+                                int64_t d_row_stride, void* cuda_stream);
 
 /* Text of the last CUDA runtime error, or of the last device-flag / trace-validation failure,
  * seen by this stack ("" if none). */

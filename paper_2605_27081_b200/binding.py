@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(_PKG, "libremoe.so")
 REMOE_OK = 0
 REMOE_E_ARG, REMOE_E_CAPACITY, REMOE_E_NOT_LOADED, REMOE_E_NOT_PINNED = -1, -2, -3, -4
 REMOE_E_CUDA, REMOE_E_DEVICE_FLAG, REMOE_E_UNSUPPORTED, REMOE_E_NOMEM, REMOE_E_ORDER = -5, -6, -7, -8, -9
-REMOE_F32, REMOE_BF16, REMOE_FP8_E4M3, REMOE_INT4_G32 = 0, 1, 2, 3
+REMOE_F32, REMOE_BF16, REMOE_FP8_E4M3, REMOE_INT4_G32, REMOE_F16 = 0, 1, 2, 3, 4
+REMOE_ROWS_MAX_VOCAB, REMOE_ROWS_MAX_TOP = 1048576, 256
 REMOE_POLICY_LRU, REMOE_POLICY_FIFO, REMOE_POLICY_LFU = 0, 1, 2
 
 EXPORTS = [
@@ -27,6 +28,7 @@ EXPORTS = [
     "remoe_set_profiling", "remoe_kernel_time", "remoe_launch_count", "remoe_last_cuda_error", "remoe_stack_destroy",
     "remoe_strerror", "remoe_expert_ffn_static", "remoe_reuse_mass", "remoe_step_history", "remoe_tpot_proxy", "remoe_decode_step_chained",
     "remoe_expert_load", "remoe_decode_steps", "remoe_order_check_counts", "remoe_cache_snapshot",
+    "remoe_token_logprobs", "remoe_token_logprobs_backward", "remoe_distill_topk", "remoe_distill_topk_backward",
 ]
 
 
@@ -81,6 +83,11 @@ def lib():
         L.remoe_order_check_counts.argtypes = [vp, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)]
         L.remoe_expert_ffn_static.argtypes = [i32, i32, i32, C.POINTER(vp), C.POINTER(i32), C.POINTER(C.c_float),
                                               vp, vp, vp]
+        i64, f32 = C.c_int64, C.c_float
+        L.remoe_token_logprobs.argtypes = [i32, i32, i32, vp, i64, f32, i32p, i32, f32p, f32p, i32p, f32p, f32p, vp]
+        L.remoe_token_logprobs_backward.argtypes = [i32, i32, i32, vp, i64, f32, i32p, f32p, f32p, f32p, vp, i64, vp]
+        L.remoe_distill_topk.argtypes = [i32, i32, i32, vp, i64, f32, i32, i32p, f32p, i32, f32p, f32p, f32p, vp, i64, vp]
+        L.remoe_distill_topk_backward.argtypes = [i32, i32, i32, vp, i64, f32, i32, i32p, f32p, f32p, f32p, vp, i64, vp]
         L.remoe_reuse_mass.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(C.c_uint64), vp]
         L.remoe_step_history.argtypes = [vp, i32, i32, vp, vp, C.POINTER(i32)]
         L.remoe_expert_load.argtypes = [vp, i32, vp, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(i32)]
@@ -227,6 +234,36 @@ def remoe_expert_ffn_static(hidden, weight_dtype, expert_blocks_dev, inter, scal
     scales_a = (C.c_float * n)(*[float(x) for x in scales])
     return lib().remoe_expert_ffn_static(int(hidden), int(weight_dtype), n, ptrs, inter_a, scales_a,
                                          _ptr(hidden_in), _ptr(hidden_out), cuda_stream)
+
+
+# Rows of logits: device tensors or addresses, outputs allocated by the caller, None where the C entry takes NULL.
+
+def remoe_token_logprobs(n_rows, vocab, dtype, logits, row_stride, inv_temperature, tokens, top_k, logprob, entropy,
+                         top_ids, top_logprob, row_stats, cuda_stream=None):
+    return lib().remoe_token_logprobs(n_rows, vocab, dtype, _ptr(logits), row_stride, inv_temperature, _ptr(tokens), top_k,
+                                      _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprob), _ptr(row_stats),
+                                      cuda_stream)
+
+
+def remoe_token_logprobs_backward(n_rows, vocab, dtype, logits, row_stride, inv_temperature, tokens, row_stats,
+                                  grad_logprob, grad_entropy, d_logits, d_row_stride, cuda_stream=None):
+    return lib().remoe_token_logprobs_backward(n_rows, vocab, dtype, _ptr(logits), row_stride, inv_temperature, _ptr(tokens),
+                                               _ptr(row_stats), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(d_logits),
+                                               d_row_stride, cuda_stream)
+
+
+def remoe_distill_topk(n_rows, vocab, dtype, logits, row_stride, inv_temperature, n_top, teacher_ids, teacher_logprobs,
+                       tail, row_weight, loss, row_stats, d_logits, d_row_stride, cuda_stream=None):
+    return lib().remoe_distill_topk(n_rows, vocab, dtype, _ptr(logits), row_stride, inv_temperature, n_top, _ptr(teacher_ids),
+                                    _ptr(teacher_logprobs), int(tail), _ptr(row_weight), _ptr(loss), _ptr(row_stats),
+                                    _ptr(d_logits), d_row_stride, cuda_stream)
+
+
+def remoe_distill_topk_backward(n_rows, vocab, dtype, logits, row_stride, inv_temperature, n_top, teacher_ids,
+                                teacher_logprobs, row_stats, grad_loss, d_logits, d_row_stride, cuda_stream=None):
+    return lib().remoe_distill_topk_backward(n_rows, vocab, dtype, _ptr(logits), row_stride, inv_temperature, n_top,
+                                             _ptr(teacher_ids), _ptr(teacher_logprobs), _ptr(row_stats), _ptr(grad_loss),
+                                             _ptr(d_logits), d_row_stride, cuda_stream)
 
 
 def remoe_reuse_mass(h, layer=-1, last_mass=None):

@@ -1,0 +1,394 @@
+// Shared parts of the operators on rows of logits (token_logprobs.cu, distill.cu): how a row is cut into units, the
+// one-pass softmax sums of a row, and their joins within a block and across a cluster.
+//
+// Units.  A row of V elements starts `pad` elements behind a 16-byte boundary.  It is cut into units of eight
+// elements that start on such boundaries; position p = id + pad of an element gives its unit p / 8.  All units but the
+// first (pad > 0) and the last (ragged) are loaded and stored with 16-byte instructions; those two go element by
+// element, so nothing outside the row is touched whatever its length, address and stride.
+//
+// Sums.  With m the largest logit and c = log2(e) / temperature, a row's state is
+//   m,  R = sum of 2^((x - m) c) over all elements but one that equals m,  U = sum of (x - m) c 2^((x - m) c),
+// so Z = 1 + R, ln Z = log1p(R) and the entropy is ln Z - ln 2 U / Z.  Leaving the largest element out of R keeps
+// ln Z exact where one token has nearly all of the mass (R = 1e-7 would be lost in a sum that starts at one).
+// A thread keeps its largest element M apart: every element meets M in a max/min pair, the larger stays M and the
+// smaller goes into the sum.  The sum is taken relative to a reference, an earlier M, that moves only when M has
+// risen 2^40 above it; a running maximum would cost a branch in nearly every step of a warp.
+// Differences are taken before the scaling: rows of the type's lowest value stay uniform, none becomes inf - inf.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+namespace remoe {
+namespace rows {
+
+constexpr float kInf = HUGE_VALF;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+__device__ __forceinline__ float nan_value() { return __int_as_float(0x7fffffff); }
+constexpr float kReferenceRise = 40.f;      // log2 of how far a thread's sum may grow above its reference's one
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float y;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// Two float32 in one 64-bit register for the packed instructions of sm_100.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pack2(float lo, float hi) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+// ---- element types -------------------------------------------------------------------------------------------
+// Four words of two elements each; float32 words are the packed pairs above.
+template <typename T>
+struct Elem;
+
+template <>
+struct Elem<float> {
+  typedef f2 Word;
+  static constexpr int kUnusedBits = 0;       // low bits of the value as a float32 that are always zero
+  static __device__ __forceinline__ Word lowest() { return pack2(-kInf, -kInf); }
+  static __device__ __forceinline__ f2 widen(Word w) { return w; }
+  static __device__ __forceinline__ Word narrow(f2 v) { return v; }
+  static __device__ __forceinline__ void order(Word& hi, Word& lo) {   // hi, lo = max, min per half; NaN goes to both
+    float a0, a1, b0, b1;
+    unpack2(hi, a0, a1);
+    unpack2(lo, b0, b1);
+    hi = pack2(max_nan(a0, b0), max_nan(a1, b1));
+    lo = pack2(min_nan(a0, b0), min_nan(a1, b1));
+  }
+  static __device__ __forceinline__ float get(const float* p) { return *p; }
+  static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
+};
+
+template <>
+struct Elem<__nv_bfloat16> {
+  typedef uint32_t Word;
+  static constexpr int kUnusedBits = 16;
+  static __device__ __forceinline__ Word lowest() { return 0xff80ff80u; }
+  static __device__ __forceinline__ f2 widen(Word w) { return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+  static __device__ __forceinline__ Word narrow(f2 v) {
+    float lo, hi;
+    unpack2(v, lo, hi);
+    Word w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    return w;
+  }
+  static __device__ __forceinline__ void order(Word& hi, Word& lo) {
+    Word a;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(hi), "r"(lo));
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(hi), "r"(lo));
+    hi = a;
+  }
+  static __device__ __forceinline__ float get(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+  static __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+};
+
+template <>
+struct Elem<__half> {
+  typedef uint32_t Word;
+  static constexpr int kUnusedBits = 13;
+  static __device__ __forceinline__ Word lowest() { return 0xfc00fc00u; }
+  static __device__ __forceinline__ f2 widen(Word w) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return pack2(v.x, v.y);
+  }
+  static __device__ __forceinline__ Word narrow(f2 v) {
+    float lo, hi;
+    unpack2(v, lo, hi);
+    Word w;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(hi), "f"(lo));
+    return w;
+  }
+  static __device__ __forceinline__ void order(Word& hi, Word& lo) {
+    Word a;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(a) : "r"(hi), "r"(lo));
+    asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(hi), "r"(lo));
+    hi = a;
+  }
+  static __device__ __forceinline__ float get(const __half* p) { return __half2float(*p); }
+  static __device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
+};
+
+// ---- units ---------------------------------------------------------------------------------------------------
+
+template <typename T>
+struct Unit {
+  typename Elem<T>::Word w[4];
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(Elem<T>::widen(w[i]), v[2 * i], v[2 * i + 1]);
+  }
+  __device__ __forceinline__ void set(const float (&v)[8]) {   // values that came from the type: no rounding
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = Elem<T>::narrow(pack2(v[2 * i], v[2 * i + 1]));
+  }
+};
+
+// Elements between the 16-byte boundary at or before `row` and `row`.
+template <typename T>
+__host__ __device__ __forceinline__ int row_pad(const T* row) { return (int)((reinterpret_cast<uintptr_t>(row) & 15u) / sizeof(T)); }
+
+// p: 16-byte aligned, eight elements of the row.  Loads bypass L1: a row is read once or twice, the second time
+// long after the first.
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store16(void* p, const uint4& v) {
+  asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void load_unit(const T* p, Unit<T>& u) {
+  const uint4 v = load16(p);
+  u.w[0] = v.x; u.w[1] = v.y; u.w[2] = v.z; u.w[3] = v.w;
+}
+template <>
+__device__ __forceinline__ void load_unit<float>(const float* p, Unit<float>& u) {
+  const uint4 a = load16(p), b = load16(p + 4);
+  u.w[0] = pack2(__uint_as_float(a.x), __uint_as_float(a.y));
+  u.w[1] = pack2(__uint_as_float(a.z), __uint_as_float(a.w));
+  u.w[2] = pack2(__uint_as_float(b.x), __uint_as_float(b.y));
+  u.w[3] = pack2(__uint_as_float(b.z), __uint_as_float(b.w));
+}
+template <typename T>
+__device__ __forceinline__ void store_unit(T* p, const Unit<T>& u) {
+  store16(p, make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
+}
+template <>
+__device__ __forceinline__ void store_unit<float>(float* p, const Unit<float>& u) {
+  float v[8];
+  u.values(v);
+  store16(p, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+  store16(p + 4, make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])));
+}
+
+// Unit u of a row, element by element; what lies outside the row reads as -inf and is not stored.
+template <typename T>
+__device__ __forceinline__ void load_ragged(const T* row, int V, int pad, int u, Unit<T>& out) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int id = 8 * u + j - pad;
+    v[j] = id >= 0 && id < V ? Elem<T>::get(row + id) : -kInf;
+  }
+  out.set(v);
+}
+template <typename T>
+__device__ __forceinline__ void store_ragged(T* row, int V, int pad, int u, const Unit<T>& in) {
+  float v[8];
+  in.values(v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int id = 8 * u + j - pad;
+    if (id >= 0 && id < V) Elem<T>::put(row + id, v[j]);
+  }
+}
+
+// The units [first, last) of a row that one block works on; [full0, full1) of them are whole and aligned.
+struct Slice {
+  int pad, first, last, full0, full1;
+  __device__ __forceinline__ Slice(int V, int pad_, int part, int parts) : pad(pad_) {
+    const int units = (V + pad + 7) >> 3, per = (units + parts - 1) / parts;
+    first = min(part * per, units);
+    last = min(first + per, units);
+    full0 = max(first, pad > 0 ? 1 : 0);
+    full1 = min(last, (V + pad) >> 3);
+  }
+  // The i-th ragged unit of the slice (at most two), or -1.
+  __device__ __forceinline__ int ragged(int i) const {
+    const int head = first < last && first < full0 ? first : -1;
+    const int tail = last > first && last - 1 >= full1 && last - 1 != head ? last - 1 : -1;
+    return i == 0 ? head : tail;
+  }
+  __device__ __forceinline__ int length(int V) const { return max(0, min(V, 8 * last - pad) - max(0, 8 * first - pad)); }   // elements
+  __device__ __forceinline__ bool holds(int id) const { const int u = (id + pad) >> 3; return u >= first && u < last; }
+};
+
+// ---- one-pass sums -------------------------------------------------------------------------------------------
+
+struct State {
+  float m, R, U;     // m = -inf: no live element; R = NaN: the row holds a NaN or +inf
+};
+
+__device__ __forceinline__ State merge(const State& a, const State& b, float c) {
+  const bool swap = b.m > a.m;
+  const State h = swap ? b : a, l = swap ? a : b;
+  if (l.m == -kInf) return h;
+  const float d = (l.m - h.m) * c, r = ex2(d);
+  State s;
+  s.m = h.m;
+  s.R = h.R + (1.f + l.R) * r;
+  s.U = h.U + r * l.U + (r == 0.f ? 0.f : r * d * (1.f + l.R));
+  return s;
+}
+
+// One thread's running sums over the units it is given.
+template <typename T>
+struct Stream {
+  typename Elem<T>::Word M;
+  float ref, limit, c;
+  f2 R, U;
+  __device__ __forceinline__ explicit Stream(float c_) : M(Elem<T>::lowest()), ref(0.f), limit(-kInf), c(c_), R(0), U(0) {}
+
+  template <int N>
+  __device__ __forceinline__ void add(Unit<T> (&u)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) Elem<T>::order(M, u[i].w[j]);
+    float m0, m1;
+    unpack2(Elem<T>::widen(M), m0, m1);
+    const float m = fmaxf(m0, m1);
+    if (m > limit) {                                   // the first live element, or far above the reference
+      if (limit > -kInf) {
+        const float d = (ref - m) * c, r = ex2(d);
+        const f2 r2 = pack2(r, r);
+        if (r > 0.f) U = mul2(r2, fma2(R, pack2(d, d), U));
+        else U = 0;
+        R = mul2(R, r2);
+      }
+      ref = m;
+      limit = m + kReferenceRise / c;
+    }
+    const f2 nref = pack2(-ref, -ref), cc = pack2(c, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f2 d = mul2(add2(Elem<T>::widen(u[i].w[j]), nref), cc);
+        float d0, d1;
+        unpack2(d, d0, d1);
+        const f2 e = pack2(ex2(d0), ex2(d1));
+        R = add2(R, e);
+        // -inf would give 0 * inf; 2^-200 is 0 in float32 already
+        U = fma2(e, pack2(max_nan(d0, -200.f), max_nan(d1, -200.f)), U);
+      }
+  }
+
+  // Largest element seen (-inf if none; NaN if there was one).
+  __device__ __forceinline__ float top() const {
+    float a, b;
+    unpack2(Elem<T>::widen(M), a, b);
+    return max_nan(a, b);
+  }
+
+  __device__ __forceinline__ State finish() const {
+    float a, b, r0, r1, u0, u1;
+    unpack2(Elem<T>::widen(M), a, b);
+    unpack2(R, r0, r1);
+    unpack2(U, u0, u1);
+    const float hi = max_nan(a, b), lo = min_nan(a, b);
+    if (hi == -kInf) return State{hi, 0.f, 0.f};
+    if (!(hi < kInf)) return State{0.f, nan_value(), nan_value()};
+    const float dl = (lo - hi) * c, el = ex2(dl);       // the smaller half's largest is an element of the sum like others
+    const float d = (ref - hi) * c, r = ex2(d);
+    State s;
+    s.m = hi;
+    s.R = (r0 + r1) * r + el;
+    s.U = r * (u0 + u1) + r * d * (r0 + r1) + (el == 0.f ? 0.f : el * dl);
+    return s;
+  }
+};
+
+__device__ __forceinline__ State shuffle_down(const State& s, int by, int width) {
+  return State{__shfl_down_sync(0xffffffffu, s.m, by, width), __shfl_down_sync(0xffffffffu, s.R, by, width),
+               __shfl_down_sync(0xffffffffu, s.U, by, width)};
+}
+
+// Joins the threads' states in a fixed order; the result is in *out (shared memory) after a __syncthreads().
+template <int NT>
+__device__ __forceinline__ void join_block(State s, float c, State* per_warp, State* out) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s = merge(s, shuffle_down(s, o, 32), c);
+  if ((threadIdx.x & 31) == 0) per_warp[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    constexpr int W = NT / 32;
+    s = threadIdx.x < W ? per_warp[threadIdx.x] : State{-kInf, 0.f, 0.f};
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+      if (o < W) s = merge(s, shuffle_down(s, o, 32), c);
+    if (threadIdx.x == 0) *out = s;
+  }
+}
+
+// ---- clusters --------------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ unsigned cluster_rank() {
+  unsigned r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Address of this block's shared variable `p` as it is in block `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote_shared(const void* p, unsigned rank) {
+  uint32_t a = (uint32_t)__cvta_generic_to_shared(p), r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float load_remote(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long load_remote64(uint32_t a) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+  return v;
+}
+// State of all blocks of the cluster, joined in rank order (the same in every block).  Call behind cluster_sync().
+__device__ __forceinline__ State join_cluster(const State* mine, int parts, float c) {
+  State s{-kInf, 0.f, 0.f};
+  for (int i = 0; i < parts; ++i) {
+    const State o{load_remote(remote_shared(&mine->m, i)), load_remote(remote_shared(&mine->R, i)), load_remote(remote_shared(&mine->U, i))};
+    s = merge(s, o, c);
+  }
+  return s;
+}
+
+// Whole number in the order of the values (NaN aside); -0 equals +0.
+__device__ __forceinline__ uint32_t order_key(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+
+}  // namespace rows
+}  // namespace remoe

@@ -1,0 +1,91 @@
+// Host side shared by the operators on rows of logits: argument checks, the device of a call, launches.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <cmath>
+
+#include "remoe.h"
+
+namespace remoe {
+namespace rows {
+
+// Makes the device of `ptr` current for the call and puts the caller's back; err_code() tells a pointer that is no
+// device memory (REMOE_E_ARG) from a failing runtime call (REMOE_E_CUDA).
+class PointerDevice {
+ public:
+  explicit PointerDevice(const void* ptr) {
+    cudaPointerAttributes at;
+    if (cudaPointerGetAttributes(&at, ptr) != cudaSuccess) {
+      cudaGetLastError();
+      code_ = REMOE_E_CUDA;
+      return;
+    }
+    if (at.type != cudaMemoryTypeDevice && at.type != cudaMemoryTypeManaged) {
+      code_ = REMOE_E_ARG;
+      return;
+    }
+    if (cudaGetDevice(&prev_) != cudaSuccess) { code_ = REMOE_E_CUDA; return; }
+    device_ = at.device;
+    if (prev_ != device_) {
+      if (cudaSetDevice(device_) != cudaSuccess) { code_ = REMOE_E_CUDA; return; }
+      switched_ = true;
+    }
+  }
+  ~PointerDevice() {
+    if (switched_) cudaSetDevice(prev_);
+  }
+  PointerDevice(const PointerDevice&) = delete;
+  PointerDevice& operator=(const PointerDevice&) = delete;
+  int err_code() const { return code_; }
+
+ private:
+  int prev_ = -1, device_ = -1, code_ = REMOE_OK;
+  bool switched_ = false;
+};
+
+inline int element_size(int32_t dtype) { return dtype == REMOE_F32 ? 4 : dtype == REMOE_BF16 || dtype == REMOE_F16 ? 2 : 0; }
+inline bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
+
+// More blocks than a grid holds (cudaErrorInvalidConfiguration) is a shape that the kernels are not built for.
+inline int status(cudaError_t e) { return e == cudaSuccess ? REMOE_OK : e == cudaErrorInvalidConfiguration ? REMOE_E_UNSUPPORTED : REMOE_E_CUDA; }
+
+// What every operator asks of its rows.
+inline int check_rows(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits, int64_t row_stride, float inv_temperature) {
+  if (n_rows < 0 || vocab < 1 || !logits) return REMOE_E_ARG;
+  if (dtype == REMOE_FP8_E4M3 || dtype == REMOE_INT4_G32) return REMOE_E_UNSUPPORTED;
+  if (!element_size(dtype)) return REMOE_E_ARG;
+  if (vocab > REMOE_ROWS_MAX_VOCAB) return REMOE_E_UNSUPPORTED;
+  if (row_stride < vocab && n_rows > 1) return REMOE_E_ARG;
+  if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature)) return REMOE_E_ARG;
+  if (misaligned(logits, element_size(dtype))) return REMOE_E_ARG;
+  return REMOE_OK;
+}
+
+// Blocks that share a row.  With fewer rows than keep the GPU's memory busy (two blocks an SM), a row is cut into up to
+// eight parts of at least `least` units, one part per block of a cluster.
+inline int parts_of_row(int32_t n_rows, int32_t vocab, int least) {
+  int parts = 1;
+  while (parts < 8 && (int64_t)n_rows * parts < 296 && (vocab / 8) / (2 * parts) >= least) parts *= 2;
+  return parts;
+}
+
+template <typename Kernel, typename Args>
+inline cudaError_t launch_rows(Kernel kernel, int32_t n_rows, int parts, int threads, size_t smem, cudaStream_t stream, const Args& args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)n_rows * (unsigned)parts);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)parts;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+
+}  // namespace rows
+}  // namespace remoe
