@@ -353,7 +353,7 @@ int remoe_expert_ffn_static(int32_t hidden, int32_t weight_dtype, int32_t n_expe
  *   Errors: ARG (null or misaligned pointers, sizes, strides, rows in host memory), UNSUPPORTED (FP8 or 4-bit rows, vocab or
  *   top_k beyond the limits below, more blocks than a grid holds), CUDA.
  */
-#define REMOE_ROWS_MAX_VOCAB 1048576
+#define REMOE_ROWS_MAX_VOCAB 393216
 #define REMOE_ROWS_MAX_TOP 256
 
 /*

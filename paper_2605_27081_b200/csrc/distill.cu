@@ -22,7 +22,7 @@ struct DistillArgs {
   const void* logits;
   void* d_logits;
   int64_t stride, d_stride;
-  int V, n_rows, parts, K, tail;
+  int V, n_rows, parts, slice_bytes, K, tail;
   float s;
   const int32_t* ids;
   const float *y, *weight;
@@ -30,39 +30,24 @@ struct DistillArgs {
   const float* stats_in;
 };
 
-__device__ __forceinline__ double warp_sum(double v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// What the gradient of a row needs.
-struct RowGrad {
-  float m_rest, coef;        // outside the list: coef * 2^((x - m_rest) c)
-  float m;
-  double ln_z, ln_q, weight; // in the list: weight * (e^{(x - m) s - ln_z} - e^{y - ln_q})
-  int kind;                  // 0: left out (zeros), 1: takes part
+// What the block shares of a row between its two passes.
+struct RowShared {
+  float m_rest, coef;              // outside the list: coef * 2^((x - m_rest) c)
+  double of_e, of_q, weight;       // in the list: weight * (of_e * e - of_q * q)
+  int kind;                        // 0: left out (zeros), 1: takes part
 };
 
-struct EntryShared {
-  int id[kMaxList];          // -1: unused entry
-  float y[kMaxList];
-  float x[kMaxList];
-  int first[kMaxList];       // no entry before it has its id
-  int bad, twice;
-  RowGrad g;
-};
-
-// Gradient at entry k, for the first entry of its id: the list's probabilities of that id summed in order.
-__device__ __forceinline__ float entry_gradient(const RowGrad& g, double s, const int* id, const float* y, int K, int k, float x, bool twice) {
+// Gradient in the list from the row_stats: weight * (e^{(x - m) s - ln Z} - sum of e^{y - ln Q} over the entries of its id, in order).
+__device__ __forceinline__ float entry_gradient(float m, float ln_z, float ln_q, double s, double weight, const int* id, const float* y, int K, int k,
+                                                float x, bool twice) {
   double q = 0.0;
   if (twice) {
     for (int j = k; j < K; ++j)
-      if (id[j] == id[k]) q += exp((double)y[j] - g.ln_q);
+      if (id[j] == id[k]) q += exp((double)y[j] - ln_q);
   } else {
-    q = exp((double)y[k] - g.ln_q);
+    q = exp((double)y[k] - ln_q);
   }
-  return (float)(g.weight * (exp(((double)x - g.m) * s - g.ln_z) - q));
+  return (float)(weight * (exp(((double)x - m) * s - ln_z) - q));
 }
 
 // Gradient outside the list, of one unit.
@@ -78,214 +63,232 @@ __device__ __forceinline__ void rest_grad_unit(Unit<T>& q, float m, float c, flo
   }
 }
 
+// Elements [e0, e1) of a row that lies at any address: whole units in one store each, the ends element by element.
+template <typename T, typename F>
+__device__ __forceinline__ void write_elements(T* out, int e0, int e1, int n_threads, F value) {
+  const int pad = row_pad(out), u0 = (e0 + pad + 7) >> 3, u1 = (e1 + pad) >> 3, tid = threadIdx.x;
+  for (int u = u0 + tid; u < u1; u += n_threads) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = value(8 * u + j - pad);
+    Unit<T> q;
+    q.set(v);
+    store_unit(out - pad + 8 * (int64_t)u, q);
+  }
+  const int head = min(8 * u0 - pad, e1), tail = max(8 * u1 - pad, head);
+  if (tid < 8) {
+    if (e0 + tid < head) Elem<T>::put(out + e0 + tid, value(e0 + tid));
+  } else if (tid < 16) {
+    const int i = tail + tid - 8;
+    if (i < e1) Elem<T>::put(out + i, value(i));
+  }
+}
+
 template <typename T>
 __device__ __forceinline__ void fill_unit(Unit<T>& q, float x) {
   const float v[8] = {x, x, x, x, x, x, x, x};
   q.set(v);
 }
 
-// One row per cluster of `parts` blocks.
+struct ListSums {
+  double z, q, qy, qx;             // sum over the list of e^{(x - m_list) s} (each id once), q, q (y - shift), q (x - m_list) s
+};
+__device__ __forceinline__ ListSums warp_sum(ListSums v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    v.z += __shfl_xor_sync(0xffffffffu, v.z, o);
+    v.q += __shfl_xor_sync(0xffffffffu, v.q, o);
+    v.qy += __shfl_xor_sync(0xffffffffu, v.qy, o);
+    v.qx += __shfl_xor_sync(0xffffffffu, v.qx, o);
+  }
+  return v;
+}
+
+// One row per cluster of `parts` blocks, each block's slice of it in shared memory; at most one entry of the list a thread.
+//
+// While the slice is on its way, the list's side is computed: a few numbers, in 64 bits, since the loss is a small
+// difference of large terms.  Its sums are taken relative to the list's own largest element, so they wait for nothing.
+// Then the list's elements are taken out of the slice (set to -inf where they lie in shared memory), the rest is summed in one
+// pass, blocks and list are joined, and the gradient is computed from the slice and written.
 template <typename T, int NT, bool GRAD>
-__global__ void __launch_bounds__(NT) distill_rows_kernel(const __grid_constant__ DistillArgs a) {
-  __shared__ State per_warp[NT / 32];
+__global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __grid_constant__ DistillArgs a) {
+  constexpr int W = NT / 32;
+  __shared__ State per_warp[W];
   __shared__ State mine;
-  __shared__ EntryShared en;
-  extern __shared__ __align__(16) unsigned listed_words[];     // one byte per unit of the slice: which elements are in the list
-  const unsigned char* listed = reinterpret_cast<const unsigned char*>(listed_words);
+  __shared__ uint64_t bar;
+  __shared__ __align__(16) int s_id[NT];
+  __shared__ float s_y[NT];
+  __shared__ float warp_m[W], warp_y[W];
+  __shared__ ListSums warp_sums[W];
+  __shared__ int s_bad, s_twice;
+  __shared__ RowShared rs;
+  extern __shared__ __align__(16) unsigned char units[];
   const int part = a.parts > 1 ? (int)cluster_rank() : 0;
   const int64_t r = blockIdx.x / a.parts;
   const T* row = static_cast<const T*>(a.logits) + r * a.stride;
   const int V = a.V, K = a.K, tid = threadIdx.x;
   const float c = a.s * kLog2e;
   const float weight = a.weight ? a.weight[r] : 1.f;
+  const Slice sl(V, row_pad(row), part, a.parts);
+  const int n_units = sl.last - sl.first;
+  const int e0 = max(0, 8 * sl.first - sl.pad), e1 = min(V, 8 * sl.last - sl.pad);      // the elements of the slice
   T* out = GRAD ? static_cast<T*>(a.d_logits) + r * a.d_stride : nullptr;
-  const int out_pad = GRAD ? row_pad(out) : 0;
-  const Slice so(V, out_pad, part, a.parts);                   // the part of the gradient that this block writes
   const bool leader = part == 0 && tid == 0;
 
-  if (weight != 0.f) {
-    const Slice sl(V, row_pad(row), part, a.parts);
-    for (int i = tid; i < (sl.last - sl.first + 3) / 4; i += NT) listed_words[i] = 0;
-    if (tid == 0) en.bad = en.twice = 0;
-    __syncthreads();
-    for (int k = tid; k < K; k += NT) {
-      const int id = a.ids[r * K + k];
-      const float y = a.y[r * K + k];
-      const bool used = id >= 0 && id < V;
-      if (id < -1 || id >= V || (id >= 0 && !(y < kInf))) en.bad = 1;
-      en.id[k] = used ? id : -1;
-      en.y[k] = used ? y : -kInf;
-      en.x[k] = used ? Elem<T>::get(row + id) : -kInf;
-      if (used && sl.holds(id)) {
-        const int p = id + sl.pad - 8 * sl.first;
-        atomicOr(&listed_words[p >> 5], 1u << (p & 31));
-      }
+  if (weight == 0.f) {                                    // the whole cluster
+    if (leader) {
+      if (a.loss) a.loss[r] = 0.f;
+      if (a.stats)
+        for (int i = 0; i < 8; ++i) a.stats[8 * r + i] = 0.f;
     }
-    __syncthreads();
-    for (int k = tid; k < K; k += NT) {
-      bool first = true;
-      for (int j = 0; j < k; ++j) first = first && en.id[j] != en.id[k];
-      en.first[k] = first && en.id[k] >= 0;
-      if (!first && en.id[k] >= 0) en.twice = 1;
-    }
-
-    // the sums of what is not listed
-    constexpr int N = sizeof(T) == 2 ? 4 : 2;
-    Stream<T> st(c);
-    const T* base = row - sl.pad;
-    auto without_listed = [&](Unit<T>& q, int u) {
-      const unsigned bits = listed[u - sl.first];
-      if (bits) {
-        float v[8];
-        q.values(v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = bits >> j & 1u ? -kInf : v[j];
-        q.set(v);
-      }
-    };
-    int u = sl.full0 + tid;
-    for (; u + (N - 1) * NT < sl.full1; u += N * NT) {
-      Unit<T> q[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) load_unit(base + 8 * (int64_t)(u + i * NT), q[i]);
-#pragma unroll
-      for (int i = 0; i < N; ++i) without_listed(q[i], u + i * NT);
-      st.add(q);
-    }
-    for (; u < sl.full1; u += NT) {
-      Unit<T> q[1];
-      load_unit(base + 8 * (int64_t)u, q[0]);
-      without_listed(q[0], u);
-      st.add(q);
-    }
-    if (tid < 2 && sl.ragged(tid) >= 0) {
-      Unit<T> q[1];
-      load_ragged(row, V, sl.pad, sl.ragged(tid), q[0]);
-      without_listed(q[0], sl.ragged(tid));
-      st.add(q);
-    }
-    join_block<NT>(st.finish(), c, per_warp, &mine);
-    __syncthreads();
-    if (a.parts > 1) cluster_sync();
-
-    // The list's side: a few numbers, in 64 bits, since the loss is a small difference of its terms.
-    if (tid < 32) {
-      const State rest = a.parts > 1 ? join_cluster(&mine, a.parts, c) : mine;
-      const double s = a.s;
-      float m = rest.m, ytop = -kInf;
-      for (int k = tid; k < K; k += 32) {
-        m = max_nan(m, en.x[k]);
-        ytop = fmaxf(ytop, en.y[k]);
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-        ytop = fmaxf(ytop, __shfl_xor_sync(0xffffffffu, ytop, o));
-      }
-      const bool some = ytop > -kInf, alive = m != -kInf, others = rest.m > -kInf;   // NaN: alive
-      double z = 0.0, qs = 0.0;
-      if (alive) {
-        for (int k = tid; k < K; k += 32) {
-          if (en.first[k]) z += exp(((double)en.x[k] - m) * s);
-          if (some) qs += exp((double)en.y[k] - (a.tail ? 0.0 : (double)ytop));
-        }
-      }
-      z = warp_sum(z) + (others ? exp(((double)rest.m - m) * s) * (1.0 + (double)rest.R) : 0.0);
-      qs = warp_sum(qs);
-      const double ln_z = log(z), ln_q = a.tail || !some ? 0.0 : (double)ytop + log(qs);
-      const double q_rest = a.tail && others ? fmax(0.0, 1.0 - qs) : 0.0;
-      const double ln_p_rest = ((double)rest.m - m) * s + log1p((double)rest.R) - ln_z;
-      double loss = 0.0;
-      for (int k = tid; k < K; k += 32) {
-        const double ln = (double)en.y[k] - ln_q, q = exp(ln);
-        if (q != 0.0) loss += q * (ln - (((double)en.x[k] - m) * s - ln_z));
-      }
-      loss = warp_sum(loss);
-      if (q_rest > 0.0) loss += q_rest * (log(q_rest) - ln_p_rest);
-      if (tid == 0) {
-        const bool in = some && alive;
-        const float poison = en.bad ? nan_value() : 0.f;
-        const double c_rest = others ? exp(ln_p_rest) - q_rest : 0.0;
-        RowGrad& g = en.g;
-        g.kind = en.bad || in;
-        g.m_rest = others ? rest.m : 0.f;
-        g.coef = (others ? (float)((double)a.s * weight * c_rest / (1.0 + (double)rest.R)) : 0.f) + poison;
-        g.m = m;
-        g.ln_z = ln_z + poison;
-        g.ln_q = ln_q;
-        g.weight = (double)a.s * weight;
-        if (leader) {
-          if (a.loss) a.loss[r] = (in ? (float)loss : 0.f) + poison;
-          if (a.stats) {
-            float* o = a.stats + 8 * r;
-            o[0] = m; o[1] = (float)ln_z; o[2] = rest.m; o[3] = others ? log1pf(rest.R) : -kInf;
-            o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = (in ? 1.f : 0.f) + poison; o[7] = 0.f;
-          }
-        }
-      }
-    }
-    __syncthreads();
-  } else if (leader) {
-    if (a.loss) a.loss[r] = 0.f;
-    if (a.stats)
-      for (int i = 0; i < 8; ++i) a.stats[8 * r + i] = 0.f;
+    if (GRAD) write_elements(out, e0, e1, NT, [](int) { return 0.f; });
+    return;
   }
 
+  if (tid == 0) s_bad = s_twice = 0;
+  start_slice(row, V, sl, units, &bar);
+  const double s = a.s;
+  int id = -1;
+  float y = -kInf, x = -kInf;
+  bool bad = false;
+  if (tid < K) {
+    id = a.ids[r * K + tid];
+    y = a.y[r * K + tid];
+    bad = id < -1 || id >= V || (id >= 0 && !(y < kInf));
+    if (id < 0 || id >= V) { id = -1; y = -kInf; }
+    else x = Elem<T>::get(row + id);
+  }
+  s_id[tid] = id;
+  s_y[tid] = y;
+  float m_list = x, y_top = y;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    m_list = max_nan(m_list, __shfl_xor_sync(0xffffffffu, m_list, o));
+    y_top = fmaxf(y_top, __shfl_xor_sync(0xffffffffu, y_top, o));
+  }
+  if ((tid & 31) == 0) { warp_m[tid >> 5] = m_list; warp_y[tid >> 5] = y_top; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    m_list = max_nan(m_list, warp_m[w]);
+    y_top = fmaxf(y_top, warp_y[w]);
+  }
+  const bool some = y_top > -kInf;
+  const double shift = a.tail || !some ? 0.0 : (double)y_top;
+  bool first = id >= 0;                                   // no entry before this one has its id
+  if (first) {
+    const int4* ids4 = reinterpret_cast<const int4*>(s_id);
+    for (int j = 0; j < (tid >> 2); ++j) {
+      const int4 v = ids4[j];
+      first = first && v.x != id && v.y != id && v.z != id && v.w != id;
+    }
+    for (int j = tid & ~3; j < tid; ++j) first = first && s_id[j] != id;
+    if (!first) s_twice = 1;
+  }
+  if (bad) s_bad = 1;
+  const double x_shift = m_list != -kInf ? (double)m_list : 0.0;
+  double e = 0.0, q = 0.0;
+  if (first && m_list != -kInf) e = exp(((double)x - m_list) * s);
+  if (y > -kInf) q = exp((double)y - shift);
+  {
+    ListSums v{e, q, 0.0, 0.0};
+    if (q != 0.0) { v.qy = q * ((double)y - shift); v.qx = q * (((double)x - x_shift) * s); }
+    v = warp_sum(v);
+    if ((tid & 31) == 0) warp_sums[tid >> 5] = v;
+  }
+
+  const bool arrived = wait_slice(&bar);
+  if (id >= e0 && id < e1) reinterpret_cast<T*>(units)[id + sl.pad - 8 * sl.first] = Elem<T>::masked();
+  __syncthreads();
+  constexpr int N = sizeof(T) == 2 ? 4 : 2;
+  Stream<T, false, false> st(c);
+  {
+    int u = tid;
+    for (; u + (N - 1) * NT < n_units; u += N * NT) {
+      Unit<T> v[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) load_shared_unit(units, u + i * NT, v[i]);
+      st.add(v);
+    }
+    for (; u < n_units; u += NT) {
+      Unit<T> v[1];
+      load_shared_unit(units, u, v[0]);
+      st.add(v);
+    }
+  }
+  join_block<NT>(arrived ? st.finish() : State{0.f, nan_value(), nan_value()}, c, per_warp, &mine);
+  if (a.parts > 1) {
+    cluster_sync();
+  }
+  if (tid < 32) {
+    __syncwarp();
+    const State rest = a.parts > 1 ? join_cluster(&mine, a.parts, c) : mine;
+    ListSums v = warp_sums[0];
+    for (int w = 1; w < W; ++w) { v.z += warp_sums[w].z; v.q += warp_sums[w].q; v.qy += warp_sums[w].qy; v.qx += warp_sums[w].qx; }
+    const float m = max_nan(rest.m, m_list);
+    const bool alive = m != -kInf, others = rest.m > -kInf;      // a NaN is alive
+    const double grow = 1.0 + (double)rest.R;
+    const double of_rest = others ? exp(((double)rest.m - m) * s) : 0.0, of_list = m_list != -kInf ? exp(((double)m_list - m) * s) : 0.0;
+    const double z = of_rest * grow + of_list * v.z, ln_z = log(z), ln_rest = log(grow);
+    const double of_q = a.tail || !some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !some ? 0.0 : shift + log(v.q);
+    const double q_all = v.q * of_q, q_rest = a.tail && others ? fmax(0.0, 1.0 - v.q) : 0.0;
+    const double ln_p_rest = ((double)rest.m - m) * s + ln_rest - ln_z;
+    double loss = (v.qy - v.qx) * of_q + (((double)m - x_shift) * s + ln_z - (ln_q - shift)) * q_all;
+    if (q_rest > 0.0) loss += q_rest * (log(q_rest) - ln_p_rest);
+    const double c_rest = others ? of_rest * grow / z - q_rest : 0.0;
+    if (tid == 0) {
+      const bool in = some && alive;
+      const float poison = s_bad ? nan_value() : 0.f;
+      rs.kind = s_bad || in;
+      rs.m_rest = others ? rest.m : 0.f;
+      rs.coef = (others ? (float)(s * weight * c_rest / grow) : 0.f) + poison;
+      rs.of_e = of_list / z + poison;
+      rs.of_q = of_q;
+      rs.weight = s * weight;
+      if (leader) {
+        if (a.loss) a.loss[r] = (in ? (float)loss : 0.f) + poison;
+        if (a.stats) {
+          float* o = a.stats + 8 * r;
+          o[0] = m; o[1] = (float)ln_z; o[2] = rest.m; o[3] = others ? (float)ln_rest : -kInf;
+          o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = (in ? 1.f : 0.f) + poison; o[7] = 0.f;
+        }
+      }
+    }
+  }
+  if (a.parts > 1) {
+    __syncwarp();
+    cluster_arrive();                                     // this block has read what it needs of the others
+  }
   if (GRAD) {
-    const bool zero = weight == 0.f || en.g.kind == 0;
-    const bool alike = row_pad(row) == out_pad;
-    float m_rest = 0.f, coef = 0.f;
-    if (!zero) { m_rest = en.g.m_rest; coef = en.g.coef; }
-    constexpr int N = sizeof(T) == 2 ? 4 : 2;
-    const T* in_base = row - out_pad;
-    T* out_base = out - out_pad;
-    if (alike) {
-      int u = so.full0 + tid;
-      for (; u < so.full1; u += N * NT) {
-        Unit<T> q[N];
-        if (!zero) {
-#pragma unroll
-          for (int i = 0; i < N; ++i)
-            if (u + i * NT < so.full1) load_unit(in_base + 8 * (int64_t)(u + i * NT), q[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-          if (u + i * NT < so.full1) {
-            if (zero) fill_unit(q[i], 0.f);
-            else rest_grad_unit(q[i], m_rest, c, coef);
-            store_unit(out_base + 8 * (int64_t)(u + i * NT), q[i]);
-          }
-      }
+    __syncthreads();
+    if (rs.kind == 0) {
+      write_elements(out, e0, e1, NT, [](int) { return 0.f; });
     } else {
-      for (int u = so.full0 + tid; u < so.full1; u += NT) {
-        Unit<T> q;
-        if (zero) {
-          fill_unit(q, 0.f);
-        } else {
-          load_ragged(row, V, out_pad, u, q);
-          rest_grad_unit(q, m_rest, c, coef);
+      const float m_rest = rs.m_rest, coef = rs.coef;
+      if (row_pad(out) == sl.pad) {
+        for (int u = tid; u < n_units; u += NT) {
+          Unit<T> v;
+          load_shared_unit(units, u, v);
+          rest_grad_unit(v, m_rest, c, coef);
+          const int g = sl.first + u;
+          if (g >= sl.full0 && g < sl.full1) store_unit(out - sl.pad + 8 * (int64_t)g, v);
+          else store_ragged(out, V, sl.pad, g, v);
         }
-        store_unit(out_base + 8 * (int64_t)u, q);
-      }
-    }
-    if (tid < 2 && so.ragged(tid) >= 0) {
-      Unit<T> q;
-      if (zero) {
-        fill_unit(q, 0.f);
       } else {
-        load_ragged(row, V, out_pad, so.ragged(tid), q);
-        rest_grad_unit(q, m_rest, c, coef);
+        const T* own = reinterpret_cast<const T*>(units) + sl.pad - 8 * sl.first;
+        write_elements(out, e0, e1, NT, [&](int i) { return coef * ex2((Elem<T>::get(own + i) - m_rest) * c); });
       }
-      store_ragged(out, V, out_pad, so.ragged(tid), q);
-    }
-    if (!zero) {
-      __syncthreads();                        // the list's elements go over what was just written there
-      for (int k = tid; k < K; k += NT)
-        if (en.first[k] && so.holds(en.id[k]))
-          Elem<T>::put(out + en.id[k], entry_gradient(en.g, a.s, en.id, en.y, K, k, en.x[k], en.twice));
+      __syncthreads();                                    // the list's elements go over what was just written there
+      if (first && id >= e0 && id < e1) {
+        double of_id = q;
+        if (s_twice)
+          for (int j = tid + 1; j < K; ++j)
+            if (s_id[j] == id && s_y[j] > -kInf) of_id += exp((double)s_y[j] - shift);
+        Elem<T>::put(out + id, (float)(rs.weight * (e * rs.of_e - of_id * rs.of_q)));
+      }
     }
   }
-  if (a.parts > 1) cluster_sync();            // no block leaves while another reads its shared memory
+  if (a.parts > 1) cluster_wait();                        // no block leaves while another reads its shared memory
 }
 
 // Rows of up to 256 elements: LPR lanes a row, eight elements a lane, the list laid out over the row's elements in shared
@@ -391,7 +394,7 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
       top = max_nan(top, listed >> j & 1u ? v[j] : -kInf);
     }
     w[0].set(x);
-    Stream<T> st(c);
+    Stream<T, false, false> st(c);
     st.add(w);
     State rest = st.finish();
 #pragma unroll
@@ -513,11 +516,7 @@ __global__ void __launch_bounds__(kBackThreads) distill_backward_kernel(const __
       }
     }
   __syncthreads();
-  if (mine) {
-    RowGrad g;
-    g.m = o[0]; g.ln_z = o[1]; g.ln_q = o[5]; g.weight = (double)a.s * weight;
-    Elem<T>::put(out + id, entry_gradient(g, a.s, s_id, s_y, K, tid, x, twice));
-  }
+  if (mine) Elem<T>::put(out + id, entry_gradient(o[0], o[1], o[5], a.s, (double)a.s * weight, s_id, s_y, K, tid, x, twice));
 }
 
 template <typename T>
@@ -537,17 +536,6 @@ cudaError_t launch_small(const DistillArgs& a, bool backward, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-template <typename T, int NT, bool GRAD>
-cudaError_t launch_distill_rows(const DistillArgs& a, cudaStream_t st) {
-  static std::atomic<bool> allowed[kMaxDevices];
-  const size_t smem = (((size_t)(a.V + 14) / 8 + a.parts - 1) / a.parts + 3) / 4 * 4;
-  if (smem > 40 * 1024) {
-    const cudaError_t e = allow_dynamic_smem(distill_rows_kernel<T, NT, GRAD>, REMOE_ROWS_MAX_VOCAB / 8 + 64, allowed);
-    if (e != cudaSuccess) return e;
-  }
-  return launch_rows(distill_rows_kernel<T, NT, GRAD>, a.n_rows, a.parts, NT, smem, st, a);
-}
-
 template <typename T>
 cudaError_t launch_distill(DistillArgs a, bool backward, cudaStream_t st) {
   if (a.V <= kSmallVocab) return launch_small<T>(a, backward, st);
@@ -559,9 +547,13 @@ cudaError_t launch_distill(DistillArgs a, bool backward, cudaStream_t st) {
     distill_backward_kernel<T><<<(unsigned)blocks, kBackThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
-  a.parts = parts_of_row(a.n_rows, a.V, 512);
-  if (a.V >= 8192) return a.d_logits ? launch_distill_rows<T, 512, true>(a, st) : launch_distill_rows<T, 512, false>(a, st);
-  return a.d_logits ? launch_distill_rows<T, 128, true>(a, st) : launch_distill_rows<T, 128, false>(a, st);
+  a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));
+  a.slice_bytes = slice_bytes(a.V, sizeof(T), a.parts);
+  if (a.V >= 8192 || a.K > 128)
+    return a.d_logits ? launch_resident<distill_rows_kernel<T, 256, true>, 256>(a, 0, st)
+                      : launch_resident<distill_rows_kernel<T, 256, false>, 256>(a, 0, st);
+  return a.d_logits ? launch_resident<distill_rows_kernel<T, 128, true>, 128>(a, 0, st)
+                    : launch_resident<distill_rows_kernel<T, 128, false>, 128>(a, 0, st);
 }
 
 int run_distill(const DistillArgs& a, int32_t dtype, bool backward, void* cuda_stream) {
@@ -596,7 +588,7 @@ extern "C" int remoe_distill_topk(int32_t n_rows, int32_t vocab, int32_t dtype, 
                                   const float* teacher_logprobs_dev, int32_t tail, const float* row_weight_dev, float* loss_dev,
                                   float* row_stats_dev, void* d_logits_dev, int64_t d_row_stride, void* cuda_stream) {
   using namespace remoe::rows;
-  DistillArgs a{logits_dev, d_logits_dev, row_stride, d_row_stride, vocab, n_rows, 1, n_top, tail, inv_temperature,
+  DistillArgs a{logits_dev, d_logits_dev, row_stride, d_row_stride, vocab, n_rows, 1, 0, n_top, tail, inv_temperature,
                 teacher_ids_dev, teacher_logprobs_dev, row_weight_dev, loss_dev, row_stats_dev, nullptr};
   const int rc = check_distill(a, dtype);
   if (rc != REMOE_OK) return rc;
@@ -610,7 +602,7 @@ extern "C" int remoe_distill_topk_backward(int32_t n_rows, int32_t vocab, int32_
                                            const float* row_stats_dev, const float* grad_loss_dev, void* d_logits_dev,
                                            int64_t d_row_stride, void* cuda_stream) {
   using namespace remoe::rows;
-  DistillArgs a{logits_dev, d_logits_dev, row_stride, d_row_stride, vocab, n_rows, 1, n_top, 0, inv_temperature,
+  DistillArgs a{logits_dev, d_logits_dev, row_stride, d_row_stride, vocab, n_rows, 1, 0, n_top, 0, inv_temperature,
                 teacher_ids_dev, teacher_logprobs_dev, grad_loss_dev, nullptr, nullptr, row_stats_dev};
   const int rc = check_distill(a, dtype);
   if (rc != REMOE_OK) return rc;

@@ -22,6 +22,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "tma_ring.cuh"
+
 namespace remoe {
 namespace rows {
 
@@ -90,6 +92,16 @@ struct Elem<float> {
     hi = pack2(max_nan(a0, b0), max_nan(a1, b1));
     lo = pack2(min_nan(a0, b0), min_nan(a1, b1));
   }
+  static constexpr bool kLifts = false;         // no packed maximum: the exponent is clamped instead
+  static constexpr float kFloor = -kInf;
+  static __device__ __forceinline__ Word lift(Word w) { return w; }
+  static __device__ __forceinline__ Word larger(Word a, Word b) {
+    float a0, a1, b0, b1;
+    unpack2(a, a0, a1);
+    unpack2(b, b0, b1);
+    return pack2(max_nan(a0, b0), max_nan(a1, b1));
+  }
+  static __device__ __forceinline__ float masked() { return -kInf; }
   static __device__ __forceinline__ float get(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 };
@@ -113,6 +125,15 @@ struct Elem<__nv_bfloat16> {
     asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(lo) : "r"(hi), "r"(lo));
     hi = a;
   }
+  static constexpr bool kLifts = true;
+  static constexpr float kFloor = -1152921504606846976.f;
+  static __device__ __forceinline__ Word larger(Word a, Word b) {
+    Word r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ Word lift(Word w) { return larger(w, 0xdd80dd80u); }   // at least kFloor
+  static __device__ __forceinline__ __nv_bfloat16 masked() { return __ushort_as_bfloat16((unsigned short)0xff80); }
   static __device__ __forceinline__ float get(const __nv_bfloat16* p) { return __bfloat162float(*p); }
   static __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 };
@@ -139,6 +160,15 @@ struct Elem<__half> {
     asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(hi), "r"(lo));
     hi = a;
   }
+  static constexpr bool kLifts = true;
+  static constexpr float kFloor = -65504.f;
+  static __device__ __forceinline__ Word larger(Word a, Word b) {
+    Word r;
+    asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ Word lift(Word w) { return larger(w, 0xfbfffbffu); }   // at least kFloor
+  static __device__ __forceinline__ __half masked() { return __ushort_as_half((unsigned short)0xfc00); }
   static __device__ __forceinline__ float get(const __half* p) { return __half2float(*p); }
   static __device__ __forceinline__ void put(__half* p, float v) { *p = __float2half_rn(v); }
 };
@@ -239,6 +269,47 @@ struct Slice {
   __device__ __forceinline__ bool holds(int id) const { const int u = (id + pad) >> 3; return u >= first && u < last; }
 };
 
+// ---- a slice in shared memory ----------------------------------------------------------------------------------
+// A block brings its slice of the row into shared memory with bulk copies and works on it there: the whole slice is in
+// flight at once whatever the threads' registers hold, and what is looked at again (candidates of the top elements, the
+// gradient's second pass) is not read from memory again.  Blocks are small enough for several to lie on an SM, so that
+// one's loads overlap another's arithmetic and stores.
+
+template <typename T>
+__device__ __forceinline__ void load_shared_unit(const unsigned char* units, int i, Unit<T>& u) {
+  const uint4 v = reinterpret_cast<const uint4*>(units)[i];
+  u.w[0] = v.x; u.w[1] = v.y; u.w[2] = v.z; u.w[3] = v.w;
+}
+template <>
+__device__ __forceinline__ void load_shared_unit<float>(const unsigned char* units, int i, Unit<float>& u) {
+  const ulonglong2 a = reinterpret_cast<const ulonglong2*>(units)[2 * i], b = reinterpret_cast<const ulonglong2*>(units)[2 * i + 1];
+  u.w[0] = a.x; u.w[1] = a.y; u.w[2] = b.x; u.w[3] = b.y;
+}
+
+constexpr uint32_t kCopyBytes = 32768;        // of one bulk copy at most
+
+// Starts the copies (thread 0) and brings the ragged units element by element (the next sixteen threads), -inf around the
+// row.  The caller synchronises the block, then every thread waits for `bar` with wait_slice.
+template <typename T>
+__device__ __forceinline__ void start_slice(const T* row, int V, const Slice& sl, unsigned char* units, uint64_t* bar) {
+  constexpr uint32_t kUnit = 8 * sizeof(T);
+  const int tid = threadIdx.x;
+  if (tid == 0) {
+    ring::mbar_init(bar, 1);
+    ring::mbar_fence_init();
+    const uint32_t bytes = sl.full1 > sl.full0 ? (uint32_t)(sl.full1 - sl.full0) * kUnit : 0u;
+    ring::mbar_expect_tx(bar, bytes);
+    const unsigned char* src = reinterpret_cast<const unsigned char*>(row - sl.pad + 8 * (int64_t)sl.full0);
+    unsigned char* dst = units + (size_t)(sl.full0 - sl.first) * kUnit;
+    for (uint32_t o = 0; o < bytes; o += kCopyBytes) ring::bulk_g2s(dst + o, src + o, min(kCopyBytes, bytes - o), bar);
+  } else if (tid >= 32 && tid < 48) {
+    const int u = sl.ragged((tid >> 3) & 1), id = 8 * u + (tid & 7) - sl.pad;
+    if (u >= 0) reinterpret_cast<T*>(units)[8 * (u - sl.first) + (tid & 7)] = id >= 0 && id < V ? row[id] : Elem<T>::masked();
+  }
+}
+// False if the copies have not arrived within the limit of a wait and of another one: the row is given up as NaN.
+__device__ __forceinline__ bool wait_slice(uint64_t* bar) { return ring::mbar_wait(bar, 0) || ring::mbar_wait(bar, 0); }
+
 // ---- one-pass sums -------------------------------------------------------------------------------------------
 
 struct State {
@@ -258,46 +329,76 @@ __device__ __forceinline__ State merge(const State& a, const State& b, float c) 
 }
 
 // One thread's running sums over the units it is given.
-template <typename T>
+//   EXACT: R leaves the largest element out (otherwise 1 + R is the plain sum, good to a rounding); ENTROPY: U is kept.
+// Two ways to the exponent.  Near: fma(x, c, -k) with k a whole number near m c, one packed instruction whose only error is
+// the rounding of its result (k is exact, and so is any change of it).  Far, for values so large that x c has no
+// fraction left or overflows (rows of the type's lowest value): (x - m) c.
+// The near way takes -inf as a large negative number where U is kept, since 0 * inf is none; it is used only where
+// that number is 2^-160 of the reference or less.
+template <typename T, bool EXACT, bool ENTROPY>
 struct Stream {
   typename Elem<T>::Word M;
-  float ref, limit, c;
+  float ref, k, limit, c;
+  bool far;
   f2 R, U;
-  __device__ __forceinline__ explicit Stream(float c_) : M(Elem<T>::lowest()), ref(0.f), limit(-kInf), c(c_), R(0), U(0) {}
+  __device__ __forceinline__ explicit Stream(float c_) : M(Elem<T>::lowest()), ref(0.f), k(0.f), limit(-kInf), c(c_), far(false), R(0), U(0) {}
+
+  __device__ __forceinline__ void move_reference(float m) {
+    const float t = m * c;
+    const bool go_far = !(fabsf(t) < 1048576.f && c < 1e15f && (m - Elem<T>::kFloor) * c >= 160.f);
+    const float nk = rintf(t);
+    if (limit > -kInf) {
+      const float d = far || go_far ? (ref - m) * c : k - nk, r = ex2(d);
+      const f2 r2 = pack2(r, r);
+      if (ENTROPY) U = r > 0.f ? mul2(r2, fma2(R, pack2(d, d), U)) : 0ull;
+      R = mul2(R, r2);
+    } else {
+      R = U = 0ull;                                    // masked elements only so far
+    }
+    far = go_far;
+    k = nk;
+    ref = m;
+    limit = m + kReferenceRise / c;
+  }
 
   template <int N>
   __device__ __forceinline__ void add(Unit<T> (&u)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) Elem<T>::order(M, u[i].w[j]);
+      for (int j = 0; j < 4; ++j) {
+        if (EXACT) Elem<T>::order(M, u[i].w[j]);
+        else M = Elem<T>::larger(M, u[i].w[j]);
+      }
     float m0, m1;
     unpack2(Elem<T>::widen(M), m0, m1);
     const float m = fmaxf(m0, m1);
-    if (m > limit) {                                   // the first live element, or far above the reference
-      if (limit > -kInf) {
-        const float d = (ref - m) * c, r = ex2(d);
-        const f2 r2 = pack2(r, r);
-        if (r > 0.f) U = mul2(r2, fma2(R, pack2(d, d), U));
-        else U = 0;
-        R = mul2(R, r2);
-      }
-      ref = m;
-      limit = m + kReferenceRise / c;
+    if (m > limit) move_reference(m);                  // the first live element, or far above the reference
+    const f2 cc = pack2(c, c);
+    if (far) {
+      const f2 nref = pack2(-ref, -ref);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) accumulate(mul2(add2(Elem<T>::widen(u[i].w[j]), nref), cc), true);
+    } else {
+      const f2 nk = pack2(-k, -k);
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (ENTROPY) u[i].w[j] = Elem<T>::lift(u[i].w[j]);
+          accumulate(fma2(Elem<T>::widen(u[i].w[j]), cc, nk), !Elem<T>::kLifts);
+        }
     }
-    const f2 nref = pack2(-ref, -ref), cc = pack2(c, c);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f2 d = mul2(add2(Elem<T>::widen(u[i].w[j]), nref), cc);
-        float d0, d1;
-        unpack2(d, d0, d1);
-        const f2 e = pack2(ex2(d0), ex2(d1));
-        R = add2(R, e);
-        // -inf would give 0 * inf; 2^-200 is 0 in float32 already
-        U = fma2(e, pack2(max_nan(d0, -200.f), max_nan(d1, -200.f)), U);
-      }
+  }
+
+  __device__ __forceinline__ void accumulate(f2 d, bool clamp) {
+    float d0, d1;
+    unpack2(d, d0, d1);
+    const f2 e = pack2(ex2(d0), ex2(d1));
+    R = add2(R, e);
+    if (ENTROPY) U = fma2(e, clamp ? pack2(max_nan(d0, -200.f), max_nan(d1, -200.f)) : d, U);   // 2^-200 is 0 in float32
   }
 
   // Largest element seen (-inf if none; NaN if there was one).
@@ -315,12 +416,18 @@ struct Stream {
     const float hi = max_nan(a, b), lo = min_nan(a, b);
     if (hi == -kInf) return State{hi, 0.f, 0.f};
     if (!(hi < kInf)) return State{0.f, nan_value(), nan_value()};
-    const float dl = (lo - hi) * c, el = ex2(dl);       // the smaller half's largest is an element of the sum like others
-    const float d = (ref - hi) * c, r = ex2(d);
+    const float d = far ? (ref - hi) * c : -fmaf(hi, c, -k), r = ex2(d);
     State s;
     s.m = hi;
-    s.R = (r0 + r1) * r + el;
-    s.U = r * (u0 + u1) + r * d * (r0 + r1) + (el == 0.f ? 0.f : el * dl);
+    s.R = (r0 + r1) * r;
+    s.U = ENTROPY ? r * (u0 + u1) + r * d * (r0 + r1) : 0.f;
+    if (EXACT) {                                        // the smaller half's largest is an element of the sum like others
+      const float dl = (lo - hi) * c, el = ex2(dl);
+      s.R += el;
+      if (ENTROPY && el > 0.f) s.U += el * dl;
+    } else {
+      s.R -= 1.f;
+    }
     return s;
   }
 };
@@ -354,8 +461,11 @@ __device__ __forceinline__ unsigned cluster_rank() {
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
 // Address of this block's shared variable `p` as it is in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t remote_shared(const void* p, unsigned rank) {
@@ -373,14 +483,15 @@ __device__ __forceinline__ unsigned long long load_remote64(uint32_t a) {
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
   return v;
 }
-// State of all blocks of the cluster, joined in rank order (the same in every block).  Call behind cluster_sync().
+// State of all blocks of the cluster (`parts`: a power of two up to eight), the same in every thread of every block.  Whole
+// warps, behind cluster_sync().
 __device__ __forceinline__ State join_cluster(const State* mine, int parts, float c) {
+  const int lane = threadIdx.x & 31;
   State s{-kInf, 0.f, 0.f};
-  for (int i = 0; i < parts; ++i) {
-    const State o{load_remote(remote_shared(&mine->m, i)), load_remote(remote_shared(&mine->R, i)), load_remote(remote_shared(&mine->U, i))};
-    s = merge(s, o, c);
-  }
-  return s;
+  if (lane < parts)
+    s = State{load_remote(remote_shared(&mine->m, lane)), load_remote(remote_shared(&mine->R, lane)), load_remote(remote_shared(&mine->U, lane))};
+  for (int o = parts >> 1; o; o >>= 1) s = merge(s, shuffle_down(s, o, 32), c);
+  return State{__shfl_sync(0xffffffffu, s.m, 0), __shfl_sync(0xffffffffu, s.R, 0), __shfl_sync(0xffffffffu, s.U, 0)};
 }
 
 // Whole number in the order of the values (NaN aside); -0 equals +0.

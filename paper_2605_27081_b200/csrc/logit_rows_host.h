@@ -7,6 +7,7 @@
 #include <cmath>
 
 #include "remoe.h"
+#include "remoe_internal.cuh"
 
 namespace remoe {
 namespace rows {
@@ -45,6 +46,9 @@ class PointerDevice {
   bool switched_ = false;
 };
 
+constexpr int64_t kSliceBytes = 52 * 1024;     // of a row in one block, where eight blocks are enough for that
+constexpr size_t kSmemLimit = 220 * 1024;      // dynamic shared memory of a block; the longest float32 row needs 216 KB in eight
+
 inline int element_size(int32_t dtype) { return dtype == REMOE_F32 ? 4 : dtype == REMOE_BF16 || dtype == REMOE_F16 ? 2 : 0; }
 inline bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
@@ -63,28 +67,36 @@ inline int check_rows(int32_t n_rows, int32_t vocab, int32_t dtype, const void* 
   return REMOE_OK;
 }
 
-// Blocks that share a row.  With fewer rows than keep the GPU's memory busy (two blocks an SM), a row is cut into up to
-// eight parts of at least `least` units, one part per block of a cluster.
-inline int parts_of_row(int32_t n_rows, int32_t vocab, int least) {
+// Blocks that share a row, one part of it in the shared memory of each: a power of two up to eight, so that four blocks
+// of 256 threads lie on an SM with 52 KB each; more where there are few rows, down to 8 KB.
+inline int parts_of_row(int32_t n_rows, int32_t vocab, int size) {
   int parts = 1;
-  while (parts < 8 && (int64_t)n_rows * parts < 296 && (vocab / 8) / (2 * parts) >= least) parts *= 2;
+  while (parts < 8 && (int64_t)vocab * size > (int64_t)parts * kSliceBytes) parts *= 2;
+  while (parts < 8 && (int64_t)n_rows * parts < 296 && (int64_t)vocab * size > (int64_t)parts * 16384) parts *= 2;
   return parts;
 }
+// Shared memory of a part: whole units of eight elements, whatever the row's alignment.
+inline int slice_bytes(int32_t vocab, int size, int parts) { return ((vocab + 14) / 8 + parts - 1) / parts * 8 * size; }
 
-template <typename Kernel, typename Args>
-inline cudaError_t launch_rows(Kernel kernel, int32_t n_rows, int parts, int threads, size_t smem, cudaStream_t stream, const Args& args) {
+// One launch of `Kernel`, a cluster of args.parts blocks for each row.
+template <auto Kernel, int NT, typename Args>
+inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStream_t stream) {
+  static std::atomic<bool> ready[kMaxDevices];
+  const size_t smem = (size_t)args.slice_bytes + more_smem;
+  const cudaError_t e = allow_dynamic_smem(Kernel, kSmemLimit, ready);
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)n_rows * (unsigned)parts);
-  cfg.blockDim = dim3((unsigned)threads);
+  cfg.gridDim = dim3((unsigned)args.n_rows * (unsigned)args.parts);
+  cfg.blockDim = dim3(NT);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)parts;
+  at[0].val.clusterDim.x = (unsigned)args.parts;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = parts > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kernel, args);
+  cfg.numAttrs = args.parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, Kernel, args);
 }
 
 }  // namespace rows

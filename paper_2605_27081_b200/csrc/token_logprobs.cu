@@ -16,7 +16,7 @@ constexpr int kSmallVocab = 256;        // up to here a row is held by a group o
 struct LogprobArgs {
   const void* logits;
   int64_t stride;
-  int V, n_rows, parts, top_k;
+  int V, n_rows, parts, slice_bytes, top_k;
   float s;
   const int32_t* tokens;
   float *logprob, *entropy, *top_logprob, *stats;
@@ -36,29 +36,25 @@ struct TopShared {
 
 __device__ __forceinline__ unsigned long long full_key(uint32_t k, int id) { return ((unsigned long long)k << 32) | (0xffffffffu - (uint32_t)id); }
 
-// Any unit of the slice, whole or ragged.
-template <typename T>
-__device__ __forceinline__ void read_unit(const T* row, int V, const Slice& sl, int u, Unit<T>& out) {
-  if (u >= sl.full0 && u < sl.full1) load_unit(row - sl.pad + 8 * u, out);
-  else load_ragged(row, V, sl.pad, u, out);
+// A block's slice in shared memory, as the selection looks at it: calls f(key, id) for the elements of unit i.
+template <typename T, typename F>
+__device__ __forceinline__ void each_element(const unsigned char* units, const Slice& sl, int V, int i, F f) {
+  Unit<T> q;
+  load_shared_unit(units, i, q);
+  float v[8];
+  q.values(v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int id = 8 * (sl.first + i) + j - sl.pad;
+    if (id >= 0 && id < V) f(order_key(v[j]), id);
+  }
 }
 
-// Elements of the whole slice whose key is above / at or above `t`.
+// Elements of the slice at or above `t`.
 template <typename T, int NT>
-__device__ int count_keys(const T* row, int V, const Slice& sl, uint32_t t, bool equal_too, int* warp_count) {
+__device__ int count_keys(const unsigned char* units, const Slice& sl, int V, uint32_t t, int* warp_count) {
   int n = 0;
-  for (int u = sl.first + (int)threadIdx.x; u < sl.last; u += NT) {
-    Unit<T> q;
-    read_unit(row, V, sl, u, q);
-    float v[8];
-    q.values(v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int id = 8 * u + j - sl.pad;
-      const uint32_t k = order_key(v[j]);
-      n += id >= 0 && id < V && (equal_too ? k >= t : k > t);
-    }
-  }
+  for (int i = threadIdx.x; i < sl.last - sl.first; i += NT) each_element<T>(units, sl, V, i, [&](uint32_t k, int) { n += k >= t; });
   n = __reduce_add_sync(0xffffffffu, n);
   __syncthreads();
   if ((threadIdx.x & 31) == 0) warp_count[threadIdx.x >> 5] = n;
@@ -68,85 +64,68 @@ __device__ int count_keys(const T* row, int V, const Slice& sl, uint32_t t, bool
   return all;
 }
 
-// The `want` largest elements of the slice (fewer than or as many as it has), sorted, to sh.sorted.
+// The `want` largest elements of the slice, sorted, to sh.sorted.
 //
-// A thread has kept the largest of the elements that it saw.  The want-th largest of these NT numbers is a lower
-// bound t for the want-th largest element, and only threads whose largest reaches t can hold one: their units (a
-// few per cent of the row) are read again, out of L2, and what reaches t is sorted by counting for each
-// the keys above it.  t may be rounded down to fewer bits, which adds candidates, never loses one.
-// Many equal elements (masked rows) and rows whose large elements sit in few threads overflow the lists; those rows
-// are finished by scans that are exact whatever the data.
+// A thread has kept the largest of its elements (units tid, tid + NT, ...).  The want-th largest of these NT numbers is a
+// lower bound t for the want-th largest element, and only threads whose largest reaches t hold such elements: their
+// units (a few per cent of the slice) are looked at again, and what is above t is sorted by counting for each
+// the keys above it.  t may be rounded down to fewer bits, which adds candidates and never loses one.
+// Elements equal to t matter only where too few are above it.  Where few threads hold t they are listed with the others;
+// in masked rows nearly all elements are equal, and those of the lowest indices are taken in one ordered scan that
+// stops as soon as there are enough.  Rows whose large elements sit in few threads overflow the list: then the
+// want-th largest value is found by its bits, with a count over the slice for each.
 template <typename T, int NT>
-__device__ void select_top(const T* row, int V, const Slice& sl, float mine, int want, TopShared<NT>& sh) {
-  const int tid = threadIdx.x;
+__device__ void select_top(const unsigned char* units, const Slice& sl, int V, float mine, int want, TopShared<NT>& sh) {
+  const int tid = threadIdx.x, n_units = sl.last - sl.first;
   unsigned long long* const ties = sh.above + kCandidates;
   uint32_t t = 0;
-  const uint32_t key = mine == mine && sl.first + tid < sl.last ? order_key(mine) : 0;   // no unit: below all values
+  const uint32_t key = mine == mine && tid < n_units ? order_key(mine) : 0;   // no unit: below all values
   if (tid == 0) sh.n_columns = sh.n_above = sh.n_ties = 0;
   constexpr int kLow = Elem<T>::kUnusedBits;          // the key's bits that say nothing for a 16-bit type
+  int holders = NT;                                   // threads whose largest is at least t
   for (int b = 31; b >= kLow; --b) {
     const uint32_t cand = t | (1u << b);
     const int n = __syncthreads_count(key >= cand);
     if (n >= want) {
       t = cand;
+      holders = n;
       if (n <= want + want / 4 + 4) break;
     }
   }
   if (!(t & 0x80000000u)) t |= (1u << kLow) - 1u;      // they are ones in a negative value's key
+  const bool list_ties = holders <= 2 * want + 32;
   __syncthreads();
-  if (key >= t) sh.columns[atomicAdd(&sh.n_columns, 1)] = tid;
+  if (key > t || (list_ties && key == t)) sh.columns[atomicAdd(&sh.n_columns, 1)] = tid;
   __syncthreads();
-  auto push = [&](float x, int id) {
-    const uint32_t k = order_key(x);
+  const int nc = sh.n_columns, rounds = (n_units + NT - 1) / NT;
+  auto push = [&](uint32_t k, int id) {
     if (k > t) {
       const int i = atomicAdd(&sh.n_above, 1);
       if (i < kCandidates) sh.above[i] = full_key(k, id);
-    } else if (k == t) {
+    } else if (list_ties && k == t) {
       const int i = atomicAdd(&sh.n_ties, 1);
       if (i < kTies) ties[i] = full_key(k, id);
     }
   };
-  const int rounds = (sl.full1 - sl.full0 + NT - 1) / NT, nc = sh.n_columns;
-  for (int w = tid; w < nc * rounds + 2; w += NT) {
-    const int u = w < nc * rounds ? sl.full0 + (w / nc) * NT + sh.columns[w % nc] : sl.ragged(w - nc * rounds);
-    if (u < 0 || u >= (w < nc * rounds ? sl.full1 : sl.last)) continue;
-    Unit<T> q;
-    read_unit(row, V, sl, u, q);
-    float v[8];
-    q.values(v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int id = 8 * u + j - sl.pad;
-      if (id >= 0 && id < V) push(v[j], id);
-    }
+  for (int w = tid; w < nc * rounds; w += NT) {
+    const int i = (w / nc) * NT + sh.columns[w % nc];
+    if (i < n_units) each_element<T>(units, sl, V, i, push);
   }
   __syncthreads();
-  int na = sh.n_above, nt = sh.n_ties;
-  if (na > kCandidates && na >= want) {
-    // too many above t: find the value of the want-th largest element by its bits, then collect what is above it
+  int na = sh.n_above, nt = list_ties ? sh.n_ties : kTies + 1;
+  if (na > kCandidates) {
     __syncthreads();
     uint32_t v = 0;
     for (int b = 31; b >= 0; --b)
-      if (count_keys<T, NT>(row, V, sl, v | (1u << b), true, sh.warp_count) >= want) v |= 1u << b;
+      if (count_keys<T, NT>(units, sl, V, v | (1u << b), sh.warp_count) >= want) v |= 1u << b;
     t = v;
     __syncthreads();
     if (tid == 0) sh.n_above = 0;
     __syncthreads();
-    for (int u = sl.first + tid; u < sl.last; u += NT) {
-      Unit<T> q;
-      read_unit(row, V, sl, u, q);
-      float x[8];
-      q.values(x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int id = 8 * u + j - sl.pad;
-        const uint32_t k = order_key(x[j]);
-        if (id >= 0 && id < V && k > t) {
-          const int i = atomicAdd(&sh.n_above, 1);
-          if (i < kCandidates) sh.above[i] = full_key(k, id);
-        }
-      }
-    }
+    for (int i = tid; i < n_units; i += NT)
+      each_element<T>(units, sl, V, i, [&](uint32_t k, int id) {
+        if (k > t) sh.above[atomicAdd(&sh.n_above, 1)] = full_key(k, id);      // fewer than `want`
+      });
     __syncthreads();
     na = sh.n_above;
     nt = kTies + 1;
@@ -155,61 +134,56 @@ __device__ void select_top(const T* row, int V, const Slice& sl, float mine, int
   if (na < want) {
     used_ties = nt;
     if (nt > kTies) {
-      // more equal elements than fit: take those of the lowest indices, in order, until there are enough
       const int need = want - na;
       int have = 0;
-      for (int base = sl.first; base < sl.last && have < need; base += NT) {
-        const int u = base + tid;
+      for (int base = 0; base < n_units && have < need; base += NT) {
         unsigned hits = 0;
-        if (u < sl.last) {
-          Unit<T> q;
-          read_unit(row, V, sl, u, q);
-          float x[8];
-          q.values(x);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int id = 8 * u + j - sl.pad;
-            if (id >= 0 && id < V && order_key(x[j]) == t) hits |= 1u << j;
-          }
-        }
-        int before = __popc(hits);
+        if (base + tid < n_units)
+          each_element<T>(units, sl, V, base + tid, [&](uint32_t k, int id) { hits |= k == t ? 1u << ((id + sl.pad) & 7) : 0u; });
+        int upto = __popc(hits);
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const int up = __shfl_up_sync(0xffffffffu, before, o);
-          if ((tid & 31) >= o) before += up;
+          const int up = __shfl_up_sync(0xffffffffu, upto, o);
+          if ((tid & 31) >= o) upto += up;
         }
         __syncthreads();
-        if ((tid & 31) == 31) sh.warp_count[tid >> 5] = before;
+        if ((tid & 31) == 31) sh.warp_count[tid >> 5] = upto;
         __syncthreads();
-        int at = have + before - __popc(hits), all = 0;
+        int at = have + upto - __popc(hits), all = 0;
         for (int w = 0; w < NT / 32; ++w) {
           if (w < (tid >> 5)) at += sh.warp_count[w];
           all += sh.warp_count[w];
         }
-        for (; hits && at < need; hits &= hits - 1, ++at) ties[at] = full_key(t, 8 * u + __ffs(hits) - 1 - sl.pad);
+        for (; hits && at < need; hits &= hits - 1, ++at)
+          ties[at] = full_key(t, 8 * (sl.first + base + tid) + __ffs(hits) - 1 - sl.pad);
         have += all;
       }
       used_ties = min(need, have);
       __syncthreads();
     }
   }
+  // four neighbouring lanes count for one key
   const int n = na + used_ties;
-  for (int i = tid; i < n; i += NT) {
-    const unsigned long long k = i < na ? sh.above[i] : ties[i - na];
+  for (int b = 0; b < 4 * n; b += NT) {
+    const int i = (b + tid) >> 2;
+    const unsigned long long k = i < na ? sh.above[i] : i < n ? ties[i - na] : 0ull;
     int rank = 0;
-    for (int j = 0; j < na; ++j) rank += sh.above[j] > k;
-    for (int j = 0; j < used_ties; ++j) rank += ties[j] > k;
-    if (rank < want) sh.sorted[rank] = k;
+    for (int j = tid & 3; j < na; j += 4) rank += sh.above[j] > k;
+    for (int j = tid & 3; j < used_ties; j += 4) rank += ties[j] > k;
+    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+    if (i < n && (tid & 3) == 0 && rank < want) sh.sorted[rank] = k;
   }
   __syncthreads();
 }
 
-// One row per cluster of `parts` blocks (one block where there are many rows).
+// One row per cluster of `parts` blocks, each block's slice of it in shared memory.
 template <typename T, int NT, bool TOP>
-__global__ void __launch_bounds__(NT) logprob_rows_kernel(const __grid_constant__ LogprobArgs a) {
+__global__ void __launch_bounds__(NT, 1024 / NT) logprob_rows_kernel(const __grid_constant__ LogprobArgs a) {
   __shared__ State per_warp[NT / 32];
   __shared__ State mine;
-  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ uint64_t bar;
+  extern __shared__ __align__(16) unsigned char units[];       // the slice; the selection's lists behind it
   const int part = a.parts > 1 ? (int)cluster_rank() : 0;
   const int64_t r = blockIdx.x / a.parts;
   const T* row = static_cast<const T*>(a.logits) + r * a.stride;
@@ -217,6 +191,7 @@ __global__ void __launch_bounds__(NT) logprob_rows_kernel(const __grid_constant_
   const Slice sl(V, row_pad(row), part, a.parts);
   const float c = a.s * kLog2e;
   const bool leader = part == 0 && tid == 0;
+  start_slice(row, V, sl, units, &bar);
 
   int token = -1;
   float x_token = 0.f;
@@ -224,34 +199,29 @@ __global__ void __launch_bounds__(NT) logprob_rows_kernel(const __grid_constant_
     token = a.tokens[r];
     if (token >= 0 && token < V) x_token = Elem<T>::get(row + token);
   }
+  __syncthreads();
+  const bool arrived = wait_slice(&bar);
 
   constexpr int N = sizeof(T) == 2 ? 4 : 2;
-  Stream<T> st(c);
-  const T* base = row - sl.pad;
-  int u = sl.full0 + tid;
-  for (; u + (N - 1) * NT < sl.full1; u += N * NT) {
+  const int n_units = sl.last - sl.first;
+  Stream<T, true, true> st(c);
+  int u = tid;
+  for (; u + (N - 1) * NT < n_units; u += N * NT) {
     Unit<T> q[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) load_unit(base + 8 * (int64_t)(u + i * NT), q[i]);
+    for (int i = 0; i < N; ++i) load_shared_unit(units, u + i * NT, q[i]);
     st.add(q);
   }
-  for (; u < sl.full1; u += NT) {
+  for (; u < n_units; u += NT) {
     Unit<T> q[1];
-    load_unit(base + 8 * (int64_t)u, q[0]);
+    load_shared_unit(units, u, q[0]);
     st.add(q);
   }
-  if (tid < 2 && sl.ragged(tid) >= 0) {
-    Unit<T> q[1];
-    load_ragged(row, V, sl.pad, sl.ragged(tid), q[0]);
-    st.add(q);
-  }
-  join_block<NT>(st.finish(), c, per_warp, &mine);
-  TopShared<NT>& sh = *reinterpret_cast<TopShared<NT>*>(dynamic);
-  int want = 0;
+  join_block<NT>(arrived ? st.finish() : State{0.f, nan_value(), nan_value()}, c, per_warp, &mine);
+  TopShared<NT>& sh = *reinterpret_cast<TopShared<NT>*>(units + a.slice_bytes);
   if (TOP) {
-    want = min(a.top_k, sl.length(V));
-    __syncthreads();
-    if (want > 0) select_top<T, NT>(row, V, sl, st.top(), want, sh);
+    const int want = min(a.top_k, sl.length(V));
+    if (want > 0) select_top<T, NT>(units, sl, V, st.top(), want, sh);
   }
   __syncthreads();
   State all = mine;
@@ -273,7 +243,7 @@ __global__ void __launch_bounds__(NT) logprob_rows_kernel(const __grid_constant_
       o[0] = all.m; o[1] = ln_z; o[2] = h; o[3] = lp;
     }
   }
-  if (TOP) {
+  if (TOP && part == 0) {
     int32_t* ids = a.top_ids + r * a.top_k;
     float* lps = a.top_logprob + r * a.top_k;
     auto write = [&](int rank, unsigned long long k) {
@@ -282,13 +252,13 @@ __global__ void __launch_bounds__(NT) logprob_rows_kernel(const __grid_constant_
       lps[rank] = all.m == -kInf ? -kInf : (x - all.m) * a.s - ln_z;
     };
     if (!(all.R == all.R)) {
-      for (int i = tid; part == 0 && i < a.top_k; i += NT) {
+      for (int i = tid; i < a.top_k; i += NT) {
         ids[i] = -1;
         lps[i] = nan_value();
       }
     } else if (a.parts == 1) {
       for (int i = tid; i < a.top_k; i += NT) write(i, sh.sorted[i]);
-    } else if (part == 0) {
+    } else {
       // the blocks' sorted lists, one behind the other in the candidates' place; a key's rank is its place in its
       // own list plus, for each other list, the number of keys above it there
       unsigned long long* lists = sh.above;
@@ -333,7 +303,7 @@ __global__ void __launch_bounds__(256) logprob_small_kernel(const __grid_constan
   else load_ragged(row, a.V, 0, lane, q[0]);
   float v[8];
   q[0].values(v);
-  Stream<T> st(c);
+  Stream<T, true, true> st(c);
   st.add(q);
   State all = st.finish();
 #pragma unroll
@@ -493,12 +463,12 @@ cudaError_t launch_logprobs(LogprobArgs a, cudaStream_t st) {
     return cudaGetLastError();
   }
   const bool wide = a.V >= 8192 || a.top_k > 64;
-  a.parts = parts_of_row(a.n_rows, a.V, 512);
-  if (wide)
-    return top ? launch_rows(logprob_rows_kernel<T, 512, true>, a.n_rows, a.parts, 512, sizeof(TopShared<512>), st, a)
-               : launch_rows(logprob_rows_kernel<T, 512, false>, a.n_rows, a.parts, 512, 0, st, a);
-  return top ? launch_rows(logprob_rows_kernel<T, 128, true>, a.n_rows, a.parts, 128, sizeof(TopShared<128>), st, a)
-             : launch_rows(logprob_rows_kernel<T, 128, false>, a.n_rows, a.parts, 128, 0, st, a);
+  a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));
+  a.slice_bytes = slice_bytes(a.V, sizeof(T), a.parts);
+  if (wide) return top ? launch_resident<logprob_rows_kernel<T, 256, true>, 256>(a, sizeof(TopShared<256>), st)
+                       : launch_resident<logprob_rows_kernel<T, 256, false>, 256>(a, 0, st);
+  return top ? launch_resident<logprob_rows_kernel<T, 128, true>, 128>(a, sizeof(TopShared<128>), st)
+             : launch_resident<logprob_rows_kernel<T, 128, false>, 128>(a, 0, st);
 }
 
 template <typename T>
@@ -540,7 +510,7 @@ extern "C" int remoe_token_logprobs(int32_t n_rows, int32_t vocab, int32_t dtype
   if (n_rows == 0) return REMOE_OK;
   PointerDevice dev(logits_dev);
   if (dev.err_code() != REMOE_OK) return dev.err_code();
-  const LogprobArgs a{logits_dev, row_stride, vocab, n_rows, 1, top_k, inv_temperature, tokens_dev,
+  const LogprobArgs a{logits_dev, row_stride, vocab, n_rows, 1, 0, top_k, inv_temperature, tokens_dev,
                       logprob_dev, entropy_dev, top_logprob_dev, row_stats_dev, top_ids_dev};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = dtype == REMOE_F32 ? launch_logprobs<float>(a, st)

@@ -185,6 +185,22 @@ def test_confident_rows(V, dtype):
     assert bool(((got["logprob"].double() - lp).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("V", [100, 3001, 20000])
+@pytest.mark.parametrize("s", [1e-30, 1e-4, 2e-3, 40.0, 1e5, 1e25])
+def test_temperatures(V, dtype, s):
+    x, _ = rows(4, V, dtype, scale=5.0)
+    x[0, ::3] = NINF
+    x[1] = torch.finfo(x.dtype).min               # lowest values beside masked ones
+    x[1, ::2] = NINF
+    x[1, :2000] = NINF
+    x[1, V - 1] = torch.finfo(x.dtype).min
+    x[2, ::2] *= 1000
+    check_logprobs(x, s, tokens_for(4, V, skip=0), 9)
+    for r in range(4):
+        check_logprobs(x[r:r + 1], s, tokens_for(1, V, skip=0), 9)
+
+
 GRAD_SIZES = [(1, 1), (4, 2), (3, 9), (40, 64), (6, 130), (5, 256), (5, 257), (3, 2033), (3, 2041), (2, 8200), (2, 20001)]
 
 
