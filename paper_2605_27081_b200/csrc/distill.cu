@@ -104,7 +104,52 @@ __device__ __forceinline__ ListSums warp_sum(ListSums v) {
   return v;
 }
 
-// One row per cluster of `parts` blocks, each block's slice of it in shared memory; at most one entry of the list a thread.
+// What a row's list comes to, before its row is known.
+struct ListSide {
+  ListSums sums;
+  float m_list;                    // largest logit of the list
+  double shift;                    // of the list's values: the largest (tail = 0), or 0
+  bool some, bad;                  // an entry with a probability; an entry that makes the row NaN
+};
+
+// Joins list and rest of a row; writes its loss and row_stats (`out`), and what its gradient needs to rs (`share`).
+__device__ __forceinline__ void finish_row(const DistillArgs& a, int64_t r, float weight, const State& rest, const ListSide& l, bool share, bool out,
+                                           RowShared& rs) {
+  const double s = a.s;
+  const ListSums& v = l.sums;
+  const float m = max_nan(rest.m, l.m_list);
+  const bool alive = m != -kInf, others = rest.m > -kInf;        // a NaN is alive
+  const double x_shift = l.m_list != -kInf ? (double)l.m_list : 0.0;
+  const double grow = 1.0 + (double)rest.R;
+  const double of_rest = others ? exp(((double)rest.m - m) * s) : 0.0, of_list = l.m_list != -kInf ? exp(((double)l.m_list - m) * s) : 0.0;
+  const double z = of_rest * grow + of_list * v.z, ln_z = log(z), ln_rest = log(grow);
+  const double of_q = a.tail || !l.some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !l.some ? 0.0 : l.shift + log(v.q);
+  const double q_all = v.q * of_q, q_rest = a.tail && others ? fmax(0.0, 1.0 - v.q) : 0.0;
+  const double ln_p_rest = ((double)rest.m - m) * s + ln_rest - ln_z;
+  double loss = (v.qy - v.qx) * of_q + (((double)m - x_shift) * s + ln_z - (ln_q - l.shift)) * q_all;
+  if (q_rest > 0.0) loss += q_rest * (log(q_rest) - ln_p_rest);
+  const double c_rest = others ? of_rest * grow / z - q_rest : 0.0;
+  const bool in = l.some && alive;
+  const float poison = l.bad ? nan_value() : 0.f;
+  if (share) {
+    rs.kind = l.bad || in;
+    rs.m_rest = others ? rest.m : 0.f;
+    rs.coef = (others ? (float)(s * weight * c_rest / grow) : 0.f) + poison;
+    rs.of_e = of_list / z + poison;
+    rs.of_q = of_q;
+    rs.weight = s * weight;
+  }
+  if (out) {
+    if (a.loss) a.loss[r] = (in ? (float)loss : 0.f) + poison;
+    if (a.stats) {
+      float* o = a.stats + 8 * r;
+      o[0] = m; o[1] = (float)ln_z; o[2] = rest.m; o[3] = others ? (float)ln_rest : -kInf;
+      o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = (in ? 1.f : 0.f) + poison; o[7] = 0.f;
+    }
+  }
+}
+
+// Few rows: one row per cluster of `parts` blocks, each block's slice of it in shared memory; at most one entry of the list a thread.
 //
 // While the slice is on its way, the list's side is computed: a few numbers, in 64 bits, since the loss is a small
 // difference of large terms.  Its sums are taken relative to the list's own largest element, so they wait for nothing.
@@ -225,35 +270,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
     const State rest = a.parts > 1 ? join_cluster(&mine, a.parts, c) : mine;
     ListSums v = warp_sums[0];
     for (int w = 1; w < W; ++w) { v.z += warp_sums[w].z; v.q += warp_sums[w].q; v.qy += warp_sums[w].qy; v.qx += warp_sums[w].qx; }
-    const float m = max_nan(rest.m, m_list);
-    const bool alive = m != -kInf, others = rest.m > -kInf;      // a NaN is alive
-    const double grow = 1.0 + (double)rest.R;
-    const double of_rest = others ? exp(((double)rest.m - m) * s) : 0.0, of_list = m_list != -kInf ? exp(((double)m_list - m) * s) : 0.0;
-    const double z = of_rest * grow + of_list * v.z, ln_z = log(z), ln_rest = log(grow);
-    const double of_q = a.tail || !some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !some ? 0.0 : shift + log(v.q);
-    const double q_all = v.q * of_q, q_rest = a.tail && others ? fmax(0.0, 1.0 - v.q) : 0.0;
-    const double ln_p_rest = ((double)rest.m - m) * s + ln_rest - ln_z;
-    double loss = (v.qy - v.qx) * of_q + (((double)m - x_shift) * s + ln_z - (ln_q - shift)) * q_all;
-    if (q_rest > 0.0) loss += q_rest * (log(q_rest) - ln_p_rest);
-    const double c_rest = others ? of_rest * grow / z - q_rest : 0.0;
-    if (tid == 0) {
-      const bool in = some && alive;
-      const float poison = s_bad ? nan_value() : 0.f;
-      rs.kind = s_bad || in;
-      rs.m_rest = others ? rest.m : 0.f;
-      rs.coef = (others ? (float)(s * weight * c_rest / grow) : 0.f) + poison;
-      rs.of_e = of_list / z + poison;
-      rs.of_q = of_q;
-      rs.weight = s * weight;
-      if (leader) {
-        if (a.loss) a.loss[r] = (in ? (float)loss : 0.f) + poison;
-        if (a.stats) {
-          float* o = a.stats + 8 * r;
-          o[0] = m; o[1] = (float)ln_z; o[2] = rest.m; o[3] = others ? (float)ln_rest : -kInf;
-          o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = (in ? 1.f : 0.f) + poison; o[7] = 0.f;
-        }
-      }
-    }
+    const ListSide list{v, m_list, shift, some, s_bad != 0};
+    finish_row(a, r, weight, rest, list, tid == 0, leader, rs);
   }
   if (a.parts > 1) {
     __syncwarp();
@@ -289,6 +307,337 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
     }
   }
   if (a.parts > 1) cluster_wait();                        // no block leaves while another reads its shared memory
+}
+
+// ---- many rows ---------------------------------------------------------------------------------------------------
+// Persistent blocks (logit_rows.cuh).  Warps of a block, each at its own pace:
+//   producer   issues the copies;
+//   list       a row ahead: the list's sums; then it takes the list's elements out of each chunk that arrives (-inf in
+//              shared memory) and passes the chunk on to the consumers, so their loop knows nothing of lists;
+//   consumers  sum what is left; with GRAD they wait for the row's figures, go over the row downwards and write the gradient;
+//   finisher   joins sums and list, writes the loss, gives the figures to the consumers, and puts the list's gradients over what
+//              they wrote once they say that the row is written.
+#ifndef DM_NT
+#define DM_NT 128
+#define DM_B 4
+#define DM_U 6
+#define DM_NB 3
+#define DM_GB 4
+#define DM_GU 6
+#define DM_GNB 4
+#endif
+template <typename T, bool GRAD>
+struct ManyShape {
+  static constexpr int kConsumers = DM_NT, kBlocks = GRAD ? DM_GB : DM_B, kSlots = GRAD ? DM_GNB : DM_NB;
+  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? (GRAD ? DM_GU : DM_U) : 4);
+  static constexpr int kThreads = kConsumers + 96;
+  static constexpr size_t kSmem = (size_t)kChunk * kSlots;
+};
+
+struct alignas(16) ListShared {
+  int id[kMaxList];                // -1: unused entry
+  float y[kMaxList], x[kMaxList];
+  unsigned char first[kMaxList];   // no entry before it has its id
+  ListSide side;
+  int twice;
+  unsigned loose[2];               // bits of the row's ragged units that are listed
+};
+
+template <typename T, bool GRAD>
+__global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRAD>::kBlocks) distill_pipe_kernel(const __grid_constant__ DistillArgs a) {
+  typedef ManyShape<T, GRAD> Shape;
+  constexpr int NT = Shape::kConsumers, NB = Shape::kSlots, CHUNK = Shape::kChunk, PAIR = NT + 32, LISTS = kMaxList / 32;
+  typedef Chunks<T, CHUNK> C;
+  constexpr int N = C::kUnits / NT;
+  __shared__ PipeShared<NB> ps;
+  __shared__ uint64_t passed[NB];              // chunks that the list warp is done with
+  __shared__ State per_warp[2][NT / 32];
+  __shared__ ListShared lists[2];
+  __shared__ RowShared rs;
+  extern __shared__ __align__(128) unsigned char ring_buffer[];
+  const int V = a.V, K = a.K, tid = threadIdx.x, lane = tid & 31;
+  const T* logits = static_cast<const T*>(a.logits);
+  const float c = a.s * kLog2e;
+  const double s = a.s;
+  RowWeights weights(a.weight, a.n_rows);
+  if (tid == 0) {
+    init_pipe(ps, NT / 32);
+    for (int i = 0; i < NB; ++i) ring::mbar_init(&passed[i], 1);
+    ring::mbar_fence_init();
+  }
+  __syncthreads();
+  const int role = tid < NT ? 0 : (tid - NT) / 32 + 1;
+
+  if (role == 3) {
+    produce<T, NB, CHUNK, GRAD>(ps, ring_buffer, logits, a.weight, a.stride, V, a.n_rows);
+    return;
+  }
+
+  if (role == 2) {                             // list
+    int id[LISTS];                             // of the row to come; entries lane, lane + 32, ...
+    float y[LISTS], x[LISTS];
+    auto fetch_entries = [&](int64_t q) {
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) {
+        id[i] = -1;
+        y[i] = -kInf;
+        if (q < a.n_rows && lane + 32 * i < K) {
+          id[i] = a.ids[q * K + lane + 32 * i];
+          y[i] = a.y[q * K + lane + 32 * i];
+        }
+      }
+    };
+    auto fetch_logits = [&](int64_t q) {
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) x[i] = id[i] >= 0 && id[i] < V ? Elem<T>::get(logits + q * a.stride + id[i]) : -kInf;
+    };
+    int i_row = weights.next(0);
+    fetch_entries(weights.row(i_row));
+    fetch_logits(weights.row(i_row));
+    SlotOrder<NB, GRAD> slots;
+    unsigned parity = 0;
+    int turn = 0, par = 0, done = 0;
+    bool ok = true;
+    while (weights.row(i_row) < a.n_rows) {
+      const int64_t r = weights.row(i_row);
+      ListShared& l = lists[par];
+      if (done >= 2) bar_sync<kBarListFree, 64>(par);
+      bool bad = false, some = false;
+      float m_list = -kInf, y_top = -kInf;
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) {
+        const int k = lane + 32 * i;
+        bad = bad || id[i] < -1 || id[i] >= V || (id[i] >= 0 && !(y[i] < kInf));
+        if (id[i] < 0 || id[i] >= V) { id[i] = -1; y[i] = -kInf; }
+        if (k < K) { l.id[k] = id[i]; l.y[k] = y[i]; l.x[k] = x[i]; }
+        m_list = max_nan(m_list, x[i]);
+        y_top = fmaxf(y_top, y[i]);
+      }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) {
+        m_list = max_nan(m_list, __shfl_xor_sync(0xffffffffu, m_list, o));
+        y_top = fmaxf(y_top, __shfl_xor_sync(0xffffffffu, y_top, o));
+      }
+      some = y_top > -kInf;
+      const double shift = a.tail || !some ? 0.0 : (double)y_top, x_shift = m_list != -kInf ? (double)m_list : 0.0;
+      __syncwarp();
+      ListSums sums{0.0, 0.0, 0.0, 0.0};
+      bool twice = false;
+      unsigned loose = 0;
+      const Slice sl(V, row_pad(logits + r * a.stride), 0, 1);
+      int at[LISTS];                           // chunk of the entry's element (-1: in none); its place in it below
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) {
+        const int k = lane + 32 * i;
+        at[i] = -1;
+        if (32 * i >= K) continue;
+        bool first = id[i] >= 0;
+        if (first) {
+          const int4* ids4 = reinterpret_cast<const int4*>(l.id);
+          for (int j = 0; j < (k >> 2); ++j) {
+            const int4 o = ids4[j];
+            first = first && o.x != id[i] && o.y != id[i] && o.z != id[i] && o.w != id[i];
+          }
+          for (int j = k & ~3; j < k; ++j) first = first && l.id[j] != id[i];
+          twice = twice || !first;
+          const int u = (id[i] + sl.pad) >> 3;
+          if (u >= sl.full0 && u < sl.full1) at[i] = (u - sl.full0) / C::kUnits;
+          else loose |= 1u << ((id[i] + sl.pad) & 7) << (u == sl.ragged(0) ? 0 : 8);
+        }
+        if (k < K) l.first[k] = first;
+        if (first && m_list != -kInf) sums.z += exp(((double)x[i] - m_list) * s);
+        if (y[i] > -kInf) {
+          const double q = exp((double)y[i] - shift);
+          if (q != 0.0) {
+            sums.q += q;
+            sums.qy += q * ((double)y[i] - shift);
+            sums.qx += q * (((double)x[i] - x_shift) * s);
+          }
+        }
+      }
+      sums = warp_sum(sums);
+      bad = __any_sync(0xffffffffu, bad);
+      twice = __any_sync(0xffffffffu, twice);
+      loose = __reduce_or_sync(0xffffffffu, loose);
+      if (lane == 0) {
+        l.side = ListSide{sums, m_list, shift, some, bad};
+        l.twice = twice;
+        l.loose[0] = loose & 0xffu;
+        l.loose[1] = loose >> 8;
+      }
+      bar_arrive<kBarList, 64>(par);
+      int now[LISTS];
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) now[i] = id[i];
+      i_row = weights.next(i_row + 1);
+      const int64_t next = weights.row(i_row);
+      fetch_entries(next);                     // a row ahead; their logits half a row later, when the ids are here
+      const int n = C::count(sl), loads = GRAD ? n + max(0, n - NB) : n;
+      for (int ld = 0; ld < loads; ++ld) {
+        const int ch = ld < n ? ld : 2 * n - NB - 1 - ld;
+        const int sv = GRAD ? slots.slot(ch) : turn;
+        if (!GRAD) turn = turn + 1 == NB ? 0 : turn + 1;
+        if (ok) ok = ring::mbar_wait(&ps.full[sv], parity >> sv & 1u);
+        parity ^= 1u << sv;
+        if (ld < n) {
+          T* const chunk = reinterpret_cast<T*>(ring_buffer + sv * CHUNK) + sl.pad - 8 * (sl.full0 + ch * C::kUnits);
+#pragma unroll
+          for (int i = 0; i < LISTS; ++i)
+            if (at[i] == ch) chunk[now[i]] = Elem<T>::masked();
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before a later copy goes over these writes
+        }
+        __syncwarp();
+        if (lane == 0) ring::mbar_arrive(&passed[sv]);
+        if (ld == loads / 2 && next < a.n_rows) fetch_logits(next);
+      }
+      if (GRAD) slots.end_row(n);
+      par ^= 1;
+      ++done;
+    }
+    return;
+  }
+
+  if (role == 1) {                             // finisher
+    int par = 0;
+    for (int i_row = 0; weights.row(i_row) < a.n_rows; ++i_row) {
+      const int64_t r = weights.row(i_row);
+      const float weight = weights.at(i_row);
+      if (weight == 0.f) {
+        if (lane == 0 && a.loss) a.loss[r] = 0.f;
+        if (lane < 8 && a.stats) a.stats[8 * r + lane] = 0.f;
+        continue;
+      }
+      const bool later = weights.row(weights.next(weights.next(i_row + 1) + 1)) < a.n_rows;      // a row will wait for this one's buffers
+      weights.at(i_row);
+      bar_sync<kBarList, 64>(par);
+      bar_sync<kBarReady, PAIR>(par);
+      const State rest = join_warps<NT>(per_warp[par], c);
+      ListShared& l = lists[par];
+      finish_row(a, r, weight, rest, l.side, lane == 0, lane == 0, rs);
+      if (GRAD) {
+        __syncwarp();
+        bar_arrive<kBarCoef, PAIR>(0);
+        double e[LISTS], q[LISTS];             // while the consumers write
+        const RowShared g = rs;
+        const ListSide side = l.side;
+        T* out = static_cast<T*>(a.d_logits) + r * a.d_stride;
+        if (g.kind != 0) {
+#pragma unroll
+          for (int i = 0; i < LISTS; ++i) {
+            const int k = lane + 32 * i;
+            e[i] = q[i] = 0.0;
+            if (k < K && l.first[k]) {
+              if (side.m_list != -kInf) e[i] = exp(((double)l.x[k] - side.m_list) * s);
+              for (int j = k; j < (l.twice ? K : k + 1); ++j)
+                if (l.id[j] == l.id[k] && l.y[j] > -kInf) q[i] += exp((double)l.y[j] - side.shift);
+            }
+          }
+        }
+        bar_sync<kBarWritten, PAIR>(0);
+        if (g.kind != 0) {
+#pragma unroll
+          for (int i = 0; i < LISTS; ++i) {
+            const int k = lane + 32 * i;
+            if (k < K && l.first[k]) Elem<T>::put(out + l.id[k], (float)(g.weight * (e[i] * g.of_e - q[i] * g.of_q)));
+          }
+        }
+      }
+      __syncwarp();
+      if (later) {
+        bar_arrive<kBarListFree, 64>(par);
+        bar_arrive<kBarFree, PAIR>(par);
+      }
+      par ^= 1;
+    }
+    return;
+  }
+
+  Consumer<NB, GRAD> in(ps);
+  int par = 0, done = 0;
+  for (int i_row = 0; weights.row(i_row) < a.n_rows; ++i_row) {
+    const int64_t r = weights.row(i_row);
+    const T* row = logits + r * a.stride;
+    T* out = GRAD ? static_cast<T*>(a.d_logits) + r * a.d_stride : nullptr;
+    if (weights.at(i_row) == 0.f) {
+      if (GRAD) write_elements(out, 0, V, NT, [](int) { return 0.f; });
+      continue;
+    }
+    const Slice sl(V, row_pad(row), 0, 1);
+    const int chunks = C::count(sl);
+    Unit<T> loose[1];
+    const bool has_loose = tid < 2 && sl.ragged(tid) >= 0;
+    if (has_loose) load_ragged(row, V, sl.pad, sl.ragged(tid), loose[0]);
+    if (done >= 2) bar_sync<kBarFree, PAIR>(par);
+    Stream<T, false, false> st(c);
+    for (int ch = 0; ch < chunks; ++ch) {
+      const int sv = in.slot(ch), n = C::units(sl, ch);
+      in.wait_for(passed, sv);
+      const unsigned char* units = ring_buffer + sv * CHUNK;
+      if (n == C::kUnits) {
+        Unit<T> q[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_shared_unit(units, tid + i * NT, q[i]);
+        st.add(q);
+      } else {
+#pragma unroll 1
+        for (int u = tid; u < n; u += NT) {
+          Unit<T> q[1];
+          load_shared_unit(units, u, q[0]);
+          st.add(q);
+        }
+      }
+      if (!GRAD || ch < chunks - NB) in.release(sv);
+    }
+    if (has_loose) {                           // the list warp has seen to whole units only
+      Unit<T> q[1] = {loose[0]};
+      const unsigned bits = lists[par].loose[tid];
+      float v[8];
+      q[0].values(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = bits >> j & 1u ? -kInf : v[j];
+      q[0].set(v);
+      st.add(q);
+    }
+    join_warp(in.ok ? st.finish() : State{0.f, nan_value(), nan_value()}, c, per_warp[par]);
+    bar_arrive<kBarReady, PAIR>(par);
+    if (GRAD) {
+      bar_sync<kBarCoef, PAIR>(0);
+      const int kind = rs.kind;
+      const float m_rest = rs.m_rest, coef = rs.coef;
+      const bool alike = row_pad(out) == sl.pad;
+      for (int ch = chunks - 1; ch >= 0; --ch) {
+        const int sv = in.slot(ch), n = C::units(sl, ch);
+        if (ch < chunks - NB) in.wait_for(passed, sv);
+        const unsigned char* units = ring_buffer + sv * CHUNK;
+        const int64_t u0 = sl.full0 + (int64_t)ch * C::kUnits;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int u = tid + i * NT;
+          if (u < n) {
+            Unit<T> q;
+            if (kind) {
+              load_shared_unit(units, u, q);
+              rest_grad_unit(q, m_rest, c, coef);
+            } else {
+              fill_unit(q, 0.f);
+            }
+            if (alike) store_unit(out - sl.pad + 8 * (u0 + u), q);
+            else store_ragged(out, V, sl.pad, (int)u0 + u, q);
+          }
+        }
+        in.release(sv);
+      }
+      in.slots.end_row(chunks);
+      if (has_loose) {
+        if (kind) rest_grad_unit(loose[0], m_rest, c, coef);
+        else fill_unit(loose[0], 0.f);
+        store_ragged(out, V, sl.pad, sl.ragged(tid), loose[0]);
+      }
+      bar_arrive<kBarWritten, PAIR>(0);
+    }
+    par ^= 1;
+    ++done;
+  }
 }
 
 // Rows of up to 256 elements: LPR lanes a row, eight elements a lane, the list laid out over the row's elements in shared
@@ -547,6 +896,9 @@ cudaError_t launch_distill(DistillArgs a, bool backward, cudaStream_t st) {
     distill_backward_kernel<T><<<(unsigned)blocks, kBackThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
+  if (many_rows(a.n_rows, a.V))
+    return a.d_logits ? launch_pipe<distill_pipe_kernel<T, true>, ManyShape<T, true>>(a, st)
+                      : launch_pipe<distill_pipe_kernel<T, false>, ManyShape<T, false>>(a, st);
   a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));
   a.slice_bytes = slice_bytes(a.V, sizeof(T), a.parts);
   if (a.V >= 8192 || a.K > 128)

@@ -22,6 +22,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "remoe.h"
 #include "tma_ring.cuh"
 
 namespace remoe {
@@ -310,6 +311,176 @@ __device__ __forceinline__ void start_slice(const T* row, int V, const Slice& sl
 // False if the copies have not arrived within the limit of a wait and of another one: the row is given up as NaN.
 __device__ __forceinline__ bool wait_slice(uint64_t* bar) { return ring::mbar_wait(bar, 0) || ring::mbar_wait(bar, 0); }
 
+// ---- many rows: a persistent block with a ring of chunks --------------------------------------------------------
+// With at least a row for every SM, blocks stay and take row after row.  The whole units of the rows pass through a ring of
+// NB chunks in shared memory, filled by bulk copies that run ahead over the ends of rows: while a row is joined, its
+// top elements are selected or its list is prepared, the next row is already on its way.  No cluster, so no waiting for
+// other blocks: two or three blocks an SM, each with its own rows.  One warp issues the copies; the others consume, each at
+// its own pace (a warp that is done with a chunk says so on the slot's `empty` barrier).
+//
+// With BACK a row is consumed twice, first upwards, then downwards for the gradient: its last NB chunks are still there, the
+// others come again (out of L2, which holds the rows in work).  Slots are taken in the order in which they become free.
+// For chunk c of a row of n >= NB chunks that is order[c % NB] in both passes, and it leaves the order reversed for the next row;
+// a shorter row leaves its unused slots first and its own, reversed, behind them.  Producer and consumers keep that order
+// each for themselves.
+template <int NB>
+struct PipeShared {
+  uint64_t full[NB], empty[NB];
+};
+
+template <int NB, bool BACK>
+struct SlotOrder {
+  static_assert(NB <= 8, "four bits a slot");
+  unsigned order = 0x76543210u;
+  __device__ __forceinline__ int slot(int c) const { return BACK ? order >> 4 * (c % NB) & 15u : 0; }
+  __device__ __forceinline__ void end_row(int n) {
+    unsigned next = 0;
+    const int m = min(n, NB);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int from = i < NB - m ? m + i : NB - 1 - i;
+      next |= (order >> 4 * from & 15u) << 4 * i;
+    }
+    order = next;
+  }
+};
+
+template <typename T, int CHUNK>              // CHUNK: bytes
+struct Chunks {
+  static constexpr int kUnits = CHUNK / (8 * (int)sizeof(T));
+  static __device__ __forceinline__ int count(const Slice& sl) { return sl.full1 > sl.full0 ? (sl.full1 - sl.full0 + kUnits - 1) / kUnits : 0; }
+  static __device__ __forceinline__ int units(const Slice& sl, int c) { return min(kUnits, sl.full1 - sl.full0 - c * kUnits); }
+};
+
+// Thread 0, before the block's first barrier.
+template <int NB>
+__device__ __forceinline__ void init_pipe(PipeShared<NB>& ps, int consumer_warps) {
+  for (int s = 0; s < NB; ++s) {
+    ring::mbar_init(&ps.full[s], 1);
+    ring::mbar_init(&ps.empty[s], (unsigned)consumer_warps);
+  }
+  ring::mbar_fence_init();
+}
+
+// Weights of a block's rows r0, r0 + step, ..., read 32 at a time, a lane each: a load waits behind the copies on their way.
+struct RowWeights {
+  const float* weight;                        // null: all 1
+  int64_t r0, step, n_rows;
+  float mine = 1.f;
+  int have = -1;
+  __device__ __forceinline__ RowWeights(const float* w, int64_t n) : weight(w), r0(blockIdx.x), step(gridDim.x), n_rows(n) {}
+  // Weight of the block's i-th row; whole warps.
+  __device__ __forceinline__ float at(int i) {
+    if (!weight) return 1.f;
+    if (i >> 5 != have) {
+      have = i >> 5;
+      const int64_t r = r0 + (int64_t)((i & ~31) + (int)(threadIdx.x & 31)) * step;
+      mine = r < n_rows ? weight[r] : 0.f;
+    }
+    return __shfl_sync(0xffffffffu, mine, i & 31);
+  }
+  __device__ __forceinline__ int64_t row(int i) const { return r0 + (int64_t)i * step; }
+  // The first row from i on that counts; its row() is n_rows or more if there is none.
+  __device__ __forceinline__ int next(int i) {
+    while (row(i) < n_rows && at(i) == 0.f) ++i;
+    return i;
+  }
+};
+
+// One warp: all copies of the block's rows, issued by its first lane.  Rows with weight 0 (weight may be null) are passed over.
+template <typename T, int NB, int CHUNK, bool BACK>
+__device__ void produce(PipeShared<NB>& ps, unsigned char* buf, const T* logits, const float* weight, int64_t stride, int V, int n_rows) {
+  typedef Chunks<T, CHUNK> C;
+  SlotOrder<NB, BACK> slots;
+  unsigned used = 0, parity = 0;              // by slot: loaded before; parity of its last load
+  int turn = 0;
+  bool ok = true;
+  RowWeights weights(weight, n_rows);
+  for (int i = weights.next(0); weights.row(i) < n_rows; i = weights.next(i + 1)) {
+    if ((threadIdx.x & 31) != 0 || !ok) continue;
+    const int64_t r = weights.row(i);
+    const T* row = logits + r * stride;
+    const Slice sl(V, row_pad(row), 0, 1);
+    const int n = C::count(sl), loads = BACK ? n + max(0, n - NB) : n;
+    const T* base = row - sl.pad + 8 * (int64_t)sl.full0;
+    for (int l = 0; l < loads; ++l) {
+      const int c = l < n ? l : 2 * n - NB - 1 - l;
+      const int s = BACK ? slots.slot(c) : turn;
+      if (!BACK) turn = turn + 1 == NB ? 0 : turn + 1;
+      if (used >> s & 1u) {
+        if (!ring::mbar_wait(&ps.empty[s], parity >> s & 1u)) { ok = false; break; }
+        parity ^= 1u << s;
+      }
+      used |= 1u << s;
+      const uint32_t bytes = (uint32_t)C::units(sl, c) * (8 * (uint32_t)sizeof(T));
+      ring::mbar_expect_tx(&ps.full[s], bytes);
+      ring::bulk_g2s(buf + (size_t)s * CHUNK, base + 8 * (int64_t)c * C::kUnits, bytes, &ps.full[s]);
+    }
+    if (BACK) slots.end_row(n);
+  }
+  // no copy is on its way when the thread leaves: each slot's last load has arrived (its parity is that of its `empty` phases)
+  for (int s = 0; s < NB; ++s)
+    if (used >> s & 1u) ring::mbar_wait(&ps.full[s], parity >> s & 1u);
+}
+
+// A consumer's side of the ring.
+template <int NB, bool BACK>
+struct Consumer {
+  PipeShared<NB>& ps;
+  SlotOrder<NB, BACK> slots;
+  unsigned parity = 0;
+  int turn = 0;
+  bool ok = true;                             // false once a wait has run out: what follows is NaN
+  __device__ __forceinline__ explicit Consumer(PipeShared<NB>& p) : ps(p) {}
+  __device__ __forceinline__ int slot(int c) const { return BACK ? slots.slot(c) : turn; }
+  __device__ __forceinline__ void wait(int s) {
+    if (ok) ok = ring::mbar_wait(&ps.full[s], parity >> s & 1u);
+  }
+  // The same on another barrier of the slot, which somebody passes the chunk on with.
+  __device__ __forceinline__ void wait_for(uint64_t* bars, int s) {
+    if (ok) ok = ring::mbar_wait(&bars[s], parity >> s & 1u);
+  }
+  // The warp is done with slot s.
+  __device__ __forceinline__ void release(int s) {
+    parity ^= 1u << s;
+    if (!BACK) turn = turn + 1 == NB ? 0 : turn + 1;
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) ring::mbar_arrive(&ps.empty[s]);
+  }
+};
+
+// Named barriers of a block.  kBarGroup: over a group of NT threads; kBarFinish: over each of the two groups of finishers; kBarReady,
+// kBarFree: between consumers and finishers, two each, by the row's parity; the others: see distill.cu.
+constexpr int kBarGroup = 1, kBarFinish = 2, kBarReady = 4, kBarFree = 6, kBarList = 8, kBarListFree = 10, kBarCoef = 12, kBarWritten = 13;
+template <int NT>
+__device__ __forceinline__ void sync_threads() { asm volatile("bar.sync %0, %1;" ::"n"(kBarGroup), "n"(NT) : "memory"); }
+
+// A group of threads of the block: its barrier.
+template <int NT>
+struct WholeGroup {                           // all consumers, or all threads of the block
+  static constexpr int kThreads = NT;
+  __device__ __forceinline__ void sync() const { sync_threads<NT>(); }
+};
+
+// One of two barriers, by the row's parity (their numbers are immediates: a register would claim all of the block's sixteen).
+template <int ID, int NT>
+__device__ __forceinline__ void bar_sync(int parity) {
+  if (parity) asm volatile("bar.sync %0, %1;" ::"n"(ID + 1), "n"(NT) : "memory");
+  else asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(NT) : "memory");
+}
+template <int NT>
+struct FinishGroup {                          // the finishers of the rows of one parity
+  static constexpr int kThreads = NT;
+  int parity;
+  __device__ __forceinline__ void sync() const { bar_sync<kBarFinish, NT>(parity); }
+};
+template <int ID, int NT>
+__device__ __forceinline__ void bar_arrive(int parity) {
+  __threadfence_block();
+  if (parity) asm volatile("bar.arrive %0, %1;" ::"n"(ID + 1), "n"(NT) : "memory");
+  else asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(NT) : "memory");
+}
+
 // ---- one-pass sums -------------------------------------------------------------------------------------------
 
 struct State {
@@ -401,6 +572,20 @@ struct Stream {
     if (ENTROPY) U = fma2(e, clamp ? pack2(max_nan(d0, -200.f), max_nan(d1, -200.f)) : d, U);   // 2^-200 is 0 in float32
   }
 
+  // For callers that want the largest element of each of several segments: ends one (its largest is top() before the call), and
+  // folds it into `all`, the largest element so far; finish() is called with M = all.
+  __device__ __forceinline__ void close_segment(typename Elem<T>::Word& all) {
+    typename Elem<T>::Word lo = M;
+    Elem<T>::order(all, lo);
+    if (far) {
+      accumulate(mul2(add2(Elem<T>::widen(lo), pack2(-ref, -ref)), pack2(c, c)), true);
+    } else {
+      if (ENTROPY) lo = Elem<T>::lift(lo);
+      accumulate(fma2(Elem<T>::widen(lo), pack2(c, c), pack2(-k, -k)), !Elem<T>::kLifts);
+    }
+    M = Elem<T>::lowest();
+  }
+
   // Largest element seen (-inf if none; NaN if there was one).
   __device__ __forceinline__ float top() const {
     float a, b;
@@ -437,13 +622,31 @@ __device__ __forceinline__ State shuffle_down(const State& s, int by, int width)
                __shfl_down_sync(0xffffffffu, s.U, by, width)};
 }
 
+// The same with one barrier, which the caller has: each warp's state before it, the block's in every lane of the calling
+// warp behind it.
+__device__ __forceinline__ void join_warp(State s, float c, State* per_warp) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s = merge(s, shuffle_down(s, o, 32), c);
+  if ((threadIdx.x & 31) == 0) per_warp[threadIdx.x >> 5] = s;
+}
+template <int NT>
+__device__ __forceinline__ State join_warps(const State* per_warp, float c) {
+  constexpr int W = NT / 32;
+  const int lane = threadIdx.x & 31;
+  State s = lane < W ? per_warp[lane] : State{-kInf, 0.f, 0.f};
+#pragma unroll
+  for (int o = 16; o; o >>= 1)
+    if (o < W) s = merge(s, shuffle_down(s, o, 32), c);
+  return State{__shfl_sync(0xffffffffu, s.m, 0), __shfl_sync(0xffffffffu, s.R, 0), __shfl_sync(0xffffffffu, s.U, 0)};
+}
+
 // Joins the threads' states in a fixed order; the result is in *out (shared memory) after a __syncthreads().
 template <int NT>
 __device__ __forceinline__ void join_block(State s, float c, State* per_warp, State* out) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) s = merge(s, shuffle_down(s, o, 32), c);
   if ((threadIdx.x & 31) == 0) per_warp[threadIdx.x >> 5] = s;
-  __syncthreads();
+  sync_threads<NT>();
   if (threadIdx.x < 32) {
     constexpr int W = NT / 32;
     s = threadIdx.x < W ? per_warp[threadIdx.x] : State{-kInf, 0.f, 0.f};

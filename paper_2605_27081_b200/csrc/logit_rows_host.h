@@ -99,5 +99,19 @@ inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStrea
   return cudaLaunchKernelEx(&cfg, Kernel, args);
 }
 
+// Rows enough for persistent blocks that take whole rows.
+inline bool many_rows(int32_t n_rows, int32_t vocab) { return vocab >= 8192 && n_rows >= 148; }
+
+// One launch of persistent blocks.
+template <auto Kernel, typename Shape, typename Args>
+inline cudaError_t launch_pipe(const Args& args, cudaStream_t stream) {
+  static std::atomic<bool> ready[kMaxDevices];
+  const cudaError_t e = allow_dynamic_smem(Kernel, Shape::kSmem, ready);
+  if (e != cudaSuccess) return e;
+  const int most = 148 * Shape::kBlocks;
+  Kernel<<<(unsigned)(args.n_rows < most ? args.n_rows : most), Shape::kThreads, Shape::kSmem, stream>>>(args);
+  return cudaGetLastError();
+}
+
 }  // namespace rows
 }  // namespace remoe

@@ -4,13 +4,24 @@
 //   p = softmax(s x), lp = s (x_token - m) - ln Z, H = ln Z - (1/Z) sum s (x - m) e^{s (x - m)}
 //   dx = s [ g_lp (1[v = token] - p) - g_H p (ln p + H) ]
 #include "logit_rows.cuh"
+#ifndef MANY_NT
+#define MANY_NT 128
+#define MANY_B 5
+#define MANY_U 6
+#define MANY_NB 3
+#define MANY_NTT 256
+#define MANY_BT 2
+#define MANY_UT 6
+#define MANY_NBT 2
+#define MANY_FT 128
+#define MANY_G 1
+#define MANY_AT 6
+#endif
 #include "logit_rows_host.h"
 
 namespace remoe {
 namespace rows {
 
-constexpr int kCandidates = 1536;       // elements above the threshold that one block can hold
-constexpr int kTies = 512;              // elements equal to it
 constexpr int kSmallVocab = 256;        // up to here a row is held by a group of lanes, one unit per lane
 
 struct LogprobArgs {
@@ -23,166 +34,348 @@ struct LogprobArgs {
   int32_t* top_ids;
 };
 
-// Shared memory of the selection.  Keys hold (value, then lowest index first): all distinct.
-template <int NT>
-struct TopShared {
-  static_assert(kCandidates + kTies >= 8 * REMOE_ROWS_MAX_TOP, "the lists of eight blocks");
-  unsigned long long above[kCandidates + kTies];      // the ties' list lies behind it; both hold the lists of a join later
+// Shared memory of the selection: room for CAND keys, COLUMNS groups to look at again.  Keys hold (value, then lowest index
+// first): all distinct, none zero.
+template <int CAND, int COLUMNS>
+struct alignas(16) TopShared {
+  static constexpr int kCand = CAND, kColumns = COLUMNS;
+  static_assert(CAND >= 2 * REMOE_ROWS_MAX_TOP && CAND % 8 == 0, "");
+  unsigned long long cand[CAND + 8];
   unsigned long long sorted[REMOE_ROWS_MAX_TOP];
-  int columns[NT];
-  int n_columns, n_above, n_ties;
-  int warp_count[NT / 32];
+  unsigned short columns[COLUMNS];
+  int n_columns, n_cand;
+  int warp_count[16];
 };
 
 __device__ __forceinline__ unsigned long long full_key(uint32_t k, int id) { return ((unsigned long long)k << 32) | (0xffffffffu - (uint32_t)id); }
 
-// A block's slice in shared memory, as the selection looks at it: calls f(key, id) for the elements of unit i.
-template <typename T, typename F>
-__device__ __forceinline__ void each_element(const unsigned char* units, const Slice& sl, int V, int i, F f) {
-  Unit<T> q;
-  load_shared_unit(units, i, q);
+// What the selection looks at: units 0 .. n_units - 1, unit i holding the elements from 8 i + id0 on, those of [0, V) valid.
+// NT threads have each seen some of them; key(i): of the largest element that thread i has seen (0: none).  A column is a
+// group of units whose largest element is known; bit g of columns(i, t): column(i, g) of thread i may reach t.
+//
+// A block's slice in shared memory; column t: units t, t + NT, ...
+template <typename T, int NT>
+struct SharedSource {
+  static constexpr int kKeys = NT, kAtOnce = 4;
+  const unsigned char* units;
+  int n_units, id0, V;
+  const uint32_t* keys;
+  __device__ __forceinline__ uint32_t key(int i) const { return keys[i]; }
+  __device__ __forceinline__ void load(int i, Unit<T>& q) const { load_shared_unit(units, i, q); }
+  __device__ __forceinline__ int per_column() const { return (n_units + NT - 1) / NT; }
+  __device__ __forceinline__ int loose() const { return 0; }           // units in no column
+  __device__ __forceinline__ int loose_unit(int) const { return -1; }
+  __device__ __forceinline__ int unit(int column, int k) const {
+    const int i = column + k * NT;
+    return i < n_units ? i : -1;
+  }
+  __device__ __forceinline__ unsigned columns(int, uint32_t) const { return 1u; }
+  __device__ __forceinline__ int column(int i, int) const { return i; }
+};
+// A row in memory that passed through a pipe; column (segment, t): thread t's units of the segment's chunks.
+constexpr int kSegments = 16;
+template <typename T, int NT, int UNITS>
+struct RowSource {
+  static constexpr int kKeys = NT, kAtOnce = MANY_AT;
+  const T* row;
+  int n_units, id0, V, full0, full1, pad;
+  const uint32_t* keys;
+  const unsigned short* seg;                       // [segment][NT] upper halves of the keys of the largest elements
+  int segments, seg_chunks;
+  __device__ __forceinline__ uint32_t key(int i) const { return keys[i]; }
+  __device__ __forceinline__ void load(int i, Unit<T>& q) const {
+    if (i >= full0 && i < full1) load_unit(row - pad + 8 * (int64_t)i, q);
+    else load_ragged(row, V, pad, i, q);
+  }
+  __device__ __forceinline__ int per_column() const { return seg_chunks * (UNITS / NT); }
+  __device__ __forceinline__ int loose() const { return 2; }
+  __device__ __forceinline__ int loose_unit(int i) const { return i == 0 ? (full0 > 0 ? 0 : -1) : (full1 < n_units && n_units - 1 >= full0 ? n_units - 1 : -1); }
+  __device__ __forceinline__ int unit(int column, int k) const {
+    const int i = full0 + (column / NT) * seg_chunks * UNITS + k * NT + column % NT;
+    return i < full1 ? i : -1;
+  }
+  __device__ __forceinline__ unsigned columns(int i, uint32_t t) const {
+    unsigned hits = 0;
+#pragma unroll
+    for (int g = 0; g < kSegments; ++g) hits |= seg[g * NT + i] >= t >> 16 ? 1u << g : 0u;
+    return hits & ((1u << segments) - 1u);
+  }
+  __device__ __forceinline__ int column(int i, int g) const { return g * NT + i; }
+};
+
+// Bit j: element j of unit i, held in q, is valid and above `least` (or equal to it, where `equal`).
+template <typename T, typename Source>
+__device__ __forceinline__ unsigned hits_of(const Source& src, int i, const Unit<T>& q, float least, bool equal) {
   float v[8];
   q.values(v);
+  unsigned hits = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int id = 8 * (sl.first + i) + j - sl.pad;
-    if (id >= 0 && id < V) f(order_key(v[j]), id);
+  for (int j = 0; j < 8; ++j) hits |= v[j] > least || (equal && v[j] == least) ? 1u << j : 0u;
+  const int lo = -(8 * i + src.id0), hi = src.V - (8 * i + src.id0);
+  return hits & (lo > 0 ? 0xffu << lo : 0xffu) & (hi < 8 ? (1u << max(hi, 0)) - 1u : 0xffu);
+}
+template <typename T>
+__device__ __forceinline__ float element_of(const Unit<T>& q, int j) {
+  float v[8];
+  q.values(v);
+  float x = v[0];
+#pragma unroll
+  for (int m = 1; m < 8; ++m) x = j == m ? v[m] : x;
+  return x;
+}
+__device__ __forceinline__ int scan_warp(int n) {        // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, n, o);
+    if ((threadIdx.x & 31) >= o) n += up;
   }
+  return n;
 }
 
-// Elements of the slice at or above `t`.
-template <typename T, int NT>
-__device__ int count_keys(const unsigned char* units, const Slice& sl, int V, uint32_t t, int* warp_count) {
-  int n = 0;
-  for (int i = threadIdx.x; i < sl.last - sl.first; i += NT) each_element<T>(units, sl, V, i, [&](uint32_t k, int) { n += k >= t; });
+// Sum over the group's threads, in every one.
+template <typename Group>
+__device__ __forceinline__ int group_sum(const Group& group, int tid, int n, int* warp_count) {
   n = __reduce_add_sync(0xffffffffu, n);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) warp_count[threadIdx.x >> 5] = n;
-  __syncthreads();
+  if ((tid & 31) == 0) warp_count[tid >> 5] = n;
+  group.sync();
   int all = 0;
-  for (int w = 0; w < NT / 32; ++w) all += warp_count[w];
+#pragma unroll
+  for (int w = 0; w < Group::kThreads / 32; ++w) all += warp_count[w];
+  group.sync();
   return all;
 }
 
-// The `want` largest elements of the slice, sorted, to sh.sorted.
+// The `want` largest elements of the source, sorted, to sh.sorted, by a group of FT threads (tid: 0 .. FT - 1).
 //
-// A thread has kept the largest of its elements (units tid, tid + NT, ...).  The want-th largest of these NT numbers is a
-// lower bound t for the want-th largest element, and only threads whose largest reaches t hold such elements: their
-// units (a few per cent of the slice) are looked at again, and what is above t is sorted by counting for each
-// the keys above it.  t may be rounded down to fewer bits, which adds candidates and never loses one.
-// Elements equal to t matter only where too few are above it.  Where few threads hold t they are listed with the others;
-// in masked rows nearly all elements are equal, and those of the lowest indices are taken in one ordered scan that
-// stops as soon as there are enough.  Rows whose large elements sit in few threads overflow the list: then the
-// want-th largest value is found by its bits, with a count over the slice for each.
-template <typename T, int NT>
-__device__ void select_top(const unsigned char* units, const Slice& sl, int V, float mine, int want, TopShared<NT>& sh) {
-  const int tid = threadIdx.x, n_units = sl.last - sl.first;
-  unsigned long long* const ties = sh.above + kCandidates;
-  uint32_t t = 0;
-  const uint32_t key = mine == mine && tid < n_units ? order_key(mine) : 0;   // no unit: below all values
-  if (tid == 0) sh.n_columns = sh.n_above = sh.n_ties = 0;
-  constexpr int kLow = Elem<T>::kUnusedBits;          // the key's bits that say nothing for a 16-bit type
-  int holders = NT;                                   // threads whose largest is at least t
-  for (int b = 31; b >= kLow; --b) {
-    const uint32_t cand = t | (1u << b);
-    const int n = __syncthreads_count(key >= cand);
-    if (n >= want) {
-      t = cand;
-      holders = n;
-      if (n <= want + want / 4 + 4) break;
-    }
-  }
-  if (!(t & 0x80000000u)) t |= (1u << kLow) - 1u;      // they are ones in a negative value's key
-  const bool list_ties = holders <= 2 * want + 32;
-  __syncthreads();
-  if (key > t || (list_ties && key == t)) sh.columns[atomicAdd(&sh.n_columns, 1)] = tid;
-  __syncthreads();
-  const int nc = sh.n_columns, rounds = (n_units + NT - 1) / NT;
-  auto push = [&](uint32_t k, int id) {
-    if (k > t) {
-      const int i = atomicAdd(&sh.n_above, 1);
-      if (i < kCandidates) sh.above[i] = full_key(k, id);
-    } else if (list_ties && k == t) {
-      const int i = atomicAdd(&sh.n_ties, 1);
-      if (i < kTies) ties[i] = full_key(k, id);
-    }
-  };
-  for (int w = tid; w < nc * rounds; w += NT) {
-    const int i = (w / nc) * NT + sh.columns[w % nc];
-    if (i < n_units) each_element<T>(units, sl, V, i, push);
-  }
-  __syncthreads();
-  int na = sh.n_above, nt = list_ties ? sh.n_ties : kTies + 1;
-  if (na > kCandidates) {
-    __syncthreads();
-    uint32_t v = 0;
-    for (int b = 31; b >= 0; --b)
-      if (count_keys<T, NT>(units, sl, V, v | (1u << b), sh.warp_count) >= want) v |= 1u << b;
-    t = v;
-    __syncthreads();
-    if (tid == 0) sh.n_above = 0;
-    __syncthreads();
-    for (int i = tid; i < n_units; i += NT)
-      each_element<T>(units, sl, V, i, [&](uint32_t k, int id) {
-        if (k > t) sh.above[atomicAdd(&sh.n_above, 1)] = full_key(k, id);      // fewer than `want`
-      });
-    __syncthreads();
-    na = sh.n_above;
-    nt = kTies + 1;
-  }
-  int used_ties = 0;
-  if (na < want) {
-    used_ties = nt;
-    if (nt > kTies) {
-      const int need = want - na;
-      int have = 0;
-      for (int base = 0; base < n_units && have < need; base += NT) {
-        unsigned hits = 0;
-        if (base + tid < n_units)
-          each_element<T>(units, sl, V, base + tid, [&](uint32_t k, int id) { hits |= k == t ? 1u << ((id + sl.pad) & 7) : 0u; });
-        int upto = __popc(hits);
+// If t is such that `want` of the source's keys reach it, it is a lower bound of the want-th largest element, and only
+// columns whose largest reaches t hold such elements: their units (a few per cent) are looked at again, what reaches t is
+// listed, and the list is sorted by counting for each key the keys above it.  A lower t adds candidates and never
+// loses an element.
+// First t: each warp finds the value that its share of `want` of its part of the keys reach, by bits, and the least of these is
+// taken; one barrier.  Where that lets too much through, or a warp's share is large, t is found over the whole group, a
+// barrier for each bit.
+// In masked rows nearly all elements are equal and t is their value.  Then only what is above t is listed, and what is missing
+// are the elements equal to t of the lowest indices, found in one ordered scan that stops as soon as there are enough.
+// Rows whose large elements sit in few columns overflow the list all the same: there the want-th largest value is found by
+// its bits, with a count over the source for each.
+// Lists are filled with one addition per warp, the places within it from a scan: an addition for each entry, one behind
+// the other, took 140 cycles an entry.
+template <typename T, typename Group, typename Source, typename Shared>
+__device__ void select_top(const Group& group, const Source& src, int tid, int want, Shared& sh) {
+  constexpr int FT = Group::kThreads, kLow = Elem<T>::kUnusedBits, W = FT / 32, KPT = Source::kKeys / FT;   // kLow: the key's bits that say nothing
+  constexpr uint32_t kMasked = 0x007fffffu;                                           // key of -inf, the least there is
+  static_assert(Source::kKeys % FT == 0, "");
+  const int n_units = src.n_units, lane = tid & 31;
+  uint32_t key[KPT];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int up = __shfl_up_sync(0xffffffffu, upto, o);
-          if ((tid & 31) >= o) upto += up;
-        }
-        __syncthreads();
-        if ((tid & 31) == 31) sh.warp_count[tid >> 5] = upto;
-        __syncthreads();
-        int at = have + upto - __popc(hits), all = 0;
-        for (int w = 0; w < NT / 32; ++w) {
-          if (w < (tid >> 5)) at += sh.warp_count[w];
-          all += sh.warp_count[w];
-        }
-        for (; hits && at < need; hits &= hits - 1, ++at)
-          ties[at] = full_key(t, 8 * (sl.first + base + tid) + __ffs(hits) - 1 - sl.pad);
-        have += all;
+  for (int i = 0; i < KPT; ++i) key[i] = src.key(tid + i * FT);
+  auto reach = [&](uint32_t x) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) n += key[i] >= x;
+    return n;
+  };
+  // Places for n entries of each lane in a list whose length is *length.
+  auto places = [&](int n, int* length) {
+    const int upto = scan_warp(n);
+    int at = 0;
+    if (lane == 31 && upto) at = atomicAdd(length, upto);
+    return __shfl_sync(0xffffffffu, at, 31) + upto - n;
+  };
+  uint32_t t = 0;
+  bool equal = true;                                      // elements equal to t are listed, too
+  int n_cand = Shared::kCand + 1;
+  for (int attempt = 4 * want <= Source::kKeys && n_units >= Source::kKeys ? 0 : 1; attempt < 2 && n_cand > Shared::kCand; ++attempt) {
+    t = 0;
+    if (tid == 0) sh.n_columns = sh.n_cand = 0;
+    if (attempt == 0) {
+      const int share = (want + W - 1) / W;
+      static_assert(Source::kKeys / W < 1024, "three counts in one word");
+      for (int b = 30; b >= (kLow & ~1); b -= 2) {         // two bits at a time
+        const uint32_t one = 1u << b;
+        const unsigned n = __reduce_add_sync(0xffffffffu, (unsigned)reach(t + one) | (unsigned)reach(t + 2 * one) << 10 | (unsigned)reach(t + 3 * one) << 20);
+        const int n1 = n & 1023u, n2 = n >> 10 & 1023u, n3 = n >> 20;
+        const int m = n3 >= share ? 3 : n2 >= share ? 2 : n1 >= share ? 1 : 0;
+        t += m * one;
+        const int got = m == 3 ? n3 : m == 2 ? n2 : n1;
+        if (m && got <= share + share / 8 + 1) break;
       }
-      used_ties = min(need, have);
-      __syncthreads();
+      if (lane == 0) sh.warp_count[tid >> 5] = (int)t;
+      group.sync();
+#pragma unroll
+      for (int w = 0; w < W; ++w) t = min(t, (uint32_t)sh.warp_count[w]);
+      group.sync();
+    } else {
+      for (int b = 31; b >= kLow; --b) {
+        const uint32_t cand = t | (1u << b);
+        const int n = group_sum(group, tid, reach(cand), sh.warp_count);
+        if (n >= want) {
+          t = cand;
+          if (n <= want + want / 4 + 4) break;
+        }
+      }
+    }
+    if (!(t & 0x80000000u)) t |= (1u << kLow) - 1u;      // ones in a negative value's key
+    t = max(t, kMasked);
+    equal = group_sum(group, tid, reach(t), sh.warp_count) <= 2 * want + 32;
+    unsigned mine[KPT];
+    int n_mine = 0;
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+      mine[i] = key[i] > t || (equal && key[i] == t) ? src.columns(tid + i * FT, t) : 0u;
+      n_mine += __popc(mine[i]);
+    }
+    int at = places(n_mine, &sh.n_columns);
+#pragma unroll
+    for (int i = 0; i < KPT; ++i)
+      for (; mine[i]; mine[i] &= mine[i] - 1, ++at)
+        if (at < Shared::kColumns) sh.columns[at] = (unsigned short)src.column(tid + i * FT, __ffs(mine[i]) - 1);
+    group.sync();
+    const int nc = sh.n_columns;
+    if (nc <= Shared::kColumns) {
+      const float least = key_value(t);
+      const int per = src.per_column(), groups = nc + (src.loose() ? 1 : 0);
+      // eight lanes a column, kAtOnce columns at once; the loose units as one more column
+      constexpr int kAtOnce = Source::kAtOnce;
+      for (int k0 = 0; k0 < per; k0 += 8)
+        for (int g0 = tid >> 3; g0 - (tid >> 3 & 3) < groups; g0 += FT / 8 * kAtOnce) {
+          Unit<T> q[kAtOnce];
+          int unit[kAtOnce];
+          const int k = k0 + (tid & 7);
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) {
+            const int g = g0 + i * (FT / 8);
+            unit[i] = -1;
+            if (g < nc) unit[i] = k < per ? src.unit(sh.columns[g], k) : -1;
+            else if (g == nc && k < src.loose()) unit[i] = src.loose_unit(k);
+            if (unit[i] >= 0) src.load(unit[i], q[i]);
+          }
+          unsigned long long hits = 0;
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i)
+            if (unit[i] >= 0) hits |= (unsigned long long)hits_of<T>(src, unit[i], q[i], least, equal) << 8 * i;
+          int place = places(__popcll(hits), &sh.n_cand);
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i)
+            for (unsigned h = (unsigned)(hits >> 8 * i) & 0xffu; h; h &= h - 1, ++place) {
+              const int m = __ffs(h) - 1;
+              if (place < Shared::kCand) sh.cand[place] = full_key(order_key(element_of<T>(q[i], m)), 8 * unit[i] + m + src.id0);
+            }
+        }
+    }
+    group.sync();
+    n_cand = nc <= Shared::kColumns ? sh.n_cand : Shared::kCand + 1;
+    group.sync();
+  }
+  if (n_cand > Shared::kCand) {
+    uint32_t v = 0;
+    for (int b = 31; b >= 0; --b) {
+      const uint32_t cand = v | 1u << b;
+      int n = 0;
+      if (cand > kMasked) {
+        const float least = key_value(cand);
+        for (int i = tid; i < n_units; i += FT) {
+          Unit<T> q;
+          src.load(i, q);
+          n += __popc(hits_of<T>(src, i, q, least, true));
+        }
+      } else {
+        n = tid == 0 ? src.V : 0;                         // all of them
+      }
+      if (group_sum(group, tid, n, sh.warp_count) >= want) v = cand;
+    }
+    t = max(v, kMasked);
+    equal = false;
+    if (tid == 0) sh.n_cand = 0;
+    group.sync();
+    for (int i = tid; i < n_units; i += FT) {             // fewer than `want` elements in all
+      Unit<T> q;
+      src.load(i, q);
+      for (unsigned h = hits_of<T>(src, i, q, key_value(t), false); h; h &= h - 1) {
+        const int m = __ffs(h) - 1, place = atomicAdd(&sh.n_cand, 1);
+        if (place < Shared::kCand) sh.cand[place] = full_key(order_key(element_of<T>(q, m)), 8 * i + m + src.id0);
+      }
+    }
+    group.sync();
+    n_cand = min(sh.n_cand, want);
+  }
+  if (n_cand < want && !equal) {
+    const float least = key_value(t);
+    for (int base = 0; base < n_units && n_cand < want; base += FT) {
+      unsigned hits = 0;
+      if (base + tid < n_units) {
+        Unit<T> q;
+        src.load(base + tid, q);
+        hits = hits_of<T>(src, base + tid, q, least, true) & ~hits_of<T>(src, base + tid, q, least, false);
+      }
+      const int upto = scan_warp(__popc(hits));
+      if (lane == 31) sh.warp_count[tid >> 5] = upto;
+      group.sync();
+      int at = n_cand + upto - __popc(hits), all = 0;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (w < (tid >> 5)) at += sh.warp_count[w];
+        all += sh.warp_count[w];
+      }
+      group.sync();
+      for (; hits && at < want; hits &= hits - 1, ++at) sh.cand[at] = full_key(t, 8 * (base + tid) + __ffs(hits) - 1 + src.id0);
+      n_cand = min(want, n_cand + all);
     }
   }
-  // four neighbouring lanes count for one key
-  const int n = na + used_ties;
-  for (int b = 0; b < 4 * n; b += NT) {
-    const int i = (b + tid) >> 2;
-    const unsigned long long k = i < na ? sh.above[i] : i < n ? ties[i - na] : 0ull;
+  if (tid < 8) sh.cand[n_cand + tid] = 0ull;              // the counts below take eight keys at a time
+  group.sync();
+  for (int i = tid; i < n_cand; i += FT) {
+    const unsigned long long k = sh.cand[i];
     int rank = 0;
-    for (int j = tid & 3; j < na; j += 4) rank += sh.above[j] > k;
-    for (int j = tid & 3; j < used_ties; j += 4) rank += ties[j] > k;
-    rank += __shfl_xor_sync(0xffffffffu, rank, 1);
-    rank += __shfl_xor_sync(0xffffffffu, rank, 2);
-    if (i < n && (tid & 3) == 0 && rank < want) sh.sorted[rank] = k;
+    for (int j = 0; j < n_cand; j += 8) {
+      ulonglong2 o[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = *reinterpret_cast<const ulonglong2*>(&sh.cand[j + 2 * m]);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) rank += (o[m].x > k) + (o[m].y > k);
+    }
+    if (rank < want) sh.sorted[rank] = k;
   }
-  __syncthreads();
+  group.sync();
 }
 
-// One row per cluster of `parts` blocks, each block's slice of it in shared memory.
+__device__ __forceinline__ uint32_t top_key(float top) { return top == top ? order_key(top) : 0u; }
+
+// What a row's outputs come from, once it is joined.
+struct RowResult {
+  State all;
+  float ln_z;
+};
+__device__ __forceinline__ RowResult row_result(const State& all) { return RowResult{all, all.m == -kInf ? -kInf : log1pf(all.R)}; }
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, const RowResult& w, int token, float x_token) {
+  const bool none = w.all.m == -kInf;
+  const float h = none ? 0.f : w.ln_z - kLn2 * w.all.U / (1.f + w.all.R);
+  float lp = 0.f;
+  if (token >= 0 && token < a.V) lp = none ? -kInf : (x_token - w.all.m) * a.s - w.ln_z;
+  else if (token != -1) lp = nan_value();
+  if (a.logprob) a.logprob[r] = lp;
+  if (a.entropy) a.entropy[r] = h;
+  if (a.stats) {
+    float* o = a.stats + 4 * r;
+    o[0] = w.all.m; o[1] = w.ln_z; o[2] = h; o[3] = lp;
+  }
+}
+__device__ __forceinline__ void write_alternative(const LogprobArgs& a, int64_t r, const RowResult& w, int rank, unsigned long long key) {
+  const float x = key_value((uint32_t)(key >> 32));
+  const bool bad = !(w.all.R == w.all.R);
+  a.top_ids[r * a.top_k + rank] = bad ? -1 : (int32_t)(0xffffffffu - (uint32_t)key);
+  a.top_logprob[r * a.top_k + rank] = bad ? nan_value() : w.all.m == -kInf ? -kInf : (x - w.all.m) * a.s - w.ln_z;
+}
+
+typedef TopShared<8 * REMOE_ROWS_MAX_TOP, 256> FewShared;   // room for the lists of a cluster's eight blocks
+
+// Few rows: one row per cluster of `parts` blocks, each block's slice of it in shared memory.
 template <typename T, int NT, bool TOP>
 __global__ void __launch_bounds__(NT, 1024 / NT) logprob_rows_kernel(const __grid_constant__ LogprobArgs a) {
   __shared__ State per_warp[NT / 32];
   __shared__ State mine;
   __shared__ uint64_t bar;
+  __shared__ uint32_t keys[TOP ? NT : 1];                      // each thread reads its own
   extern __shared__ __align__(16) unsigned char units[];       // the slice; the selection's lists behind it
   const int part = a.parts > 1 ? (int)cluster_rank() : 0;
   const int64_t r = blockIdx.x / a.parts;
@@ -218,10 +411,12 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_rows_kernel(const __gri
     st.add(q);
   }
   join_block<NT>(arrived ? st.finish() : State{0.f, nan_value(), nan_value()}, c, per_warp, &mine);
-  TopShared<NT>& sh = *reinterpret_cast<TopShared<NT>*>(units + a.slice_bytes);
+  FewShared& sh = *reinterpret_cast<FewShared*>(units + a.slice_bytes);
   if (TOP) {
     const int want = min(a.top_k, sl.length(V));
-    if (want > 0) select_top<T, NT>(units, sl, V, st.top(), want, sh);
+    const SharedSource<T, NT> src{units, n_units, 8 * sl.first - sl.pad, V, keys};
+    keys[tid] = tid < n_units ? top_key(st.top()) : 0u;
+    if (want > 0) select_top<T>(WholeGroup<NT>{}, src, tid, want, sh);
   }
   __syncthreads();
   State all = mine;
@@ -229,39 +424,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_rows_kernel(const __gri
     cluster_sync();
     if (part == 0) all = join_cluster(&mine, a.parts, c);
   }
-  const float ln_z = all.m == -kInf ? -kInf : log1pf(all.R);
-  if (leader) {
-    const bool none = all.m == -kInf;
-    const float h = none ? 0.f : ln_z - kLn2 * all.U / (1.f + all.R);
-    float lp = 0.f;
-    if (token >= 0 && token < V) lp = none ? -kInf : (x_token - all.m) * a.s - ln_z;
-    else if (token != -1) lp = nan_value();
-    if (a.logprob) a.logprob[r] = lp;
-    if (a.entropy) a.entropy[r] = h;
-    if (a.stats) {
-      float* o = a.stats + 4 * r;
-      o[0] = all.m; o[1] = ln_z; o[2] = h; o[3] = lp;
-    }
-  }
+  const RowResult res = row_result(all);
+  if (leader) write_row(a, r, res, token, x_token);
   if (TOP && part == 0) {
-    int32_t* ids = a.top_ids + r * a.top_k;
-    float* lps = a.top_logprob + r * a.top_k;
-    auto write = [&](int rank, unsigned long long k) {
-      const float x = key_value((uint32_t)(k >> 32));
-      ids[rank] = (int32_t)(0xffffffffu - (uint32_t)k);
-      lps[rank] = all.m == -kInf ? -kInf : (x - all.m) * a.s - ln_z;
-    };
-    if (!(all.R == all.R)) {
-      for (int i = tid; i < a.top_k; i += NT) {
-        ids[i] = -1;
-        lps[i] = nan_value();
-      }
-    } else if (a.parts == 1) {
-      for (int i = tid; i < a.top_k; i += NT) write(i, sh.sorted[i]);
+    if (a.parts == 1 || !(all.R == all.R)) {
+      for (int i = tid; i < a.top_k; i += NT) write_alternative(a, r, res, i, sh.sorted[i]);
     } else {
       // the blocks' sorted lists, one behind the other in the candidates' place; a key's rank is its place in its
       // own list plus, for each other list, the number of keys above it there
-      unsigned long long* lists = sh.above;
+      unsigned long long* lists = sh.cand;
       const int K = a.top_k;
       for (int i = tid; i < a.parts * K; i += NT) {
         const int p = i / K, j = i - p * K;
@@ -283,11 +454,137 @@ __global__ void __launch_bounds__(NT, 1024 / NT) logprob_rows_kernel(const __gri
           }
           rank += lo;
         }
-        if (rank < K) write(rank, k);
+        if (rank < K) write_alternative(a, r, res, rank, k);
       }
     }
   }
   if (a.parts > 1) cluster_sync();       // no block leaves while another reads its shared memory
+}
+
+typedef TopShared<768, 1024> ManyShared;
+
+// Shape of the persistent blocks: threads that consume, threads that finish rows, blocks an SM, units of a chunk for each
+// consumer, chunks in the ring.
+template <typename T, bool TOP>
+struct ManyShape {
+  static constexpr int kConsumers = TOP ? MANY_NTT : MANY_NT, kFinishers = TOP ? MANY_FT : 32, kGroups = TOP ? MANY_G : 1, kBlocks = TOP ? MANY_BT : MANY_B;
+  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? (TOP ? MANY_UT : MANY_U) : 4), kSlots = TOP ? MANY_NBT : MANY_NB;
+  static constexpr int kThreads = kConsumers + 32 + kGroups * kFinishers;
+  static constexpr size_t kSegBytes = (size_t)kSegments * kConsumers * sizeof(short);
+  static constexpr size_t kSmem = (size_t)kChunk * kSlots + (TOP ? kGroups * sizeof(ManyShared) + 2 * kSegBytes : 0);
+};
+
+// What the consumers hand over at the end of a row, twice.
+template <int NT, bool TOP>
+struct Handover {
+  State per_warp[NT / 32];
+  uint32_t keys[TOP ? NT : 1];
+};
+
+// Many rows: persistent blocks, each takes row after row through its ring of chunks.  One warp issues the copies, the
+// consumers sum, and two groups of finishers, each for every second row, join a row's sums, select its top elements and write
+// while the consumers are at the next rows (two ahead at most).  A finisher's loads queue behind the copies on their way to
+// the SM, 3 to 5 us, which is why there are two groups.
+template <typename T, bool TOP>
+__global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>::kBlocks) logprob_pipe_kernel(const __grid_constant__ LogprobArgs a) {
+  typedef ManyShape<T, TOP> Shape;
+  constexpr int NT = Shape::kConsumers, FT = Shape::kFinishers, NB = Shape::kSlots, CHUNK = Shape::kChunk, ALL = NT + FT;          // of a handover
+  typedef Chunks<T, CHUNK> C;
+  constexpr int N = C::kUnits / NT;
+  static_assert(C::kUnits % NT == 0, "whole units for every thread");
+  __shared__ PipeShared<NB> ps;
+  __shared__ Handover<NT, TOP> over[2];
+  extern __shared__ __align__(128) unsigned char ring_buffer[];
+  const int V = a.V, tid = threadIdx.x;
+  const T* logits = static_cast<const T*>(a.logits);
+  const float c = a.s * kLog2e;
+  if (tid == 0) init_pipe(ps, NT / 32);
+  __syncthreads();
+
+  if (tid >= NT + Shape::kGroups * FT) {       // the last warp
+    produce<T, NB, CHUNK, false>(ps, ring_buffer, logits, nullptr, a.stride, V, a.n_rows);
+    return;
+  }
+  unsigned char* const lists = ring_buffer + NB * CHUNK;
+  auto segments_of = [&](int parity) { return reinterpret_cast<unsigned short*>(lists + Shape::kGroups * sizeof(ManyShared) + parity * Shape::kSegBytes); };
+  if (tid >= NT) {
+    constexpr int G = Shape::kGroups;
+    const int g = (tid - NT) / FT, ft = (tid - NT) % FT;         // with two groups, each has the rows of one parity
+    ManyShared& sh = *reinterpret_cast<ManyShared*>(lists + g * sizeof(ManyShared));
+    const FinishGroup<FT> group{g};
+    int par = g;
+    for (int64_t r = (int64_t)blockIdx.x + g * (int64_t)gridDim.x; r < a.n_rows; r += G * (int64_t)gridDim.x, par ^= G & 1) {
+      const T* row = logits + r * a.stride;
+      const Slice sl(V, row_pad(row), 0, 1);
+      int token = -1;
+      T x_token = Elem<T>::masked();
+      if (ft == 0 && a.tokens) {
+        token = a.tokens[r];
+        if (token >= 0 && token < V) x_token = row[token];
+      }
+      bar_sync<kBarReady, ALL>(par);
+      const Handover<NT, TOP>& o = over[par];
+      const RowResult res = row_result(join_warps<NT>(o.per_warp, c));
+      if (ft == 0) write_row(a, r, res, token, Elem<T>::get(&x_token));
+      if (TOP) {
+        const int chunks = C::count(sl), seg_chunks = (chunks + kSegments - 1) / kSegments;
+        const RowSource<T, NT, C::kUnits> src{row, sl.last, -sl.pad, V, sl.full0, sl.full1, sl.pad, o.keys, segments_of(par), (chunks + seg_chunks - 1) / seg_chunks, seg_chunks};
+        select_top<T>(group, src, ft, a.top_k, sh);
+        for (int i = ft; i < a.top_k; i += FT) write_alternative(a, r, res, i, sh.sorted[i]);
+        group.sync();                          // the lists are free again
+      }
+      if (r + 2 * (int64_t)gridDim.x < a.n_rows) bar_arrive<kBarFree, ALL>(par);
+    }
+    return;
+  }
+
+  int par = 0;                                 // parity of the block's row
+  Consumer<NB, false> in(ps);
+  for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x, par ^= 1) {
+    const T* row = logits + r * a.stride;
+    const Slice sl(V, row_pad(row), 0, 1);
+    const int chunks = C::count(sl), seg_chunks = (chunks + kSegments - 1) / kSegments;
+    unsigned short* const seg = segments_of(par);
+    Unit<T> loose[1];
+    const bool has_loose = tid < 2 && sl.ragged(tid) >= 0;
+    if (has_loose) load_ragged(row, V, sl.pad, sl.ragged(tid), loose[0]);
+    if (r >= 2 * (int64_t)gridDim.x) bar_sync<kBarFree, ALL>(par);
+    Stream<T, true, true> st(c);
+    typename Elem<T>::Word all = Elem<T>::lowest();
+    for (int ch = 0, in_seg = 0, g = 0; ch < chunks; ++ch) {
+      const int s = in.slot(ch), n = C::units(sl, ch);
+      in.wait(s);
+      const unsigned char* units = ring_buffer + s * CHUNK;
+      if (n == C::kUnits) {
+        Unit<T> q[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) load_shared_unit(units, tid + i * NT, q[i]);
+        st.add(q);
+      } else {
+#pragma unroll 1
+        for (int u = tid; u < n; u += NT) {
+          Unit<T> q[1];
+          load_shared_unit(units, u, q[0]);
+          st.add(q);
+        }
+      }
+      in.release(s);
+      if (TOP && (++in_seg == seg_chunks || ch + 1 == chunks)) {
+        seg[g * NT + tid] = (unsigned short)(top_key(st.top()) >> 16);
+        st.close_segment(all);
+        in_seg = 0;
+        ++g;
+      }
+    }
+    if (has_loose) st.add(loose);
+    if (TOP) {
+      st.close_segment(all);
+      st.M = all;
+      over[par].keys[tid] = top_key(st.top());
+    }
+    join_warp(in.ok ? st.finish() : State{0.f, nan_value(), nan_value()}, c, over[par].per_warp);
+    bar_arrive<kBarReady, ALL>(par);
+  }
 }
 
 // Rows of up to 256 elements: LPR lanes a row, eight elements a lane, all in registers.
@@ -462,12 +759,16 @@ cudaError_t launch_logprobs(LogprobArgs a, cudaStream_t st) {
     else logprob_small_kernel<T, 32><<<((unsigned)a.n_rows + 7) / 8, 256, 0, st>>>(a);
     return cudaGetLastError();
   }
+  if (many_rows(a.n_rows, a.V) && (!top || a.V >= 32768)) {
+    return top ? launch_pipe<logprob_pipe_kernel<T, true>, ManyShape<T, true>>(a, st)
+               : launch_pipe<logprob_pipe_kernel<T, false>, ManyShape<T, false>>(a, st);
+  }
   const bool wide = a.V >= 8192 || a.top_k > 64;
   a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));
   a.slice_bytes = slice_bytes(a.V, sizeof(T), a.parts);
-  if (wide) return top ? launch_resident<logprob_rows_kernel<T, 256, true>, 256>(a, sizeof(TopShared<256>), st)
+  if (wide) return top ? launch_resident<logprob_rows_kernel<T, 256, true>, 256>(a, sizeof(FewShared), st)
                        : launch_resident<logprob_rows_kernel<T, 256, false>, 256>(a, 0, st);
-  return top ? launch_resident<logprob_rows_kernel<T, 128, true>, 128>(a, sizeof(TopShared<128>), st)
+  return top ? launch_resident<logprob_rows_kernel<T, 128, true>, 128>(a, sizeof(FewShared), st)
              : launch_resident<logprob_rows_kernel<T, 128, false>, 128>(a, 0, st);
 }
 

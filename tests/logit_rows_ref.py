@@ -79,23 +79,23 @@ def distill(logits, s, ids, y, tail, weight):
     y = torch.where(used, y.double(), torch.full_like(y, NINF, dtype=torch.float64))
     some = (y > NINF).any(1)
     if not tail:
-        y = y - torch.where(some, y.logsumexp(1), torch.zeros(T, dtype=torch.float64)).unsqueeze(1)
+        y = y - torch.where(some, y.logsumexp(1), torch.zeros(T, dtype=torch.float64, device=logits.device)).unsqueeze(1)
     q = y.exp()
-    listed = torch.zeros(T, V, dtype=torch.int32).scatter_add_(1, i, used.int()) > 0
+    listed = torch.zeros(T, V, dtype=torch.int32, device=logits.device).scatter_add_(1, i, used.int()) > 0
     ln_p = lp.gather(1, i)
     loss = torch.where(q > 0, q * (y - ln_p), torch.zeros_like(q)).sum(1)
     size = torch.where(q > 0, q * (y.abs() + ln_p.abs() + 1), torch.zeros_like(q)).sum(1)
     outside = lp.masked_fill(listed, NINF)
     others = (outside > NINF).any(1)
-    p_rest = torch.where(others, outside.masked_fill(~others.unsqueeze(1), 0.0).logsumexp(1).exp(), torch.zeros(T, dtype=torch.float64))
-    q_rest = (1 - q.sum(1)).clamp(min=0) if tail else torch.zeros(T, dtype=torch.float64)
+    p_rest = torch.where(others, outside.masked_fill(~others.unsqueeze(1), 0.0).logsumexp(1).exp(), torch.zeros(T, dtype=torch.float64, device=logits.device))
+    q_rest = (1 - q.sum(1)).clamp(min=0) if tail else torch.zeros(T, dtype=torch.float64, device=logits.device)
     q_rest = torch.where(others, q_rest, torch.zeros_like(q_rest))
     both = q_rest > 0
     ln_pr = torch.where(others, outside.masked_fill(~others.unsqueeze(1), 0.0).logsumexp(1), torch.zeros_like(p_rest))
     loss = loss + torch.where(both, q_rest * (q_rest.clamp(min=1e-300).log() - ln_pr), torch.zeros_like(loss))
     size = size + torch.where(both, q_rest * (q_rest.clamp(min=1e-300).log().abs() + ln_pr.abs() + 1), torch.zeros_like(loss))
     p = lp.exp()
-    qd = torch.zeros(T, V, dtype=torch.float64).scatter_add_(1, i, q * used)
+    qd = torch.zeros(T, V, dtype=torch.float64, device=logits.device).scatter_add_(1, i, q * used)
     soft_rest = torch.where(others.unsqueeze(1), (outside - ln_pr.unsqueeze(1)).exp(), torch.zeros_like(p)).masked_fill(listed, 0.0)
     dx = torch.where(listed, p - qd, soft_rest * (p_rest - q_rest).unsqueeze(1))
     dsize = torch.where(listed, p + qd, soft_rest * (p_rest + q_rest).unsqueeze(1))
@@ -106,10 +106,11 @@ def distill(logits, s, ids, y, tail, weight):
             "grad": (dx * (s * w).unsqueeze(1)).masked_fill(zero, 0.0), "grad_size": (dsize * (s * w.abs()).unsqueeze(1)).masked_fill(zero, 0.0)}
 
 
-def check_grad(got, want, size, vocab, what=""):
-    """A gradient against its 64-bit value: one rounding to its type, and the float32 arithmetic behind it."""
+def check_grad(got, want, size, vocab, what="", factor=1.0):
+    """A gradient against its 64-bit value: one rounding to its type, and the float32 arithmetic behind it.  An
+    exponential below 2^-126 is flushed to zero before it is multiplied by up to `factor` (temperature times weight)."""
     fi = torch.finfo(got.dtype)
-    tol = want.abs() * (fi.eps / 2) + size * (2 * rel(vocab) + 40 * U) + fi.smallest_normal * fi.eps / 2 + 2.0 ** -126
+    tol = want.abs() * (fi.eps / 2) + size * (2 * rel(vocab) + 40 * U) + fi.smallest_normal * fi.eps / 2 + 2.0 ** -126 * max(1.0, factor)
     err = (got.double() - want).abs()
     assert bool((err <= tol).all()), (what, float((err - tol).max()), float(err.max()))
 

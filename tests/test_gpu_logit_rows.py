@@ -59,8 +59,7 @@ def logprobs(view, s, tokens, top, stats=True):
 
 def check_logprobs(view, s, tokens, top):
     V = view.shape[1]
-    x = view.cpu()
-    got, want = logprobs(view, s, tokens, top), ref.logprobs(x, s, tokens.cpu(), top)
+    got, want = logprobs(view, s, tokens, top), {k: v.cpu() for k, v in ref.logprobs(view, s, tokens, top).items()}
     tz, lnv = ref.rel(V), math.log(V + 1)
     ref.close(got["logprob"], want["logprob"], tz + ref.U * (8 * want["logprob"].abs() + 2 * lnv), "logprob")
     ref.close(got["entropy"], want["entropy"], (1 + 2 * lnv) * tz + ref.U * 4 * lnv, "entropy")
@@ -94,6 +93,21 @@ def test_logprobs_sizes(T, V, dtype):
         top = min(V, 1 + (T * 7 + V) % 23)
         check_logprobs(view, s, tokens_for(T, V), top)
         check_logprobs(view, s, tokens_for(T, V), 0)
+
+
+# rows enough for the persistent blocks: fewer rows than blocks, more, several a block; rows shorter than the ring, longer
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("T,V,top", [(148, 8192, 0), (150, 9001, 1), (297, 12288, 256), (700, 8199, 30), (160, 33001, 64), (310, 65536, 20), (149, 150001, 100)])
+def test_logprobs_many_rows(T, V, top, dtype):
+    for pad, offset, s in [(0, 0, 1.0), (1, 3, 0.7)]:
+        view, _ = rows(T, V, dtype, seed=V, pad=pad, offset=offset)
+        sp = special_rows(V, view.dtype)
+        view[5:5 + sp.shape[0]] = sp.cuda()
+        view[-sp.shape[0]:] = sp.cuda()
+        view[30, 7] = NAN
+        view[31, V - 1] = INF
+        view[32, (torch.arange(V, device="cuda") // 8) % 512 < 200] += 40
+        check_logprobs(view, s, tokens_for(T, V), top)
 
 
 @pytest.mark.parametrize("dtype", list(DT))
@@ -287,9 +301,9 @@ def test_backward_leaves_out_and_poisons():
 def teacher(x, K, s, seed=5, kind="near"):
     """ids [T, K] and log probabilities of a teacher near the student, on the CPU."""
     g = torch.Generator().manual_seed(seed)
-    t = torch.log_softmax((x.double() + torch.randn(x.shape, generator=g).double()) * s, 1)
+    t = torch.log_softmax((x.cuda().double() + torch.randn(x.shape, generator=g).cuda().double()) * s, 1)
     v, i = t.topk(K, 1)
-    return i.int().contiguous(), v.float().contiguous()
+    return i.int().cpu().contiguous(), v.float().cpu().contiguous()
 
 
 def run_distill(view, s, ids, y, tail, weight, out=None, stats=False):
@@ -305,21 +319,22 @@ def run_distill(view, s, ids, y, tail, weight, out=None, stats=False):
 
 def check_distill(view, s, ids, y, tail, weight, oplace=(0, 0)):
     T, V = view.shape
-    want = ref.distill(view.cpu(), s, ids, y, tail, weight)
     ids, y, weight = ids.cuda(), y.cuda(), weight.cuda()
+    want = ref.distill(view, s, ids, y, tail, weight)
+    factor = s * float(weight.abs().max())
     code = {torch.float32: rb.REMOE_F32, torch.bfloat16: rb.REMOE_BF16, torch.float16: rb.REMOE_F16}[view.dtype]
     tol = want["size"].nan_to_num(0, posinf=0) * (ref.rel(V) + 4 * ref.U) + ref.U * want["loss"].abs().nan_to_num(0, posinf=0)
     loss, _ = run_distill(view, s, ids, y, tail, weight)
-    ref.close(loss.cpu(), want["loss"], tol, "loss")
+    ref.close(loss, want["loss"], tol, "loss")
     out, flat = place(torch.zeros(T, V, dtype=view.dtype), *oplace)
     before = flat.clone()
     loss2, st = run_distill(view, s, ids, y, tail, weight, out, stats=True)
     assert torch.equal(loss.nan_to_num(9.0), loss2.nan_to_num(9.0))
-    ref.check_grad(out.cpu(), want["grad"], want["grad_size"], V, "gradient with the loss")
+    ref.check_grad(out, want["grad"], want["grad_size"], V, "gradient with the loss", factor)
     untouched(out, flat, before)
     out2, flat2 = place(torch.zeros(T, V, dtype=view.dtype), *oplace)
     assert rb.remoe_distill_topk_backward(T, V, code, view, view.stride(0), s, ids.shape[1], ids, y, st, weight, out2, out2.stride(0), stream()) == 0
-    ref.check_grad(out2.cpu(), want["grad"], want["grad_size"], V, "gradient apart")
+    ref.check_grad(out2, want["grad"], want["grad_size"], V, "gradient apart", factor)
     untouched(out2, flat2, before)
     for apart in (False, True):                    # in place
         again = view.clone(memory_format=torch.preserve_format)
@@ -349,6 +364,30 @@ def test_distill_sizes(T, V, K, dtype, tail):
         weight[::3] *= -1 if T > 2 else 1
         if T > 1:
             weight[1] = 0.0
+        check_distill(view, s, ids, y, tail, weight, oplace)
+
+
+# rows enough for the persistent blocks: rows of one chunk, of fewer chunks than the ring has, of more; several rows a block
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("T,V,K", [(148, 8192, 1), (150, 9001, 256), (700, 8199, 30), (1300, 8192, 5), (160, 33001, 64), (310, 65536, 20), (149, 150001, 100), (900, 20011, 33)])
+def test_distill_many_rows(T, V, K, dtype, tail):
+    for pad, offset, oplace, s in [(0, 0, (0, 0), 1.0), (1, 3, (1, 3), 0.7), (5, 0, (2, 1), 1.5)]:
+        view, _ = rows(T, V, dtype, seed=V + K, pad=pad, offset=offset)
+        sp = special_rows(V, view.dtype)
+        g = torch.Generator().manual_seed(6)
+        ids, y = teacher(view.cpu(), K, s)
+        weight = torch.rand(T, generator=g) + 0.5
+        weight[torch.rand(T, generator=g) < 0.3] = 0.0
+        weight[::7] *= -1
+        view[3:3 + sp.shape[0]] = sp.cuda()
+        view[-sp.shape[0]:] = sp.cuda()
+        ids[20, 0] = V - 1                              # the ends of a row
+        ids[21:25, K - 1] = 0
+        if K > 4:
+            ids[30:60, 1] = -1
+            ids[40:70, 3] = ids[40:70, 2]               # an id twice
+            ids[50] = -1
         check_distill(view, s, ids, y, tail, weight, oplace)
 
 
