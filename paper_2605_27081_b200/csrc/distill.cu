@@ -312,8 +312,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
 // ---- many rows ---------------------------------------------------------------------------------------------------
 // Persistent blocks (logit_rows.cuh).  Warps of a block, each at its own pace:
 //   producer   issues the copies;
-//   list       a row ahead: the list's sums; then it takes the list's elements out of each chunk that arrives (-inf in
-//              shared memory) and passes the chunk on to the consumers, so their loop knows nothing of lists;
+//   listers    two, for every second row each, up to two rows ahead: read the lists and compute their sums (two dependent loads
+//              behind the copies on their way take 5 us each);
+//   passer     takes the list's elements out of each chunk that arrives (-inf in shared memory) and passes the chunk on to the
+//              consumers, so their loop knows nothing of lists;
 //   consumers  sum what is left; with GRAD they wait for the row's figures, go over the row downwards and write the gradient;
 //   finisher   joins sums and list, writes the loss, gives the figures to the consumers, and puts the list's gradients over what
 //              they wrote once they say that the row is written.
@@ -322,15 +324,16 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
 #define DM_B 4
 #define DM_U 6
 #define DM_NB 3
+#define DM_GNT 128
 #define DM_GB 4
 #define DM_GU 6
 #define DM_GNB 4
 #endif
 template <typename T, bool GRAD>
 struct ManyShape {
-  static constexpr int kConsumers = DM_NT, kBlocks = GRAD ? DM_GB : DM_B, kSlots = GRAD ? DM_GNB : DM_NB;
+  static constexpr int kConsumers = GRAD ? DM_GNT : DM_NT, kBlocks = GRAD ? DM_GB : DM_B, kSlots = GRAD ? DM_GNB : DM_NB;
   static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? (GRAD ? DM_GU : DM_U) : 4);
-  static constexpr int kThreads = kConsumers + 96;
+  static constexpr int kThreads = kConsumers + 160;
   static constexpr size_t kSmem = (size_t)kChunk * kSlots;
 };
 
@@ -339,9 +342,10 @@ struct alignas(16) ListShared {
   float y[kMaxList], x[kMaxList];
   unsigned char first[kMaxList];   // no entry before it has its id
   ListSide side;
-  int twice;
+  int twice;                       // an id stands in the list more than once
   unsigned loose[2];               // bits of the row's ragged units that are listed
 };
+constexpr int kHash = 2 * kMaxList;   // table in which the lister looks for ids that come twice
 
 template <typename T, bool GRAD>
 __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRAD>::kBlocks) distill_pipe_kernel(const __grid_constant__ DistillArgs a) {
@@ -353,6 +357,7 @@ __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRA
   __shared__ uint64_t passed[NB];              // chunks that the list warp is done with
   __shared__ State per_warp[2][NT / 32];
   __shared__ ListShared lists[2];
+  __shared__ __align__(16) int seen_by[2][kHash];
   __shared__ RowShared rs;
   extern __shared__ __align__(128) unsigned char ring_buffer[];
   const int V = a.V, K = a.K, tid = threadIdx.x, lane = tid & 31;
@@ -368,110 +373,121 @@ __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRA
   __syncthreads();
   const int role = tid < NT ? 0 : (tid - NT) / 32 + 1;
 
-  if (role == 3) {
+  if (role == 5) {
     produce<T, NB, CHUNK, GRAD>(ps, ring_buffer, logits, a.weight, a.stride, V, a.n_rows);
     return;
   }
 
-  if (role == 2) {                             // list
-    int id[LISTS];                             // of the row to come; entries lane, lane + 32, ...
-    float y[LISTS], x[LISTS];
-    auto fetch_entries = [&](int64_t q) {
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) {
-        id[i] = -1;
-        y[i] = -kInf;
-        if (q < a.n_rows && lane + 32 * i < K) {
-          id[i] = a.ids[q * K + lane + 32 * i];
-          y[i] = a.y[q * K + lane + 32 * i];
-        }
-      }
-    };
-    auto fetch_logits = [&](int64_t q) {
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) x[i] = id[i] >= 0 && id[i] < V ? Elem<T>::get(logits + q * a.stride + id[i]) : -kInf;
-    };
+  if (role >= 3) {                             // listers
+    const int par = role - 3;
+    int* const seen = seen_by[par];
     int i_row = weights.next(0);
-    fetch_entries(weights.row(i_row));
-    fetch_logits(weights.row(i_row));
-    SlotOrder<NB, GRAD> slots;
-    unsigned parity = 0;
-    int turn = 0, par = 0, done = 0;
-    bool ok = true;
-    while (weights.row(i_row) < a.n_rows) {
+    if (par) i_row = weights.next(i_row + 1);
+    for (int done = 0; weights.row(i_row) < a.n_rows; i_row = weights.next(weights.next(i_row + 1) + 1), ++done) {
       const int64_t r = weights.row(i_row);
       ListShared& l = lists[par];
-      if (done >= 2) bar_sync<kBarListFree, 64>(par);
-      bool bad = false, some = false;
+      int id[LISTS];                           // entries lane, lane + 32, ...
+      float y[LISTS];
+      T x[LISTS];                              // as loaded: a conversion would wait for it
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) {
+        const int k = lane + 32 * i;
+        id[i] = k < K ? a.ids[r * K + k] : -1;
+        y[i] = k < K ? a.y[r * K + k] : -kInf;
+      }
+      if (done >= 1) bar_sync<kBarListFree, 64>(par);
+#pragma unroll
+      for (int i = 0; i < kHash / 128; ++i) reinterpret_cast<int4*>(seen)[lane + 32 * i] = make_int4(-1, -1, -1, -1);
+      const Slice sl(V, row_pad(logits + r * a.stride), 0, 1);
+      bool bad = false, twice = false;
       float m_list = -kInf, y_top = -kInf;
+      unsigned loose = 0;
 #pragma unroll
       for (int i = 0; i < LISTS; ++i) {
         const int k = lane + 32 * i;
         bad = bad || id[i] < -1 || id[i] >= V || (id[i] >= 0 && !(y[i] < kInf));
         if (id[i] < 0 || id[i] >= V) { id[i] = -1; y[i] = -kInf; }
-        if (k < K) { l.id[k] = id[i]; l.y[k] = y[i]; l.x[k] = x[i]; }
-        m_list = max_nan(m_list, x[i]);
+        x[i] = id[i] >= 0 ? logits[r * a.stride + id[i]] : Elem<T>::masked();
+        if (k < K) { l.id[k] = id[i]; l.y[k] = y[i]; l.first[k] = id[i] >= 0; }
         y_top = fmaxf(y_top, y[i]);
+        const int u = (id[i] + sl.pad) >> 3;
+        if (id[i] >= 0 && !(u >= sl.full0 && u < sl.full1)) loose |= 1u << ((id[i] + sl.pad) & 7) << (u == sl.ragged(0) ? 0 : 8);
+      }
+      loose = __reduce_or_sync(0xffffffffu, loose);
+      if (lane == 0) { l.loose[0] = loose & 0xffu; l.loose[1] = loose >> 8; }
+      __syncwarp();
+      bar_arrive<kBarIds, 64>(par);
+      // an id that is in the table already stands in the list twice: rare, and worked out entry by entry
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i)
+        if (id[i] >= 0)
+          for (int h = (int)((unsigned)id[i] * 2654435761u >> 16) & (kHash - 1);; h = (h + 1) & (kHash - 1)) {
+            const int was = atomicCAS(&seen[h], -1, id[i]);
+            if (was == -1) break;
+            if (was == id[i]) { twice = true; break; }
+          }
+      twice = __any_sync(0xffffffffu, twice);
+      if (twice)
+        for (int k = lane; k < K; k += 32)
+          for (int j = 0; j < k; ++j)
+            if (l.id[j] == l.id[k]) l.first[k] = 0;
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < LISTS; ++i) {
+        const int k = lane + 32 * i;
+        if (k < K) l.x[k] = Elem<T>::get(&x[i]);
+        m_list = max_nan(m_list, Elem<T>::get(&x[i]));
       }
 #pragma unroll
       for (int o = 16; o; o >>= 1) {
         m_list = max_nan(m_list, __shfl_xor_sync(0xffffffffu, m_list, o));
         y_top = fmaxf(y_top, __shfl_xor_sync(0xffffffffu, y_top, o));
       }
-      some = y_top > -kInf;
+      const bool some = y_top > -kInf;
       const double shift = a.tail || !some ? 0.0 : (double)y_top, x_shift = m_list != -kInf ? (double)m_list : 0.0;
-      __syncwarp();
       ListSums sums{0.0, 0.0, 0.0, 0.0};
-      bool twice = false;
-      unsigned loose = 0;
-      const Slice sl(V, row_pad(logits + r * a.stride), 0, 1);
-      int at[LISTS];                           // chunk of the entry's element (-1: in none); its place in it below
 #pragma unroll
       for (int i = 0; i < LISTS; ++i) {
-        const int k = lane + 32 * i;
-        at[i] = -1;
         if (32 * i >= K) continue;
-        bool first = id[i] >= 0;
-        if (first) {
-          const int4* ids4 = reinterpret_cast<const int4*>(l.id);
-          for (int j = 0; j < (k >> 2); ++j) {
-            const int4 o = ids4[j];
-            first = first && o.x != id[i] && o.y != id[i] && o.z != id[i] && o.w != id[i];
-          }
-          for (int j = k & ~3; j < k; ++j) first = first && l.id[j] != id[i];
-          twice = twice || !first;
-          const int u = (id[i] + sl.pad) >> 3;
-          if (u >= sl.full0 && u < sl.full1) at[i] = (u - sl.full0) / C::kUnits;
-          else loose |= 1u << ((id[i] + sl.pad) & 7) << (u == sl.ragged(0) ? 0 : 8);
-        }
-        if (k < K) l.first[k] = first;
-        if (first && m_list != -kInf) sums.z += exp(((double)x[i] - m_list) * s);
+        const int k = lane + 32 * i;
+        if (k < K && l.first[k] && m_list != -kInf) sums.z += exp(((double)Elem<T>::get(&x[i]) - m_list) * s);
         if (y[i] > -kInf) {
           const double q = exp((double)y[i] - shift);
           if (q != 0.0) {
             sums.q += q;
             sums.qy += q * ((double)y[i] - shift);
-            sums.qx += q * (((double)x[i] - x_shift) * s);
+            sums.qx += q * (((double)Elem<T>::get(&x[i]) - x_shift) * s);
           }
         }
       }
       sums = warp_sum(sums);
       bad = __any_sync(0xffffffffu, bad);
-      twice = __any_sync(0xffffffffu, twice);
-      loose = __reduce_or_sync(0xffffffffu, loose);
       if (lane == 0) {
         l.side = ListSide{sums, m_list, shift, some, bad};
         l.twice = twice;
-        l.loose[0] = loose & 0xffu;
-        l.loose[1] = loose >> 8;
       }
+      __syncwarp();
       bar_arrive<kBarList, 64>(par);
-      int now[LISTS];
+    }
+    return;
+  }
+
+  if (role == 2) {                             // passer
+    SlotOrder<NB, GRAD> slots;
+    unsigned parity = 0;
+    int turn = 0, par = 0;
+    bool ok = true;
+    for (int i_row = weights.next(0); weights.row(i_row) < a.n_rows; i_row = weights.next(i_row + 1), par ^= 1) {
+      const Slice sl(V, row_pad(logits + weights.row(i_row) * a.stride), 0, 1);
+      bar_sync<kBarIds, 64>(par);
+      const ListShared& l = lists[par];
+      int id[LISTS], at[LISTS];                // entries lane, lane + 32, ...; chunk of each (-1: in none)
 #pragma unroll
-      for (int i = 0; i < LISTS; ++i) now[i] = id[i];
-      i_row = weights.next(i_row + 1);
-      const int64_t next = weights.row(i_row);
-      fetch_entries(next);                     // a row ahead; their logits half a row later, when the ids are here
+      for (int i = 0; i < LISTS; ++i) {
+        id[i] = lane + 32 * i < K ? l.id[lane + 32 * i] : -1;
+        const int u = (id[i] + sl.pad) >> 3;
+        at[i] = id[i] >= 0 && u >= sl.full0 && u < sl.full1 ? (u - sl.full0) / C::kUnits : -1;
+      }
       const int n = C::count(sl), loads = GRAD ? n + max(0, n - NB) : n;
       for (int ld = 0; ld < loads; ++ld) {
         const int ch = ld < n ? ld : 2 * n - NB - 1 - ld;
@@ -481,18 +497,16 @@ __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRA
         parity ^= 1u << sv;
         if (ld < n) {
           T* const chunk = reinterpret_cast<T*>(ring_buffer + sv * CHUNK) + sl.pad - 8 * (sl.full0 + ch * C::kUnits);
+          bool wrote = false;
 #pragma unroll
           for (int i = 0; i < LISTS; ++i)
-            if (at[i] == ch) chunk[now[i]] = Elem<T>::masked();
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before a later copy goes over these writes
+            if (at[i] == ch) { chunk[id[i]] = Elem<T>::masked(); wrote = true; }
+          if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before a later copy goes over it
         }
         __syncwarp();
         if (lane == 0) ring::mbar_arrive(&passed[sv]);
-        if (ld == loads / 2 && next < a.n_rows) fetch_logits(next);
       }
       if (GRAD) slots.end_row(n);
-      par ^= 1;
-      ++done;
     }
     return;
   }

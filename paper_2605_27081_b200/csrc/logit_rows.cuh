@@ -451,7 +451,7 @@ struct Consumer {
 
 // Named barriers of a block.  kBarGroup: over a group of NT threads; kBarFinish: over each of the two groups of finishers; kBarReady,
 // kBarFree: between consumers and finishers, two each, by the row's parity; the others: see distill.cu.
-constexpr int kBarGroup = 1, kBarFinish = 2, kBarReady = 4, kBarFree = 6, kBarList = 8, kBarListFree = 10, kBarCoef = 12, kBarWritten = 13;
+constexpr int kBarGroup = 1, kBarFinish = 2, kBarReady = 4, kBarFree = 6, kBarIds = 8, kBarList = 10, kBarListFree = 12, kBarCoef = 14, kBarWritten = 15;
 template <int NT>
 __device__ __forceinline__ void sync_threads() { asm volatile("bar.sync %0, %1;" ::"n"(kBarGroup), "n"(NT) : "memory"); }
 

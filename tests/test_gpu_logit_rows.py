@@ -329,7 +329,7 @@ def check_distill(view, s, ids, y, tail, weight, oplace=(0, 0)):
     out, flat = place(torch.zeros(T, V, dtype=view.dtype), *oplace)
     before = flat.clone()
     loss2, st = run_distill(view, s, ids, y, tail, weight, out, stats=True)
-    assert torch.equal(loss.nan_to_num(9.0), loss2.nan_to_num(9.0))
+    ref.close(loss2, want["loss"], tol, "loss with the gradient")      # summed in another order than without: not the same bits
     ref.check_grad(out, want["grad"], want["grad_size"], V, "gradient with the loss", factor)
     untouched(out, flat, before)
     out2, flat2 = place(torch.zeros(T, V, dtype=view.dtype), *oplace)
