@@ -65,8 +65,8 @@ __device__ __forceinline__ void rest_grad_unit(Unit<T>& q, float m, float c, flo
 
 // Elements [e0, e1) of a row that lies at any address: whole units in one store each, the ends element by element.
 template <typename T, typename F>
-__device__ __forceinline__ void write_elements(T* out, int e0, int e1, int n_threads, F value) {
-  const int pad = row_pad(out), u0 = (e0 + pad + 7) >> 3, u1 = (e1 + pad) >> 3, tid = threadIdx.x;
+__device__ __forceinline__ void write_elements(T* out, int e0, int e1, int n_threads, int tid, F value) {
+  const int pad = row_pad(out), u0 = (e0 + pad + 7) >> 3, u1 = (e1 + pad) >> 3;
   for (int u = u0 + tid; u < u1; u += n_threads) {
     float v[8];
 #pragma unroll
@@ -121,21 +121,23 @@ __device__ __forceinline__ void finish_row(const DistillArgs& a, int64_t r, floa
   const bool alive = m != -kInf, others = rest.m > -kInf;        // a NaN is alive
   const double x_shift = l.m_list != -kInf ? (double)l.m_list : 0.0;
   const double grow = 1.0 + (double)rest.R;
-  const double of_rest = others ? exp(((double)rest.m - m) * s) : 0.0, of_list = l.m_list != -kInf ? exp(((double)l.m_list - m) * s) : 0.0;
-  const double z = of_rest * grow + of_list * v.z, ln_z = log(z), ln_rest = log(grow);
-  const double of_q = a.tail || !l.some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !l.some ? 0.0 : l.shift + log(v.q);
+  // one of the two is 1; the other's float32 rounding is that of a part of Z
+  const float c = a.s * kLog2e;
+  const double of_rest = others ? (double)ex2((rest.m - m) * c) : 0.0, of_list = l.m_list != -kInf ? (double)ex2((l.m_list - m) * c) : 0.0;
+  const double z = of_rest * grow + of_list * v.z, inv_z = 1.0 / z, ln_z = ln_wide(z), ln_rest = ln_wide(grow);
+  const double of_q = a.tail || !l.some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !l.some ? 0.0 : l.shift + ln_wide(v.q);
   const double q_all = v.q * of_q, q_rest = a.tail && others ? fmax(0.0, 1.0 - v.q) : 0.0;
   const double ln_p_rest = ((double)rest.m - m) * s + ln_rest - ln_z;
   double loss = (v.qy - v.qx) * of_q + (((double)m - x_shift) * s + ln_z - (ln_q - l.shift)) * q_all;
-  if (q_rest > 0.0) loss += q_rest * (log(q_rest) - ln_p_rest);
-  const double c_rest = others ? of_rest * grow / z - q_rest : 0.0;
+  if (q_rest > 0.0) loss += q_rest * (ln_wide(q_rest) - ln_p_rest);
+  const double c_rest = others ? of_rest * grow * inv_z - q_rest : 0.0;
   const bool in = l.some && alive;
   const float poison = l.bad ? nan_value() : 0.f;
   if (share) {
     rs.kind = l.bad || in;
     rs.m_rest = others ? rest.m : 0.f;
-    rs.coef = (others ? (float)(s * weight * c_rest / grow) : 0.f) + poison;
-    rs.of_e = of_list / z + poison;
+    rs.coef = (others ? (float)(s * weight * c_rest) / (float)grow : 0.f) + poison;
+    rs.of_e = of_list * inv_z + poison;
     rs.of_q = of_q;
     rs.weight = s * weight;
   }
@@ -186,7 +188,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
       if (a.stats)
         for (int i = 0; i < 8; ++i) a.stats[8 * r + i] = 0.f;
     }
-    if (GRAD) write_elements(out, e0, e1, NT, [](int) { return 0.f; });
+    if (GRAD) write_elements(out, e0, e1, NT, tid, [](int) { return 0.f; });
     return;
   }
 
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
   if (GRAD) {
     __syncthreads();
     if (rs.kind == 0) {
-      write_elements(out, e0, e1, NT, [](int) { return 0.f; });
+      write_elements(out, e0, e1, NT, tid, [](int) { return 0.f; });
     } else {
       const float m_rest = rs.m_rest, coef = rs.coef;
       if (row_pad(out) == sl.pad) {
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
         }
       } else {
         const T* own = reinterpret_cast<const T*>(units) + sl.pad - 8 * sl.first;
-        write_elements(out, e0, e1, NT, [&](int i) { return coef * ex2((Elem<T>::get(own + i) - m_rest) * c); });
+        write_elements(out, e0, e1, NT, tid, [&](int i) { return coef * ex2((Elem<T>::get(own + i) - m_rest) * c); });
       }
       __syncthreads();                                    // the list's elements go over what was just written there
       if (first && id >= e0 && id < e1) {
@@ -310,61 +312,225 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
 }
 
 // ---- many rows ---------------------------------------------------------------------------------------------------
-// Persistent blocks (logit_rows.cuh).  Warps of a block, each at its own pace:
-//   producer   issues the copies;
-//   listers    two, for every second row each, up to two rows ahead: read the lists and compute their sums (two dependent loads
-//              behind the copies on their way take 5 us each);
-//   passer     takes the list's elements out of each chunk that arrives (-inf in shared memory) and passes the chunk on to the
-//              consumers, so their loop knows nothing of lists;
-//   consumers  sum what is left; with GRAD they wait for the row's figures, go over the row downwards and write the gradient;
-//   finisher   joins sums and list, writes the loss, gives the figures to the consumers, and puts the list's gradients over what
-//              they wrote once they say that the row is written.
-#ifndef DM_NT
-#define DM_NT 128
-#define DM_B 4
-#define DM_U 6
-#define DM_NB 3
-#define DM_GNT 128
-#define DM_GB 4
-#define DM_GU 6
-#define DM_GNB 4
-#endif
-template <typename T, bool GRAD>
-struct ManyShape {
-  static constexpr int kConsumers = GRAD ? DM_GNT : DM_NT, kBlocks = GRAD ? DM_GB : DM_B, kSlots = GRAD ? DM_GNB : DM_NB;
-  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? (GRAD ? DM_GU : DM_U) : 4);
-  static constexpr int kThreads = kConsumers + 160;
-  static constexpr size_t kSmem = (size_t)kChunk * kSlots;
-};
-
+// Persistent blocks (logit_rows.cuh).  The list's elements are taken out of each chunk that arrives (-inf in shared memory)
+// by a warp between the copies and the consumers, so their loop knows nothing of lists.
 struct alignas(16) ListShared {
   int id[kMaxList];                // -1: unused entry
   float y[kMaxList], x[kMaxList];
   unsigned char first[kMaxList];   // no entry before it has its id
   ListSide side;
   int twice;                       // an id stands in the list more than once
-  unsigned loose[2];               // bits of the row's ragged units that are listed
+  unsigned loose[2];               // bits of the slice's ragged units that are listed
 };
-constexpr int kHash = 2 * kMaxList;   // table in which the lister looks for ids that come twice
+constexpr int kHash = 2 * kMaxList, kLists = kMaxList / 32;      // table in which ids that come twice are looked for; entries a lane
 
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRAD>::kBlocks) distill_pipe_kernel(const __grid_constant__ DistillArgs a) {
-  typedef ManyShape<T, GRAD> Shape;
-  constexpr int NT = Shape::kConsumers, NB = Shape::kSlots, CHUNK = Shape::kChunk, PAIR = NT + 32, LISTS = kMaxList / 32;
+// One warp's registers for the list of a row: entries lane, lane + 32, ...
+template <typename T>
+struct ListFetch {
+  int id[kLists];
+  float y[kLists];
+  T x[kLists];                     // as loaded: a conversion would wait for it
+  __device__ __forceinline__ void entries(const DistillArgs& a, int64_t r) {
+#pragma unroll
+    for (int i = 0; i < kLists; ++i) {
+      const int k = (threadIdx.x & 31) + 32 * i;
+      id[i] = -1;
+      y[i] = -kInf;
+      if (k < a.K && r < a.n_rows) { id[i] = a.ids[r * a.K + k]; y[i] = a.y[r * a.K + k]; }
+    }
+  }
+  __device__ __forceinline__ void logits(const DistillArgs& a, int64_t r) {
+#pragma unroll
+    for (int i = 0; i < kLists; ++i)
+      x[i] = id[i] >= 0 && id[i] < a.V ? static_cast<const T*>(a.logits)[r * a.stride + id[i]] : Elem<T>::masked();
+  }
+};
+
+// One warp: brings a fetched list into l and computes its sums.  `ids_out` is called when ids and loose are in place, the rest follows.
+template <typename T, typename Ids>
+__device__ __forceinline__ void lay_list(const DistillArgs& a, ListFetch<T>& f, const Slice& sl, ListShared& l, int* seen, Ids ids_out) {
+  const int lane = threadIdx.x & 31, V = a.V, K = a.K;
+  const double s = a.s;
+  int (&id)[kLists] = f.id;
+  float (&y)[kLists] = f.y;
+  T (&x)[kLists] = f.x;
+#pragma unroll
+  for (int i = 0; i < kHash / 128; ++i) reinterpret_cast<int4*>(seen)[lane + 32 * i] = make_int4(-1, -1, -1, -1);
+  bool bad = false, twice = false;
+  float m_list = -kInf, y_top = -kInf;
+  unsigned loose = 0;
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) {
+    const int k = lane + 32 * i;
+    bad = bad || id[i] < -1 || id[i] >= V || (id[i] >= 0 && !(y[i] < kInf));
+    if (id[i] < 0 || id[i] >= V) { id[i] = -1; y[i] = -kInf; }
+    if (k < K) { l.id[k] = id[i]; l.y[k] = y[i]; l.first[k] = id[i] >= 0; }
+    y_top = fmaxf(y_top, y[i]);
+    const int u = (id[i] + sl.pad) >> 3;
+    if (id[i] >= 0 && sl.holds(id[i]) && !(u >= sl.full0 && u < sl.full1)) loose |= 1u << ((id[i] + sl.pad) & 7) << (u == sl.ragged(0) ? 0 : 8);
+  }
+  loose = __reduce_or_sync(0xffffffffu, loose);
+  if (lane == 0) { l.loose[0] = loose & 0xffu; l.loose[1] = loose >> 8; }
+  __syncwarp();
+  ids_out();
+  // an id that is in the table already stands in the list twice: rare, and worked out entry by entry
+#pragma unroll
+  for (int i = 0; i < kLists; ++i)
+    if (id[i] >= 0)
+      for (int h = (int)((unsigned)id[i] * 2654435761u >> 16) & (kHash - 1);; h = (h + 1) & (kHash - 1)) {
+        const int was = atomicCAS(&seen[h], -1, id[i]);
+        if (was == -1) break;
+        if (was == id[i]) { twice = true; break; }
+      }
+  twice = __any_sync(0xffffffffu, twice);
+  if (twice)
+    for (int k = lane; k < K; k += 32)
+      for (int j = 0; j < k; ++j)
+        if (l.id[j] == l.id[k]) l.first[k] = 0;
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) {
+    const int k = lane + 32 * i;
+    if (k < K) l.x[k] = Elem<T>::get(&x[i]);
+    m_list = max_nan(m_list, Elem<T>::get(&x[i]));
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    m_list = max_nan(m_list, __shfl_xor_sync(0xffffffffu, m_list, o));
+    y_top = fmaxf(y_top, __shfl_xor_sync(0xffffffffu, y_top, o));
+  }
+  const bool some = y_top > -kInf;
+  const double shift = a.tail || !some ? 0.0 : (double)y_top, x_shift = m_list != -kInf ? (double)m_list : 0.0;
+  ListSums sums{0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) {
+    if (32 * i >= K) continue;
+    const int k = lane + 32 * i;
+    const double xi = Elem<T>::get(&x[i]);
+    if (k < K && l.first[k] && m_list != -kInf) sums.z += exp((xi - m_list) * s);
+    if (y[i] > -kInf) {
+      const double q = exp((double)y[i] - shift);
+      if (q != 0.0) {
+        sums.q += q;
+        sums.qy += q * ((double)y[i] - shift);
+        sums.qx += q * ((xi - x_shift) * s);
+      }
+    }
+  }
+  sums = warp_sum(sums);
+  bad = __any_sync(0xffffffffu, bad);
+  if (lane == 0) {
+    l.side = ListSide{sums, m_list, shift, some, bad};
+    l.twice = twice;
+  }
+  __syncwarp();
+}
+
+// One warp: takes the listed elements of a slice out of its chunks and passes them on.
+template <typename T, int NB, int CHUNK>
+__device__ __forceinline__ void pass_chunks(const Slice& sl, const ListShared& l, int K, unsigned char* buf, RingPlace<NB>& in, uint64_t* full, uint64_t* passed) {
+  typedef Chunks<T, CHUNK> C;
+  const int lane = threadIdx.x & 31;
+  int id[kLists], at[kLists];              // entries lane, lane + 32, ...; chunk of each (-1: in none)
+#pragma unroll
+  for (int i = 0; i < kLists; ++i) {
+    id[i] = lane + 32 * i < K ? l.id[lane + 32 * i] : -1;
+    const int u = (id[i] + sl.pad) >> 3;
+    at[i] = id[i] >= 0 && u >= sl.full0 && u < sl.full1 ? (u - sl.full0) / C::kUnits : -1;
+  }
+  const int n = C::count(sl);
+  for (int ch = 0; ch < n; ++ch) {
+    in.wait(full);
+    T* const chunk = reinterpret_cast<T*>(buf + in.slot * CHUNK) + sl.pad - 8 * (sl.full0 + ch * C::kUnits);
+    bool wrote = false;
+#pragma unroll
+    for (int i = 0; i < kLists; ++i)
+      if (at[i] == ch) { chunk[id[i]] = Elem<T>::masked(); wrote = true; }
+    if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before a later copy goes over it
+    in.pass(passed);
+  }
+}
+
+// Sums of what is left of a slice, by NT threads (tid: 0 .. NT - 1); `empty`: where they say that a chunk may go, or null.
+template <typename T, int NT, int NB, int CHUNK>
+__device__ __forceinline__ State sum_slice(const T* row, int V, const Slice& sl, const ListShared& l, const unsigned char* buf, float c, int tid,
+                                           RingPlace<NB>& in, uint64_t* passed, uint64_t* empty) {
   typedef Chunks<T, CHUNK> C;
   constexpr int N = C::kUnits / NT;
+  static_assert(C::kUnits % NT == 0, "whole units for every thread");
+  Unit<T> loose[1];
+  const bool has_loose = tid < 2 && sl.ragged(tid) >= 0;
+  if (has_loose) load_ragged(row, V, sl.pad, sl.ragged(tid), loose[0]);
+  Stream<T, false, false> st(c);
+  const int chunks = C::count(sl);
+  for (int ch = 0; ch < chunks; ++ch) {
+    const int n = C::units(sl, ch);
+    in.wait(passed);
+    const unsigned char* units = buf + in.slot * CHUNK;
+    if (n == C::kUnits) {
+      Unit<T> q[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) load_shared_unit(units, tid + i * NT, q[i]);
+      st.add(q);
+    } else {
+#pragma unroll 1
+      for (int u = tid; u < n; u += NT) {
+        Unit<T> q[1];
+        load_shared_unit(units, u, q[0]);
+        st.add(q);
+      }
+    }
+    if (empty) in.pass(empty);
+    else in.advance();
+  }
+  if (has_loose) {                         // those are not in the ring; the chunks' barriers have made the list visible
+    const unsigned bits = l.loose[tid];
+    float v[8];
+    loose[0].values(v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = bits >> j & 1u ? -kInf : v[j];
+    loose[0].set(v);
+    st.add(loose);
+  }
+  return in.ok ? st.finish() : State{0.f, nan_value(), nan_value()};
+}
+
+// The loss alone.  Warps of a block, each at its own pace:
+//   producer   issues the copies;
+//   listers    two, for every second row each, up to two rows ahead: read the lists and compute their sums (two dependent loads
+//              behind the copies on their way take 5 us each);
+//   passer     takes the list's elements out of the chunks;
+//   consumers  sum what is left;
+//   finisher   joins sums and list and writes the loss.
+#ifndef DM_NT
+#define DM_NT 128
+#define DM_B 4
+#define DM_U 6
+#define DM_NB 3
+#endif
+template <typename T>
+struct LossShape {
+  static constexpr int kConsumers = DM_NT, kBlocks = DM_B, kSlots = DM_NB;
+  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? DM_U : 4);
+  static constexpr int kThreads = kConsumers + 160;
+  static constexpr size_t kSmem = (size_t)kChunk * kSlots;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(LossShape<T>::kThreads, LossShape<T>::kBlocks) distill_loss_kernel(const __grid_constant__ DistillArgs a) {
+  typedef LossShape<T> Shape;
+  constexpr int NT = Shape::kConsumers, NB = Shape::kSlots, CHUNK = Shape::kChunk, PAIR = NT + 32;
   __shared__ PipeShared<NB> ps;
-  __shared__ uint64_t passed[NB];              // chunks that the list warp is done with
+  __shared__ uint64_t passed[NB];              // chunks that the passer is done with
   __shared__ State per_warp[2][NT / 32];
   __shared__ ListShared lists[2];
-  __shared__ __align__(16) int seen_by[2][kHash];
-  __shared__ RowShared rs;
+  __shared__ __align__(16) int seen[2][kHash];
+  __shared__ RowShared unused;
   extern __shared__ __align__(128) unsigned char ring_buffer[];
-  const int V = a.V, K = a.K, tid = threadIdx.x, lane = tid & 31;
+  const int V = a.V, tid = threadIdx.x, lane = tid & 31;
   const T* logits = static_cast<const T*>(a.logits);
   const float c = a.s * kLog2e;
-  const double s = a.s;
-  RowWeights weights(a.weight, a.n_rows);
+  RowWeights weights(a.weight, a.n_rows, blockIdx.x, gridDim.x);
   if (tid == 0) {
     init_pipe(ps, NT / 32);
     for (int i = 0; i < NB; ++i) ring::mbar_init(&passed[i], 1);
@@ -372,146 +538,31 @@ __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRA
   }
   __syncthreads();
   const int role = tid < NT ? 0 : (tid - NT) / 32 + 1;
+  auto slice_of = [&](int64_t r) { return Slice(V, row_pad(logits + r * a.stride), 0, 1); };
 
   if (role == 5) {
-    produce<T, NB, CHUNK, GRAD>(ps, ring_buffer, logits, a.weight, a.stride, V, a.n_rows);
-    return;
-  }
-
-  if (role >= 3) {                             // listers
+    produce<T, NB, CHUNK>(ps, ring_buffer, weights, logits, a.stride, V, 0, 1);
+  } else if (role >= 3) {                      // listers
     const int par = role - 3;
-    int* const seen = seen_by[par];
     int i_row = weights.next(0);
     if (par) i_row = weights.next(i_row + 1);
-    for (int done = 0; weights.row(i_row) < a.n_rows; i_row = weights.next(weights.next(i_row + 1) + 1), ++done) {
+    for (bool again = false; weights.row(i_row) < a.n_rows; i_row = weights.next(weights.next(i_row + 1) + 1), again = true) {
       const int64_t r = weights.row(i_row);
-      ListShared& l = lists[par];
-      int id[LISTS];                           // entries lane, lane + 32, ...
-      float y[LISTS];
-      T x[LISTS];                              // as loaded: a conversion would wait for it
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) {
-        const int k = lane + 32 * i;
-        id[i] = k < K ? a.ids[r * K + k] : -1;
-        y[i] = k < K ? a.y[r * K + k] : -kInf;
-      }
-      if (done >= 1) bar_sync<kBarListFree, 64>(par);
-#pragma unroll
-      for (int i = 0; i < kHash / 128; ++i) reinterpret_cast<int4*>(seen)[lane + 32 * i] = make_int4(-1, -1, -1, -1);
-      const Slice sl(V, row_pad(logits + r * a.stride), 0, 1);
-      bool bad = false, twice = false;
-      float m_list = -kInf, y_top = -kInf;
-      unsigned loose = 0;
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) {
-        const int k = lane + 32 * i;
-        bad = bad || id[i] < -1 || id[i] >= V || (id[i] >= 0 && !(y[i] < kInf));
-        if (id[i] < 0 || id[i] >= V) { id[i] = -1; y[i] = -kInf; }
-        x[i] = id[i] >= 0 ? logits[r * a.stride + id[i]] : Elem<T>::masked();
-        if (k < K) { l.id[k] = id[i]; l.y[k] = y[i]; l.first[k] = id[i] >= 0; }
-        y_top = fmaxf(y_top, y[i]);
-        const int u = (id[i] + sl.pad) >> 3;
-        if (id[i] >= 0 && !(u >= sl.full0 && u < sl.full1)) loose |= 1u << ((id[i] + sl.pad) & 7) << (u == sl.ragged(0) ? 0 : 8);
-      }
-      loose = __reduce_or_sync(0xffffffffu, loose);
-      if (lane == 0) { l.loose[0] = loose & 0xffu; l.loose[1] = loose >> 8; }
-      __syncwarp();
-      bar_arrive<kBarIds, 64>(par);
-      // an id that is in the table already stands in the list twice: rare, and worked out entry by entry
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i)
-        if (id[i] >= 0)
-          for (int h = (int)((unsigned)id[i] * 2654435761u >> 16) & (kHash - 1);; h = (h + 1) & (kHash - 1)) {
-            const int was = atomicCAS(&seen[h], -1, id[i]);
-            if (was == -1) break;
-            if (was == id[i]) { twice = true; break; }
-          }
-      twice = __any_sync(0xffffffffu, twice);
-      if (twice)
-        for (int k = lane; k < K; k += 32)
-          for (int j = 0; j < k; ++j)
-            if (l.id[j] == l.id[k]) l.first[k] = 0;
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) {
-        const int k = lane + 32 * i;
-        if (k < K) l.x[k] = Elem<T>::get(&x[i]);
-        m_list = max_nan(m_list, Elem<T>::get(&x[i]));
-      }
-#pragma unroll
-      for (int o = 16; o; o >>= 1) {
-        m_list = max_nan(m_list, __shfl_xor_sync(0xffffffffu, m_list, o));
-        y_top = fmaxf(y_top, __shfl_xor_sync(0xffffffffu, y_top, o));
-      }
-      const bool some = y_top > -kInf;
-      const double shift = a.tail || !some ? 0.0 : (double)y_top, x_shift = m_list != -kInf ? (double)m_list : 0.0;
-      ListSums sums{0.0, 0.0, 0.0, 0.0};
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) {
-        if (32 * i >= K) continue;
-        const int k = lane + 32 * i;
-        if (k < K && l.first[k] && m_list != -kInf) sums.z += exp(((double)Elem<T>::get(&x[i]) - m_list) * s);
-        if (y[i] > -kInf) {
-          const double q = exp((double)y[i] - shift);
-          if (q != 0.0) {
-            sums.q += q;
-            sums.qy += q * ((double)y[i] - shift);
-            sums.qx += q * (((double)Elem<T>::get(&x[i]) - x_shift) * s);
-          }
-        }
-      }
-      sums = warp_sum(sums);
-      bad = __any_sync(0xffffffffu, bad);
-      if (lane == 0) {
-        l.side = ListSide{sums, m_list, shift, some, bad};
-        l.twice = twice;
-      }
-      __syncwarp();
+      ListFetch<T> f;
+      f.entries(a, r);
+      f.logits(a, r);
+      if (again) bar_sync<kBarListFree, 64>(par);
+      lay_list<T>(a, f, slice_of(r), lists[par], seen[par], [&] { bar_arrive<kBarIds, 64>(par); });
       bar_arrive<kBarList, 64>(par);
     }
-    return;
-  }
-
-  if (role == 2) {                             // passer
-    SlotOrder<NB, GRAD> slots;
-    unsigned parity = 0;
-    int turn = 0, par = 0;
-    bool ok = true;
+  } else if (role == 2) {                      // passer
+    RingPlace<NB> in;
+    int par = 0;
     for (int i_row = weights.next(0); weights.row(i_row) < a.n_rows; i_row = weights.next(i_row + 1), par ^= 1) {
-      const Slice sl(V, row_pad(logits + weights.row(i_row) * a.stride), 0, 1);
       bar_sync<kBarIds, 64>(par);
-      const ListShared& l = lists[par];
-      int id[LISTS], at[LISTS];                // entries lane, lane + 32, ...; chunk of each (-1: in none)
-#pragma unroll
-      for (int i = 0; i < LISTS; ++i) {
-        id[i] = lane + 32 * i < K ? l.id[lane + 32 * i] : -1;
-        const int u = (id[i] + sl.pad) >> 3;
-        at[i] = id[i] >= 0 && u >= sl.full0 && u < sl.full1 ? (u - sl.full0) / C::kUnits : -1;
-      }
-      const int n = C::count(sl), loads = GRAD ? n + max(0, n - NB) : n;
-      for (int ld = 0; ld < loads; ++ld) {
-        const int ch = ld < n ? ld : 2 * n - NB - 1 - ld;
-        const int sv = GRAD ? slots.slot(ch) : turn;
-        if (!GRAD) turn = turn + 1 == NB ? 0 : turn + 1;
-        if (ok) ok = ring::mbar_wait(&ps.full[sv], parity >> sv & 1u);
-        parity ^= 1u << sv;
-        if (ld < n) {
-          T* const chunk = reinterpret_cast<T*>(ring_buffer + sv * CHUNK) + sl.pad - 8 * (sl.full0 + ch * C::kUnits);
-          bool wrote = false;
-#pragma unroll
-          for (int i = 0; i < LISTS; ++i)
-            if (at[i] == ch) { chunk[id[i]] = Elem<T>::masked(); wrote = true; }
-          if (wrote) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // before a later copy goes over it
-        }
-        __syncwarp();
-        if (lane == 0) ring::mbar_arrive(&passed[sv]);
-      }
-      if (GRAD) slots.end_row(n);
+      pass_chunks<T, NB, CHUNK>(slice_of(weights.row(i_row)), lists[par], a.K, ring_buffer, in, ps.full, passed);
     }
-    return;
-  }
-
-  if (role == 1) {                             // finisher
+  } else if (role == 1) {                      // finisher
     int par = 0;
     for (int i_row = 0; weights.row(i_row) < a.n_rows; ++i_row) {
       const int64_t r = weights.row(i_row);
@@ -522,40 +573,9 @@ __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRA
         continue;
       }
       const bool later = weights.row(weights.next(weights.next(i_row + 1) + 1)) < a.n_rows;      // a row will wait for this one's buffers
-      weights.at(i_row);
       bar_sync<kBarList, 64>(par);
       bar_sync<kBarReady, PAIR>(par);
-      const State rest = join_warps<NT>(per_warp[par], c);
-      ListShared& l = lists[par];
-      finish_row(a, r, weight, rest, l.side, lane == 0, lane == 0, rs);
-      if (GRAD) {
-        __syncwarp();
-        bar_arrive<kBarCoef, PAIR>(0);
-        double e[LISTS], q[LISTS];             // while the consumers write
-        const RowShared g = rs;
-        const ListSide side = l.side;
-        T* out = static_cast<T*>(a.d_logits) + r * a.d_stride;
-        if (g.kind != 0) {
-#pragma unroll
-          for (int i = 0; i < LISTS; ++i) {
-            const int k = lane + 32 * i;
-            e[i] = q[i] = 0.0;
-            if (k < K && l.first[k]) {
-              if (side.m_list != -kInf) e[i] = exp(((double)l.x[k] - side.m_list) * s);
-              for (int j = k; j < (l.twice ? K : k + 1); ++j)
-                if (l.id[j] == l.id[k] && l.y[j] > -kInf) q[i] += exp((double)l.y[j] - side.shift);
-            }
-          }
-        }
-        bar_sync<kBarWritten, PAIR>(0);
-        if (g.kind != 0) {
-#pragma unroll
-          for (int i = 0; i < LISTS; ++i) {
-            const int k = lane + 32 * i;
-            if (k < K && l.first[k]) Elem<T>::put(out + l.id[k], (float)(g.weight * (e[i] * g.of_e - q[i] * g.of_q)));
-          }
-        }
-      }
+      finish_row(a, r, weight, join_warps<NT>(per_warp[par], c), lists[par].side, false, lane == 0, unused);
       __syncwarp();
       if (later) {
         bar_arrive<kBarListFree, 64>(par);
@@ -563,94 +583,15 @@ __global__ void __launch_bounds__(ManyShape<T, GRAD>::kThreads, ManyShape<T, GRA
       }
       par ^= 1;
     }
-    return;
-  }
-
-  Consumer<NB, GRAD> in(ps);
-  int par = 0, done = 0;
-  for (int i_row = 0; weights.row(i_row) < a.n_rows; ++i_row) {
-    const int64_t r = weights.row(i_row);
-    const T* row = logits + r * a.stride;
-    T* out = GRAD ? static_cast<T*>(a.d_logits) + r * a.d_stride : nullptr;
-    if (weights.at(i_row) == 0.f) {
-      if (GRAD) write_elements(out, 0, V, NT, [](int) { return 0.f; });
-      continue;
+  } else {                                     // consumers
+    RingPlace<NB> in;
+    int par = 0, done = 0;
+    for (int i_row = weights.next(0); weights.row(i_row) < a.n_rows; i_row = weights.next(i_row + 1), par ^= 1, ++done) {
+      const T* row = logits + weights.row(i_row) * a.stride;
+      if (done >= 2) bar_sync<kBarFree, PAIR>(par);
+      join_warp(sum_slice<T, NT, NB, CHUNK>(row, V, slice_of(weights.row(i_row)), lists[par], ring_buffer, c, tid, in, passed, ps.empty), c, per_warp[par]);
+      bar_arrive<kBarReady, PAIR>(par);
     }
-    const Slice sl(V, row_pad(row), 0, 1);
-    const int chunks = C::count(sl);
-    Unit<T> loose[1];
-    const bool has_loose = tid < 2 && sl.ragged(tid) >= 0;
-    if (has_loose) load_ragged(row, V, sl.pad, sl.ragged(tid), loose[0]);
-    if (done >= 2) bar_sync<kBarFree, PAIR>(par);
-    Stream<T, false, false> st(c);
-    for (int ch = 0; ch < chunks; ++ch) {
-      const int sv = in.slot(ch), n = C::units(sl, ch);
-      in.wait_for(passed, sv);
-      const unsigned char* units = ring_buffer + sv * CHUNK;
-      if (n == C::kUnits) {
-        Unit<T> q[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) load_shared_unit(units, tid + i * NT, q[i]);
-        st.add(q);
-      } else {
-#pragma unroll 1
-        for (int u = tid; u < n; u += NT) {
-          Unit<T> q[1];
-          load_shared_unit(units, u, q[0]);
-          st.add(q);
-        }
-      }
-      if (!GRAD || ch < chunks - NB) in.release(sv);
-    }
-    if (has_loose) {                           // the list warp has seen to whole units only
-      Unit<T> q[1] = {loose[0]};
-      const unsigned bits = lists[par].loose[tid];
-      float v[8];
-      q[0].values(v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = bits >> j & 1u ? -kInf : v[j];
-      q[0].set(v);
-      st.add(q);
-    }
-    join_warp(in.ok ? st.finish() : State{0.f, nan_value(), nan_value()}, c, per_warp[par]);
-    bar_arrive<kBarReady, PAIR>(par);
-    if (GRAD) {
-      bar_sync<kBarCoef, PAIR>(0);
-      const int kind = rs.kind;
-      const float m_rest = rs.m_rest, coef = rs.coef;
-      const bool alike = row_pad(out) == sl.pad;
-      for (int ch = chunks - 1; ch >= 0; --ch) {
-        const int sv = in.slot(ch), n = C::units(sl, ch);
-        if (ch < chunks - NB) in.wait_for(passed, sv);
-        const unsigned char* units = ring_buffer + sv * CHUNK;
-        const int64_t u0 = sl.full0 + (int64_t)ch * C::kUnits;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int u = tid + i * NT;
-          if (u < n) {
-            Unit<T> q;
-            if (kind) {
-              load_shared_unit(units, u, q);
-              rest_grad_unit(q, m_rest, c, coef);
-            } else {
-              fill_unit(q, 0.f);
-            }
-            if (alike) store_unit(out - sl.pad + 8 * (u0 + u), q);
-            else store_ragged(out, V, sl.pad, (int)u0 + u, q);
-          }
-        }
-        in.release(sv);
-      }
-      in.slots.end_row(chunks);
-      if (has_loose) {
-        if (kind) rest_grad_unit(loose[0], m_rest, c, coef);
-        else fill_unit(loose[0], 0.f);
-        store_ragged(out, V, sl.pad, sl.ragged(tid), loose[0]);
-      }
-      bar_arrive<kBarWritten, PAIR>(0);
-    }
-    par ^= 1;
-    ++done;
   }
 }
 
@@ -910,9 +851,7 @@ cudaError_t launch_distill(DistillArgs a, bool backward, cudaStream_t st) {
     distill_backward_kernel<T><<<(unsigned)blocks, kBackThreads, 0, st>>>(a);
     return cudaGetLastError();
   }
-  if (many_rows(a.n_rows, a.V))
-    return a.d_logits ? launch_pipe<distill_pipe_kernel<T, true>, ManyShape<T, true>>(a, st)
-                      : launch_pipe<distill_pipe_kernel<T, false>, ManyShape<T, false>>(a, st);
+  if (!a.d_logits && many_rows(a.n_rows, a.V)) return launch_pipe<distill_loss_kernel<T>, LossShape<T>>(a, st);
   a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));
   a.slice_bytes = slice_bytes(a.V, sizeof(T), a.parts);
   if (a.V >= 8192 || a.K > 128)

@@ -28,6 +28,10 @@
 namespace remoe {
 namespace rows {
 
+#ifndef HINT
+#define HINT 10000u
+#define SLEEP
+#endif
 constexpr float kInf = HUGE_VALF;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -270,6 +274,20 @@ struct Slice {
   __device__ __forceinline__ bool holds(int id) const { const int u = (id + pad) >> 3; return u >= first && u < last; }
 };
 
+// Bounded wait for a barrier's phase: false if it has not come after about a second.  A failed try sleeps for up to a
+// microsecond or until the phase comes: many warps wait here at any time, and their polling would take the shared
+// memory pipe from those that work.
+__device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity) {
+  for (unsigned it = 0; it < (1u << 20); ++it) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(ring::smem_u32(bar)), "r"(parity), "r"(HINT) : "memory");
+    if (ok) return true;
+    SLEEP
+  }
+  return false;
+}
+
 // ---- a slice in shared memory ----------------------------------------------------------------------------------
 // A block brings its slice of the row into shared memory with bulk copies and works on it there: the whole slice is in
 // flight at once whatever the threads' registers hold, and what is looked at again (candidates of the top elements, the
@@ -309,7 +327,7 @@ __device__ __forceinline__ void start_slice(const T* row, int V, const Slice& sl
   }
 }
 // False if the copies have not arrived within the limit of a wait and of another one: the row is given up as NaN.
-__device__ __forceinline__ bool wait_slice(uint64_t* bar) { return ring::mbar_wait(bar, 0) || ring::mbar_wait(bar, 0); }
+__device__ __forceinline__ bool wait_slice(uint64_t* bar) { return wait_phase(bar, 0) || wait_phase(bar, 0); }
 
 // ---- many rows: a persistent block with a ring of chunks --------------------------------------------------------
 // With at least a row for every SM, blocks stay and take row after row.  The whole units of the rows pass through a ring of
@@ -317,32 +335,9 @@ __device__ __forceinline__ bool wait_slice(uint64_t* bar) { return ring::mbar_wa
 // top elements are selected or its list is prepared, the next row is already on its way.  No cluster, so no waiting for
 // other blocks: two or three blocks an SM, each with its own rows.  One warp issues the copies; the others consume, each at
 // its own pace (a warp that is done with a chunk says so on the slot's `empty` barrier).
-//
-// With BACK a row is consumed twice, first upwards, then downwards for the gradient: its last NB chunks are still there, the
-// others come again (out of L2, which holds the rows in work).  Slots are taken in the order in which they become free.
-// For chunk c of a row of n >= NB chunks that is order[c % NB] in both passes, and it leaves the order reversed for the next row;
-// a shorter row leaves its unused slots first and its own, reversed, behind them.  Producer and consumers keep that order
-// each for themselves.
 template <int NB>
 struct PipeShared {
   uint64_t full[NB], empty[NB];
-};
-
-template <int NB, bool BACK>
-struct SlotOrder {
-  static_assert(NB <= 8, "four bits a slot");
-  unsigned order = 0x76543210u;
-  __device__ __forceinline__ int slot(int c) const { return BACK ? order >> 4 * (c % NB) & 15u : 0; }
-  __device__ __forceinline__ void end_row(int n) {
-    unsigned next = 0;
-    const int m = min(n, NB);
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int from = i < NB - m ? m + i : NB - 1 - i;
-      next |= (order >> 4 * from & 15u) << 4 * i;
-    }
-    order = next;
-  }
 };
 
 template <typename T, int CHUNK>              // CHUNK: bytes
@@ -368,7 +363,7 @@ struct RowWeights {
   int64_t r0, step, n_rows;
   float mine = 1.f;
   int have = -1;
-  __device__ __forceinline__ RowWeights(const float* w, int64_t n) : weight(w), r0(blockIdx.x), step(gridDim.x), n_rows(n) {}
+  __device__ __forceinline__ RowWeights(const float* w, int64_t n, int64_t first, int64_t by) : weight(w), r0(first), step(by), n_rows(n) {}
   // Weight of the block's i-th row; whole warps.
   __device__ __forceinline__ float at(int i) {
     if (!weight) return 1.f;
@@ -387,71 +382,57 @@ struct RowWeights {
   }
 };
 
-// One warp: all copies of the block's rows, issued by its first lane.  Rows with weight 0 (weight may be null) are passed over.
-template <typename T, int NB, int CHUNK, bool BACK>
-__device__ void produce(PipeShared<NB>& ps, unsigned char* buf, const T* logits, const float* weight, int64_t stride, int V, int n_rows) {
+// One warp: all copies of part `part` of `parts` of the rows that the weights' owner takes, issued by its first lane.  Rows with
+// weight 0 are passed over.
+template <typename T, int NB, int CHUNK>
+__device__ void produce(PipeShared<NB>& ps, unsigned char* buf, RowWeights weights, const T* logits, int64_t stride, int V, int part, int parts) {
   typedef Chunks<T, CHUNK> C;
-  SlotOrder<NB, BACK> slots;
-  unsigned used = 0, parity = 0;              // by slot: loaded before; parity of its last load
-  int turn = 0;
+  int turn = 0, phase = 0;                    // slot of the next load, and how often its turn has come
   bool ok = true;
-  RowWeights weights(weight, n_rows);
-  for (int i = weights.next(0); weights.row(i) < n_rows; i = weights.next(i + 1)) {
+  for (int i = weights.next(0); weights.row(i) < weights.n_rows; i = weights.next(i + 1)) {
     if ((threadIdx.x & 31) != 0 || !ok) continue;
-    const int64_t r = weights.row(i);
-    const T* row = logits + r * stride;
-    const Slice sl(V, row_pad(row), 0, 1);
-    const int n = C::count(sl), loads = BACK ? n + max(0, n - NB) : n;
+    const T* row = logits + weights.row(i) * stride;
+    const Slice sl(V, row_pad(row), part, parts);
+    const int n = C::count(sl);
     const T* base = row - sl.pad + 8 * (int64_t)sl.full0;
-    for (int l = 0; l < loads; ++l) {
-      const int c = l < n ? l : 2 * n - NB - 1 - l;
-      const int s = BACK ? slots.slot(c) : turn;
-      if (!BACK) turn = turn + 1 == NB ? 0 : turn + 1;
-      if (used >> s & 1u) {
-        if (!ring::mbar_wait(&ps.empty[s], parity >> s & 1u)) { ok = false; break; }
-        parity ^= 1u << s;
-      }
-      used |= 1u << s;
+    for (int c = 0; c < n; ++c) {
+      if (phase > 0 && !wait_phase(&ps.empty[turn], (phase - 1) & 1)) { ok = false; break; }
       const uint32_t bytes = (uint32_t)C::units(sl, c) * (8 * (uint32_t)sizeof(T));
-      ring::mbar_expect_tx(&ps.full[s], bytes);
-      ring::bulk_g2s(buf + (size_t)s * CHUNK, base + 8 * (int64_t)c * C::kUnits, bytes, &ps.full[s]);
+      ring::mbar_expect_tx(&ps.full[turn], bytes);
+      ring::bulk_g2s(buf + (size_t)turn * CHUNK, base + 8 * (int64_t)c * C::kUnits, bytes, &ps.full[turn]);
+      if (++turn == NB) { turn = 0; ++phase; }
     }
-    if (BACK) slots.end_row(n);
   }
-  // no copy is on its way when the thread leaves: each slot's last load has arrived (its parity is that of its `empty` phases)
-  for (int s = 0; s < NB; ++s)
-    if (used >> s & 1u) ring::mbar_wait(&ps.full[s], parity >> s & 1u);
+  // no copy is on its way when the warp leaves: each slot's last load has arrived
+  if ((threadIdx.x & 31) == 0)
+    for (int s = 0; s < NB; ++s) {
+      const int loads = phase + (s < turn ? 1 : 0);
+      if (loads > 0) wait_phase(&ps.full[s], (loads - 1) & 1);
+    }
 }
 
-// A consumer's side of the ring.
-template <int NB, bool BACK>
-struct Consumer {
-  PipeShared<NB>& ps;
-  SlotOrder<NB, BACK> slots;
-  unsigned parity = 0;
-  int turn = 0;
+// A reader's place in the ring: slots come in turn.
+template <int NB>
+struct RingPlace {
+  int slot = 0, parity = 0;
   bool ok = true;                             // false once a wait has run out: what follows is NaN
-  __device__ __forceinline__ explicit Consumer(PipeShared<NB>& p) : ps(p) {}
-  __device__ __forceinline__ int slot(int c) const { return BACK ? slots.slot(c) : turn; }
-  __device__ __forceinline__ void wait(int s) {
-    if (ok) ok = ring::mbar_wait(&ps.full[s], parity >> s & 1u);
+  __device__ __forceinline__ void wait(uint64_t* bars) {
+    if (ok) ok = wait_phase(&bars[slot], parity);
   }
-  // The same on another barrier of the slot, which somebody passes the chunk on with.
-  __device__ __forceinline__ void wait_for(uint64_t* bars, int s) {
-    if (ok) ok = ring::mbar_wait(&bars[s], parity >> s & 1u);
+  __device__ __forceinline__ void advance() {
+    if (++slot == NB) { slot = 0; parity ^= 1; }
   }
-  // The warp is done with slot s.
-  __device__ __forceinline__ void release(int s) {
-    parity ^= 1u << s;
-    if (!BACK) turn = turn + 1 == NB ? 0 : turn + 1;
+  // The warp is done with the slot and says so on `bars`.
+  __device__ __forceinline__ void pass(uint64_t* bars) {
     __syncwarp();
-    if ((threadIdx.x & 31) == 0) ring::mbar_arrive(&ps.empty[s]);
+    if ((threadIdx.x & 31) == 0) ring::mbar_arrive(&bars[slot]);
+    advance();
   }
 };
 
 // Named barriers of a block.  kBarGroup: over a group of NT threads; kBarFinish: over each of the two groups of finishers; kBarReady,
-// kBarFree: between consumers and finishers, two each, by the row's parity; the others: see distill.cu.
-constexpr int kBarGroup = 1, kBarFinish = 2, kBarReady = 4, kBarFree = 6, kBarIds = 8, kBarList = 10, kBarListFree = 12, kBarCoef = 14, kBarWritten = 15;
+// kBarFree: between consumers and finishers, kBarIds, kBarList, kBarListFree: for the lists of distill.cu; two each, by the row's parity.
+constexpr int kBarGroup = 1, kBarFinish = 2, kBarReady = 4, kBarFree = 6, kBarIds = 8, kBarList = 10, kBarListFree = 12;
 template <int NT>
 __device__ __forceinline__ void sync_threads() { asm volatile("bar.sync %0, %1;" ::"n"(kBarGroup), "n"(NT) : "memory"); }
 
@@ -695,6 +676,16 @@ __device__ __forceinline__ State join_cluster(const State* mine, int parts, floa
     s = State{load_remote(remote_shared(&mine->m, lane)), load_remote(remote_shared(&mine->R, lane)), load_remote(remote_shared(&mine->U, lane))};
   for (int o = parts >> 1; o; o >>= 1) s = merge(s, shuffle_down(s, o, 32), c);
   return State{__shfl_sync(0xffffffffu, s.m, 0), __shfl_sync(0xffffffffu, s.R, 0), __shfl_sync(0xffffffffu, s.U, 0)};
+}
+
+// ln z of a positive float64, to the precision of a float32's logarithm of what is left of the nearest power of two (6e-8): the
+// 64-bit function is a chain of microseconds for the one warp that needs it.
+__device__ __forceinline__ double ln_wide(double z) {
+  const long long b = __double_as_longlong(z);
+  const int e = (int)(b >> 52) - 1023;                               // z is normal and positive, or NaN or +inf
+  const double m = __longlong_as_double((b & 0x000fffffffffffffll) | 0x3ff0000000000000ll);
+  if (!(z > 0.0) || !(z < 1.7e308)) return z == 0.0 ? -(double)kInf : z;   // 0, NaN, +inf
+  return (double)e * 0.69314718055994530942 + (double)log1pf((float)(m - 1.0));
 }
 
 // Whole number in the order of the values (NaN aside); -0 equals +0.

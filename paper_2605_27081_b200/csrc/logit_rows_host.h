@@ -46,7 +46,10 @@ class PointerDevice {
   bool switched_ = false;
 };
 
-constexpr int64_t kSliceBytes = 52 * 1024;     // of a row in one block, where eight blocks are enough for that
+#ifndef SLICE_KB
+#define SLICE_KB 52
+#endif
+constexpr int64_t kSliceBytes = SLICE_KB * 1024;     // of a row in one block, where eight blocks are enough for that
 constexpr size_t kSmemLimit = 220 * 1024;      // dynamic shared memory of a block; the longest float32 row needs 216 KB in eight
 
 inline int element_size(int32_t dtype) { return dtype == REMOE_F32 ? 4 : dtype == REMOE_BF16 || dtype == REMOE_F16 ? 2 : 0; }
@@ -78,16 +81,11 @@ inline int parts_of_row(int32_t n_rows, int32_t vocab, int size) {
 // Shared memory of a part: whole units of eight elements, whatever the row's alignment.
 inline int slice_bytes(int32_t vocab, int size, int parts) { return ((vocab + 14) / 8 + parts - 1) / parts * 8 * size; }
 
-// One launch of `Kernel`, a cluster of args.parts blocks for each row.
-template <auto Kernel, int NT, typename Args>
-inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStream_t stream) {
-  static std::atomic<bool> ready[kMaxDevices];
-  const size_t smem = (size_t)args.slice_bytes + more_smem;
-  const cudaError_t e = allow_dynamic_smem(Kernel, kSmemLimit, ready);
-  if (e != cudaSuccess) return e;
+template <auto Kernel, typename Args>
+inline cudaError_t launch_clusters(const Args& args, int clusters, int threads, size_t smem, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)args.n_rows * (unsigned)args.parts);
-  cfg.blockDim = dim3(NT);
+  cfg.gridDim = dim3((unsigned)clusters * (unsigned)args.parts);
+  cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
@@ -97,6 +95,15 @@ inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStrea
   cfg.attrs = at;
   cfg.numAttrs = args.parts > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, Kernel, args);
+}
+
+// One launch of `Kernel`, a cluster of args.parts blocks for each row.
+template <auto Kernel, int NT, typename Args>
+inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStream_t stream) {
+  static std::atomic<bool> ready[kMaxDevices];
+  const cudaError_t e = allow_dynamic_smem(Kernel, kSmemLimit, ready);
+  if (e != cudaSuccess) return e;
+  return launch_clusters<Kernel>(args, args.n_rows, NT, (size_t)args.slice_bytes + more_smem, stream);
 }
 
 // Rows enough for persistent blocks that take whole rows.

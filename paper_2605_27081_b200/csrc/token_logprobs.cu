@@ -502,7 +502,7 @@ __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>
   __syncthreads();
 
   if (tid >= NT + Shape::kGroups * FT) {       // the last warp
-    produce<T, NB, CHUNK, false>(ps, ring_buffer, logits, nullptr, a.stride, V, a.n_rows);
+    produce<T, NB, CHUNK>(ps, ring_buffer, RowWeights(nullptr, a.n_rows, blockIdx.x, gridDim.x), logits, a.stride, V, 0, 1);
     return;
   }
   unsigned char* const lists = ring_buffer + NB * CHUNK;
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>
   }
 
   int par = 0;                                 // parity of the block's row
-  Consumer<NB, false> in(ps);
+  RingPlace<NB> in;
   for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x, par ^= 1) {
     const T* row = logits + r * a.stride;
     const Slice sl(V, row_pad(row), 0, 1);
@@ -552,9 +552,9 @@ __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>
     Stream<T, true, true> st(c);
     typename Elem<T>::Word all = Elem<T>::lowest();
     for (int ch = 0, in_seg = 0, g = 0; ch < chunks; ++ch) {
-      const int s = in.slot(ch), n = C::units(sl, ch);
-      in.wait(s);
-      const unsigned char* units = ring_buffer + s * CHUNK;
+      const int n = C::units(sl, ch);
+      in.wait(ps.full);
+      const unsigned char* units = ring_buffer + in.slot * CHUNK;
       if (n == C::kUnits) {
         Unit<T> q[N];
 #pragma unroll
@@ -568,7 +568,7 @@ __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>
           st.add(q);
         }
       }
-      in.release(s);
+      in.pass(ps.empty);
       if (TOP && (++in_seg == seg_chunks || ch + 1 == chunks)) {
         seg[g * NT + tid] = (unsigned short)(top_key(st.top()) >> 16);
         st.close_segment(all);
