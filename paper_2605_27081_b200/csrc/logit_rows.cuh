@@ -462,6 +462,62 @@ __device__ __forceinline__ void bar_arrive(int parity) {
   else asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(NT) : "memory");
 }
 
+// ---- element-wise passes ---------------------------------------------------------------------------------------
+// A block's piece [u0, u1) of a row's units, written to `out` through f(unit number, unit), 64 bytes a thread at a time; the first
+// are loaded before it is known whether the row counts.  Stores are whole units of `out`; loads are where `row` lies alike.
+// Many small blocks hide the latency better than loads a step ahead (275 us against 264 for 4096 x 102400 bf16: the registers
+// cost more blocks than the loads gain).
+constexpr int kPieceThreads = 256;
+template <typename T>
+struct Piece {
+  static constexpr int kUnits = sizeof(T) == 2 ? 4 : 2;
+  const T* row;
+  T* out;
+  int V, pad, full0, full1, u0, u1;
+  bool alike;
+  __device__ __forceinline__ Piece(const T* row_, T* out_, int V_, int part, int parts) : row(row_), out(out_), V(V_), pad(row_pad(out_)) {
+    const int units = (V + pad + 7) >> 3, per = (units + parts - 1) / parts;
+    alike = row_pad(row_) == pad;
+    full0 = pad > 0 ? 1 : 0;
+    full1 = (V + pad) >> 3;
+    u0 = min(part * per, units);
+    u1 = min(u0 + per, units);
+  }
+  __device__ __forceinline__ void load(int u, Unit<T>& q) const {
+    if (alike && u >= full0 && u < full1) load_unit(row - pad + 8 * (int64_t)u, q);
+    else load_ragged(row, V, pad, u, q);
+  }
+  __device__ __forceinline__ void store(int u, const Unit<T>& q) const {
+    if (u >= full0 && u < full1) store_unit(out - pad + 8 * (int64_t)u, q);
+    else store_ragged(out, V, pad, u, q);
+  }
+  __device__ __forceinline__ void load_batch(int u, Unit<T> (&q)[kUnits]) const {
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+      if (u + i * kPieceThreads < u1) load(u + i * kPieceThreads, q[i]);
+  }
+  template <typename F>
+  __device__ __forceinline__ void run(Unit<T> (&q)[kUnits], F f) const {
+    for (int u = u0 + threadIdx.x; u < u1;) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+        if (u + i * kPieceThreads < u1) f(u + i * kPieceThreads, q[i]);
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+        if (u + i * kPieceThreads < u1) store(u + i * kPieceThreads, q[i]);
+      u += kPieceThreads * kUnits;
+      load_batch(u, q);
+    }
+  }
+  // The same where the row is not looked at: every element is `value`.
+  __device__ __forceinline__ void fill(float value) const {
+    const float v[8] = {value, value, value, value, value, value, value, value};
+    Unit<T> q;
+    q.set(v);
+    for (int u = u0 + threadIdx.x; u < u1; u += kPieceThreads) store(u, q);
+  }
+};
+
 // ---- one-pass sums -------------------------------------------------------------------------------------------
 
 struct State {

@@ -120,5 +120,11 @@ inline cudaError_t launch_pipe(const Args& args, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
+// Blocks a row for the element-wise passes: of about `piece` bytes each.
+inline int pieces_of_row(int32_t vocab, int size, int piece) {
+  const int64_t bytes = (int64_t)vocab * size;
+  return (int)(bytes <= piece ? 1 : (bytes + piece / 2) / piece);
+}
+
 }  // namespace rows
 }  // namespace remoe

@@ -676,13 +676,15 @@ __device__ __forceinline__ void logprob_grad_unit(Unit<T>& q, float m, float c, 
   }
 }
 
-constexpr int kGradThreads = 256, kGradUnits = 4;
+constexpr int kGradThreads = 256;
+template <typename T>
+constexpr int kGradUnits = sizeof(T) == 2 ? 4 : 1;
 
-// Element-wise: what a row's gradient shares is in its row_stats.  Long rows: `tiles` blocks a row, each thread four
-// units.  Short rows (SMALL): one unit a thread over all rows' units.
+// Element-wise: what a row's gradient shares is in its row_stats.  Long rows: `tiles` blocks a row, each thread 64 bytes
+// (32 of float32: twice the registers a byte).  Short rows (SMALL): one unit a thread over all rows' units.
 template <typename T, bool SMALL>
 __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const __grid_constant__ LogprobGradArgs a) {
-  constexpr int N = SMALL ? 1 : kGradUnits;
+  constexpr int N = SMALL ? 1 : kGradUnits<T>;
   int64_t r;
   int u0;
   if (SMALL) {
@@ -774,14 +776,14 @@ cudaError_t launch_logprobs(LogprobArgs a, cudaStream_t st) {
 
 template <typename T>
 cudaError_t launch_logprobs_grad(LogprobGradArgs a, cudaStream_t st) {
-  const int units = (a.V + 15) >> 3;                       // any alignment
+  const int units = (a.V + 14) >> 3;                       // any alignment
   int64_t blocks;
   const bool small = units <= kGradThreads;
   if (small) {
     a.tiles = units;
     blocks = ((int64_t)a.n_rows * units + kGradThreads - 1) / kGradThreads;
   } else {
-    a.tiles = (units + kGradThreads * kGradUnits - 1) / (kGradThreads * kGradUnits);
+    a.tiles = (units + kGradThreads * kGradUnits<T> - 1) / (kGradThreads * kGradUnits<T>);
     blocks = (int64_t)a.n_rows * a.tiles;
   }
   if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
