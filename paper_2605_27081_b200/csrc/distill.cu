@@ -507,16 +507,10 @@ __device__ __forceinline__ State sum_slice(const T* row, int V, const Slice& sl,
 //   passer     takes the list's elements out of the chunks;
 //   consumers  sum what is left;
 //   finisher   joins sums and list and writes the loss.
-#ifndef DM_NT
-#define DM_NT 128
-#define DM_B 4
-#define DM_U 6
-#define DM_NB 3
-#endif
 template <typename T>
 struct LossShape {
-  static constexpr int kConsumers = DM_NT, kBlocks = DM_B, kSlots = DM_NB;
-  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? DM_U : 4);
+  static constexpr int kConsumers = 128, kBlocks = 4, kSlots = 3;
+  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? 6 : 4);
   static constexpr int kThreads = kConsumers + 160;
   static constexpr size_t kSmem = (size_t)kChunk * kSlots;
 };
@@ -641,6 +635,7 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
   __syncwarp();
   bool bad = false;
   float ytop = -kInf;
+#pragma unroll 4
   for (int k = lane; k < K; k += LPR) {
     const int id = a.ids[rr * K + k];
     const float y = a.y[rr * K + k];
@@ -656,6 +651,7 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
   ytop = group_max(ytop);
   const bool some = ytop > -kInf;
   bool twice = false;
+#pragma unroll 4
   for (int k = lane; k < K; k += LPR) twice = twice || (s_id[gi][k] >= 0 && s_owner[gi][s_id[gi][k]] != k);
   twice = group_any(twice);
   double ln_q = 0.0, qs = 0.0, entropy = 0.0;     // entropy: sum of q ln q over the list
@@ -663,12 +659,14 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
     ln_q = a.stats_in[8 * rr + 5];
   } else if (some) {
     const double shift = a.tail ? 0.0 : (double)ytop;
+#pragma unroll 4
     for (int k = lane; k < K; k += LPR) qs += a.tail ? exp((double)s_y[gi][k]) : (double)exp32((double)s_y[gi][k] - shift);
   }
   if (!BACKWARD) {
     qs = group_sum(qs);
     ln_q = a.tail || !some ? 0.0 : (double)ytop + ln_wide(qs);
   }
+#pragma unroll 4
   for (int k = lane; k < K; k += LPR) {
     const int id = s_id[gi][k];
     if (id < 0) continue;

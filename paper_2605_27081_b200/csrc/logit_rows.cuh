@@ -28,10 +28,6 @@
 namespace remoe {
 namespace rows {
 
-#ifndef HINT
-#define HINT 10000u
-#define SLEEP
-#endif
 constexpr float kInf = HUGE_VALF;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -274,16 +270,14 @@ struct Slice {
   __device__ __forceinline__ bool holds(int id) const { const int u = (id + pad) >> 3; return u >= first && u < last; }
 };
 
-// Bounded wait for a barrier's phase: false if it has not come after about a second.  A failed try sleeps for up to a
-// microsecond or until the phase comes: many warps wait here at any time, and their polling would take the shared
-// memory pipe from those that work.
+// Bounded wait for a barrier's phase: false if it has not come after a second or so.  A failed try sleeps for up to ten
+// microseconds or until the phase comes.
 __device__ __forceinline__ bool wait_phase(uint64_t* bar, uint32_t parity) {
-  for (unsigned it = 0; it < (1u << 20); ++it) {
+  for (unsigned it = 0; it < (1u << 17); ++it) {
     uint32_t ok;
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(ring::smem_u32(bar)), "r"(parity), "r"(HINT) : "memory");
+                 : "=r"(ok) : "r"(ring::smem_u32(bar)), "r"(parity), "r"(10000u) : "memory");
     if (ok) return true;
-    SLEEP
   }
   return false;
 }
@@ -430,8 +424,8 @@ struct RingPlace {
   }
 };
 
-// Named barriers of a block.  kBarGroup: over a group of NT threads; kBarFinish: over each of the two groups of finishers; kBarReady,
-// kBarFree: between consumers and finishers, kBarIds, kBarList, kBarListFree: for the lists of distill.cu; two each, by the row's parity.
+// Named barriers of a block.  kBarGroup: over a group of NT threads; kBarFinish: over the finishers; kBarReady, kBarFree: between
+// consumers and finishers, kBarIds, kBarList, kBarListFree: for the lists of distill.cu, two each, by the row's parity.
 constexpr int kBarGroup = 1, kBarFinish = 2, kBarReady = 4, kBarFree = 6, kBarIds = 8, kBarList = 10, kBarListFree = 12;
 template <int NT>
 __device__ __forceinline__ void sync_threads() { asm volatile("bar.sync %0, %1;" ::"n"(kBarGroup), "n"(NT) : "memory"); }
@@ -450,10 +444,9 @@ __device__ __forceinline__ void bar_sync(int parity) {
   else asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(NT) : "memory");
 }
 template <int NT>
-struct FinishGroup {                          // the finishers of the rows of one parity
+struct FinishGroup {                          // the finishers
   static constexpr int kThreads = NT;
-  int parity;
-  __device__ __forceinline__ void sync() const { bar_sync<kBarFinish, NT>(parity); }
+  __device__ __forceinline__ void sync() const { bar_sync<kBarFinish, NT>(0); }
 };
 template <int ID, int NT>
 __device__ __forceinline__ void bar_arrive(int parity) {

@@ -46,10 +46,7 @@ class PointerDevice {
   bool switched_ = false;
 };
 
-#ifndef SLICE_KB
-#define SLICE_KB 52
-#endif
-constexpr int64_t kSliceBytes = SLICE_KB * 1024;     // of a row in one block, where eight blocks are enough for that
+constexpr int64_t kSliceBytes = 52 * 1024;     // of a row in one block, where eight blocks are enough for that
 constexpr size_t kSmemLimit = 220 * 1024;      // dynamic shared memory of a block; the longest float32 row needs 216 KB in eight
 
 inline int element_size(int32_t dtype) { return dtype == REMOE_F32 ? 4 : dtype == REMOE_BF16 || dtype == REMOE_F16 ? 2 : 0; }

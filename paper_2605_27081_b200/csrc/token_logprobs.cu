@@ -4,19 +4,6 @@
 //   p = softmax(s x), lp = s (x_token - m) - ln Z, H = ln Z - (1/Z) sum s (x - m) e^{s (x - m)}
 //   dx = s [ g_lp (1[v = token] - p) - g_H p (ln p + H) ]
 #include "logit_rows.cuh"
-#ifndef MANY_NT
-#define MANY_NT 128
-#define MANY_B 5
-#define MANY_U 6
-#define MANY_NB 3
-#define MANY_NTT 256
-#define MANY_BT 2
-#define MANY_UT 6
-#define MANY_NBT 2
-#define MANY_FT 128
-#define MANY_G 1
-#define MANY_AT 6
-#endif
 #include "logit_rows_host.h"
 
 namespace remoe {
@@ -76,7 +63,7 @@ struct SharedSource {
 constexpr int kSegments = 16;
 template <typename T, int NT, int UNITS>
 struct RowSource {
-  static constexpr int kKeys = NT, kAtOnce = MANY_AT;
+  static constexpr int kKeys = NT, kAtOnce = 6;
   const T* row;
   int n_units, id0, V, full0, full1, pad;
   const uint32_t* keys;
@@ -467,11 +454,11 @@ typedef TopShared<768, 1024> ManyShared;
 // consumer, chunks in the ring.
 template <typename T, bool TOP>
 struct ManyShape {
-  static constexpr int kConsumers = TOP ? MANY_NTT : MANY_NT, kFinishers = TOP ? MANY_FT : 32, kGroups = TOP ? MANY_G : 1, kBlocks = TOP ? MANY_BT : MANY_B;
-  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? (TOP ? MANY_UT : MANY_U) : 4), kSlots = TOP ? MANY_NBT : MANY_NB;
-  static constexpr int kThreads = kConsumers + 32 + kGroups * kFinishers;
+  static constexpr int kConsumers = TOP ? 256 : 128, kFinishers = TOP ? 128 : 32, kBlocks = TOP ? 2 : 5;
+  static constexpr int kChunk = kConsumers * 16 * (sizeof(T) == 2 ? 6 : 4), kSlots = TOP ? 2 : 3;
+  static constexpr int kThreads = kConsumers + 32 + kFinishers;
   static constexpr size_t kSegBytes = (size_t)kSegments * kConsumers * sizeof(short);
-  static constexpr size_t kSmem = (size_t)kChunk * kSlots + (TOP ? kGroups * sizeof(ManyShared) + 2 * kSegBytes : 0);
+  static constexpr size_t kSmem = (size_t)kChunk * kSlots + (TOP ? sizeof(ManyShared) + 2 * kSegBytes : 0);
 };
 
 // What the consumers hand over at the end of a row, twice.
@@ -482,9 +469,10 @@ struct Handover {
 };
 
 // Many rows: persistent blocks, each takes row after row through its ring of chunks.  One warp issues the copies, the
-// consumers sum, and two groups of finishers, each for every second row, join a row's sums, select its top elements and write
-// while the consumers are at the next rows (two ahead at most).  A finisher's loads queue behind the copies on their way to
-// the SM, 3 to 5 us, which is why there are two groups.
+// consumers sum, and the finishers join a row's sums, select its top elements and write while the consumers are at the next
+// row already (two ahead at most).  What bounds it: without alternatives the memory (4096 x 102400 bf16: 135 us, 0.95 of the copy
+// rate); with them the finishers, 15 us a row, since their loads queue for 3 to 5 us behind the copies on their way to the SM
+// (2048 x 131072 bf16, 64 alternatives: 131 to 136 us; 110 without the selection).
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>::kBlocks) logprob_pipe_kernel(const __grid_constant__ LogprobArgs a) {
   typedef ManyShape<T, TOP> Shape;
@@ -501,19 +489,18 @@ __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>
   if (tid == 0) init_pipe(ps, NT / 32);
   __syncthreads();
 
-  if (tid >= NT + Shape::kGroups * FT) {       // the last warp
+  if (tid >= NT + FT) {                        // the last warp
     produce<T, NB, CHUNK>(ps, ring_buffer, RowWeights(nullptr, a.n_rows, blockIdx.x, gridDim.x), logits, a.stride, V, 0, 1);
     return;
   }
   unsigned char* const lists = ring_buffer + NB * CHUNK;
-  auto segments_of = [&](int parity) { return reinterpret_cast<unsigned short*>(lists + Shape::kGroups * sizeof(ManyShared) + parity * Shape::kSegBytes); };
+  auto segments_of = [&](int parity) { return reinterpret_cast<unsigned short*>(lists + sizeof(ManyShared) + parity * Shape::kSegBytes); };
   if (tid >= NT) {
-    constexpr int G = Shape::kGroups;
-    const int g = (tid - NT) / FT, ft = (tid - NT) % FT;         // with two groups, each has the rows of one parity
-    ManyShared& sh = *reinterpret_cast<ManyShared*>(lists + g * sizeof(ManyShared));
-    const FinishGroup<FT> group{g};
-    int par = g;
-    for (int64_t r = (int64_t)blockIdx.x + g * (int64_t)gridDim.x; r < a.n_rows; r += G * (int64_t)gridDim.x, par ^= G & 1) {
+    const int ft = tid - NT;
+    ManyShared& sh = *reinterpret_cast<ManyShared*>(lists);
+    const FinishGroup<FT> group;
+    int par = 0;                               // parity of the block's row
+    for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x, par ^= 1) {
       const T* row = logits + r * a.stride;
       const Slice sl(V, row_pad(row), 0, 1);
       int token = -1;
