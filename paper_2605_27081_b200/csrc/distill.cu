@@ -126,9 +126,10 @@ __device__ __forceinline__ void finish_row(const DistillArgs& a, int64_t r, floa
   const bool alive = m != -kInf, others = rest.m > -kInf;        // a NaN is alive
   const double x_shift = l.m_list != -kInf ? (double)l.m_list : 0.0;
   const double grow = 1.0 + (double)rest.R;
-  // one of the two is 1; the other's float32 rounding is that of a part of Z
-  const float c = a.s * kLog2e;
-  const double of_rest = others ? (double)ex2((rest.m - m) * c) : 0.0, of_list = l.m_list != -kInf ? (double)ex2((l.m_list - m) * c) : 0.0;
+  // one of the two is 1, or both are
+  const bool list_on_top = l.m_list >= rest.m;
+  const double lesser = others && l.m_list != -kInf ? exp(((double)(list_on_top ? rest.m : l.m_list) - m) * s) : 1.0;
+  const double of_rest = !others ? 0.0 : list_on_top ? lesser : 1.0, of_list = l.m_list == -kInf ? 0.0 : list_on_top ? 1.0 : lesser;
   const double z = of_rest * grow + of_list * v.z, inv_z = 1.0 / z, ln_z = ln_wide(z), ln_rest = ln_wide(grow);
   const double of_q = a.tail || !l.some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !l.some ? 0.0 : l.shift + ln_wide(v.q);
   const double q_all = v.q * of_q, q_rest = a.tail && others ? fmax(0.0, 1.0 - v.q) : 0.0;

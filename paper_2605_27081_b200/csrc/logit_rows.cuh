@@ -327,7 +327,7 @@ __device__ __forceinline__ bool wait_slice(uint64_t* bar) { return wait_phase(ba
 // With at least a row for every SM, blocks stay and take row after row.  The whole units of the rows pass through a ring of
 // NB chunks in shared memory, filled by bulk copies that run ahead over the ends of rows: while a row is joined, its
 // top elements are selected or its list is prepared, the next row is already on its way.  No cluster, so no waiting for
-// other blocks: two or three blocks an SM, each with its own rows.  One warp issues the copies; the others consume, each at
+// other blocks: two to five blocks an SM, each with its own rows.  One warp issues the copies; the others consume, each at
 // its own pace (a warp that is done with a chunk says so on the slot's `empty` barrier).
 template <int NB>
 struct PipeShared {
@@ -458,8 +458,6 @@ __device__ __forceinline__ void bar_arrive(int parity) {
 // ---- element-wise passes ---------------------------------------------------------------------------------------
 // A block's piece [u0, u1) of a row's units, written to `out` through f(unit number, unit), 64 bytes a thread at a time; the first
 // are loaded before it is known whether the row counts.  Stores are whole units of `out`; loads are where `row` lies alike.
-// Many small blocks hide the latency better than loads a step ahead (275 us against 264 for 4096 x 102400 bf16: the registers
-// cost more blocks than the loads gain).
 constexpr int kPieceThreads = 256;
 template <typename T>
 struct Piece {

@@ -38,16 +38,18 @@ __device__ __forceinline__ unsigned long long full_key(uint32_t k, int id) { ret
 
 // What the selection looks at: units 0 .. n_units - 1, unit i holding the elements from 8 i + id0 on, those of [0, V) valid.
 // NT threads have each seen some of them; key(i): of the largest element that thread i has seen (0: none).  A column is a
-// group of units whose largest element is known; bit g of columns(i, t): column(i, g) of thread i may reach t.
+// group of units whose largest element is known; bit g of columns(i, t): column(i, g) of thread i may reach t; reach(i, t): how
+// many of them do, for a t whose bits below kReachLow are zero.
 //
 // A block's slice in shared memory; column t: units t, t + NT, ...
 template <typename T, int NT>
 struct SharedSource {
-  static constexpr int kKeys = NT, kAtOnce = 4;
+  static constexpr int kKeys = NT, kAtOnce = 4, kReachLow = 0;
   const unsigned char* units;
   int n_units, id0, V;
   const uint32_t* keys;
   __device__ __forceinline__ uint32_t key(int i) const { return keys[i]; }
+  __device__ __forceinline__ int reach(int i, uint32_t t) const { return keys[i] >= t; }
   __device__ __forceinline__ void load(int i, Unit<T>& q) const { load_shared_unit(units, i, q); }
   __device__ __forceinline__ int per_column() const { return (n_units + NT - 1) / NT; }
   __device__ __forceinline__ int loose() const { return 0; }           // units in no column
@@ -63,13 +65,14 @@ struct SharedSource {
 constexpr int kSegments = 16;
 template <typename T, int NT, int UNITS>
 struct RowSource {
-  static constexpr int kKeys = NT, kAtOnce = 6;
+  static constexpr int kKeys = NT, kAtOnce = 6, kReachLow = 16;
   const T* row;
   int n_units, id0, V, full0, full1, pad;
   const uint32_t* keys;
   const unsigned short* seg;                       // [segment][NT] upper halves of the keys of the largest elements
   int segments, seg_chunks;
   __device__ __forceinline__ uint32_t key(int i) const { return keys[i]; }
+  __device__ __forceinline__ int reach(int i, uint32_t t) const { return __popc(columns(i, t)); }
   __device__ __forceinline__ void load(int i, Unit<T>& q) const {
     if (i >= full0 && i < full1) load_unit(row - pad + 8 * (int64_t)i, q);
     else load_ragged(row, V, pad, i, q);
@@ -139,8 +142,8 @@ __device__ __forceinline__ int group_sum(const Group& group, int tid, int n, int
 // listed, and the list is sorted by counting for each key the keys above it.  A lower t adds candidates and never
 // loses an element.
 // First t: each warp finds the value that its share of `want` of its part of the keys reach, by bits, and the least of these is
-// taken; one barrier.  Where that lets too much through, or a warp's share is large, t is found over the whole group, a
-// barrier for each bit.
+// taken; one barrier.  Where that lets too much through, or a warp's share is large, t is found from the columns' largest
+// elements over the whole group, a barrier for each bit.
 // In masked rows nearly all elements are equal and t is their value.  Then only what is above t is listed, and what is missing
 // are the elements equal to t of the lowest indices, found in one ordered scan that stops as soon as there are enough.
 // Rows whose large elements sit in few columns overflow the list all the same: there the want-th largest value is found by
@@ -193,9 +196,11 @@ __device__ void select_top(const Group& group, const Source& src, int tid, int w
       for (int w = 0; w < W; ++w) t = min(t, (uint32_t)sh.warp_count[w]);
       group.sync();
     } else {
-      for (int b = 31; b >= kLow; --b) {
+      for (int b = 31; b >= (kLow > Source::kReachLow ? kLow : Source::kReachLow); --b) {
         const uint32_t cand = t | (1u << b);
-        const int n = group_sum(group, tid, reach(cand), sh.warp_count);
+        int n = 0;
+        for (int i = tid; i < Source::kKeys; i += FT) n += src.reach(i, cand);
+        n = group_sum(group, tid, n, sh.warp_count);
         if (n >= want) {
           t = cand;
           if (n <= want + want / 4 + 4) break;

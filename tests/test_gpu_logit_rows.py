@@ -97,7 +97,7 @@ def test_logprobs_sizes(T, V, dtype):
 
 # rows enough for the persistent blocks: fewer rows than blocks, more, several a block; rows shorter than the ring, longer
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("T,V,top", [(148, 8192, 0), (150, 9001, 1), (297, 12288, 256), (700, 8199, 30), (160, 33001, 64), (310, 65536, 20), (149, 150001, 100)])
+@pytest.mark.parametrize("T,V,top", [(148, 8192, 0), (150, 9001, 1), (297, 12288, 256), (700, 8199, 30), (160, 33001, 64), (310, 65536, 20), (149, 150001, 100), (150, 40009, 256), (148, 131072, 255)])
 def test_logprobs_many_rows(T, V, top, dtype):
     for pad, offset, s in [(0, 0, 1.0), (1, 3, 0.7)]:
         view, _ = rows(T, V, dtype, seed=V, pad=pad, offset=offset)
@@ -428,6 +428,37 @@ def test_distill_where_little_is_left_outside(V):
     check_distill(view, 1.0, ids, y, 1, torch.ones(6))
 
 
+@pytest.mark.parametrize("dtype", list(DT))
+def test_distill_poison_many_rows(dtype):
+    T, V = 400, 12000
+    x, _ = rows(T, V, dtype, pad=1)
+    ids = torch.randint(0, V, (T, 4), generator=torch.Generator().manual_seed(2)).int()
+    y = torch.log(torch.full((T, 4), 0.2))
+    x[10, 9] = NAN
+    x[11, ids[11, 0].item()] = NAN
+    x[12, V - 1] = INF
+    x[13, ids[13, 2].item()] = INF
+    ids[14, 1] = V
+    ids[15, 0] = -5
+    y[16, 3] = NAN
+    y[17, 3] = INF
+    w = torch.ones(T)
+    x[300:310, 7] = NAN
+    w[300:310] = 0.0
+    ids, y, w = ids.cuda(), y.cuda(), w.cuda()
+    out = torch.full((T, V), 3.0, dtype=x.dtype, device="cuda")
+    for o in (None, out):
+        loss, st = run_distill(x, 1.0, ids, y, 1, w, o, stats=True)
+        assert bool(torch.isnan(loss[10:18]).all()) and bool((loss[300:310] == 0).all())
+        fine = torch.ones(T, dtype=torch.bool, device="cuda")
+        fine[10:18] = False
+        assert bool(torch.isfinite(loss[fine]).all())
+    out2 = torch.full_like(out, 3.0)
+    assert rb.remoe_distill_topk_backward(T, V, DT[dtype][1], x, x.stride(0), 1.0, 4, ids, y, st, w, out2, V, stream()) == 0
+    for o in (out, out2):
+        assert bool(torch.isnan(o[10:18]).all()) and bool((o[300:310] == 0).all()) and bool(torch.isfinite(o[fine]).all())
+
+
 @pytest.mark.parametrize("V", [40, 600, 20000])
 def test_distill_poison(V):
     x, _ = rows(7, V, "f32")
@@ -592,3 +623,40 @@ def test_host_rows_are_refused():
     assert rb.remoe_token_logprobs(2, 64, rb.REMOE_F32, x, 64, 1.0, None, 0, None, out, None, None, None, stream()) == rb.REMOE_E_ARG
     pinned = x.pin_memory()
     assert rb.remoe_token_logprobs(2, 64, rb.REMOE_F32, pinned, 64, 1.0, None, 0, None, out, None, None, None, stream()) == rb.REMOE_E_ARG
+
+
+def test_drift_of_a_rerouted_stack():
+    """What the operators are for here: a chained stack with the cache-aware rerouting bonus, its answers against those
+    of the stack without it.  (The head that turns hidden states into logits is the caller's: a matrix product.)"""
+    import synth
+    from paper_2605_27081_b200.loader import LoadedWorkload
+    H, V, T, K = 512, 4097, 24, 32
+    shape = synth.Shape(3, H, 32, 4, 96, 1, 64, 1, 0, 1, 1)
+    head = torch.randn(V, H, generator=torch.Generator().manual_seed(3)).cuda() / math.sqrt(H) * 3
+    rng = torch.Generator().manual_seed(4)
+    inputs = torch.randn(T, 1, H, generator=rng).cuda()
+
+    def answers(beta):
+        wl = LoadedWorkload(shape, 6, seed=0)
+        try:
+            if beta:
+                wl.stack.set_reroute_beta(beta)
+            out = torch.empty(T, 1, H, device="cuda")
+            ids, gates = torch.empty(3, 1, 4, dtype=torch.int32, device="cuda"), torch.empty(3, 1, 4, device="cuda")
+            for t in range(T):
+                wl.stack.decode_step_chained(inputs[t], out[t], None, ids, gates)
+            torch.cuda.synchronize()
+            return (out.view(T, H) @ head.T).contiguous()
+        finally:
+            wl.close()
+
+    plain, same, moved = answers(0.0), answers(0.0), answers(4.0)
+    tok = plain.argmax(1).int()
+    rec = logprobs(plain, 1.0, tok, K)
+    ids, y, w = rec["top_ids"].cuda(), rec["top_logprobs"].cuda(), torch.ones(T, device="cuda")
+    assert torch.equal(rec["top_ids"][:, 0], tok.cpu())
+    none, _ = run_distill(same, 1.0, ids, y, 1, w)
+    some, _ = run_distill(moved, 1.0, ids, y, 1, w)
+    want = ref.distill(moved, 1.0, ids, y, 1, w)
+    ref.close(some, want["loss"], want["size"] * (ref.rel(V) + 4 * ref.U) + ref.U * want["loss"].abs(), "drift")
+    assert float(none.abs().max()) <= 40 * ref.rel(V) and float(some.max()) > 1e-4
