@@ -376,17 +376,16 @@ struct RowWeights {
   }
 };
 
-// One warp: all copies of part `part` of `parts` of the rows that the weights' owner takes, issued by its first lane.  Rows with
-// weight 0 are passed over.
+// One warp: all copies of the rows that the weights' owner takes, issued by its first lane.  Rows with weight 0 are passed over.
 template <typename T, int NB, int CHUNK>
-__device__ void produce(PipeShared<NB>& ps, unsigned char* buf, RowWeights weights, const T* logits, int64_t stride, int V, int part, int parts) {
+__device__ void produce(PipeShared<NB>& ps, unsigned char* buf, RowWeights weights, const T* logits, int64_t stride, int V) {
   typedef Chunks<T, CHUNK> C;
   int turn = 0, phase = 0;                    // slot of the next load, and how often its turn has come
   bool ok = true;
   for (int i = weights.next(0); weights.row(i) < weights.n_rows; i = weights.next(i + 1)) {
     if ((threadIdx.x & 31) != 0 || !ok) continue;
     const T* row = logits + weights.row(i) * stride;
-    const Slice sl(V, row_pad(row), part, parts);
+    const Slice sl(V, row_pad(row), 0, 1);
     const int n = C::count(sl);
     const T* base = row - sl.pad + 8 * (int64_t)sl.full0;
     for (int c = 0; c < n; ++c) {
@@ -413,14 +412,14 @@ struct RingPlace {
   __device__ __forceinline__ void wait(uint64_t* bars) {
     if (ok) ok = wait_phase(&bars[slot], parity);
   }
-  __device__ __forceinline__ void advance() {
-    if (++slot == NB) { slot = 0; parity ^= 1; }
-  }
-  // The warp is done with the slot and says so on `bars`.
-  __device__ __forceinline__ void pass(uint64_t* bars) {
+  // The warp is done with the slot and says so on `bars`.  The next copy into the slot is not ordered behind loads out of it
+  // that are still on their way to registers, so the arrival is made to depend on something that was computed from all
+  // of them (`seen`, any value): it decides which lane arrives.
+  __device__ __forceinline__ void pass(uint64_t* bars, bool seen) {
+    const int lane = __any_sync(0xffffffffu, seen) ? 1 : 0;
     __syncwarp();
-    if ((threadIdx.x & 31) == 0) ring::mbar_arrive(&bars[slot]);
-    advance();
+    if ((threadIdx.x & 31) == lane) ring::mbar_arrive(&bars[slot]);
+    if (++slot == NB) { slot = 0; parity ^= 1; }
   }
 };
 

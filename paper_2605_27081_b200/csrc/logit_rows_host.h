@@ -103,7 +103,9 @@ inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStrea
   return launch_clusters<Kernel>(args, args.n_rows, NT, (size_t)args.slice_bytes + more_smem, stream);
 }
 
-// Rows enough for persistent blocks that take whole rows.
+// Rows enough for persistent blocks that take whole rows: one for each SM.  (257 rows of 50257 fp16 with 5 alternatives: 16 us this
+// way, 19 with a cluster a row; 2048 of 131072 bf16 with 64: 135 against 568, since each of a row's blocks selects as
+// much as one for the whole row would.)  Shorter rows are over before such a block's warps have handed them on.
 inline bool many_rows(int32_t n_rows, int32_t vocab) { return vocab >= 8192 && n_rows >= 148; }
 
 // One launch of persistent blocks.
@@ -117,7 +119,8 @@ inline cudaError_t launch_pipe(const Args& args, cudaStream_t stream) {
   return cudaGetLastError();
 }
 
-// Blocks a row for the element-wise passes: of about `piece` bytes each.
+// Blocks a row for the element-wise passes: of about `piece` bytes each.  (The distillation's gradient with 128 entries a row, 2048 x
+// 131072 bf16: 402 us in pieces of 16 KB, each of which reads the list, 264 of 32, 212 of 128.)
 inline int pieces_of_row(int32_t vocab, int size, int piece) {
   const int64_t bytes = (int64_t)vocab * size;
   return (int)(bytes <= piece ? 1 : (bytes + piece / 2) / piece);
