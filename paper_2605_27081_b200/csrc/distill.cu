@@ -831,26 +831,21 @@ __global__ void __launch_bounds__(kPieceThreads, 6) distill_backward_kernel(cons
   }
 }
 
-template <typename T>
+template <typename T, int LPR>
 cudaError_t launch_small(const DistillArgs& a, bool backward, cudaStream_t st) {
-  const bool narrow = a.V <= 64;
-  const unsigned blocks = narrow ? ((unsigned)a.n_rows + 31) / 32 : ((unsigned)a.n_rows + 7) / 8;
-  if (backward) {
-    if (narrow) distill_small_kernel<T, 8, true, true><<<blocks, 256, 0, st>>>(a);
-    else distill_small_kernel<T, 32, true, true><<<blocks, 256, 0, st>>>(a);
-  } else if (a.d_logits) {
-    if (narrow) distill_small_kernel<T, 8, true, false><<<blocks, 256, 0, st>>>(a);
-    else distill_small_kernel<T, 32, true, false><<<blocks, 256, 0, st>>>(a);
-  } else {
-    if (narrow) distill_small_kernel<T, 8, false, false><<<blocks, 256, 0, st>>>(a);
-    else distill_small_kernel<T, 32, false, false><<<blocks, 256, 0, st>>>(a);
-  }
+  const unsigned blocks = ((unsigned)a.n_rows + 256 / LPR - 1) / (256 / LPR);
+  if (backward) distill_small_kernel<T, LPR, true, true><<<blocks, 256, 0, st>>>(a);
+  else if (a.d_logits) distill_small_kernel<T, LPR, true, false><<<blocks, 256, 0, st>>>(a);
+  else distill_small_kernel<T, LPR, false, false><<<blocks, 256, 0, st>>>(a);
   return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t launch_distill(DistillArgs a, bool backward, cudaStream_t st) {
-  if (a.V <= kSmallVocab) return launch_small<T>(a, backward, st);
+  if (a.V <= kSmallVocab)
+    return a.V <= 64    ? launch_small<T, 8>(a, backward, st)
+           : a.V <= 128 ? launch_small<T, 16>(a, backward, st)
+                        : launch_small<T, 32>(a, backward, st);
   if (backward) {
     a.parts = pieces_of_row(a.V, sizeof(T), 128 * 1024);
     const int64_t blocks = (int64_t)a.n_rows * a.parts;

@@ -81,8 +81,8 @@ def tokens_for(T, V, seed=1, skip=0.2):
 
 
 # lengths: one element, within one unit, group of 8 lanes, of 32, one block of 128 threads, of 512, several parts of a row
-SIZES = [(1, 1), (3, 2), (5, 7), (33, 64), (7, 65), (9, 255), (9, 256), (3, 257), (5, 1000), (2, 1021), (4, 4099), (3, 8192), (2, 12345),
-         (1, 40007), (5, 33001), (300, 300)]
+SIZES = [(1, 1), (3, 2), (5, 7), (33, 64), (7, 65), (37, 128), (18, 129), (9, 255), (9, 256), (3, 257),
+         (5, 1000), (2, 1021), (4, 4099), (3, 8192), (2, 12345), (1, 40007), (5, 33001), (300, 300)]
 
 
 @pytest.mark.parametrize("dtype", list(DT))
@@ -349,8 +349,8 @@ def check_distill(view, s, ids, y, tail, weight, oplace=(0, 0)):
     return loss.cpu(), out
 
 
-DISTILL_SIZES = [(1, 1, 1), (3, 2, 1), (2, 9, 9), (40, 64, 64), (33, 64, 6), (6, 130, 8), (5, 256, 256), (5, 257, 256), (3, 1021, 31),
-                 (2, 4099, 64), (2, 9000, 256), (1, 40007, 100), (3, 33001, 20)]
+DISTILL_SIZES = [(1, 1, 1), (3, 2, 1), (2, 9, 9), (40, 64, 64), (33, 64, 6), (6, 65, 65), (37, 128, 20), (6, 130, 8),
+                 (5, 256, 256), (5, 257, 256), (3, 1021, 31), (2, 4099, 64), (2, 9000, 256), (1, 40007, 100), (3, 33001, 20)]
 
 
 @pytest.mark.parametrize("tail", [0, 1])
