@@ -608,7 +608,7 @@ __device__ __forceinline__ float exp32(double x) { return ex2((float)x * kLog2e)
 // Rows of up to 256 elements: LPR lanes a row, eight elements a lane, the list laid out over the row's elements in shared
 // memory.  BACKWARD takes what rows share from row_stats instead of computing it.  Exponentials are float32, sums and
 // the loss's logarithms 64 bits: the terms' own errors are relative (2e-7) and do not grow where list and row nearly agree,
-// while 64-bit exponentials took half of the time (13312 rows of 64: 18 us).  The list's sum is one where it is
+// while 64-bit exponentials took a third of the time (13312 rows of 64: 12 us with float32 ones, 18 with 64-bit ones).  The list's sum is one where it is
 // subtracted from one (tail).
 template <typename T, int LPR, bool GRAD, bool BACKWARD>
 __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constant__ DistillArgs a) {

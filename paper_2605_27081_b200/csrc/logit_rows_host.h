@@ -80,6 +80,7 @@ inline int slice_bytes(int32_t vocab, int size, int parts) { return ((vocab + 14
 
 template <auto Kernel, typename Args>
 inline cudaError_t launch_clusters(const Args& args, int clusters, int threads, size_t smem, cudaStream_t stream) {
+  if ((int64_t)clusters * args.parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)clusters * (unsigned)args.parts);
   cfg.blockDim = dim3((unsigned)threads);
