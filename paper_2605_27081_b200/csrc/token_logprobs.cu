@@ -770,7 +770,11 @@ cudaError_t launch_logprobs(LogprobArgs a, cudaStream_t st) {
     return top ? launch_pipe<logprob_pipe_kernel<T, true>, ManyShape<T, true>>(a, st)
                : launch_pipe<logprob_pipe_kernel<T, false>, ManyShape<T, false>>(a, st);
   }
-  const bool wide = a.V >= 8192 || a.top_k > 64;
+  // 256 threads a block for long rows and for many alternatives; with few of those the selection's fixed steps weigh more than the
+  // pass, and more blocks of 128 lie beside one another.  (5000 rows of 9000 bf16, 20 alternatives: 64 us with 128 threads, 81 with
+  // 256; of 16000: 91 and 94, with 64 alternatives 135 and 118.)
+  const bool few = a.top_k > 0 && a.top_k <= 32;
+  const bool wide = a.V >= (few ? 32768 : 8192) || a.top_k > 64;
   a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));
   a.slice_bytes = slice_bytes(a.V, sizeof(T), a.parts);
   if (wide) return top ? launch_resident<logprob_rows_kernel<T, 256, true>, 256>(a, sizeof(FewShared), st)

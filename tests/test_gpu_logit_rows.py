@@ -111,6 +111,13 @@ def test_logprobs_many_rows(T, V, top, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("T,V,top", [(1, 8192, 32), (200, 16001, 32), (200, 16001, 33), (3, 32767, 32), (700, 9001, 1), (160, 26700, 20)])
+def test_few_alternatives_of_middling_rows(T, V, top, dtype):
+    view, _ = rows(T, V, dtype, seed=T + top, pad=1)
+    check_logprobs(view, 0.8, tokens_for(T, V), top)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("V,top", [(64, 64), (200, 200), (256, 256), (300, 256), (1500, 65), (2000, 256), (5000, 64), (9001, 256), (70000, 256), (70000, 1)])
 def test_many_alternatives(V, top, dtype):
     for T in (1, 4):
