@@ -396,12 +396,15 @@ int remoe_token_logprobs_backward(int32_t n_rows, int32_t vocab, int32_t dtype, 
  *   tail = 1:  q = exp of the values, and all that is not listed is one more class: with q_r = max(0, 1 - sum q) and p_r = the
  *              student's probability outside the list, loss gains q_r (ln q_r - ln p_r).  The term is left out where the student has
  *              no live element outside the list.
+ *   The gradient is that of this loss: inv_temperature * row_weight * (Q p - q) on the list, inv_temperature * row_weight * p (Q - q_r / p_r)
+ *   outside it.  Q, the sum of the q and of the q_r in the loss, is 1 for most lists; with tail it is less where the student has no
+ *   live element outside the list, and more where the values sum to more than one.
  *   row_weight        [n_rows] float32 or NULL (= 1): weight of the row in the gradient (not in loss).  0 leaves the row out: it is
  *                     not looked at, loss and gradient are 0 (padding of a batch).
  *   loss              [n_rows] float32 or NULL; 0 for rows without a usable entry and rows of -inf alone; +inf where the student
  *                     masks a token that the teacher allows (the gradient stays finite)
  *   row_stats         [n_rows, 8] float32 or NULL, for the backward call: m, ln Z (as above), the same two of the elements outside the
- *                     list, p_r - q_r, ln of the list's sum (tail = 0), 1 if the row takes part, unused
+ *                     list, Q p_r - q_r, ln of the list's sum (tail = 0), 1 if the row takes part, Q - 1
  *   d_logits          [n_rows, vocab] of dtype or NULL: gradient of sum_t row_weight[t] * loss[t]
  * A row with an id outside [-1, vocab), or a NaN or +inf among its values, gives NaN.
  */

@@ -4,10 +4,12 @@
 // S: the ids of the list.  q = softmax of the list's values, or (tail) their exp with q_r = 1 - sum q as one more
 // class for all that is not listed; p_r = the student's mass outside S.
 //   loss = sum_S q (ln q - ln p) + q_r (ln q_r - ln p_r)
-//   dx_v = s w (p_v - q_v)                            v in S
-//          s w (p_r - q_r) e^{s x_v} / sum_{not S}    v not in S
-// The second line is p_v (1 - q_r / p_r), written so that it holds where the student leaves nearly nothing outside S:
-// the sum outside S is taken over those elements alone, not as a difference.
+//   dx_v = s w (Q p_v - q_v)                            v in S
+//          s w (Q p_r - q_r) e^{s x_v} / sum_{not S}    v not in S
+// Q is the sum of the q and of the q_r that is in the loss.  It is 1 for most lists; with tail it is not where q_r is left out (no live
+// element outside S) or cut to 0 (values that sum to more than one).  The second line is p_v (Q - q_r / p_r), written so that
+// it holds where the student leaves nearly nothing outside S: the sum outside S is taken over those elements alone, not as a
+// difference.
 #include <type_traits>
 
 #include "logit_rows.cuh"
@@ -39,10 +41,11 @@ struct RowShared {
   int kind;                        // 0: left out (zeros), 1: takes part
 };
 
-// Gradient in the list from the row_stats: weight * (e^{(x - m) s - ln Z} - sum of e^{y - ln Q} over the entries of its id, in order).
+// Gradient in the list from the row_stats: weight * (Q e^{(x - m) s - ln Z} - sum of e^{y - ln_q} over the entries of its id, in order),
+// with `over` = Q - 1.
 // In 64 bits for float32 results, whose rounding a difference of float32 exponentials would exceed; in float32 for the others.
 template <typename T>
-__device__ __forceinline__ float entry_gradient(float m, float ln_z, float ln_q, float s, float weight, const int* id, const float* y, int K, int k,
+__device__ __forceinline__ float entry_gradient(float m, float ln_z, float ln_q, float over, float s, float weight, const int* id, const float* y, int K, int k,
                                                 float x, bool twice) {
   typedef typename std::conditional<sizeof(T) == 4, double, float>::type R;
   auto e = [](R v) {
@@ -52,7 +55,8 @@ __device__ __forceinline__ float entry_gradient(float m, float ln_z, float ln_q,
   R q = 0;
   for (int j = k; j < (twice ? K : k + 1); ++j)
     if (id[j] == id[k]) q += e((R)y[j] - ln_q);
-  return (float)((R)s * weight * (e(((R)x - m) * s - ln_z) - q));
+  const R p = e(((R)x - m) * s - ln_z);
+  return (float)((R)s * weight * (p - q + (R)over * p));
 }
 
 // Gradient outside the list, of one unit.
@@ -133,17 +137,18 @@ __device__ __forceinline__ void finish_row(const DistillArgs& a, int64_t r, floa
   const double z = of_rest * grow + of_list * v.z, inv_z = 1.0 / z, ln_z = ln_wide(z), ln_rest = ln_wide(grow);
   const double of_q = a.tail || !l.some ? 1.0 : 1.0 / v.q, ln_q = a.tail || !l.some ? 0.0 : l.shift + ln_wide(v.q);
   const double q_all = v.q * of_q, q_rest = a.tail && others ? fmax(0.0, 1.0 - v.q) : 0.0;
+  const double over = !a.tail || !l.some ? 0.0 : others ? fmax(0.0, v.q - 1.0) : v.q - 1.0;        // Q - 1
   const double ln_p_rest = ((double)rest.m - m) * s + ln_rest - ln_z;
   double loss = (v.qy - v.qx) * of_q + (((double)m - x_shift) * s + ln_z - (ln_q - l.shift)) * q_all;
   if (q_rest > 0.0) loss += q_rest * (ln_wide(q_rest) - ln_p_rest);
-  const double c_rest = others ? of_rest * grow * inv_z - q_rest : 0.0;
+  const double p_rest = others ? of_rest * grow * inv_z : 0.0, c_rest = p_rest - q_rest + over * p_rest;
   const bool in = l.some && alive;
   const float poison = l.bad ? nan_value() : 0.f;
   if (share) {
     rs.kind = l.bad || in;
     rs.m_rest = others ? rest.m : 0.f;
     rs.coef = (others ? (float)(s * weight * c_rest) / (float)grow : 0.f) + poison;
-    rs.of_e = of_list * inv_z + poison;
+    rs.of_e = (1.0 + over) * of_list * inv_z + poison;
     rs.of_q = of_q;
     rs.weight = s * weight;
   }
@@ -152,7 +157,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs& a, int64_t r, floa
     if (a.stats) {
       float* o = a.stats + 8 * r;
       o[0] = m; o[1] = (float)ln_z; o[2] = rest.m; o[3] = others ? (float)ln_rest : -kInf;
-      o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = (in ? 1.f : 0.f) + poison; o[7] = 0.f;
+      o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = (in ? 1.f : 0.f) + poison; o[7] = (float)over;
     }
   }
 }
@@ -698,12 +703,12 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
 #pragma unroll
   for (int j = 0; j < 8; ++j) listed |= s_owner[gi][8 * lane + j] >= 0 ? 1u << j : 0u;
 
-  float m, m_rest, coef, flag, inv_z;
+  float m, m_rest, coef, flag, inv_z;             // inv_z: Q / Z
   double ln_z;
   if (BACKWARD) {
     const float* o = a.stats_in + 8 * rr;
     m = o[0]; ln_z = o[1]; flag = o[6];
-    inv_z = ex2(-(float)ln_z * kLog2e);
+    inv_z = (1.f + o[7]) * ex2(-(float)ln_z * kLog2e);
     const bool others = o[2] > -kInf;
     m_rest = others ? o[2] : 0.f;
     coef = others ? a.s * weight * o[4] * ex2(-o[3] * kLog2e) : 0.f;
@@ -746,19 +751,20 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
       }
     loss = group_sum(loss);
     if (q_rest > 0.0) loss += q_rest * (ln_wide(q_rest) - ln_p_rest);
-    const double c_rest = others ? of_rest / z - q_rest : 0.0;
+    const float over = !a.tail || !some ? 0.f : (float)(others ? fmax(0.0, qs - 1.0) : qs - 1.0);   // Q - 1
+    const double p_rest = others ? of_rest / z : 0.0, c_rest = p_rest - q_rest + over * p_rest;
     const bool in = some && alive;
     flag = bad ? nan_value() : in ? 1.f : 0.f;
     m_rest = others ? rest.m : 0.f;
     coef = others ? (float)(s * weight * c_rest) / (1.f + rest.R) : 0.f;
-    inv_z = (float)(1.0 / z);
+    inv_z = (1.f + over) * (float)(1.0 / z);
     if (there && lane == 0) {
       const bool counts = weight != 0.f;
       if (a.loss) a.loss[r] = !counts ? 0.f : bad ? nan_value() : in ? (float)loss : 0.f;
       if (a.stats) {
         float* o = a.stats + 8 * r;
         o[0] = m; o[1] = (float)ln_z; o[2] = rest.m; o[3] = others ? (float)ln_rest : -kInf;
-        o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = counts ? flag : 0.f; o[7] = 0.f;
+        o[4] = (float)c_rest; o[5] = (float)ln_q; o[6] = counts ? flag : 0.f; o[7] = over;
       }
     }
   }
@@ -827,7 +833,7 @@ __global__ void __launch_bounds__(kPieceThreads, 6) distill_backward_kernel(cons
         twice = true;
         if (j < tid) mine = false;
       }
-    if (mine) Elem<T>::put(out + id, entry_gradient<T>(m, ln_z, ln_q, a.s, weight, s_id, s_y, K, tid, Elem<T>::get(&x), twice));
+    if (mine) Elem<T>::put(out + id, entry_gradient<T>(m, ln_z, ln_q, a.stats_in[8 * r + 7], a.s, weight, s_id, s_y, K, tid, Elem<T>::get(&x), twice));
   }
 }
 

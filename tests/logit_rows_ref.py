@@ -97,8 +97,10 @@ def distill(logits, s, ids, y, tail, weight):
     p = lp.exp()
     qd = torch.zeros(T, V, dtype=torch.float64, device=logits.device).scatter_add_(1, i, q * used)
     soft_rest = torch.where(others.unsqueeze(1), (outside - ln_pr.unsqueeze(1)).exp(), torch.zeros_like(p)).masked_fill(listed, 0.0)
-    dx = torch.where(listed, p - qd, soft_rest * (p_rest - q_rest).unsqueeze(1))
-    dsize = torch.where(listed, p + qd, soft_rest * (p_rest + q_rest).unsqueeze(1))
+    # loss = sum q ln q - sum q ln p, and every ln p has the derivative 1[same element] - p: the sum of the q goes with p
+    q_all = q.sum(1) + q_rest
+    dx = torch.where(listed, q_all.unsqueeze(1) * p - qd, soft_rest * (q_all * p_rest - q_rest).unsqueeze(1))
+    dsize = torch.where(listed, q_all.unsqueeze(1) * p + qd, soft_rest * (q_all * p_rest + q_rest).unsqueeze(1))
     w = weight.double()
     inside = some & ~empty & (w != 0)
     zero = ~inside.unsqueeze(1)
