@@ -546,7 +546,8 @@ struct Stream {
     const bool go_far = !(fabsf(t) < 1048576.f && c < 1e15f && (m - Elem<T>::kFloor) * c >= 160.f);
     const float nk = rintf(t);
     if (limit > -kInf) {
-      const float d = far || go_far ? (ref - m) * c : k - nk, r = ex2(d);
+      // from the reference that the sums are relative to (2^(ref c) far, 2^k near) to the new one (2^(m c) or 2^nk)
+      const float d = far ? (go_far ? (ref - m) * c : fmaf(ref, c, -nk)) : go_far ? -fmaf(m, c, -k) : k - nk, r = ex2(d);
       const f2 r2 = pack2(r, r);
       if (ENTROPY) U = r > 0.f ? mul2(r2, fma2(R, pack2(d, d), U)) : 0ull;
       R = mul2(R, r2);

@@ -114,3 +114,80 @@ def test_distill_gradient_of_uneven_lists(T, V, K, dtype, tail):
         for what, o in got.items():
             ref.check_grad(o.masked_fill(view == NINF, 0.0), grad, size, V, what, s * 1.5)
         close_to_loss(loss, want.detach(), view, s, ids, y, tail, w)
+
+
+# ---- sums that change their reference ------------------------------------------------------------------------------
+# A thread's sum is kept relative to a reference that moves when an element lies 40 powers of two above it, in one of two ways to the
+# exponent.  Rows in which each thread sees three levels in turn: a first one, many elements just under 40 powers of two above it
+# (they do not move the reference and have nearly all of the mass), and some just over 40 above it, which do, across a boundary between
+# the two ways: |m c| = 2^20, or (fp16, bf16) 160 powers of two above the type's lowest value or -2^60.
+
+LEVELS = {  # type, inverse temperature, first level, its step from row to row, second, third (differences)
+    "f32 up": ("f32", 1.0, 726802.0, 0.0625, 27.5, 28.0),
+    "f32 down": ("f32", 1.0, -726830.0, 0.0625, 27.5, 28.0),
+    "f32 cold": ("f32", 40.0, 18170.0, 1 / 512, 0.6875, 0.697265625),
+    "f32 colder": ("f32", 1e4, 72.68, 2.0 ** -17, 0.00275, 0.00279),
+    "f16": ("f16", 1 / 727, 0.0, 1.0, 20096.0, 20288.0),
+    "bf16": ("bf16", 7.8e-17, 0.0, 2.0 ** 52, 3.52e17, 3.58e17),
+}
+
+
+def level_rows(kind, T, V, first, last):
+    """[T, V]: `first` elements of the first level, the third level in the last `last` elements."""
+    dtype, s, base, step, second, third = LEVELS[kind]
+    x = torch.empty(T, V, dtype=torch.float64)
+    low = (base + step * (torch.arange(T) % 16).double()).unsqueeze(1)
+    x[:] = low + second
+    x[:, :first] = low
+    x[:, V - last:] = low + third
+    x[:, torch.arange(V) % 7 == 3] = low
+    return x.to(DT[dtype][0]).cuda(), s
+
+
+def sums_tolerance(V):
+    # as in rel(); and each term's exponent is taken from the reference, up to 41 powers of two away: 41 ln 2 u for its rounding, as much
+    # again for the factor from the reference to the maximum
+    return ref.rel(V) + 2 * 41 * ref.U
+
+
+@pytest.mark.parametrize("kind", list(LEVELS))
+@pytest.mark.parametrize("T,V,top", [(300, 1536, 0), (300, 6144, 5), (300, 12288, 1), (300, 18432, 0), (160, 8192, 0), (160, 36864, 3), (150, 49152, 0),
+                                     (40, 24576, 7), (1, 98304, 2)])
+def test_sums_across_the_two_ways(kind, T, V, top):
+    half = V // 3
+    for first, last in [(half, half), (half, 64), (max(64, V - 2 * 6144), 6144), (2048, 2048), (V // 4, V // 2)]:
+        if first + last >= V:
+            continue
+        x, s = level_rows(kind, T, V, first, last)
+        tok = torch.arange(T, dtype=torch.int32, device="cuda") * 37 % V
+        got = logprobs(x, s, tok, top)
+        want = {k: v.cpu() for k, v in ref.logprobs(x, s, tok, top).items()}
+        tz, lnv = sums_tolerance(V), math.log(V + 1)
+        ref.close(got["row_stats"][:, 1], want["ln_z"], tz + ref.U * 2 * lnv, "ln Z")
+        ref.close(got["logprob"], want["logprob"], tz + ref.U * (8 * want["logprob"].abs() + 2 * lnv), "logprob")
+        # the mean of |d| is taken from sums relative to the reference, up to 41 ln 2 = 28.4 nats away
+        ref.close(got["entropy"], want["entropy"], (1 + 2 * lnv + 2 * 28.4) * tz + ref.U * 4 * lnv, "entropy")
+
+
+@pytest.mark.parametrize("kind", list(LEVELS))
+@pytest.mark.parametrize("T,V", [(300, 1536), (300, 6144), (300, 18432), (150, 49152), (300, 24576), (40, 24576), (1, 98304)])
+def test_distill_sums_across_the_two_ways(kind, T, V):
+    half = V // 3
+    for first, last in [(half, half), (half, 64), (2048, 2048), (V // 4, V // 2), (max(64, V - 2 * 8192), 8192)]:
+        if first + last >= V:
+            continue
+        x, s = level_rows(kind, T, V, first, last)
+        ids = (torch.arange(4).unsqueeze(0) * (V // 4) + torch.arange(T).unsqueeze(1) % 50).int().cuda()
+        y = torch.log(torch.tensor([0.4, 0.1, 0.2, 0.1])).expand(T, 4).contiguous().cuda()
+        w = torch.ones(T, device="cuda")
+        want = ref.distill(x, s, ids, y, 1, w)
+        tol = want["size"] * (sums_tolerance(V) + 4 * ref.U) + ref.U * want["loss"].abs()
+        loss, _ = run_distill(x, s, ids, y, 1, w)
+        ref.close(loss, want["loss"], tol, "loss")
+        out = torch.empty_like(x)
+        loss, st = run_distill(x, s, ids, y, 1, w, out, stats=True)
+        ref.close(loss, want["loss"], tol, "loss with the gradient")
+        # by the gradient's bound, with the wider one of the sums
+        fi = torch.finfo(x.dtype)
+        tol = want["grad"].abs() * (fi.eps / 2) + want["grad_size"] * (2 * sums_tolerance(V) + 40 * ref.U) + fi.smallest_normal * fi.eps / 2 + 2.0 ** -126
+        assert bool(((out.double() - want["grad"]).abs() <= tol).all())
