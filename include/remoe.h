@@ -343,14 +343,14 @@ int remoe_expert_ffn_static(int32_t hidden, int32_t weight_dtype, int32_t n_expe
  *   - Rows: logits_dev holds n_rows rows of `vocab` elements, `row_stride` elements apart (>= vocab; a row may start at any
  *     element address, 16-byte aligned rows are fastest).  dtype REMOE_F32, REMOE_BF16 or REMOE_F16.  Everything is computed in
  *     float32 or wider and rounded once.  1 <= vocab <= REMOE_ROWS_MAX_VOCAB; n_rows = 0 does nothing.  p below is
- *     softmax(inv_temperature * row), inv_temperature finite and > 0.
+ *     softmax(inv_temperature * row), 2^-100 <= inv_temperature <= 2^100.
  *   - The device is the one that logits_dev lies on (it need not be current; the stream and all other pointers belong to it).
  *   - -inf is a masked element (probability 0, gradient 0).  A row of -inf alone has no distribution: its log probabilities
  *     are -inf, its entropy, losses and gradients 0.  The type's lowest value is an ordinary value (a row of it is
  *     uniform).  A row that holds a NaN or +inf gives NaN wherever its values enter.
  *   - A gradient may be written in place (d_logits_dev == logits_dev with the same stride); other overlap of outputs with
  *     inputs or one another is not allowed.  What lies between rows is left as it was.
- *   Errors: ARG (null or misaligned pointers, sizes, strides, rows in host memory), UNSUPPORTED (FP8 or 4-bit rows, vocab or
+ *   Errors: ARG (null or misaligned pointers, sizes, strides, the temperature, rows in host memory), UNSUPPORTED (FP8 or 4-bit rows, vocab or
  *   top_k beyond the limits below, more blocks than a grid holds), CUDA.
  */
 #define REMOE_ROWS_MAX_VOCAB 393216

@@ -4,8 +4,6 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
-#include <cmath>
-
 #include "remoe.h"
 #include "remoe_internal.cuh"
 
@@ -49,6 +47,10 @@ class PointerDevice {
 constexpr int64_t kSliceBytes = 52 * 1024;     // of a row in one block, where eight blocks are enough for that
 constexpr size_t kSmemLimit = 220 * 1024;      // dynamic shared memory of a block; the longest float32 row needs 216 KB in eight
 
+// Range of the inverse temperature.  Above, its product with log2(e) leaves float32 from 2.36e38 on (0 * inf for the largest element); below,
+// a difference of logits beyond float32 may still be a distance that counts, where it reads as -inf (from about 3e-37 on).
+constexpr float kLeastInverse = 0x1p-100f, kLargestInverse = 0x1p100f;
+
 inline int element_size(int32_t dtype) { return dtype == REMOE_F32 ? 4 : dtype == REMOE_BF16 || dtype == REMOE_F16 ? 2 : 0; }
 inline bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
 
@@ -62,7 +64,7 @@ inline int check_rows(int32_t n_rows, int32_t vocab, int32_t dtype, const void* 
   if (!element_size(dtype)) return REMOE_E_ARG;
   if (vocab > REMOE_ROWS_MAX_VOCAB) return REMOE_E_UNSUPPORTED;
   if (row_stride < vocab && n_rows > 1) return REMOE_E_ARG;
-  if (!(inv_temperature > 0.f) || !std::isfinite(inv_temperature)) return REMOE_E_ARG;
+  if (!(inv_temperature >= kLeastInverse && inv_temperature <= kLargestInverse)) return REMOE_E_ARG;      // NaN, too
   if (misaligned(logits, element_size(dtype))) return REMOE_E_ARG;
   return REMOE_OK;
 }

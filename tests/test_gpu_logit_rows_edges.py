@@ -191,3 +191,22 @@ def test_distill_sums_across_the_two_ways(kind, T, V):
         fi = torch.finfo(x.dtype)
         tol = want["grad"].abs() * (fi.eps / 2) + want["grad_size"] * (2 * sums_tolerance(V) + 40 * ref.U) + fi.smallest_normal * fi.eps / 2 + 2.0 ** -126
         assert bool(((out.double() - want["grad"]).abs() <= tol).all())
+
+
+# ---- the ends of what is allowed -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("V", [40, 700, 9000])
+@pytest.mark.parametrize("s", [2.0 ** -100, 2.0 ** 100])
+def test_least_and_largest_inverse_temperature(V, dtype, s):
+    T = 4
+    view, _ = rows_of.rows(T, V, dtype, seed=V)
+    view[1] = 2.0                                # uniform at any temperature
+    view[2, 7] = view[2].max()                   # two largest elements share the mass of a cold row
+    tok = view.argmax(1).int()
+    rows_of.check_logprobs(view, s, tok, 5)
+    ids, y = rows_of.teacher(view.cpu(), 5, 1.0)
+    w = torch.ones(T, device="cuda")
+    want = ref.distill(view, s, ids.cuda(), y.cuda(), 0, w)
+    loss, _ = run_distill(view, s, ids.cuda(), y.cuda(), 0, w)
+    ref.close(loss, want["loss"], want["size"] * (ref.rel(V) + 4 * ref.U) + ref.U * want["loss"].abs(), "loss")
