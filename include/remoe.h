@@ -377,7 +377,8 @@ int remoe_token_logprobs(int32_t n_rows, int32_t vocab, int32_t dtype, const voi
  * Gradient of sum_t grad_logprob[t] * logprob[t] + grad_entropy[t] * entropy[t] with respect to the logits, from the same
  * logits, tokens and temperature and the row_stats of the forward call.  Either of grad_logprob and grad_entropy ([n_rows]
  * float32) may be NULL (= 0).  A row whose two gradients are 0 (grad_logprob counts as 0 where the token is -1) is
- * not read: its gradient is 0 whatever it holds.  top_logprob carries no gradient.
+ * not read: its gradient is 0 whatever it holds.  A token outside [0, vocab) other than -1 makes a row with grad_logprob != 0 NaN; the
+ * entropy's gradient does not look at the token.  top_logprob carries no gradient.
  *   d_logits     [n_rows, vocab] of dtype, rows d_row_stride elements apart
  */
 int remoe_token_logprobs_backward(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits_dev,

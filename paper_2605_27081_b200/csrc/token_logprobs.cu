@@ -706,11 +706,13 @@ __global__ void __launch_bounds__(kGradThreads) logprob_grad_kernel(const __grid
   const int full0 = pad > 0 ? 1 : 0, full1 = (V + pad) >> 3, units = (V + pad + 7) >> 3;
 
   const float m = a.stats[4 * r], ln_z = a.stats[4 * r + 1], h = a.stats[4 * r + 2];
-  const int token = a.tokens ? a.tokens[r] : -1;
+  int token = a.tokens ? a.tokens[r] : -1;
+  const bool outside = token < -1 || token >= V;
   const float g = a.g_logprob && token != -1 ? a.g_logprob[r] : 0.f;
+  if (outside) token = -1;                    // the entropy's gradient knows no token
   const float gh = a.g_entropy ? a.g_entropy[r] : 0.f;
   const bool zero = (g == 0.f && gh == 0.f) || m == -kInf;
-  const bool bad = !zero && (token < -1 || token >= V);
+  const bool bad = !zero && outside && g != 0.f;
   const float inv_z = ex2(-ln_z * kLog2e), c = a.s * kLog2e;
   const float A = -a.s * (g + gh * (h - ln_z)) * inv_z, B = -a.s * gh * kLn2 * inv_z;
   Unit<T> q[N];

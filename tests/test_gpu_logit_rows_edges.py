@@ -210,3 +210,21 @@ def test_least_and_largest_inverse_temperature(V, dtype, s):
     want = ref.distill(view, s, ids.cuda(), y.cuda(), 0, w)
     loss, _ = run_distill(view, s, ids.cuda(), y.cuda(), 0, w)
     ref.close(loss, want["loss"], want["size"] * (ref.rel(V) + 4 * ref.U) + ref.U * want["loss"].abs(), "loss")
+
+
+@pytest.mark.parametrize("V", [50, 700, 20001])
+def test_entropy_gradient_beside_a_bad_token(V):
+    """A token outside the vocabulary has no log probability (NaN); the entropy's gradient does not look at it."""
+    T = 6
+    view, _ = rows_of.rows(T, V, "f32", seed=V, pad=1)
+    tok = torch.tensor([V, -2, 2 ** 31 - 1, -2 ** 31, V + 3, 3], dtype=torch.int32, device="cuda")
+    st = logprobs(view, 0.9, tok, 0)["row_stats"].cuda()
+    g_ent = torch.tensor([1.0, 0.5, -1.0, 2.0, 1.0, 1.0], device="cuda")
+    want, size = ref.logprobs_grad(view, 0.9, torch.full_like(tok, -1), None, g_ent)
+    for g_lp in (None, torch.zeros(T, device="cuda")):
+        out = torch.full((T, V), 3.0, device="cuda")
+        assert rb.remoe_token_logprobs_backward(T, V, rb.REMOE_F32, view, view.stride(0), 0.9, tok, st, g_lp, g_ent, out, V, stream()) == 0
+        ref.check_grad(out, want, size, V)
+    g_lp = torch.ones(T, device="cuda")
+    assert rb.remoe_token_logprobs_backward(T, V, rb.REMOE_F32, view, view.stride(0), 0.9, tok, st, g_lp, g_ent, out, V, stream()) == 0
+    assert bool(torch.isnan(out[:5]).all()) and bool(torch.isfinite(out[5]).all())
