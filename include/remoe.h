@@ -403,7 +403,7 @@ int remoe_token_logprobs_backward(int32_t n_rows, int32_t vocab, int32_t dtype, 
  *   row_weight        [n_rows] float32 or NULL (= 1): weight of the row in the gradient (not in loss).  0 leaves the row out: it is
  *                     not looked at, loss and gradient are 0 (padding of a batch).
  *   loss              [n_rows] float32 or NULL; 0 for rows without a usable entry and rows of -inf alone; +inf where the student
- *                     masks a token that the teacher allows (the gradient stays finite)
+ *                     masks a token that the teacher allows (q > 0 as a float64; the gradient stays finite)
  *   row_stats         [n_rows, 8] float32 or NULL, for the backward call: m, ln Z (as above), the same two of the elements outside the
  *                     list, Q p_r - q_r, ln of the list's sum (tail = 0), 1 if the row takes part, Q - 1
  *   d_logits          [n_rows, vocab] of dtype or NULL: gradient of sum_t row_weight[t] * loss[t]

@@ -609,12 +609,13 @@ __global__ void __launch_bounds__(LossShape<T>::kThreads, LossShape<T>::kBlocks)
 }
 
 __device__ __forceinline__ float exp32(double x) { return ex2((float)x * kLog2e); }
+constexpr double kFaintLog = -745.0;            // e^x of less is 0 in 64 bits as well
 
 // Rows of up to 256 elements: LPR lanes a row, eight elements a lane, the list laid out over the row's elements in shared
 // memory.  BACKWARD takes what rows share from row_stats instead of computing it.  Exponentials are float32, sums and
 // the loss's logarithms 64 bits: the terms' own errors are relative (2e-7) and do not grow where list and row nearly agree,
 // while 64-bit exponentials took a third of the time (13312 rows of 64: 12 us with float32 ones, 18 with 64-bit ones).  The list's sum is one where it is
-// subtracted from one (tail).
+// subtracted from one (tail), and so are probabilities that a float32 exponential flushes to zero, in a walk of their own.
 template <typename T, int LPR, bool GRAD, bool BACKWARD>
 __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constant__ DistillArgs a) {
   constexpr int G = 256 / LPR, W = 8 * LPR;       // rows a block; entries and elements a row at most
@@ -669,6 +670,7 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
   for (int k = lane; k < K; k += LPR) twice = twice || (s_id[gi][k] >= 0 && s_owner[gi][s_id[gi][k]] != k);
   twice = group_any(twice);
   double ln_q = 0.0, qs = 0.0, entropy = 0.0;     // entropy: sum of q ln q over the list
+  bool faint = false;                             // q that is 0 as float32 (but may be infinitely or greatly far from p)
   if (BACKWARD) {
     ln_q = a.stats_in[8 * rr + 5];
   } else if (some) {
@@ -687,6 +689,7 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
     const double ln = (double)s_y[gi][k] - ln_q;
     float p = exp32(ln);
     if (p != 0.f) entropy += p * ln;
+    else faint = faint || ln > kFaintLog;
     if (twice) {
       for (int j = 0; j < k; ++j)
         if (s_id[gi][j] == id) p = -1.f;          // the first entry of the id has summed it
@@ -748,6 +751,12 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
       if (listed >> j & 1u) {
         const float p = s_q[gi][8 * lane + j];
         if (p != 0.f) loss -= p * (((double)v[j] - m) * s - ln_z);
+      }
+    if (group_any(faint))
+      for (int k = lane; k < K; k += LPR) {
+        const int id = s_id[gi][k];
+        const double ln = id >= 0 ? (double)s_y[gi][k] - ln_q : 0.0;
+        if (ln > kFaintLog && exp32(ln) == 0.f) loss += exp(ln) * (ln - (((double)Elem<T>::get(row + id) - m) * s - ln_z));
       }
     loss = group_sum(loss);
     if (q_rest > 0.0) loss += q_rest * (ln_wide(q_rest) - ln_p_rest);

@@ -228,3 +228,25 @@ def test_entropy_gradient_beside_a_bad_token(V):
     g_lp = torch.ones(T, device="cuda")
     assert rb.remoe_token_logprobs_backward(T, V, rb.REMOE_F32, view, view.stride(0), 0.9, tok, st, g_lp, g_ent, out, V, stream()) == 0
     assert bool(torch.isnan(out[:5]).all()) and bool(torch.isfinite(out[5]).all())
+
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("V", [20, 64, 100, 256, 300, 20000])
+def test_faint_probabilities_of_the_teacher(V, tail):
+    """q below float32's least normal value is a probability all the same: a student that masks its token has an infinite loss, and
+    one that gives the token the type's lowest value a large one."""
+    T = 6
+    x = torch.randn(T, V, generator=torch.Generator().manual_seed(V)).cuda()
+    ids = torch.arange(3, dtype=torch.int32).expand(T, 3).contiguous().cuda()
+    y = torch.tensor([[0.4, 0.3, 0.0]]).log().expand(T, 3).clone()
+    y[:, 2] = torch.tensor([-90.0, -90.0, -700.0, -88.0, -800.0, NINF])
+    x[0, 2], x[2, 2], x[4, 2], x[5, 2] = NINF, NINF, NINF, NINF
+    x[3, 2] = torch.finfo(torch.float32).min
+    w, y = torch.ones(T, device="cuda"), y.cuda()
+    want = ref.distill(x, 1.0, ids, y, tail, w)
+    assert bool(torch.isinf(want["loss"][[0, 2]]).all()) and bool(torch.isfinite(want["loss"][[1, 3, 4, 5]]).all()) and want["loss"][3] > 2
+    out = torch.empty_like(x)
+    for o in (None, out):
+        loss, _ = run_distill(x, 1.0, ids, y, tail, w, o)
+        ref.close(loss, want["loss"], want["size"].nan_to_num(0, posinf=0) * (ref.rel(V) + 4 * ref.U), "loss")
+    ref.check_grad(out, want["grad"], want["grad_size"], V)
