@@ -172,6 +172,7 @@ int dev_alloc(remoe_stack* s, T** p, size_t count) {
   void* q = nullptr;
   cudaError_t e = cudaMalloc(&q, count * sizeof(T) > 0 ? count * sizeof(T) : 16);
   if (e != cudaSuccess) {
+    cudaGetLastError();                         // told here: a later launch that reads the error state is not the one that failed
     fail_cuda(s, e, "cudaMalloc");
     return e == cudaErrorMemoryAllocation ? REMOE_E_NOMEM : REMOE_E_CUDA;
   }
@@ -185,6 +186,7 @@ int host_alloc(remoe_stack* s, T** p, size_t count) {
   void* q = nullptr;
   cudaError_t e = cudaMallocHost(&q, count * sizeof(T) > 0 ? count * sizeof(T) : 16);
   if (e != cudaSuccess) {
+    cudaGetLastError();
     fail_cuda(s, e, "cudaMallocHost");
     return REMOE_E_NOMEM;
   }

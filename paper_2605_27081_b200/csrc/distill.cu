@@ -848,11 +848,10 @@ __global__ void __launch_bounds__(kPieceThreads, 6) distill_backward_kernel(cons
 
 template <typename T, int LPR>
 cudaError_t launch_small(const DistillArgs& a, bool backward, cudaStream_t st) {
-  const unsigned blocks = ((unsigned)a.n_rows + 256 / LPR - 1) / (256 / LPR);
-  if (backward) distill_small_kernel<T, LPR, true, true><<<blocks, 256, 0, st>>>(a);
-  else if (a.d_logits) distill_small_kernel<T, LPR, true, false><<<blocks, 256, 0, st>>>(a);
-  else distill_small_kernel<T, LPR, false, false><<<blocks, 256, 0, st>>>(a);
-  return cudaGetLastError();
+  const int64_t blocks = ((int64_t)a.n_rows + 256 / LPR - 1) / (256 / LPR);
+  return backward     ? launch<distill_small_kernel<T, LPR, true, true>>(a, blocks, 1, 256, 0, st)
+         : a.d_logits ? launch<distill_small_kernel<T, LPR, true, false>>(a, blocks, 1, 256, 0, st)
+                      : launch<distill_small_kernel<T, LPR, false, false>>(a, blocks, 1, 256, 0, st);
 }
 
 template <typename T>
@@ -863,10 +862,7 @@ cudaError_t launch_distill(DistillArgs a, bool backward, cudaStream_t st) {
                         : launch_small<T, 32>(a, backward, st);
   if (backward) {
     a.parts = pieces_of_row(a.V, sizeof(T), 128 * 1024);
-    const int64_t blocks = (int64_t)a.n_rows * a.parts;
-    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-    distill_backward_kernel<T><<<(unsigned)blocks, kPieceThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    return launch<distill_backward_kernel<T>>(a, (int64_t)a.n_rows * a.parts, 1, kPieceThreads, 0, st);
   }
   if (!a.d_logits && many_rows(a.n_rows, a.V)) return launch_pipe<distill_loss_kernel<T>, LossShape<T>>(a, st);
   a.parts = parts_of_row(a.n_rows, a.V, sizeof(T));

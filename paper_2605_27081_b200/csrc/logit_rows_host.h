@@ -80,20 +80,21 @@ inline int parts_of_row(int32_t n_rows, int32_t vocab, int size) {
 // Shared memory of a part: whole units of eight elements, whatever the row's alignment.
 inline int slice_bytes(int32_t vocab, int size, int parts) { return ((vocab + 14) / 8 + parts - 1) / parts * 8 * size; }
 
+// One launch in clusters of `parts` blocks.  Its status is the launch's own, whatever an earlier call has left in the runtime's error state.
 template <auto Kernel, typename Args>
-inline cudaError_t launch_clusters(const Args& args, int clusters, int threads, size_t smem, cudaStream_t stream) {
-  if ((int64_t)clusters * args.parts > 0x7fffffff) return cudaErrorInvalidConfiguration;
+inline cudaError_t launch(const Args& args, int64_t blocks, int parts, int threads, size_t smem, cudaStream_t stream) {
+  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)clusters * (unsigned)args.parts);
+  cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3((unsigned)threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)args.parts;
+  at[0].val.clusterDim.x = (unsigned)parts;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = args.parts > 1 ? 1 : 0;
+  cfg.numAttrs = parts > 1 ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, Kernel, args);
 }
 
@@ -103,7 +104,7 @@ inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStrea
   static std::atomic<bool> ready[kMaxDevices];
   const cudaError_t e = allow_dynamic_smem(Kernel, kSmemLimit, ready);
   if (e != cudaSuccess) return e;
-  return launch_clusters<Kernel>(args, args.n_rows, NT, (size_t)args.slice_bytes + more_smem, stream);
+  return launch<Kernel>(args, (int64_t)args.n_rows * args.parts, args.parts, NT, (size_t)args.slice_bytes + more_smem, stream);
 }
 
 // Rows enough for persistent blocks that take whole rows: one for each SM.  (257 rows of 50257 fp16 with 5 alternatives: 16 us this
@@ -118,8 +119,7 @@ inline cudaError_t launch_pipe(const Args& args, cudaStream_t stream) {
   const cudaError_t e = allow_dynamic_smem(Kernel, Shape::kSmem, ready);
   if (e != cudaSuccess) return e;
   const int most = 148 * Shape::kBlocks;
-  Kernel<<<(unsigned)(args.n_rows < most ? args.n_rows : most), Shape::kThreads, Shape::kSmem, stream>>>(args);
-  return cudaGetLastError();
+  return launch<Kernel>(args, args.n_rows < most ? args.n_rows : most, 1, Shape::kThreads, Shape::kSmem, stream);
 }
 
 // Blocks a row for the element-wise passes: of about `piece` bytes each.  (The distillation's gradient with 128 entries a row, 2048 x

@@ -762,11 +762,10 @@ template <typename T>
 cudaError_t launch_logprobs(LogprobArgs a, cudaStream_t st) {
   const bool top = a.top_k > 0;
   if (a.V <= kSmallVocab) {
-    const unsigned n = (unsigned)a.n_rows;
-    if (a.V <= 64) logprob_small_kernel<T, 8><<<(n + 31) / 32, 256, 0, st>>>(a);
-    else if (a.V <= 128) logprob_small_kernel<T, 16><<<(n + 15) / 16, 256, 0, st>>>(a);
-    else logprob_small_kernel<T, 32><<<(n + 7) / 8, 256, 0, st>>>(a);
-    return cudaGetLastError();
+    const int64_t n = a.n_rows;
+    return a.V <= 64    ? launch<logprob_small_kernel<T, 8>>(a, (n + 31) / 32, 1, 256, 0, st)
+           : a.V <= 128 ? launch<logprob_small_kernel<T, 16>>(a, (n + 15) / 16, 1, 256, 0, st)
+                        : launch<logprob_small_kernel<T, 32>>(a, (n + 7) / 8, 1, 256, 0, st);
   }
   if (many_rows(a.n_rows, a.V) && (!top || a.V >= 32768)) {
     return top ? launch_pipe<logprob_pipe_kernel<T, true>, ManyShape<T, true>>(a, st)
@@ -788,19 +787,12 @@ cudaError_t launch_logprobs(LogprobArgs a, cudaStream_t st) {
 template <typename T>
 cudaError_t launch_logprobs_grad(LogprobGradArgs a, cudaStream_t st) {
   const int units = (a.V + 14) >> 3;                       // any alignment
-  int64_t blocks;
-  const bool small = units <= kGradThreads;
-  if (small) {
+  if (units <= kGradThreads) {
     a.tiles = units;
-    blocks = ((int64_t)a.n_rows * units + kGradThreads - 1) / kGradThreads;
-  } else {
-    a.tiles = (units + kGradThreads * kGradUnits<T> - 1) / (kGradThreads * kGradUnits<T>);
-    blocks = (int64_t)a.n_rows * a.tiles;
+    return launch<logprob_grad_kernel<T, true>>(a, ((int64_t)a.n_rows * units + kGradThreads - 1) / kGradThreads, 1, kGradThreads, 0, st);
   }
-  if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
-  if (small) logprob_grad_kernel<T, true><<<(unsigned)blocks, kGradThreads, 0, st>>>(a);
-  else logprob_grad_kernel<T, false><<<(unsigned)blocks, kGradThreads, 0, st>>>(a);
-  return cudaGetLastError();
+  a.tiles = (units + kGradThreads * kGradUnits<T> - 1) / (kGradThreads * kGradUnits<T>);
+  return launch<logprob_grad_kernel<T, false>>(a, (int64_t)a.n_rows * a.tiles, 1, kGradThreads, 0, st);
 }
 
 }  // namespace rows

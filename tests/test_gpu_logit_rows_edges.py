@@ -250,3 +250,28 @@ def test_faint_probabilities_of_the_teacher(V, tail):
         loss, _ = run_distill(x, 1.0, ids, y, tail, w, o)
         ref.close(loss, want["loss"], want["size"].nan_to_num(0, posinf=0) * (ref.rel(V) + 4 * ref.U), "loss")
     ref.check_grad(out, want["grad"], want["grad_size"], V)
+
+
+def test_a_failed_allocation_is_not_the_next_call_s():
+    """A stack too large for the device is refused; calls after it report their own outcome."""
+    T = 3
+    for V, K in [(40, 4), (700, 4), (9000, 4)]:
+        x, _ = rows_of.rows(T, V, "bf16")
+        tok = torch.zeros(T, dtype=torch.int32, device="cuda")
+        lp, one = torch.zeros(T, device="cuda"), torch.ones(T, device="cuda")
+        st, ds, d = torch.zeros(T, 4, device="cuda"), torch.zeros(T, 8, device="cuda"), torch.zeros_like(x)
+        ids, y = torch.zeros(T, K, dtype=torch.int32, device="cuda"), torch.zeros(T, K, device="cuda")
+        code = rb.REMOE_BF16
+        calls = [
+            lambda: rb.remoe_token_logprobs(T, V, code, x, V, 1.0, tok, K, lp, None, ids, y, st, stream()),
+            lambda: rb.remoe_token_logprobs_backward(T, V, code, x, V, 1.0, tok, st, one, None, d, V, stream()),
+            lambda: rb.remoe_distill_topk(T, V, code, x, V, 1.0, K, ids, y, 1, None, lp, ds, None, 0, stream()),
+            lambda: rb.remoe_distill_topk(T, V, code, x, V, 1.0, K, ids, y, 1, None, lp, ds, d, V, stream()),
+            lambda: rb.remoe_distill_topk_backward(T, V, code, x, V, 1.0, K, ids, y, ds, one, d, V, stream()),
+        ]
+        shape = dict(n_layers=64, hidden=1024, n_routed=256, top_k=4, inter_routed=8192, n_shared=0, inter_shared=0, shared_gate=0,
+                     renorm_topk=0, weight_dtype=rb.REMOE_F32, batch=1)
+        for call in calls:
+            assert rb.remoe_stack_create(shape, 256)[0] == rb.REMOE_E_NOMEM      # 1.6 TB of slots
+            assert call() == rb.REMOE_OK
+        torch.cuda.synchronize()
