@@ -333,6 +333,9 @@ __device__ void select_top(const Group& group, const Source& src, int tid, int w
 
 __device__ __forceinline__ uint32_t top_key(float top) { return top == top ? order_key(top) : 0u; }
 
+// (x - m) s, where x - m may lie beyond float32 and the product within.  Halving and doubling are exact.
+__device__ __forceinline__ float scaled_distance(float x, float m, float s) { return 2.f * ((0.5f * x - 0.5f * m) * s); }
+
 // What a row's outputs come from, once it is joined.
 struct RowResult {
   State all;
@@ -343,7 +346,7 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, const
   const bool none = w.all.m == -kInf;
   const float h = none ? 0.f : w.ln_z - kLn2 * w.all.U / (1.f + w.all.R);
   float lp = 0.f;
-  if (token >= 0 && token < a.V) lp = none ? -kInf : (x_token - w.all.m) * a.s - w.ln_z;
+  if (token >= 0 && token < a.V) lp = none ? -kInf : scaled_distance(x_token, w.all.m, a.s) - w.ln_z;
   else if (token != -1) lp = nan_value();
   if (a.logprob) a.logprob[r] = lp;
   if (a.entropy) a.entropy[r] = h;
@@ -356,7 +359,7 @@ __device__ __forceinline__ void write_alternative(const LogprobArgs& a, int64_t 
   const float x = key_value((uint32_t)(key >> 32));
   const bool bad = !(w.all.R == w.all.R);
   a.top_ids[r * a.top_k + rank] = bad ? -1 : (int32_t)(0xffffffffu - (uint32_t)key);
-  a.top_logprob[r * a.top_k + rank] = bad ? nan_value() : w.all.m == -kInf ? -kInf : (x - w.all.m) * a.s - w.ln_z;
+  a.top_logprob[r * a.top_k + rank] = bad ? nan_value() : w.all.m == -kInf ? -kInf : scaled_distance(x, w.all.m, a.s) - w.ln_z;
 }
 
 typedef TopShared<8 * REMOE_ROWS_MAX_TOP, 256> FewShared;   // room for the lists of a cluster's eight blocks
@@ -606,7 +609,7 @@ __global__ void __launch_bounds__(256) logprob_small_kernel(const __grid_constan
     const int token = a.tokens ? a.tokens[r] : -1;
     const float h = none ? 0.f : ln_z - kLn2 * all.U / (1.f + all.R);
     float lp = 0.f;
-    if (token >= 0 && token < a.V) lp = none ? -kInf : (Elem<T>::get(row + token) - all.m) * a.s - ln_z;
+    if (token >= 0 && token < a.V) lp = none ? -kInf : scaled_distance(Elem<T>::get(row + token), all.m, a.s) - ln_z;
     else if (token != -1) lp = nan_value();
     if (a.logprob) a.logprob[r] = lp;
     if (a.entropy) a.entropy[r] = h;
@@ -646,7 +649,7 @@ __global__ void __launch_bounds__(256) logprob_small_kernel(const __grid_constan
       if (there && at <= k) {
         const float x = key_value((uint32_t)(mine >> 32));
         a.top_ids[r * a.top_k + at] = bad ? -1 : (int32_t)(0xffffffffu - (uint32_t)mine);
-        a.top_logprob[r * a.top_k + at] = bad ? nan_value() : none ? -kInf : (x - all.m) * a.s - ln_z;
+        a.top_logprob[r * a.top_k + at] = bad ? nan_value() : none ? -kInf : scaled_distance(x, all.m, a.s) - ln_z;
       }
     }
   }

@@ -275,3 +275,17 @@ def test_a_failed_allocation_is_not_the_next_call_s():
             assert rb.remoe_stack_create(shape, 256)[0] == rb.REMOE_E_NOMEM      # 1.6 TB of slots
             assert call() == rb.REMOE_OK
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("V", [40, 700, 33000])
+def test_log_probabilities_of_far_apart_logits(V):
+    """Two finite logits whose difference is beyond float32 have a log probability that is not."""
+    T, s = 160, 0.25
+    x = torch.randn(T, V, generator=torch.Generator().manual_seed(V))
+    x[:, 3] = 3e38
+    x[:, 5] = -3e38
+    view, _ = place(x)
+    tok = torch.full((T,), 5, dtype=torch.int32, device="cuda")
+    for n in (T, 2):
+        got = rows_of.check_logprobs(view[:n], s, tok[:n], min(V, 40))
+        assert bool((got["logprob"] < -1.49e38).all()) and bool(torch.isfinite(got["logprob"]).all())
