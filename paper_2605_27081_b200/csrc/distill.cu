@@ -335,10 +335,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) distill_rows_kernel(const __gri
 // by a warp between the copies and the consumers, so their loop knows nothing of lists.
 struct alignas(16) ListShared {
   int id[kMaxList];                // -1: unused entry
-  float y[kMaxList], x[kMaxList];
   unsigned char first[kMaxList];   // no entry before it has its id
   ListSide side;
-  int twice;                       // an id stands in the list more than once
   unsigned loose[2];               // bits of the slice's ragged units that are listed
 };
 constexpr int kHash = 2 * kMaxList, kLists = kMaxList / 32;      // table in which ids that come twice are looked for; entries a lane
@@ -383,7 +381,7 @@ __device__ __forceinline__ void lay_list(const DistillArgs& a, ListFetch<T>& f, 
     const int k = lane + 32 * i;
     bad = bad || id[i] < -1 || id[i] >= V || (id[i] >= 0 && !(y[i] < kInf));
     if (id[i] < 0 || id[i] >= V) { id[i] = -1; y[i] = -kInf; }
-    if (k < K) { l.id[k] = id[i]; l.y[k] = y[i]; l.first[k] = id[i] >= 0; }
+    if (k < K) { l.id[k] = id[i]; l.first[k] = id[i] >= 0; }
     y_top = fmaxf(y_top, y[i]);
     const int u = (id[i] + sl.pad) >> 3;
     if (id[i] >= 0 && sl.holds(id[i]) && !(u >= sl.full0 && u < sl.full1)) loose |= 1u << ((id[i] + sl.pad) & 7) << (u == sl.ragged(0) ? 0 : 8);
@@ -408,11 +406,7 @@ __device__ __forceinline__ void lay_list(const DistillArgs& a, ListFetch<T>& f, 
         if (l.id[j] == l.id[k]) l.first[k] = 0;
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kLists; ++i) {
-    const int k = lane + 32 * i;
-    if (k < K) l.x[k] = Elem<T>::get(&x[i]);
-    m_list = max_nan(m_list, Elem<T>::get(&x[i]));
-  }
+  for (int i = 0; i < kLists; ++i) m_list = max_nan(m_list, Elem<T>::get(&x[i]));
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     m_list = max_nan(m_list, __shfl_xor_sync(0xffffffffu, m_list, o));
@@ -438,10 +432,7 @@ __device__ __forceinline__ void lay_list(const DistillArgs& a, ListFetch<T>& f, 
   }
   sums = warp_sum(sums);
   bad = __any_sync(0xffffffffu, bad);
-  if (lane == 0) {
-    l.side = ListSide{sums, m_list, shift, some, bad};
-    l.twice = twice;
-  }
+  if (lane == 0) l.side = ListSide{sums, m_list, shift, some, bad};
   __syncwarp();
 }
 

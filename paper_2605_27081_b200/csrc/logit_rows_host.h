@@ -70,7 +70,8 @@ inline int check_rows(int32_t n_rows, int32_t vocab, int32_t dtype, const void* 
 }
 
 // Blocks that share a row, one part of it in the shared memory of each: a power of two up to eight, so that four blocks
-// of 256 threads lie on an SM with 52 KB each; more where there are few rows, down to 8 KB.
+// of 256 threads lie on an SM with 52 KB each (three where the selection's lists, 19 KB, lie behind the part); more where there are few
+// rows, down to 8 KB.
 inline int parts_of_row(int32_t n_rows, int32_t vocab, int size) {
   int parts = 1;
   while (parts < 8 && (int64_t)vocab * size > (int64_t)parts * kSliceBytes) parts *= 2;
