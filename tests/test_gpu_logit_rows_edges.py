@@ -289,3 +289,90 @@ def test_log_probabilities_of_far_apart_logits(V):
     for n in (T, 2):
         got = rows_of.check_logprobs(view[:n], s, tok[:n], min(V, 40))
         assert bool((got["logprob"] < -1.49e38).all()) and bool(torch.isfinite(got["logprob"]).all())
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("T,V,K", [(5, 61, 6), (4, 250, 20), (3, 2033, 31), (3, 20001, 64), (150, 9001, 16)])
+def test_distill_in_place_leaves_the_gaps(T, V, K, dtype):
+    view, flat = rows_of.rows(T, V, dtype, seed=V, pad=5, offset=3)
+    ids, y = rows_of.teacher(view.cpu(), K, 0.9)
+    ids, y, w = ids.cuda(), y.cuda(), torch.ones(T, device="cuda")
+    before = flat.clone()
+    out = torch.empty(T, V, dtype=view.dtype, device="cuda")
+    _, st = run_distill(view, 0.9, ids, y, 1, w, out, stats=True)
+    assert torch.equal(flat, before)
+    run_distill(view, 0.9, ids, y, 1, w, view)
+    rows_of.untouched(view, flat, before)
+    view.copy_(before[3:3 + T * (V + 5)].view(T, V + 5)[:, :V])
+    assert rb.remoe_distill_topk_backward(T, V, CODE[view.dtype], view, view.stride(0), 0.9, K, ids, y, st, w, view, view.stride(0), stream()) == 0
+    rows_of.untouched(view, flat, before)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("T", [1, 149])
+def test_the_longest_rows(T, dtype):
+    V, K, s = rb.REMOE_ROWS_MAX_VOCAB, rb.REMOE_ROWS_MAX_TOP, 0.9
+    g = torch.Generator(device="cuda").manual_seed(T)
+    flat = torch.full((3 + T * (V + 1) + 16,), 777.0, dtype=DT[dtype][0], device="cuda")
+    view = flat[3:3 + T * (V + 1)].view(T, V + 1)[:, :V]
+    for t in range(T):
+        view[t] = torch.randn(V, generator=g, device="cuda") * 3
+    tok = torch.arange(T, dtype=torch.int32, device="cuda") * 2609 % V
+    tok[0] = V - 1
+    code, before = DT[dtype][1], flat.clone()
+    few = [0] if T == 1 else [0, 1, T // 2, T - 1]          # rows that are compared
+    part, ptok = view[few], tok[few]
+    tz, lnv = ref.rel(V), math.log(V + 1)
+    want = {k: v.cpu() for k, v in ref.logprobs(part, s, ptok, K).items()}
+    for top in (K, 0):
+        got = logprobs(view, s, tok, top)
+        ref.close(got["logprob"][few], want["logprob"], tz + ref.U * (8 * want["logprob"].abs() + 2 * lnv), "logprob")
+        ref.close(got["entropy"][few], want["entropy"], (1 + 2 * lnv) * tz + ref.U * 4 * lnv, "entropy")
+        if top:
+            assert torch.equal(got["top_ids"][few], want["top_ids"])
+            ids, y = got["top_ids"].cuda(), got["top_logprobs"].cuda()
+    g_lp, g_ent = torch.ones(T, device="cuda"), torch.full((T,), 0.5, device="cuda")
+    out = torch.full((T, V), 3.0, dtype=view.dtype, device="cuda")
+    stats = got["row_stats"].cuda()
+    assert rb.remoe_token_logprobs_backward(T, V, code, view, view.stride(0), s, tok, stats, g_lp, g_ent, out, V, stream()) == 0
+    dx, size = ref.logprobs_grad(part, s, ptok, g_lp[few], g_ent[few])
+    ref.check_grad(out[few], dx, size, V, "log probabilities")
+    # a teacher: the rows' own records, a little flatter, so that there is a divergence
+    y = (y * 0.9 - 0.5).contiguous()
+    w = torch.ones(T, device="cuda")
+    want = ref.distill(part, s, ids[few], y[few], 1, w[few])
+    tol = want["size"] * (ref.rel(V) + 4 * ref.U) + ref.U * want["loss"].abs()
+    loss, _ = run_distill(view, s, ids, y, 1, w)
+    ref.close(loss[few], want["loss"], tol, "loss")
+    loss, st = run_distill(view, s, ids, y, 1, w, out, stats=True)
+    ref.close(loss[few], want["loss"], tol, "loss with the gradient")
+    ref.check_grad(out[few], want["grad"], want["grad_size"], V, "gradient with the loss", s)
+    assert rb.remoe_distill_topk_backward(T, V, code, view, view.stride(0), s, K, ids, y, st, w, out, V, stream()) == 0
+    ref.check_grad(out[few], want["grad"], want["grad_size"], V, "gradient apart", s)
+    assert torch.equal(flat, before)
+    run_distill(view, s, ids, y, 1, w, view)
+    rows_of.untouched(view, flat, before)
+
+
+# ---- precision as it is, beside the worst case ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("T,V,K", [(512, 64, 64), (512, 64, 16), (300, 250, 32), (64, 1021, 32), (64, 32003, 64), (256, 151936, 64)])
+def test_root_mean_square_errors(T, V, K, tail):
+    """The worst case of rel() adds up what in earnest averages out.  What does not: the exponential's own error (at most 4 u, one
+    sign at worst), that of log2(e) / temperature (1.2 u on a mean distance of about 5), and a rounding or two of a logarithm: 4 + 6 + 3 u.
+    Sixteen u for ln Z, and for the divergence from a teacher so near that the true one is of that size itself."""
+    g = torch.Generator().manual_seed(V + K)
+    x = (torch.randn(T, V, generator=g) * 2.5 + torch.randn(T, 1, generator=g) * 4).cuda()
+    tok = x.argmax(1).int()
+    got, want = logprobs(x, 0.9, tok, 0), ref.logprobs(x, 0.9, tok, 0)
+
+    def rms(a, b):
+        return float((a.double().cpu() - b.cpu()).square().mean().sqrt())
+
+    assert rms(got["row_stats"][:, 1], want["ln_z"]) <= 16 * ref.U
+    t = torch.log_softmax((x + torch.randn(T, V, generator=g).cuda() * 1e-4).double() * 0.9, 1).topk(K, 1)
+    ids, y, w = t.indices.int(), t.values.float(), torch.ones(T, device="cuda")
+    want = ref.distill(x, 0.9, ids, y, tail, w)["loss"]
+    assert rms(run_distill(x, 0.9, ids, y, tail, w)[0], want) <= 16 * ref.U
+    assert rms(run_distill(x, 0.9, ids, y, tail, w, torch.empty_like(x))[0], want) <= 16 * ref.U
