@@ -751,13 +751,18 @@ __global__ void __launch_bounds__(256) distill_small_kernel(const __grid_constan
       }
     loss = group_sum(loss);
     if (q_rest > 0.0) loss += q_rest * (ln_wide(q_rest) - ln_p_rest);
-    const float over = !a.tail || !some ? 0.f : (float)(others ? fmax(0.0, qs - 1.0) : qs - 1.0);   // Q - 1
-    const double p_rest = others ? of_rest / z : 0.0, c_rest = p_rest - q_rest + over * p_rest;
+    inv_z = (float)(1.0 / z);
+    double c_rest = others ? of_rest / z - q_rest : 0.0;
+    float over = 0.f;                               // Q - 1
+    if (a.tail && some && (!others || qs > 1.0)) {
+      over = (float)(qs - 1.0);
+      inv_z += over * inv_z;
+      if (others) c_rest += (qs - 1.0) * (of_rest / z);
+    }
     const bool in = some && alive;
     flag = bad ? nan_value() : in ? 1.f : 0.f;
     m_rest = others ? rest.m : 0.f;
     coef = others ? (float)(s * weight * c_rest) / (1.f + rest.R) : 0.f;
-    inv_z = (1.f + over) * (float)(1.0 / z);
     if (there && lane == 0) {
       const bool counts = weight != 0.f;
       if (a.loss) a.loss[r] = !counts ? 0.f : bad ? nan_value() : in ? (float)loss : 0.f;
