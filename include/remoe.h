@@ -333,8 +333,10 @@ int remoe_expert_ffn_static(int32_t hidden, int32_t weight_dtype, int32_t n_expe
  * Operators on rows of logits.  A decode step's hidden states end in rows of logits, a router's rows are logits over
  * its experts, and the rerouting bonus, the low-precision stores and a fine-tuned router all move them: these calls say
  * what the model answers (log probabilities, entropy, top alternatives), how far it has moved from a teacher
- * (divergence from recorded top log probabilities) and give the gradients of both (the paper's objective, Eq. 3, is a
- * cross-entropy plus an anchor to the frozen model).  The paper ships no such kernels; definitions are given here.
+ * (divergence from recorded top log probabilities) and give the gradients of both.  The divergence is KL(teacher || student); the
+ * anchor of the paper's objective (Eq. 4) is the other direction, KL(gate || frozen gate), and is not what is computed
+ * here.  The stack gives out neither router logits nor vocabulary logits: the rows come from the caller's own products with its
+ * hidden states.  The paper ships no such kernels; definitions are given here.
  *
  * Common to the four calls
  *   - Stateless: no stack, no allocation, no workspace, nothing kept between calls, one kernel launch on `cuda_stream`; calls
@@ -345,7 +347,7 @@ int remoe_expert_ffn_static(int32_t hidden, int32_t weight_dtype, int32_t n_expe
  *     float32 or wider and rounded once.  1 <= vocab <= REMOE_ROWS_MAX_VOCAB; n_rows = 0 does nothing.  p below is
  *     softmax(inv_temperature * row), 2^-100 <= inv_temperature <= 2^100.
  *   - The device is the one that logits_dev lies on (it need not be current; the stream and all other pointers belong to it).
- *   - -inf is a masked element (probability 0, gradient 0).  A row of -inf alone has no distribution: its log probabilities
+ *   - -inf is a masked element (probability 0; gradient 0, but for a masked token or list entry, which has its formula's).  A row of -inf alone has no distribution: its log probabilities
  *     are -inf, its entropy, losses and gradients 0.  The type's lowest value is an ordinary value (a row of it is
  *     uniform).  A row that holds a NaN or +inf gives NaN wherever its values enter.
  *   - A gradient may be written in place (d_logits_dev == logits_dev with the same stride); other overlap of outputs with
@@ -408,6 +410,9 @@ int remoe_token_logprobs_backward(int32_t n_rows, int32_t vocab, int32_t dtype, 
  *                     list, Q p_r - q_r, ln of the list's sum (tail = 0), 1 if the row takes part, Q - 1
  *   d_logits          [n_rows, vocab] of dtype or NULL: gradient of sum_t row_weight[t] * loss[t]
  * A row with an id outside [-1, vocab), or a NaN or +inf among its values, gives NaN.
+ * Precision: the loss is a small difference of large terms, whose sums over a row and logarithms are float32.  Its absolute error was 2e-8 to
+ * 4e-8 (root mean square, 1.3e-7 at most) with tail and 5e-8 to 2e-7 (5e-7 at most) without, for rows of 64 to 393216 elements, whatever the
+ * loss itself: one row's divergence below 1e-7 is noise, of either sign.
  */
 int remoe_distill_topk(int32_t n_rows, int32_t vocab, int32_t dtype, const void* logits_dev, int64_t row_stride,
                        float inv_temperature, int32_t n_top, const int32_t* teacher_ids_dev,

@@ -170,7 +170,7 @@ __device__ __forceinline__ void finish_row(const DistillArgs& a, int64_t r, floa
 // Then the list's elements are taken out of the slice (set to -inf where they lie in shared memory), the rest is summed in one
 // pass, blocks and list are joined, and the gradient is computed from the slice and written.
 //
-// With the gradient, 4096 rows of 102400 bf16 take 382 us, 0.67 of the copy rate.  A block lives 14 us, four of them on an SM: 3.2
+// With the gradient, 4096 rows of 102400 bf16 take 386 us, 0.67 of the copy rate.  A block lives 14 us, four of them on an SM: 3.2
 // until slice and list are there, 2.5 for the first pass, 6 until the cluster's slowest block has joined and the figures are
 // there, 2.2 for the second pass; the exponentials, two an element at 16 a cycle, take 0.7 of the memory time by themselves.
 // Slower, measured: persistent blocks that take a row twice through a ring, the second time out of L2 (388 us); the same with
@@ -504,7 +504,7 @@ __device__ __forceinline__ State sum_slice(const T* row, int V, const Slice& sl,
   return in.ok ? st.finish() : State{0.f, nan_value(), nan_value()};
 }
 
-// The loss alone (1024 rows of 151936 bf16: 64 us, 0.74 of the copy rate; 10 us of them until the first lists are there and
+// The loss alone (1024 rows of 151936 bf16: 65 us, 0.73 of the copy rate; 10 us of them until the first lists are there and
 // behind the last row).  Warps of a block, each at its own pace:
 //   producer   issues the copies;
 //   listers    two, for every second row each, up to two rows ahead: read the lists and compute their sums (two dependent loads

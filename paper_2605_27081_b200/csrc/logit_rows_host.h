@@ -109,7 +109,7 @@ inline cudaError_t launch_resident(const Args& args, size_t more_smem, cudaStrea
 }
 
 // Rows enough for persistent blocks that take whole rows: one for each SM.  (257 rows of 50257 fp16 with 5 alternatives: 16 us this
-// way, 19 with a cluster a row; 2048 of 131072 bf16 with 64: 135 against 568, since each of a row's blocks selects as
+// way, one row a block, 19 with a cluster a row; 2048 of 131072 bf16 with 64: 135 against 568, since each of a row's blocks selects as
 // much as one for the whole row would.)  Shorter rows are over before such a block's warps have handed them on.
 inline bool many_rows(int32_t n_rows, int32_t vocab) { return vocab >= 8192 && n_rows >= 148; }
 

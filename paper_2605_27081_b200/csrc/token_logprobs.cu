@@ -365,8 +365,8 @@ __device__ __forceinline__ void write_alternative(const LogprobArgs& a, int64_t 
 typedef TopShared<8 * REMOE_ROWS_MAX_TOP, 256> FewShared;   // room for the lists of a cluster's eight blocks
 
 // Few rows: one row per cluster of `parts` blocks, each block's slice of it in shared memory.  One row of 102400 bf16 with 20
-// alternatives takes 11.6 us, launch included: a copy, one pass, the selection (2.3 us) and the cluster's join, one behind
-// the other.
+// alternatives takes 11.0 us, one of twenty calls in a captured graph: a copy, one pass, the selection (2.3 us) and the cluster's join, one
+// behind the other.  32 rows of 151936 float32 with 8: 14.9 us, slices of 76 KB, two blocks on an SM.
 template <typename T, int NT, bool TOP>
 __global__ void __launch_bounds__(NT, 1024 / NT) logprob_rows_kernel(const __grid_constant__ LogprobArgs a) {
   __shared__ State per_warp[NT / 32];
@@ -480,9 +480,11 @@ struct Handover {
 
 // Many rows: persistent blocks, each takes row after row through its ring of chunks.  One warp issues the copies, the
 // consumers sum, and the finishers join a row's sums, select its top elements and write while the consumers are at the next
-// row already (two ahead at most).  What bounds it: without alternatives the memory (4096 x 102400 bf16: 135 us, 0.95 of the copy
-// rate); with them the finishers, 15 us a row, since their loads queue for 3 to 5 us behind the copies on their way to the SM
-// (2048 x 131072 bf16, 64 alternatives: 131 to 136 us; 110 without the selection).
+// row already (two ahead at most).  What bounds it: without alternatives the memory (4096 x 102400 bf16, calls back to back: 135 us, 0.95
+// of the copy rate; 158 behind a kernel that has just written 256 MB); with them the finishers, 15 us a row, since their loads queue for 3
+// to 5 us behind the copies on their way to the SM (2048 x 131072 bf16, 64 alternatives: 137 us; 110 without the selection).  The float32
+// form with alternatives spills 328 bytes a thread (the 16-bit ones 56 and 8).  With fewer rows than blocks a block has one row, and
+// its selection overlaps nothing (257 x 50257 fp16, 5 alternatives: 14.8 us).
 template <typename T, bool TOP>
 __global__ void __launch_bounds__(ManyShape<T, TOP>::kThreads, ManyShape<T, TOP>::kBlocks) logprob_pipe_kernel(const __grid_constant__ LogprobArgs a) {
   typedef ManyShape<T, TOP> Shape;
@@ -685,7 +687,8 @@ constexpr int kGradThreads = 256;
 template <typename T>
 constexpr int kGradUnits = sizeof(T) == 2 ? 4 : 1;
 
-// 4096 rows of 102400 bf16, a fifth of them padding: 265 us, 5.7 TB/s, 0.87 of the copy rate on the bytes that are moved.
+// 4096 rows of 102400 bf16, a fifth of them padding: 249 us, 6.1 TB/s, 0.93 of the copy rate on the bytes that are moved (273 behind kernels that
+// leave writes in L2).
 // Element-wise: what a row's gradient shares is in its row_stats.  Long rows: `tiles` blocks a row, each thread 64 bytes
 // (32 of float32: twice the registers a byte).  Short rows (SMALL): one unit a thread over all rows' units.
 template <typename T, bool SMALL>
