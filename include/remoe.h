@@ -59,7 +59,7 @@ enum {
 };
 
 enum { REMOE_F32 = 0, REMOE_BF16 = 1, REMOE_FP8_E4M3 = 2, REMOE_INT4_G32 = 3,
-       REMOE_F16 = 4 /* rows of logits only */ };
+       REMOE_F16 = 4 /* not a type of a stack */ };
 enum { REMOE_POLICY_LRU = 0, REMOE_POLICY_FIFO = 1, REMOE_POLICY_LFU = 2 };
 
 /* Shape of the stack.  Sec. 3.1: N_r routed experts, Top-K; shared experts always active. */
@@ -429,6 +429,97 @@ int remoe_distill_topk_backward(int32_t n_rows, int32_t vocab, int32_t dtype, co
                                 const int32_t* teacher_ids_dev, const float* teacher_logprobs_dev,
                                 const float* row_stats_dev, const float* grad_loss_dev, void* d_logits_dev,
                                 int64_t d_row_stride, void* cuda_stream);
+
+/*
+ * Operators on tokens sorted by expert: an MoE layer over many tokens at once (a prompt, a training batch), with its gradients.  A
+ * decode step takes at most 1024 selections through experts that lie in a cache; these calls take any number through experts that lie
+ * in device memory, in the block layout above.  A layer is
+ *     sort -> dispatch -> ffn -> combine        and back        combine_backward -> ffn_backward -> combine (of the rows' gradients)
+ * with ids and gates from the caller's router (decode ids, or top_ids of remoe_token_logprobs over a router's rows, work as they are).
+ * An always-active shared expert is one more call of remoe_expert_ffn with one expert and offsets {0, n_tokens}, or one more id of every
+ * token.  The paper ships no such kernels; definitions are given here.
+ *
+ * Common to the six calls
+ *   - Stateless: no stack, no allocation, nothing kept between calls, no synchronisation; launches on `cuda_stream` only.  Calls on any streams may
+ *     overlap, and a call may be captured into a CUDA graph (the first capture on a device should follow one plain call there:
+ *     kernels are loaded lazily).  Results are bit-for-bit the same on every run.
+ *   - The device is the one that the buffers lie on (it need not be current; the stream belongs to it).
+ *   - Matrices have rows `..._stride` elements apart (>= their width); what lies between rows, and rows that belong to no
+ *     selection, are left as they were, and what they hold does not matter.  A matrix or list without rows may be NULL.  Outputs do not overlap inputs or one another but where it is said.
+ *   - Sums are float32, rounded once where they are stored.  NaN and infinities of a row reach what that row takes part in and nothing else.
+ *   Errors: ARG (null or misaligned pointers, sizes, strides, unknown types, host memory), UNSUPPORTED (FP8 or 4-bit rows, sizes beyond the limits
+ *   given), CUDA.
+ */
+#define REMOE_SORT_MAX_EXPERTS 1024
+
+/*
+ * The rows of the selections, in the order (expert, token, rank).
+ *   ids      [n_tokens, top_k] int32; an id outside [0, n_experts) is no selection (padding tokens, experts that live elsewhere)
+ *   rows     [n_tokens, top_k] int32: the selection's row, -1 where there is none; may be the same buffer as ids
+ *   offsets  [n_experts + 1] int32: expert e has the rows offsets[e] .. offsets[e + 1] - 1
+ * n_experts <= REMOE_SORT_MAX_EXPERTS, n_tokens * top_k < 2^31; an expert may occur twice in a token's list.
+ */
+int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_experts, const int32_t* ids_dev, int32_t* rows_dev,
+                      int32_t* offsets_dev, void* cuda_stream);
+
+/*
+ * Rows out: xs[rows[t, k]] = x[t].  dtype REMOE_F32, REMOE_BF16 or REMOE_F16 (bits are copied), any width and alignment (16-byte aligned
+ * rows are fastest).  Rows outside [0, n_rows) are left out; every row occurs at most once in `rows`.  Its gradient is remoe_expert_combine
+ * of the rows' gradients with gates NULL.
+ */
+int remoe_expert_dispatch(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const void* x_dev, int64_t x_stride,
+                          const int32_t* rows_dev, int32_t n_rows, void* xs_dev, int64_t xs_stride, void* cuda_stream);
+
+/*
+ * Rows back: out[t] = base[t] + sum_k gates[t, k] * ys[rows[t, k]], added in the order of k, then the base.  Types as above.
+ *   gates   [n_tokens, top_k] float32 or NULL (= 1)
+ *   base    [n_tokens, hidden] or NULL (= 0): a residual stream, the shared experts' sum; may be the same buffer as out (and stride)
+ * A selection without a row (outside [0, n_rows)) adds nothing, whatever its gate.
+ */
+int remoe_expert_combine(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, int32_t n_rows, const void* ys_dev,
+                         int64_t ys_stride, const int32_t* rows_dev, const float* gates_dev, const void* base_dev,
+                         int64_t base_stride, void* out_dev, int64_t out_stride, void* cuda_stream);
+
+/*
+ * Gradients of the combine: d_ys[rows[t, k]] = gates[t, k] * d_out[t] and d_gates[t, k] = <ys[rows[t, k]], d_out[t]> (0 for a selection without
+ * a row).  The gradient of base is d_out itself.  Either of d_ys and d_gates ([n_tokens, top_k] float32) may be NULL; without d_gates ys is
+ * not read and may be NULL.  d_ys may be the same buffer as ys (and stride).
+ */
+int remoe_expert_combine_backward(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const void* d_out_dev,
+                                  int64_t d_out_stride, int32_t n_rows, const void* ys_dev, int64_t ys_stride,
+                                  const int32_t* rows_dev, const float* gates_dev, void* d_ys_dev, int64_t d_ys_stride,
+                                  float* d_gates_dev, void* cuda_stream);
+
+/*
+ * The experts: for the rows offsets[e] .. offsets[e + 1] - 1 of every expert, ys = W_down (silu(W_gate xs) * (W_up xs)), on the
+ * tensor cores.
+ *   dtype       REMOE_BF16 or REMOE_F16, of xs, ys, blocks and the buffers alike (REMOE_F32: UNSUPPORTED, the tensor cores have no such product)
+ *   hidden, inter   multiples of 8, <= REMOE_FFN_MAX_WIDTH;  n_experts <= REMOE_SORT_MAX_EXPERTS;  n_rows <= 2^30
+ *   xs, ys      [n_rows, hidden]; offsets [n_experts + 1] in device memory, ascending within 0 .. n_rows (they are held to that range)
+ *   blocks      n_experts expert blocks [inter, 3, hidden], block_stride elements apart (>= 3 * inter * hidden)
+ *   act         [n_rows, inter]: work space, holds silu(gate) * up of every row afterwards, rounded to dtype, as the second product reads it
+ *   gate_up     [2, n_rows, inter] or NULL: the two products, kept for the backward call
+ * Strides are multiples of 8, pointers 16-byte aligned.  Values beyond float16's range become infinite, as they do in any float16 tensor.
+ * If an internal bounded wait ever runs out, the rows concerned are NaN rather than wrong.
+ */
+#define REMOE_FFN_MAX_WIDTH 65536
+int remoe_expert_ffn(int32_t n_rows, int32_t n_experts, int32_t hidden, int32_t inter, int32_t dtype, const void* xs_dev,
+                     int64_t xs_stride, const int32_t* offsets_dev, const void* blocks_dev, int64_t block_stride,
+                     void* gate_up_dev, void* act_dev, void* ys_dev, int64_t ys_stride, void* cuda_stream);
+
+/*
+ * Its gradients, from the same xs, offsets and blocks and the gate_up of the forward call (with a = silu(g) u taken again from the kept g and u).
+ *   d_ys      [n_rows, hidden]
+ *   work      [3, n_rows, inter]: work space, holds the gradients of g and u and a of every row afterwards, rounded to dtype
+ *   d_xs      [n_rows, hidden] or NULL; may be the same buffer as d_ys (and stride) where d_blocks is NULL
+ *   d_blocks  n_experts blocks [inter, 3, hidden], d_block_stride elements apart, or NULL (frozen experts: xs is not read and may be NULL);
+ *             overwritten, with zeros for an expert without rows
+ * One of d_xs and d_blocks at least.  Types, limits and alignment as above.
+ */
+int remoe_expert_ffn_backward(int32_t n_rows, int32_t n_experts, int32_t hidden, int32_t inter, int32_t dtype, const void* xs_dev,
+                              int64_t xs_stride, const int32_t* offsets_dev, const void* blocks_dev, int64_t block_stride,
+                              const void* gate_up_dev, const void* d_ys_dev, int64_t d_ys_stride, void* work_dev, void* d_xs_dev,
+                              int64_t d_xs_stride, void* d_blocks_dev, int64_t d_block_stride, void* cuda_stream);
 
 /* Text of the last CUDA runtime error, or of the last device-flag / trace-validation failure,
  * seen by this stack ("" if none). */

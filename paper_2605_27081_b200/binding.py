@@ -19,6 +19,7 @@ REMOE_E_ARG, REMOE_E_CAPACITY, REMOE_E_NOT_LOADED, REMOE_E_NOT_PINNED = -1, -2, 
 REMOE_E_CUDA, REMOE_E_DEVICE_FLAG, REMOE_E_UNSUPPORTED, REMOE_E_NOMEM, REMOE_E_ORDER = -5, -6, -7, -8, -9
 REMOE_F32, REMOE_BF16, REMOE_FP8_E4M3, REMOE_INT4_G32, REMOE_F16 = 0, 1, 2, 3, 4
 REMOE_ROWS_MAX_VOCAB, REMOE_ROWS_MAX_TOP = 393216, 256
+REMOE_SORT_MAX_EXPERTS, REMOE_FFN_MAX_WIDTH = 1024, 65536
 REMOE_POLICY_LRU, REMOE_POLICY_FIFO, REMOE_POLICY_LFU = 0, 1, 2
 
 EXPORTS = [
@@ -29,6 +30,8 @@ EXPORTS = [
     "remoe_strerror", "remoe_expert_ffn_static", "remoe_reuse_mass", "remoe_step_history", "remoe_tpot_proxy", "remoe_decode_step_chained",
     "remoe_expert_load", "remoe_decode_steps", "remoe_order_check_counts", "remoe_cache_snapshot",
     "remoe_token_logprobs", "remoe_token_logprobs_backward", "remoe_distill_topk", "remoe_distill_topk_backward",
+    "remoe_expert_sort", "remoe_expert_dispatch", "remoe_expert_combine", "remoe_expert_combine_backward", "remoe_expert_ffn",
+    "remoe_expert_ffn_backward",
 ]
 
 
@@ -88,6 +91,12 @@ def lib():
         L.remoe_token_logprobs_backward.argtypes = [i32, i32, i32, vp, i64, f32, i32p, f32p, f32p, f32p, vp, i64, vp]
         L.remoe_distill_topk.argtypes = [i32, i32, i32, vp, i64, f32, i32, i32p, f32p, i32, f32p, f32p, f32p, vp, i64, vp]
         L.remoe_distill_topk_backward.argtypes = [i32, i32, i32, vp, i64, f32, i32, i32p, f32p, f32p, f32p, vp, i64, vp]
+        L.remoe_expert_sort.argtypes = [i32, i32, i32, i32p, i32p, i32p, vp]
+        L.remoe_expert_dispatch.argtypes = [i32, i32, i32, i32, vp, i64, i32p, i32, vp, i64, vp]
+        L.remoe_expert_combine.argtypes = [i32, i32, i32, i32, i32, vp, i64, i32p, f32p, vp, i64, vp, i64, vp]
+        L.remoe_expert_combine_backward.argtypes = [i32, i32, i32, i32, vp, i64, i32, vp, i64, i32p, f32p, vp, i64, f32p, vp]
+        L.remoe_expert_ffn.argtypes = [i32, i32, i32, i32, i32, vp, i64, i32p, vp, i64, vp, vp, vp, i64, vp]
+        L.remoe_expert_ffn_backward.argtypes = [i32, i32, i32, i32, i32, vp, i64, i32p, vp, i64, vp, vp, i64, vp, vp, i64, vp, i64, vp]
         L.remoe_reuse_mass.argtypes = [vp, i32, C.POINTER(C.c_double), C.POINTER(C.c_uint64), vp]
         L.remoe_step_history.argtypes = [vp, i32, i32, vp, vp, C.POINTER(i32)]
         L.remoe_expert_load.argtypes = [vp, i32, vp, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(i32)]
@@ -266,6 +275,42 @@ def remoe_distill_topk_backward(n_rows, vocab, dtype, logits, row_stride, inv_te
     return lib().remoe_distill_topk_backward(n_rows, vocab, dtype, _ptr(logits), row_stride, inv_temperature, n_top,
                                              _ptr(teacher_ids), _ptr(teacher_logprobs), _ptr(row_stats), _ptr(grad_loss),
                                              _ptr(d_logits), d_row_stride, cuda_stream)
+
+
+# Tokens sorted by expert: device tensors or addresses as above.
+
+def remoe_expert_sort(n_tokens, top_k, n_experts, ids, rows, offsets, cuda_stream=None):
+    return lib().remoe_expert_sort(n_tokens, top_k, n_experts, _ptr(ids), _ptr(rows), _ptr(offsets), cuda_stream)
+
+
+def remoe_expert_dispatch(n_tokens, top_k, hidden, dtype, x, x_stride, rows, n_rows, xs, xs_stride, cuda_stream=None):
+    return lib().remoe_expert_dispatch(n_tokens, top_k, hidden, dtype, _ptr(x), x_stride, _ptr(rows), n_rows, _ptr(xs), xs_stride,
+                                       cuda_stream)
+
+
+def remoe_expert_combine(n_tokens, top_k, hidden, dtype, n_rows, ys, ys_stride, rows, gates, base, base_stride, out, out_stride,
+                         cuda_stream=None):
+    return lib().remoe_expert_combine(n_tokens, top_k, hidden, dtype, n_rows, _ptr(ys), ys_stride, _ptr(rows), _ptr(gates),
+                                      _ptr(base), base_stride, _ptr(out), out_stride, cuda_stream)
+
+
+def remoe_expert_combine_backward(n_tokens, top_k, hidden, dtype, d_out, d_out_stride, n_rows, ys, ys_stride, rows, gates, d_ys,
+                                  d_ys_stride, d_gates, cuda_stream=None):
+    return lib().remoe_expert_combine_backward(n_tokens, top_k, hidden, dtype, _ptr(d_out), d_out_stride, n_rows, _ptr(ys), ys_stride,
+                                               _ptr(rows), _ptr(gates), _ptr(d_ys), d_ys_stride, _ptr(d_gates), cuda_stream)
+
+
+def remoe_expert_ffn(n_rows, n_experts, hidden, inter, dtype, xs, xs_stride, offsets, blocks, block_stride, gate_up, act, ys, ys_stride,
+                     cuda_stream=None):
+    return lib().remoe_expert_ffn(n_rows, n_experts, hidden, inter, dtype, _ptr(xs), xs_stride, _ptr(offsets), _ptr(blocks), block_stride,
+                                  _ptr(gate_up), _ptr(act), _ptr(ys), ys_stride, cuda_stream)
+
+
+def remoe_expert_ffn_backward(n_rows, n_experts, hidden, inter, dtype, xs, xs_stride, offsets, blocks, block_stride, gate_up, d_ys,
+                              d_ys_stride, work, d_xs, d_xs_stride, d_blocks, d_block_stride, cuda_stream=None):
+    return lib().remoe_expert_ffn_backward(n_rows, n_experts, hidden, inter, dtype, _ptr(xs), xs_stride, _ptr(offsets), _ptr(blocks),
+                                           block_stride, _ptr(gate_up), _ptr(d_ys), d_ys_stride, _ptr(work), _ptr(d_xs), d_xs_stride,
+                                           _ptr(d_blocks), d_block_stride, cuda_stream)
 
 
 def remoe_reuse_mass(h, layer=-1, last_mass=None):

@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libremoe.so")
 SOURCES = ["route.cu", "ffn_stream.cu", "ffn_batched.cu", "ffn_batched_tc.cu", "api.cu", "ffn_static.cu",
-           "token_logprobs.cu", "distill.cu"]
+           "token_logprobs.cu", "distill.cu", "expert_rows.cu", "expert_products.cu"]
 
 
 def _nvcc() -> str:
