@@ -4,17 +4,19 @@
 // neighbouring SMs (tcgen05.mma with cta_group::2: each CTA stages 128 rows of M and half of the rows of N and keeps its 128 rows
 // of the fp32 result in TMEM, a lane for each m).  The side that belongs to the weights is M, so that the ragged side, the rows of an
 // expert, is N, whose width the instruction takes in steps of 32 columns:
-//   kGateUp      m = channel (gate and up rows in neighbouring lanes), n = row, k = hidden:   act = silu(g) u
-//   kDown        m = hidden,  n = row, k = channel:                                             ys = act W_down
-//   kGradAct     m = channel, n = row, k = hidden:    d act = d_ys W_down^T;   d g, d u, act by the derivative of silu(g) u
-//   kGradRows    m = hidden,  n = row, k = channel of d g, then of d u:        d_xs = d_g W_gate + d_u W_up
+//   kGateUp      m = channel (gate and up), n = row, k = hidden:              act = silu(g) u
+//   kDown        m = hidden,  n = row, k = channel:                           ys = act W_down
+//   kGradAct     m = channel, n = row, k = hidden:    d act = d_ys W_down^T;  d g, d u, act by the derivative of silu(g) u
+//   kGradRows    m = hidden,  n = row, k = channel of d g, then of d u:       d_xs = d_g W_gate + d_u W_up
 //   kGradBlocks  m = hidden,  n = channel, k = row:   d W = (d g)^T xs, (d u)^T xs, act^T d_ys, one plane of a block each
 // Operands come through tensor maps straight from where the caller keeps them: K-major tiles (k contiguous) are [128 rows x 64],
 // MN-major ones two [64 x 64] boxes with k as the rows; both are the 128-byte-swizzled images the tensor cores read.
-// Per CTA: warp 0 loads (TMA, a ring of six 32 KB stages), warp 1 of the pair's even CTA issues the products, warps 4-7 read the results out of
-// TMEM (two buffers of 256 columns, so that a tile's epilogue runs behind the next tile's products).  With k = row (kGradBlocks) an expert's
-// last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has written) would
-// enter the sums, so warp 2 stands between the copies and the products and clears it in both operands.
+// Per CTA: warp 0 loads (TMA, a ring of three stages of 128 k, 64 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 read the
+// results out of TMEM (two buffers of 256 columns, so that a tile's epilogue runs behind the next tile's products).  With k = row
+// (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
+// written) would enter the sums, so warp 2 stands between the copies and the products and clears it in both operands.
+// The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans), so
+// that rows leave in 16-byte accesses, 256 bytes of a row side by side.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -32,17 +34,23 @@ using namespace ring;
 enum Mode { kGateUp, kDown, kGradAct, kGradRows, kGradBlocks };
 
 constexpr int kTile = 256;                               // rows of M and most rows of N of a pair's tile
-constexpr int kK = 64;                                   // k of a stage: 128 bytes
-constexpr int kOperandBytes = 128 * 128;                 // a CTA's half of an operand
-constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStages = 6;
+constexpr int kK = 64;                                   // k of a piece: 128 bytes
+constexpr int kPieces = 2;                               // pieces of a stage: each thread's chain of wait, issue and commit runs once a stage
+constexpr int kOperandBytes = 128 * 128;                 // a CTA's half of an operand's piece
+constexpr int kPieceBytes = 2 * kOperandBytes;
+constexpr int kStageBytes = kPieces * kPieceBytes;
+constexpr int kStages = 3;
+constexpr int kStagingBytes = 16384;                     // of the epilogue
 constexpr int kThreads = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr unsigned kPolls = 1u << 18;                    // of a bounded wait
+constexpr int kBoxes = 5;
+// Rows of N in one copy: 16, 32, 64, 96, 128.
+__host__ __device__ constexpr int box_rows(int b) { return b == 0 ? 16 : b == 1 ? 32 : 32 * b; }
 
 struct ProductArgs {
   CUtensorMap m[2];                                      // M: blocks; kGradBlocks: xs, d_ys
-  CUtensorMap n[3];                                      // N: boxes of 16, 64 and 128 rows; kGradBlocks: n[0], boxes of 64
+  CUtensorMap n[kBoxes];                                 // N: boxes of box_rows; kGradBlocks: n[0], boxes of 64
   const int* offsets;
   int n_experts, n_rows, H, I;
   const uint16_t* gate_up;                               // kGradAct: [2, n_rows, I]
@@ -66,25 +74,19 @@ __device__ __forceinline__ uint32_t in_even_cta(const void* p) {
   asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
   return r;
 }
-__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+__device__ __forceinline__ void arrive_at(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_release_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// Bounded wait that also sees what the other CTA has released.
-__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity) {
-  for (unsigned it = 0; it < kPolls; ++it) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
-    if (ok) return true;
-  }
-  return false;
-}
 // Loads of this CTA's own shared memory; completion is counted on a barrier of either CTA of the pair.
+__device__ __forceinline__ void load_5d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
+      : "memory");
+}
 __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
   asm volatile(
       "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
@@ -117,26 +119,51 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// 32 consecutive fp32 columns of this thread's TMEM lane.
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float (&v)[32]) {
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// 16 lanes x 32 (16) fp32 columns of TMEM as 8 x 8 fragments: for the columns 8 i .. 8 i + 7 the thread holds, of lane T / 4, the columns
+// 2 (T % 4) and the next in v[4 i], v[4 i + 1], and of lane T / 4 + 8 the same in v[4 i + 2], v[4 i + 3].  The caller waits.
+__device__ __forceinline__ void tmem_fragments(uint32_t taddr, float (&v)[16]) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(taddr));
 }
+__device__ __forceinline__ void tmem_fragments(uint32_t taddr, float (&v)[8]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+// Four 8 x 8 matrices of 16-bit values between fragments and shared memory, turned over: a lane gives the address of row
+// (lane % 8) of matrix (lane / 8), a row being the fragment's column.
+__device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
+}
+__device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void epilogue_bar() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
-template <typename T> __device__ __forceinline__ uint16_t bits(float v);
-template <> __device__ __forceinline__ uint16_t bits<__nv_bfloat16>(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
-template <> __device__ __forceinline__ uint16_t bits<__half>(float v) { return __half_as_ushort(__float2half_rn(v)); }
-template <typename T> __device__ __forceinline__ float value(uint16_t b);
-template <> __device__ __forceinline__ float value<__nv_bfloat16>(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
-template <> __device__ __forceinline__ float value<__half>(uint16_t b) { return __half2float(__ushort_as_half(b)); }
+template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <typename T> __device__ __forceinline__ float2 unpack(uint32_t v);
+template <> __device__ __forceinline__ float2 unpack<__nv_bfloat16>(uint32_t v) {
+  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+template <> __device__ __forceinline__ float2 unpack<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
@@ -147,7 +174,7 @@ struct Tile {
   int m0;                                                // first row of M (kGateUp: channel)
   int plane;                                             // kGradBlocks: plane of the block
   int first_row, count;                                  // kGradBlocks: the expert's rows
-  int steps;                                             // stages of k
+  int pieces;                                            // of k
 };
 
 // The tiles of a launch in the order of experts, dealt to the pairs in turn.  Each role of a CTA walks them by itself.
@@ -177,7 +204,7 @@ struct Walk {
       g.n = min(kTile, a.I - g.row);
       g.first_row = first[g.e];
       g.count = count[g.e];
-      g.steps = (g.count + kK - 1) / kK;
+      g.pieces = (g.count + kK - 1) / kK;
     } else {
       while (e < a.n_experts && t >= upto[e + 1] * m_tiles) ++e;
       if (e >= a.n_experts) return false;
@@ -189,11 +216,20 @@ struct Walk {
       g.row = first[e] + i * size;
       g.n = min(size, count[e] - i * size);
       const int k = MODE == kDown || MODE == kGradRows ? a.I : a.H;
-      g.steps = (k + kK - 1) / kK * (MODE == kGradRows ? 2 : 1);
+      g.pieces = (k + kK - 1) / kK * (MODE == kGradRows ? 2 : 1);
     }
     g.half = (g.n + 31) / 32 * 16;
     t += (int)gridDim.x >> 1;
     return true;
+  }
+};
+
+// A place in the ring and the parity of its present use.
+struct Place {
+  int s = 0;
+  uint32_t turn = 0;
+  __device__ __forceinline__ void next() {
+    if (++s == kStages) { s = 0; turn ^= 1; }
   }
 };
 
@@ -203,7 +239,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   constexpr bool kMMajor = MODE == kDown || MODE == kGradRows || MODE == kGradBlocks, kNMajor = MODE == kGradBlocks;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + (size_t)kStages * kStageBytes);   // even CTA: both halves of a stage are there
+  unsigned char* staging = smem + (size_t)kStages * kStageBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + kStagingBytes);   // even CTA: both halves of a stage are there
   uint64_t* landed = full + kStages;                     // kRagged: this CTA's copies of a stage have landed
   uint64_t* empty = landed + kStages;                    // a stage has been read
   uint64_t* acc_full = empty + kStages;                  // [2] a result is complete
@@ -256,63 +293,79 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   cluster_sync_all();
   fence_after();
   const uint32_t tmem = *tmem_slot;
+  // After a wait that ran out a role stops, and the others of its CTA with their next tile (or their own next wait).
   auto aborted = [&]() { return *(volatile int*)abort_flag != 0; };
-  auto give_up = [&]() { *(volatile int*)abort_flag = 1; return false; };
+  auto wait = [&](uint64_t* bar, uint32_t parity, unsigned polls = kPolls) {
+    if (mbar_wait(bar, parity, polls)) return true;
+    *(volatile int*)abort_flag = 1;
+    return false;
+  };
 
   Walk<MODE> walk(a, first, count, upto);
   Tile g;
   if (warp == 0) {
     // ------------------------------------------------------------------------------------------------ copies
     if (lane == 0) {
-      int n = 0;
+      Place at;
+      int64_t stages = 0;                                // issued
       bool ok = true;
-      while (ok && walk.next(g)) {
-        const int box = kRagged ? (g.half > 64 ? 2 : 1) : g.half <= 16 ? 0 : g.half <= 64 ? 1 : 2;
-        const uint32_t n_bytes = kRagged ? box * 8192u : box == 0 ? 2048u : box == 1 ? 8192u : 16384u;
-        for (int kb = 0; kb < g.steps && ok; ++kb, ++n) {
-          const int s = n % kStages;
-          if (n >= kStages) {
-            ok = !aborted() && mbar_wait(empty + s, ((n / kStages) - 1) & 1, kPolls);
-            if (!ok) { give_up(); break; }
+      while (ok && !aborted() && walk.next(g)) {
+        int box = 0;
+        if constexpr (kRagged) box = g.half > 64 ? 2 : 1;            // copies of 64 channels
+        else while (box_rows(box) < g.half) ++box;
+        const uint32_t bytes = kOperandBytes + (kRagged ? box * 8192u : box_rows(box) * 128u);
+        const CUtensorMap* n_map = kRagged ? &a.n[0] : &a.n[box];
+        const int n_row = g.row + cta * g.half;
+        for (int p0 = 0; p0 < g.pieces; p0 += kPieces) {
+          if (stages >= kStages) {
+            ok = wait(empty + at.s, at.turn ^ 1);
+            if (!ok) break;
           }
-          const uint32_t m_dst = smem_u32(smem + (size_t)s * kStageBytes), n_dst = m_dst + kOperandBytes;
+          const int here = min(kPieces, g.pieces - p0);
           uint32_t bar;
           if constexpr (kRagged) {
-            mbar_expect_tx(landed + s, kOperandBytes + n_bytes);
-            bar = smem_u32(landed + s);
+            mbar_expect_tx(landed + at.s, here * bytes);
+            bar = smem_u32(landed + at.s);
           } else {
-            if (cta == 0) mbar_expect_tx(full + s, 2 * (kOperandBytes + n_bytes));
-            bar = in_even_cta(full + s);
+            if (cta == 0) mbar_expect_tx(full + at.s, 2 * here * bytes);
+            bar = in_even_cta(full + at.s);
           }
-          const int n_row = g.row + cta * g.half;
-          if constexpr (MODE == kGateUp) {
-            load_4d(m_dst, &a.m[0], kb * kK, 0, g.m0 + cta * 64, g.e, bar);
-            load_3d(n_dst, &a.n[box], kb * kK, n_row, 0, bar);
-          } else if constexpr (MODE == kGradAct) {
-            load_4d(m_dst, &a.m[0], kb * kK, 2, g.m0 + cta * 128, g.e, bar);
-            load_3d(n_dst, &a.n[box], kb * kK, n_row, 0, bar);
-          } else if constexpr (MODE == kDown || MODE == kGradRows) {
-            const int per = MODE == kDown ? g.steps : g.steps / 2;
-            const int j = kb >= per, k0 = (kb - j * per) * kK;
-            const int plane = MODE == kDown ? 2 : j;
-            load_4d(m_dst, &a.m[0], g.m0 + cta * 128, plane, k0, g.e, bar);
-            load_4d(m_dst + 8192, &a.m[0], g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
-            load_3d(n_dst, &a.n[box], k0, n_row, j, bar);
-          } else {
-            const int row = g.first_row + kb * kK;
-            const CUtensorMap* m = &a.m[g.plane == 2];
-            load_3d(m_dst, m, g.m0 + cta * 128, row, 0, bar);
-            load_3d(m_dst + 8192, m, g.m0 + cta * 128 + 64, row, 0, bar);
-            load_3d(n_dst, &a.n[0], n_row, row, g.plane, bar);
-            if (box == 2) load_3d(n_dst + 8192, &a.n[0], n_row + 64, row, g.plane, bar);
+          for (int p = p0; p < p0 + here; ++p) {
+            const uint32_t m_dst = smem_u32(smem) + at.s * kStageBytes + (p - p0) * kPieceBytes, n_dst = m_dst + kOperandBytes;
+            if constexpr (MODE == kGateUp) {
+              load_5d(m_dst, &a.m[0], p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
+              load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
+            } else if constexpr (MODE == kGradAct) {
+              load_4d(m_dst, &a.m[0], p * kK, 2, g.m0 + cta * 128, g.e, bar);
+              load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
+            } else if constexpr (MODE == kDown || MODE == kGradRows) {
+              const int per = MODE == kDown ? g.pieces : g.pieces / 2;
+              const int j = p >= per, k0 = (p - j * per) * kK;
+              const int plane = MODE == kDown ? 2 : j;
+              load_4d(m_dst, &a.m[0], g.m0 + cta * 128, plane, k0, g.e, bar);
+              load_4d(m_dst + 8192, &a.m[0], g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
+              load_3d(n_dst, n_map, k0, n_row, j, bar);
+            } else {
+              const int row = g.first_row + p * kK;
+              const CUtensorMap* m = &a.m[g.plane == 2];
+              load_3d(m_dst, m, g.m0 + cta * 128, row, 0, bar);
+              load_3d(m_dst + 8192, m, g.m0 + cta * 128 + 64, row, 0, bar);
+              load_3d(n_dst, n_map, n_row, row, g.plane, bar);
+              if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, g.plane, bar);
+            }
           }
+          at.next();
+          ++stages;
         }
       }
       // The last products have read their stages and their arrivals have come in before the CTA leaves; after a wait that ran out, the
       // copies under way are waited for instead.
-      for (int i = n > kStages ? n - kStages : 0; i < n; ++i) {
-        if (ok) mbar_wait(empty + i % kStages, (i / kStages) & 1, kPolls);
-        else mbar_wait((kRagged ? landed : full) + i % kStages, (i / kStages) & 1, kPolls);
+      Place back;
+      for (int64_t i = stages > kStages ? stages - kStages : 0; i < stages; ++i) {
+        back.s = (int)(i % kStages);
+        back.turn = (uint32_t)(i / kStages) & 1;
+        if (ok) wait(empty + back.s, back.turn);
+        else wait((kRagged ? landed : full) + back.s, back.turn);
       }
     }
   } else if (warp == 1) {
@@ -321,32 +374,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       // fp32 result, both operands of type T, M = 256; bit 15: M is MN-major, bit 16: N is
       constexpr uint32_t kIdesc = (1u << 4) | (kType << 7) | (kType << 10) | ((256u >> 4) << 24) | (kMMajor ? 1u << 15 : 0u) | (kNMajor ? 1u << 16 : 0u);
-      int n = 0, acc = 0;
+      // of the ring's first piece; a step of 16 k further: 32 bytes (K-major) or 16 rows of 128
+      const uint64_t m_desc = kMMajor ? operand_desc(smem_u32(smem), 8192, 1024) : operand_desc(smem_u32(smem), 16, 1024);
+      const uint64_t n_desc = kNMajor ? operand_desc(smem_u32(smem) + kOperandBytes, 8192, 1024) : operand_desc(smem_u32(smem) + kOperandBytes, 16, 1024);
+      constexpr uint32_t kMStep = (kMMajor ? 2048 : 32) >> 4, kNStep = (kNMajor ? 2048 : 32) >> 4;
+      Place at;
+      int acc = 0;
       bool ok = true;
-      while (ok && walk.next(g)) {
-        if (g.steps == 0) continue;
-        if (acc >= 2) ok = !aborted() && wait_cluster(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
+      while (!aborted() && walk.next(g)) {
+        if (g.pieces == 0) continue;
+        if (acc >= 2) ok = wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
         if (!ok) break;
         fence_after();
         const uint32_t d = tmem + (uint32_t)(acc & 1) * kTile, idesc = kIdesc | ((uint32_t)(2 * g.half) >> 3 << 17);
-        for (int kb = 0; kb < g.steps; ++kb, ++n) {
-          const int s = n % kStages;
-          ok = !aborted() && wait_cluster(full + s, (n / kStages) & 1);
+        for (int p0 = 0; p0 < g.pieces; p0 += kPieces) {
+          ok = wait(full + at.s, at.turn);
           if (!ok) break;
+          // (what warp 2 of either CTA has cleared)
+          if (kRagged && p0 + kPieces >= g.pieces) asm volatile("fence.acq_rel.cluster;" ::: "memory");
           fence_after();
-          const uint32_t m_at = smem_u32(smem + (size_t)s * kStageBytes), n_at = m_at + kOperandBytes;
+          const uint32_t stage = (uint32_t)(at.s * kStageBytes) >> 4;
 #pragma unroll
-          for (int k = 0; k < kK / 16; ++k)
-            mma_pair(d, kMMajor ? operand_desc(m_at + k * 2048, 8192, 1024) : operand_desc(m_at + k * 32, 16, 1024),
-                     kNMajor ? operand_desc(n_at + k * 2048, 8192, 1024) : operand_desc(n_at + k * 32, 16, 1024), idesc, (kb | k) ? 1u : 0u);
-          commit_pair(empty + s);
+          for (int q = 0; q < kPieces; ++q) {
+            if (p0 + q >= g.pieces) break;
+            const uint64_t dm = m_desc + stage + q * (kPieceBytes >> 4), dn = n_desc + stage + q * (kPieceBytes >> 4);
+#pragma unroll
+            for (int k = 0; k < kK / 16; ++k) mma_pair(d, dm + k * kMStep, dn + k * kNStep, idesc, (p0 | q | k) ? 1u : 0u);
+          }
+          commit_pair(empty + at.s);
+          at.next();
         }
         if (!ok) break;
         commit_pair(acc_full + (acc & 1));
         ++acc;
       }
       if (!ok) {
-        give_up();
         commit_pair(drain);                              // let the tensor cores finish before TMEM is freed
         mbar_wait(drain, 0, kPolls);
       }
@@ -354,17 +416,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   } else if (warp == 2) {
     // ------------------------------------------------------------------------------- rows behind an expert's last
     if constexpr (kRagged) {
-      int n = 0;
+      Place at;
       bool ok = true;
-      while (ok && walk.next(g)) {
-        const int chunks = g.half > 64 ? 4 : 3;
-        for (int kb = 0; kb < g.steps; ++kb, ++n) {
-          const int s = n % kStages;
-          ok = !aborted() && mbar_wait(landed + s, (n / kStages) & 1, kPolls);
+      while (ok && !aborted() && walk.next(g)) {
+        const int chunks = g.half > 64 ? 4 : 3;          // of 64 rows of k, two of M and those of N
+        for (int p0 = 0; p0 < g.pieces; p0 += kPieces) {
+          ok = wait(landed + at.s, at.turn);
           if (!ok) break;
-          const int left = g.count - kb * kK;
-          if (left < kK) {
-            unsigned char* st = smem + (size_t)s * kStageBytes;
+          const int p = g.pieces - 1, left = g.count - p * kK;       // rows of the expert's last piece
+          const bool clear = p < p0 + kPieces && left < kK;
+          if (clear) {
+            unsigned char* st = smem + (size_t)at.s * kStageBytes + (size_t)(p - p0) * kPieceBytes;
             for (int i = lane; i < chunks * (kK - left) * 8; i += 32) {
               const int line = i >> 3, c = line / (kK - left), r = left + line % (kK - left);
               *reinterpret_cast<uint4*>(st + c * 8192 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
@@ -372,83 +434,158 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
           __syncwarp();
-          if (lane == 0) arrive_cluster(in_even_cta(full + s));
+          if (lane == 0) {
+            if (clear) arrive_release_cluster(in_even_cta(full + at.s));
+            else arrive_at(in_even_cta(full + at.s));
+          }
+          at.next();
         }
       }
-      if (!ok) give_up();
     }
   } else if (warp >= 4) {
     // ------------------------------------------------------------------------------------------------ results
-    const int quad = warp & 3;
+    const int quad = warp & 3, t = tid - 128;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    int acc = 0;
+    const uint32_t stage_at = smem_u32(staging);
+    constexpr int kCols = MODE == kGradAct ? 16 : 32;    // columns of the result (rows of the output) at a time
+    constexpr int kFrag = kCols / 2;
+    int acc = 0, buffer = 0;
     bool ok = true;
     while (walk.next(g)) {
-      if (g.steps && ok) {
-        // a whole tile long: more polls for more stages
-        ok = !aborted() && mbar_wait(acc_full + (acc & 1), (acc >> 1) & 1, kPolls + (unsigned)min(g.steps, 1 << 20) * 1024u);
-        if (!ok) give_up();
+      // kGradAct: the kept gates and ups of the next columns, 16 rows x 128 channels of each, on their way behind the products
+      uint4 next_gate[2], next_up[2];
+      auto fetch = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = (i * 128 + t) >> 4, ch = g.m0 + cta * 128 + (t & 15) * 8;
+          next_gate[i] = next_up[i] = make_uint4(0, 0, 0, 0);
+          if (c0 + r < g.n && ch < a.I) {
+            const uint16_t* p = a.gate_up + (size_t)(g.row + c0 + r) * a.I + ch;
+            next_gate[i] = __ldg(reinterpret_cast<const uint4*>(p));
+            next_up[i] = __ldg(reinterpret_cast<const uint4*>(p + (size_t)a.n_rows * a.I));
+          }
+        }
+      };
+      if constexpr (MODE == kGradAct) fetch(0);
+      if (g.pieces && ok) {
+        // a whole tile long: more polls for more of k
+        ok = !aborted() && wait(acc_full + (acc & 1), (acc >> 1) & 1, kPolls + (unsigned)min(g.pieces, 1 << 20) * 1024u);
         fence_after();
       }
       const uint32_t col = tmem + lanes + (uint32_t)(acc & 1) * kTile;
-      for (int c0 = 0; c0 < g.n; c0 += 32) {
-        float v[32];
-        if (g.steps && ok) {
-          tmem_ld32(col + c0, v);
+      for (int c0 = 0; c0 < g.n; c0 += kCols) {
+        float lo[kFrag], hi[kFrag];                      // lanes 0-15 and 16-31 of the warp's quarter
+        if (g.pieces && ok) {
+          tmem_fragments(col + c0, lo);
+          tmem_fragments(col + c0 + (16u << 16), hi);
+          ld_wait();
         } else {
 #pragma unroll
-          for (int c = 0; c < 32; ++c) v[c] = ok ? 0.f : __uint_as_float(0x7fc00000u);
+          for (int i = 0; i < kFrag; ++i) lo[i] = hi[i] = ok ? 0.f : __uint_as_float(0x7fc00000u);
+        }
+        if (g.pieces && c0 + kCols >= g.n) {             // read out: the buffer is free for the products
+          fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_at(in_even_cta(acc_empty + (acc & 1)));
         }
         if constexpr (MODE == kGateUp) {
-          // even lanes hold gates, odd lanes ups of the same channel: one exchange gives each of them both of every other row
-          const int ch = g.m0 + cta * 64 + quad * 16 + (lane >> 1), odd = lane & 1;
+          // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels: 128 bytes.
+          const int rows_kept = a.kept ? 3 : 1;
 #pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const float got = __shfl_xor_sync(0xffffffffu, odd ? v[c] : v[c + 1], 1);
-            const float gate = odd ? got : v[c], up = odd ? v[c + 1] : got;
-            const int r = c0 + c + odd;
-            if (r < g.n && ch < a.I) {
-              const size_t at = (size_t)(g.row + r) * a.I + ch;
-              a.out[at] = bits<T>(gate * sigmoid(gate) * up);
-              if (a.kept) {
-                a.kept[at] = bits<T>(gate);
-                a.kept[at + (size_t)a.n_rows * a.I] = bits<T>(up);
-              }
+          for (int i = 0; i < 4; i += 2) {
+            uint32_t v[3][4];                            // act, gate, up of two groups of columns x two of channels
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float* f = (j & 1 ? hi : lo) + 4 * (i + (j >> 1));
+              v[0][j] = pack<T>(f[0] * sigmoid(f[0]) * f[2], f[1] * sigmoid(f[1]) * f[3]);
+              v[1][j] = pack<T>(f[0], f[1]);
+              v[2][j] = pack<T>(f[2], f[3]);
+            }
+            const int row = (i + (lane >> 4)) * 8 + (lane & 7), chunk = quad * 2 + ((lane >> 3) & 1);
+            const uint32_t to = stage_at + row * 128 + ((chunk ^ (row & 7)) << 4);
+            store_turned(to, v[0][0], v[0][1], v[0][2], v[0][3]);
+            if (a.kept) {
+              store_turned(to + 4096, v[1][0], v[1][1], v[1][2], v[1][3]);
+              store_turned(to + 8192, v[2][0], v[2][1], v[2][2], v[2][3]);
             }
           }
+          epilogue_bar();
+          for (int o = 0; o < rows_kept; ++o) {
+            uint16_t* out = o == 0 ? a.out : a.kept + (size_t)(o - 1) * a.n_rows * a.I;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int row = (i * 128 + t) >> 3, chunk = t & 7, ch = g.m0 + cta * 64 + chunk * 8;
+              if (c0 + row < g.n && ch < a.I)
+                *reinterpret_cast<uint4*>(out + (size_t)(g.row + c0 + row) * a.I + ch) =
+                    *reinterpret_cast<const uint4*>(staging + o * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
+            }
+          }
+          epilogue_bar();
+        } else if constexpr (MODE == kGradAct) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = (i * 128 + t) >> 4, to = row * 256 + (((t & 15) ^ (row & 7)) << 4);
+            *reinterpret_cast<uint4*>(staging + to) = next_gate[i];
+            *reinterpret_cast<uint4*>(staging + 4096 + to) = next_up[i];
+          }
+          if (c0 + kCols < g.n) fetch(c0 + kCols);
+          epilogue_bar();
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = i * 8 + (lane & 7), chunk = quad * 4 + (lane >> 3);
+            const uint32_t at = stage_at + row * 256 + ((chunk ^ (row & 7)) << 4);
+            uint32_t gates[4], ups[4], acts[4];
+            load_turned(at, gates);
+            load_turned(at + 4096, ups);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float* f = (j & 2 ? hi : lo) + 4 * i + 2 * (j & 1);
+              const float2 gate = unpack<T>(gates[j]), up = unpack<T>(ups[j]);
+              const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
+              gates[j] = pack<T>(f[0] * up.x * s0 * (1.f + gate.x * (1.f - s0)), f[1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
+              ups[j] = pack<T>(f[0] * gate.x * s0, f[1] * gate.y * s1);
+              acts[j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
+            }
+            store_turned(at, gates[0], gates[1], gates[2], gates[3]);
+            store_turned(at + 4096, ups[0], ups[1], ups[2], ups[3]);
+            store_turned(at + 8192, acts[0], acts[1], acts[2], acts[3]);
+          }
+          epilogue_bar();
+#pragma unroll
+          for (int o = 0; o < 3; ++o)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int row = (i * 128 + t) >> 4, chunk = t & 15, ch = g.m0 + cta * 128 + chunk * 8;
+              if (c0 + row < g.n && ch < a.I)
+                *reinterpret_cast<uint4*>(a.out + ((size_t)o * a.n_rows + g.row + c0 + row) * a.I + ch) =
+                    *reinterpret_cast<const uint4*>(staging + o * 4096 + row * 256 + ((chunk ^ (row & 7)) << 4));
+            }
+          epilogue_bar();
         } else {
-          const int m = g.m0 + cta * 128 + quad * 32 + lane;
-          if (m < (MODE == kGradAct ? a.I : a.H)) {
-            if constexpr (MODE == kGradAct) {
-              const size_t plane = (size_t)a.n_rows * a.I;
+          // output rows of 128 values: 256 bytes; two buffers, so that one barrier is enough
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (c0 + c < g.n) {
-                  const size_t at = (size_t)(g.row + c0 + c) * a.I + m;
-                  const float gate = value<T>(__ldg(a.gate_up + at)), up = value<T>(__ldg(a.gate_up + at + plane)), s = sigmoid(gate);
-                  a.out[at] = bits<T>(v[c] * up * s * (1.f + gate * (1.f - s)));
-                  a.out[at + plane] = bits<T>(v[c] * gate * s);
-                  a.out[at + 2 * plane] = bits<T>(gate * s * up);
-                }
-            } else if constexpr (MODE == kGradBlocks) {
-              uint16_t* out = a.out + (size_t)g.e * a.out_stride + (size_t)g.plane * a.H + m;
+          for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + (lane & 7), chunk = quad * 4 + (lane >> 3);
+            store_turned(stage_at + buffer * 8192 + row * 256 + ((chunk ^ (row & 7)) << 4), pack<T>(lo[4 * i], lo[4 * i + 1]),
+                         pack<T>(lo[4 * i + 2], lo[4 * i + 3]), pack<T>(hi[4 * i], hi[4 * i + 1]), pack<T>(hi[4 * i + 2], hi[4 * i + 3]));
+          }
+          epilogue_bar();
+          const int chunk = t & 15, m = g.m0 + cta * 128 + chunk * 8;
+          if (m < a.H) {
 #pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (c0 + c < g.n) out[(size_t)(g.row + c0 + c) * 3 * a.H] = bits<T>(v[c]);
-            } else {
-#pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (c0 + c < g.n) a.out[(size_t)(g.row + c0 + c) * a.out_stride + m] = bits<T>(v[c]);
+            for (int i = 0; i < 4; ++i) {
+              const int row = (i * 128 + t) >> 4;
+              uint16_t* out = MODE == kGradBlocks ? a.out + (size_t)g.e * a.out_stride + ((size_t)(g.row + c0 + row) * 3 + g.plane) * a.H + m
+                                                  : a.out + (size_t)(g.row + c0 + row) * a.out_stride + m;
+              if (c0 + row < g.n)
+                *reinterpret_cast<uint4*>(out) =
+                    *reinterpret_cast<const uint4*>(staging + buffer * 8192 + row * 256 + ((chunk ^ (row & 7)) << 4));
             }
           }
+          buffer ^= 1;
         }
       }
-      if (g.steps) {
-        fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_cluster(in_even_cta(acc_empty + (acc & 1)));
-        ++acc;
-      }
+      if (g.pieces) ++acc;
     }
   }
   __syncwarp();
@@ -481,12 +618,19 @@ cudaError_t encoder(EncodeTiledFn* out) {
   return cudaSuccess;
 }
 
+struct FfnCall {
+  int32_t n_rows, n_experts, hidden, inter, dtype;
+  const void* offsets;
+  const void* blocks;
+  int64_t block_stride;
+};
+
 struct Encoder {
   EncodeTiledFn fn;
   CUtensorMapDataType type;
   bool ok;
   void encode(CUtensorMap* m, const void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
-    const cuuint32_t step[4] = {1, 1, 1, 1};
+    const cuuint32_t step[5] = {1, 1, 1, 1, 1};
     ok = ok && fn(m, type, rank, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   }
@@ -497,19 +641,31 @@ struct Encoder {
     const cuuint32_t box[3] = {64, box_rows, 1};
     encode(m, p, 3, dims, strides, box);
   }
-  // expert blocks; boxes of 64 columns of `kinds` planes of `channels` channels
-  void blocks(CUtensorMap* m, const void* p, int n_experts, int H, int I, int64_t block_stride, unsigned kinds, unsigned channels) {
-    const cuuint64_t dims[4] = {(cuuint64_t)H, 3, (cuuint64_t)I, (cuuint64_t)n_experts};
-    const cuuint64_t strides[3] = {(cuuint64_t)H * 2, (cuuint64_t)H * 6, (cuuint64_t)block_stride * 2};
-    const cuuint32_t box[4] = {64, kinds, channels, 1};
-    encode(m, p, 4, dims, strides, box);
+  // expert blocks; boxes of 64 columns of one plane of `channels` channels
+  void blocks(CUtensorMap* m, const FfnCall& c, unsigned channels) {
+    const cuuint64_t dims[4] = {(cuuint64_t)c.hidden, 3, (cuuint64_t)c.inter, (cuuint64_t)c.n_experts};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.hidden * 2, (cuuint64_t)c.hidden * 6, (cuuint64_t)c.block_stride * 2};
+    const cuuint32_t box[4] = {64, 1, channels, 1};
+    encode(m, c.blocks, 4, dims, strides, box);
+  }
+  // the same with eight channels of a plane, then those of the next, as neighbours: boxes of 64 columns of gate and up of 64 channels
+  void blocks_by_eight(CUtensorMap* m, const FfnCall& c) {
+    const cuuint64_t dims[5] = {(cuuint64_t)c.hidden, 8, 3, (cuuint64_t)c.inter / 8, (cuuint64_t)c.n_experts};
+    const cuuint64_t strides[4] = {(cuuint64_t)c.hidden * 6, (cuuint64_t)c.hidden * 2, (cuuint64_t)c.hidden * 48, (cuuint64_t)c.block_stride * 2};
+    const cuuint32_t box[5] = {64, 8, 2, 8, 1};
+    encode(m, c.blocks, 5, dims, strides, box);
+  }
+  // the rows of N
+  void n_rows(ProductArgs* a, const void* p, int64_t n, int64_t columns, int64_t stride, int planes) {
+    for (int b = 0; b < kBoxes; ++b) matrix(&a->n[b], p, n, columns, stride, planes, box_rows(b));
   }
 };
 
 template <int MODE, typename T>
 cudaError_t launch_product(const ProductArgs& a, cudaStream_t stream) {
-  const size_t smem = 1024 + (size_t)kStages * kStageBytes + 256 + (size_t)(3 * a.n_experts + 1) * 4;
-  constexpr size_t kMost = 1024 + (size_t)kStages * kStageBytes + 256 + (size_t)(3 * REMOE_SORT_MAX_EXPERTS + 1) * 4;
+  constexpr size_t kFixed = 1024 + (size_t)kStages * kStageBytes + kStagingBytes + 256;
+  constexpr size_t kMost = kFixed + (size_t)(3 * REMOE_SORT_MAX_EXPERTS + 1) * 4;
+  const size_t smem = kFixed + (size_t)(3 * a.n_experts + 1) * 4;
   static_assert(kMost <= 227 * 1024, "shared memory of a CTA");
   static std::atomic<bool> ready[kMaxDevices];
   const cudaError_t e = allow_dynamic_smem(product_kernel<MODE, T>, kMost, ready);
@@ -527,13 +683,6 @@ cudaError_t launch_product(const ProductArgs& a, cudaStream_t stream) {
   cfg.stream = stream;
   return cudaLaunchKernelEx(&cfg, product_kernel<MODE, T>, a);
 }
-
-struct FfnCall {
-  int32_t n_rows, n_experts, hidden, inter, dtype;
-  const void* offsets;
-  const void* blocks;
-  int64_t block_stride;
-};
 
 int check_ffn(const FfnCall& c) {
   if (c.n_rows < 0 || c.n_experts < 1 || c.hidden < 1 || c.inter < 1) return REMOE_E_ARG;
@@ -558,16 +707,15 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   ProductArgs a{};
   a.offsets = static_cast<const int*>(c.offsets);
   a.n_experts = c.n_experts; a.n_rows = c.n_rows; a.H = c.hidden; a.I = c.inter;
-  constexpr unsigned kBox[3] = {16, 64, 128};
-  enc.blocks(&a.m[0], c.blocks, c.n_experts, c.hidden, c.inter, c.block_stride, 2, 64);
-  for (int b = 0; b < 3; ++b) enc.matrix(&a.n[b], xs, c.n_rows, c.hidden, xs_stride, 1, kBox[b]);
+  enc.blocks_by_eight(&a.m[0], c);
+  enc.n_rows(&a, xs, c.n_rows, c.hidden, xs_stride, 1);
   a.out = static_cast<uint16_t*>(act);
   a.kept = static_cast<uint16_t*>(gate_up);
   if (!enc.ok) return cudaErrorInvalidValue;
   cudaError_t e = launch_product<kGateUp, T>(a, stream);
   if (e != cudaSuccess) return e;
-  enc.blocks(&a.m[0], c.blocks, c.n_experts, c.hidden, c.inter, c.block_stride, 1, 64);
-  for (int b = 0; b < 3; ++b) enc.matrix(&a.n[b], act, c.n_rows, c.inter, c.inter, 1, kBox[b]);
+  enc.blocks(&a.m[0], c, 64);
+  enc.n_rows(&a, act, c.n_rows, c.inter, c.inter, 1);
   a.out = static_cast<uint16_t*>(ys);
   a.out_stride = ys_stride;
   if (!enc.ok) return cudaErrorInvalidValue;
@@ -580,11 +728,10 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
   ProductArgs a{};
   a.offsets = static_cast<const int*>(c.offsets);
   a.n_experts = c.n_experts; a.n_rows = c.n_rows; a.H = c.hidden; a.I = c.inter;
-  constexpr unsigned kBox[3] = {16, 64, 128};
   cudaError_t e = cudaSuccess;
   if (c.n_rows > 0) {
-    enc.blocks(&a.m[0], c.blocks, c.n_experts, c.hidden, c.inter, c.block_stride, 1, 128);
-    for (int b = 0; b < 3; ++b) enc.matrix(&a.n[b], d_ys, c.n_rows, c.hidden, d_ys_stride, 1, kBox[b]);
+    enc.blocks(&a.m[0], c, 128);
+    enc.n_rows(&a, d_ys, c.n_rows, c.hidden, d_ys_stride, 1);
     a.gate_up = static_cast<const uint16_t*>(gate_up);
     a.out = static_cast<uint16_t*>(work);
     if (!enc.ok) return cudaErrorInvalidValue;
@@ -592,8 +739,8 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
     if (e != cudaSuccess) return e;
   }
   if (d_xs && c.n_rows > 0) {
-    enc.blocks(&a.m[0], c.blocks, c.n_experts, c.hidden, c.inter, c.block_stride, 1, 64);
-    for (int b = 0; b < 3; ++b) enc.matrix(&a.n[b], work, c.n_rows, c.inter, c.inter, 2, kBox[b]);
+    enc.blocks(&a.m[0], c, 64);
+    enc.n_rows(&a, work, c.n_rows, c.inter, c.inter, 2);
     a.out = static_cast<uint16_t*>(d_xs);
     a.out_stride = d_xs_stride;
     if (!enc.ok) return cudaErrorInvalidValue;
