@@ -11,12 +11,13 @@
 //   kGradBlocks  m = hidden,  n = channel, k = row:   d W = (d g)^T xs, (d u)^T xs, act^T d_ys, one plane of a block each
 // Operands come through tensor maps straight from where the caller keeps them: K-major tiles (k contiguous) are [128 rows x 64],
 // MN-major ones two [64 x 64] boxes with k as the rows; both are the 128-byte-swizzled images the tensor cores read.
-// Per CTA: warp 0 loads (TMA, a ring of three stages of 128 k, 64 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 read the
+// Per CTA: warp 0 loads (TMA, a ring of stages of 64 k, 32 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 read the
 // results out of TMEM (two buffers of 256 columns, so that a tile's epilogue runs behind the next tile's products).  With k = row
 // (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
 // written) would enter the sums, so warp 2 stands between the copies and the products and clears it in both operands.
-// The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans), so
-// that rows leave in 16-byte accesses, 256 bytes of a row side by side.
+// The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
+// leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
+// since a copy would run over the next expert's first rows.  kGradAct's kept gates and ups come in the same way they leave, by warp 3.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -34,13 +35,9 @@ using namespace ring;
 enum Mode { kGateUp, kDown, kGradAct, kGradRows, kGradBlocks };
 
 constexpr int kTile = 256;                               // rows of M and most rows of N of a pair's tile
-constexpr int kK = 64;                                   // k of a piece: 128 bytes
-constexpr int kPieces = 2;                               // pieces of a stage: each thread's chain of wait, issue and commit runs once a stage
-constexpr int kOperandBytes = 128 * 128;                 // a CTA's half of an operand's piece
-constexpr int kPieceBytes = 2 * kOperandBytes;
-constexpr int kStageBytes = kPieces * kPieceBytes;
-constexpr int kStages = 3;
-constexpr int kStagingBytes = 16384;                     // of the epilogue
+constexpr int kK = 64;                                   // k of a stage: 128 bytes
+constexpr int kOperandBytes = 128 * 128;                 // a CTA's half of an operand's stage
+constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kThreads = 256;
 constexpr uint32_t kTmemCols = 512;
 constexpr unsigned kPolls = 1u << 18;                    // of a bounded wait
@@ -48,12 +45,26 @@ constexpr int kBoxes = 5;
 // Rows of N in one copy: 16, 32, 64, 96, 128.
 __host__ __device__ constexpr int box_rows(int b) { return b == 0 ? 16 : b == 1 ? 32 : 32 * b; }
 
+// Shared memory: ring, then the epilogue's buffers of kCols columns of the result.
+template <int MODE>
+struct Shape {
+  static constexpr int kStages = MODE == kGradAct ? 5 : 6;
+  static constexpr int kCols = MODE == kGradAct ? 16 : 32;
+  static constexpr int kBuffer = MODE == kGateUp ? 4096 : MODE == kGradAct ? 12288 : 8192;  // kGateUp: one of three outputs; kGradAct: all three
+  static constexpr int kBuffers = MODE == kGateUp || MODE == kGradAct ? 4 : 2;
+  static constexpr int kBarriers = 3 * kStages + 2 + 2 + 1 + 2 * 4;
+  static constexpr size_t kFixed = 1024 + (size_t)kStages * kStageBytes + kBuffers * kBuffer + 8 * kBarriers + 8;
+  static constexpr size_t smem(int n_experts) { return kFixed + (size_t)(3 * n_experts + 1) * 4; }
+  static_assert(smem(REMOE_SORT_MAX_EXPERTS) <= 227 * 1024, "shared memory of a CTA");
+};
+
 struct ProductArgs {
   CUtensorMap m[2];                                      // M: blocks; kGradBlocks: xs, d_ys
   CUtensorMap n[kBoxes];                                 // N: boxes of box_rows; kGradBlocks: n[0], boxes of 64
   const int* offsets;
   int n_experts, n_rows, H, I;
-  const uint16_t* gate_up;                               // kGradAct: [2, n_rows, I]
+  CUtensorMap gate_up;                                   // kGradAct: [2, n_rows, I], boxes of 16 rows
+  CUtensorMap o[2];                                      // outputs (kGateUp: act, the kept gates and ups), boxes of kCols rows
   uint16_t* out;                                         // rows or blocks; kGateUp, kGradAct: [.., n_rows, I]
   uint16_t* kept;                                        // kGateUp: [2, n_rows, I] or null
   int64_t out_stride;                                    // elements between rows (blocks)
@@ -64,6 +75,15 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+// One lane of a converged warp.  The roles that issue copies and products run with whole warps and take a lane only around the instructions
+// themselves: their operands then lie in uniform registers, as the instructions want them.  (With the loop itself in one lane an
+// MMA took 67 cycles to issue and a commit 150, more than the 512 that a stage's products run for.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -100,15 +120,14 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, in
       : "memory");
 }
 // Shared-memory matrix descriptor, 128-byte swizzle (see ffn_batched_tc.cu).
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  return (uint64_t)((addr >> 4) & 0x3fffu) | ((uint64_t)((lbo_bytes >> 4) & 0x3fffu) << 16) |
-         ((uint64_t)((sbo_bytes >> 4) & 0x3fffu) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-__device__ __forceinline__ void mma_pair(uint32_t tmem_d, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ constexpr uint32_t desc_lo(uint32_t addr, uint32_t lbo_bytes) { return (addr >> 4) | (lbo_bytes >> 4 << 16); }
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);     // eight rows of 128 bytes apart
+__device__ __forceinline__ void mma_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                         uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-      "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n\t}" ::"r"(tmem_d),
+      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // Arrives on the barrier of both CTAs once every product issued so far by this thread has completed.
@@ -146,6 +165,18 @@ __device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
                : "r"(addr)
                : "memory");
 }
+// Stores of shared memory as boxes of rows; what lies outside the tensor is left out.
+__device__ __forceinline__ void store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
+}
+__device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void epilogue_bar() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
@@ -169,12 +200,16 @@ __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f +
 
 // One tile of a pair.
 struct Tile {
-  int e, row, n;                                         // expert; first row (kGradBlocks: channel) and number of them
-  int half;                                              // rows of N in each CTA, a multiple of 16
-  int m0;                                                // first row of M (kGateUp: channel)
-  int plane;                                             // kGradBlocks: plane of the block
-  int first_row, count;                                  // kGradBlocks: the expert's rows
-  int pieces;                                            // of k
+  int e = 0, row = 0, n = 0;                                         // expert; first row (kGradBlocks: channel) and number of them
+  int half = 0;                                          // rows of N in each CTA, a multiple of 16
+  int m0 = 0;                                            // first row of M (kGateUp: channel)
+  int plane = 0;                                         // kGradBlocks: plane of the block
+  int first_row = 0, count = 0;                          // kGradBlocks: the expert's rows
+  int pieces = 0;                                        // of k
+  __device__ __forceinline__ void make_uniform() {
+    e = uniform(e); row = uniform(row); n = uniform(n); half = uniform(half); m0 = uniform(m0);
+    plane = uniform(plane); first_row = uniform(first_row); count = uniform(count); pieces = uniform(pieces);
+  }
 };
 
 // The tiles of a launch in the order of experts, dealt to the pairs in turn.  Each role of a CTA walks them by itself.
@@ -224,29 +259,34 @@ struct Walk {
   }
 };
 
-// A place in the ring and the parity of its present use.
+// A place in a ring and the parity of its present use.
+template <int N>
 struct Place {
   int s = 0;
   uint32_t turn = 0;
   __device__ __forceinline__ void next() {
-    if (++s == kStages) { s = 0; turn ^= 1; }
+    if (++s == N) { s = 0; turn ^= 1; }
   }
 };
 
 template <int MODE, typename T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
+  using S = Shape<MODE>;
+  constexpr int kStages = S::kStages, kCols = S::kCols;
   constexpr bool kRagged = MODE == kGradBlocks;          // k ends inside a stage
   constexpr bool kMMajor = MODE == kDown || MODE == kGradRows || MODE == kGradBlocks, kNMajor = MODE == kGradBlocks;
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* staging = smem + (size_t)kStages * kStageBytes;
-  uint64_t* full = reinterpret_cast<uint64_t*>(staging + kStagingBytes);   // even CTA: both halves of a stage are there
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + S::kBuffers * S::kBuffer);   // even CTA: both halves of a stage are there
   uint64_t* landed = full + kStages;                     // kRagged: this CTA's copies of a stage have landed
   uint64_t* empty = landed + kStages;                    // a stage has been read
   uint64_t* acc_full = empty + kStages;                  // [2] a result is complete
   uint64_t* acc_empty = acc_full + 2;                    // [2] even CTA: it has been read out by both
   uint64_t* drain = acc_empty + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+  uint64_t* kept_full = drain + 1;                       // [4] kGradAct: kept gates and ups are there
+  uint64_t* kept_empty = kept_full + 4;                  // [4] what replaced them has left
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(kept_empty + 4);
   int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
   int* first = abort_flag + 1;                           // [N]
   int* count = first + a.n_experts;                      // [N]
@@ -263,6 +303,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     }
     for (int b = 0; b < 2; ++b) { mbar_init(acc_full + b, 1); mbar_init(acc_empty + b, 8); }
     mbar_init(drain, 1);
+    for (int b = 0; b < 4; ++b) { mbar_init(kept_full + b, 1); mbar_init(kept_empty + b, 1); }
     mbar_fence_init();
   }
   if (warp == 2) {
@@ -301,292 +342,357 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     return false;
   };
 
+  auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+
   Walk<MODE> walk(a, first, count, upto);
   Tile g;
   if (warp == 0) {
     // ------------------------------------------------------------------------------------------------ copies
-    if (lane == 0) {
-      Place at;
-      int64_t stages = 0;                                // issued
-      bool ok = true;
-      while (ok && !aborted() && walk.next(g)) {
-        int box = 0;
-        if constexpr (kRagged) box = g.half > 64 ? 2 : 1;            // copies of 64 channels
-        else while (box_rows(box) < g.half) ++box;
-        const uint32_t bytes = kOperandBytes + (kRagged ? box * 8192u : box_rows(box) * 128u);
-        const CUtensorMap* n_map = kRagged ? &a.n[0] : &a.n[box];
-        const int n_row = g.row + cta * g.half;
-        for (int p0 = 0; p0 < g.pieces; p0 += kPieces) {
-          if (stages >= kStages) {
-            ok = wait(empty + at.s, at.turn ^ 1);
-            if (!ok) break;
-          }
-          const int here = min(kPieces, g.pieces - p0);
-          uint32_t bar;
-          if constexpr (kRagged) {
-            mbar_expect_tx(landed + at.s, here * bytes);
-            bar = smem_u32(landed + at.s);
-          } else {
-            if (cta == 0) mbar_expect_tx(full + at.s, 2 * here * bytes);
-            bar = in_even_cta(full + at.s);
-          }
-          for (int p = p0; p < p0 + here; ++p) {
-            const uint32_t m_dst = smem_u32(smem) + at.s * kStageBytes + (p - p0) * kPieceBytes, n_dst = m_dst + kOperandBytes;
-            if constexpr (MODE == kGateUp) {
-              load_5d(m_dst, &a.m[0], p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
-              load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
-            } else if constexpr (MODE == kGradAct) {
-              load_4d(m_dst, &a.m[0], p * kK, 2, g.m0 + cta * 128, g.e, bar);
-              load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
-            } else if constexpr (MODE == kDown || MODE == kGradRows) {
-              const int per = MODE == kDown ? g.pieces : g.pieces / 2;
-              const int j = p >= per, k0 = (p - j * per) * kK;
-              const int plane = MODE == kDown ? 2 : j;
-              load_4d(m_dst, &a.m[0], g.m0 + cta * 128, plane, k0, g.e, bar);
-              load_4d(m_dst + 8192, &a.m[0], g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
-              load_3d(n_dst, n_map, k0, n_row, j, bar);
-            } else {
-              const int row = g.first_row + p * kK;
-              const CUtensorMap* m = &a.m[g.plane == 2];
-              load_3d(m_dst, m, g.m0 + cta * 128, row, 0, bar);
-              load_3d(m_dst + 8192, m, g.m0 + cta * 128 + 64, row, 0, bar);
-              load_3d(n_dst, n_map, n_row, row, g.plane, bar);
-              if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, g.plane, bar);
-            }
-          }
-          at.next();
-          ++stages;
+    Place<kStages> at;
+    int64_t stages = 0;                                  // issued
+    bool ok = true;
+    const uint32_t ring = uniform((int)smem_u32(smem)), bars = uniform((int)(kRagged ? smem_u32(landed) : in_even_cta(full)));
+    while (ok && !uniform(aborted()) && uniform(walk.next(g))) {
+      g.make_uniform();
+      int box = 0;
+      if constexpr (kRagged) box = g.half > 64 ? 2 : 1;  // copies of 64 channels
+      else while (box_rows(box) < g.half) ++box;
+      const uint32_t bytes = kOperandBytes + (kRagged ? box * 8192u : box_rows(box) * 128u);
+      const CUtensorMap* n_map = kRagged ? &a.n[0] : &a.n[box];
+      const int n_row = g.row + cta * g.half;
+      for (int p = 0; p < g.pieces; ++p) {
+        if (stages >= kStages) {
+          ok = warp_wait(empty + at.s, at.turn ^ 1);
+          if (!ok) break;
         }
+        if (elect_one()) {
+          if constexpr (kRagged) mbar_expect_tx(landed + at.s, bytes);
+          else if (cta == 0) mbar_expect_tx(full + at.s, 2 * bytes);
+          const uint32_t m_dst = ring + at.s * kStageBytes, n_dst = m_dst + kOperandBytes, bar = bars + at.s * 8;
+          if constexpr (MODE == kGateUp) {
+            load_5d(m_dst, &a.m[0], p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
+            load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
+          } else if constexpr (MODE == kGradAct) {
+            load_4d(m_dst, &a.m[0], p * kK, 2, g.m0 + cta * 128, g.e, bar);
+            load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
+          } else if constexpr (MODE == kDown || MODE == kGradRows) {
+            const int per = MODE == kDown ? g.pieces : g.pieces / 2;
+            const int j = p >= per, k0 = (p - j * per) * kK;
+            const int plane = MODE == kDown ? 2 : j;
+            load_4d(m_dst, &a.m[0], g.m0 + cta * 128, plane, k0, g.e, bar);
+            load_4d(m_dst + 8192, &a.m[0], g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
+            load_3d(n_dst, n_map, k0, n_row, j, bar);
+          } else {
+            const int row = g.first_row + p * kK;
+            const CUtensorMap* m = &a.m[g.plane == 2];
+            load_3d(m_dst, m, g.m0 + cta * 128, row, 0, bar);
+            load_3d(m_dst + 8192, m, g.m0 + cta * 128 + 64, row, 0, bar);
+            load_3d(n_dst, n_map, n_row, row, g.plane, bar);
+            if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, g.plane, bar);
+          }
+        }
+        __syncwarp();
+        at.next();
+        ++stages;
       }
-      // The last products have read their stages and their arrivals have come in before the CTA leaves; after a wait that ran out, the
-      // copies under way are waited for instead.
-      Place back;
-      for (int64_t i = stages > kStages ? stages - kStages : 0; i < stages; ++i) {
-        back.s = (int)(i % kStages);
-        back.turn = (uint32_t)(i / kStages) & 1;
-        if (ok) wait(empty + back.s, back.turn);
-        else wait((kRagged ? landed : full) + back.s, back.turn);
-      }
+    }
+    // The last products have read their stages and their arrivals have come in before the CTA leaves; after a wait that ran out, the
+    // copies under way are waited for instead.
+    for (int64_t i = stages > kStages ? stages - kStages : 0; i < stages; ++i) {
+      const int s = (int)(i % kStages);
+      const uint32_t turn = (uint32_t)(i / kStages) & 1;
+      if (ok) wait(empty + s, turn);
+      else wait((kRagged ? landed : full) + s, turn);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------------------------------------ products
-    if (lane == 0 && cta == 0) {
+    if (cta == 0) {
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       // fp32 result, both operands of type T, M = 256; bit 15: M is MN-major, bit 16: N is
       constexpr uint32_t kIdesc = (1u << 4) | (kType << 7) | (kType << 10) | ((256u >> 4) << 24) | (kMMajor ? 1u << 15 : 0u) | (kNMajor ? 1u << 16 : 0u);
-      // of the ring's first piece; a step of 16 k further: 32 bytes (K-major) or 16 rows of 128
-      const uint64_t m_desc = kMMajor ? operand_desc(smem_u32(smem), 8192, 1024) : operand_desc(smem_u32(smem), 16, 1024);
-      const uint64_t n_desc = kNMajor ? operand_desc(smem_u32(smem) + kOperandBytes, 8192, 1024) : operand_desc(smem_u32(smem) + kOperandBytes, 16, 1024);
+      // of the ring's first stage; a step of 16 k further: 32 bytes (K-major) or 16 rows of 128
+      const uint32_t ring = uniform((int)smem_u32(smem)), d0 = uniform((int)tmem);
+      const uint32_t m_desc = desc_lo(ring, kMMajor ? 8192 : 16), n_desc = desc_lo(ring + kOperandBytes, kNMajor ? 8192 : 16);
       constexpr uint32_t kMStep = (kMMajor ? 2048 : 32) >> 4, kNStep = (kNMajor ? 2048 : 32) >> 4;
-      Place at;
+      Place<kStages> at;
       int acc = 0;
       bool ok = true;
-      while (!aborted() && walk.next(g)) {
+      while (!uniform(aborted()) && uniform(walk.next(g))) {
+        g.make_uniform();
         if (g.pieces == 0) continue;
-        if (acc >= 2) ok = wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
+        if (acc >= 2) ok = warp_wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
         if (!ok) break;
         fence_after();
-        const uint32_t d = tmem + (uint32_t)(acc & 1) * kTile, idesc = kIdesc | ((uint32_t)(2 * g.half) >> 3 << 17);
-        for (int p0 = 0; p0 < g.pieces; p0 += kPieces) {
-          ok = wait(full + at.s, at.turn);
+        const uint32_t d = d0 + (uint32_t)(acc & 1) * kTile, idesc = kIdesc | ((uint32_t)(2 * g.half) >> 3 << 17);
+        for (int p = 0; p < g.pieces; ++p) {
+          ok = warp_wait(full + at.s, at.turn);
           if (!ok) break;
           // (what warp 2 of either CTA has cleared)
-          if (kRagged && p0 + kPieces >= g.pieces) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          if (kRagged && p + 1 == g.pieces) asm volatile("fence.acq_rel.cluster;" ::: "memory");
           fence_after();
-          const uint32_t stage = (uint32_t)(at.s * kStageBytes) >> 4;
+          if (elect_one()) {
+            const uint32_t stage = (uint32_t)(at.s * kStageBytes) >> 4;
 #pragma unroll
-          for (int q = 0; q < kPieces; ++q) {
-            if (p0 + q >= g.pieces) break;
-            const uint64_t dm = m_desc + stage + q * (kPieceBytes >> 4), dn = n_desc + stage + q * (kPieceBytes >> 4);
-#pragma unroll
-            for (int k = 0; k < kK / 16; ++k) mma_pair(d, dm + k * kMStep, dn + k * kNStep, idesc, (p0 | q | k) ? 1u : 0u);
+            for (int k = 0; k < kK / 16; ++k)
+              mma_pair(d, m_desc + stage + k * kMStep, kDescHi, n_desc + stage + k * kNStep, kDescHi, idesc, (p | k) ? 1u : 0u);
+            commit_pair(empty + at.s);
+            if (p + 1 == g.pieces) commit_pair(acc_full + (acc & 1));
           }
-          commit_pair(empty + at.s);
+          __syncwarp();
           at.next();
         }
         if (!ok) break;
-        commit_pair(acc_full + (acc & 1));
         ++acc;
       }
       if (!ok) {
-        commit_pair(drain);                              // let the tensor cores finish before TMEM is freed
+        if (elect_one()) commit_pair(drain);             // let the tensor cores finish before TMEM is freed
         mbar_wait(drain, 0, kPolls);
       }
     }
   } else if (warp == 2) {
     // ------------------------------------------------------------------------------- rows behind an expert's last
     if constexpr (kRagged) {
-      Place at;
+      Place<kStages> at;
       bool ok = true;
       while (ok && !aborted() && walk.next(g)) {
         const int chunks = g.half > 64 ? 4 : 3;          // of 64 rows of k, two of M and those of N
-        for (int p0 = 0; p0 < g.pieces; p0 += kPieces) {
+        for (int p = 0; p < g.pieces; ++p) {
           ok = wait(landed + at.s, at.turn);
           if (!ok) break;
-          const int p = g.pieces - 1, left = g.count - p * kK;       // rows of the expert's last piece
-          const bool clear = p < p0 + kPieces && left < kK;
-          if (clear) {
-            unsigned char* st = smem + (size_t)at.s * kStageBytes + (size_t)(p - p0) * kPieceBytes;
+          const int left = g.count - p * kK;             // the expert's rows from this stage on
+          if (left < kK) {
+            unsigned char* st = smem + (size_t)at.s * kStageBytes;
             for (int i = lane; i < chunks * (kK - left) * 8; i += 32) {
               const int line = i >> 3, c = line / (kK - left), r = left + line % (kK - left);
               *reinterpret_cast<uint4*>(st + c * 8192 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            async_fence();
           }
           __syncwarp();
           if (lane == 0) {
-            if (clear) arrive_release_cluster(in_even_cta(full + at.s));
+            if (left < kK) arrive_release_cluster(in_even_cta(full + at.s));
             else arrive_at(in_even_cta(full + at.s));
           }
           at.next();
         }
       }
     }
-  } else if (warp >= 4) {
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------------------------ kept gates and ups, 16 rows a time
+    if constexpr (MODE == kGradAct) {
+      if (lane == 0) {
+        Place<4> at;
+        int64_t groups = 0;
+        bool ok = true;
+        while (ok && !aborted() && walk.next(g)) {
+          const int ch = g.m0 + cta * 128;
+          for (int c0 = 0; c0 < g.n; c0 += kCols) {
+            if (groups >= 4) {
+              ok = wait(kept_empty + at.s, at.turn ^ 1);
+              if (!ok) break;
+            }
+            const uint32_t to = smem_u32(staging) + at.s * S::kBuffer, bar = smem_u32(kept_full + at.s);
+            mbar_expect_tx(kept_full + at.s, 8192);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_3d(to + i * 2048, &a.gate_up, ch + (i & 1) * 64, g.row + c0, i >> 1, bar);
+            at.next();
+            ++groups;
+          }
+        }
+        if (!ok)                                         // copies under way land before the CTA leaves
+          for (int64_t i = groups > 4 ? groups - 4 : 0; i < groups; ++i) wait(kept_full + (int)(i % 4), (uint32_t)(i / 4) & 1);
+      }
+    }
+  } else {
     // ------------------------------------------------------------------------------------------------ results
     const int quad = warp & 3, t = tid - 128;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    const uint32_t stage_at = smem_u32(staging);
-    constexpr int kCols = MODE == kGradAct ? 16 : 32;    // columns of the result (rows of the output) at a time
     constexpr int kFrag = kCols / 2;
-    int acc = 0, buffer = 0;
+    int acc = 0;
+    int64_t groups = 0;                                  // kGradAct: of columns, so far
+    Place<S::kBuffers> at;
     bool ok = true;
+    const bool keep = MODE == kGateUp && a.kept;
     while (walk.next(g)) {
-      // kGradAct: the kept gates and ups of the next columns, 16 rows x 128 channels of each, on their way behind the products
-      uint4 next_gate[2], next_up[2];
-      auto fetch = [&](int c0) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = (i * 128 + t) >> 4, ch = g.m0 + cta * 128 + (t & 15) * 8;
-          next_gate[i] = next_up[i] = make_uint4(0, 0, 0, 0);
-          if (c0 + r < g.n && ch < a.I) {
-            const uint16_t* p = a.gate_up + (size_t)(g.row + c0 + r) * a.I + ch;
-            next_gate[i] = __ldg(reinterpret_cast<const uint4*>(p));
-            next_up[i] = __ldg(reinterpret_cast<const uint4*>(p + (size_t)a.n_rows * a.I));
-          }
-        }
-      };
-      if constexpr (MODE == kGradAct) fetch(0);
       if (g.pieces && ok) {
         // a whole tile long: more polls for more of k
         ok = !aborted() && wait(acc_full + (acc & 1), (acc >> 1) & 1, kPolls + (unsigned)min(g.pieces, 1 << 20) * 1024u);
         fence_after();
       }
       const uint32_t col = tmem + lanes + (uint32_t)(acc & 1) * kTile;
-      for (int c0 = 0; c0 < g.n; c0 += kCols) {
-        float lo[kFrag], hi[kFrag];                      // lanes 0-15 and 16-31 of the warp's quarter
+      float lo[kFrag], hi[kFrag];                        // lanes 0-15 and 16-31 of the warp's quarter
+      auto fetch = [&](int c0) {
         if (g.pieces && ok) {
           tmem_fragments(col + c0, lo);
           tmem_fragments(col + c0 + (16u << 16), hi);
+        }
+      };
+      fetch(0);
+      for (int c0 = 0; c0 < g.n; c0 += kCols) {
+        if (g.pieces && ok) {
           ld_wait();
         } else {
 #pragma unroll
           for (int i = 0; i < kFrag; ++i) lo[i] = hi[i] = ok ? 0.f : __uint_as_float(0x7fc00000u);
         }
-        if (g.pieces && c0 + kCols >= g.n) {             // read out: the buffer is free for the products
-          fence_before();
-          __syncwarp();
-          if (lane == 0) arrive_at(in_even_cta(acc_empty + (acc & 1)));
-        }
+        const bool last = c0 + kCols >= g.n, whole = MODE == kGradBlocks || c0 + kCols <= g.n;
+        auto read_out = [&]() {                          // registers are free for the next columns, or TMEM for the products
+          if (!last) {
+            fetch(c0 + kCols);
+          } else if (g.pieces) {
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(in_even_cta(acc_empty + (acc & 1)));
+          }
+        };
+        unsigned char* buffer = staging + (keep ? 0 : at.s * S::kBuffer);
+        const uint32_t buffer_at = smem_u32(buffer);
         if constexpr (MODE == kGateUp) {
-          // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels: 128 bytes.
-          const int rows_kept = a.kept ? 3 : 1;
+          // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.
+          uint32_t v[3][8];                              // act, gate, up: groups of eight columns x two of channels
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float* f = (j & 1 ? hi : lo) + 4 * (j >> 1);
+            v[0][j] = pack<T>(f[0] * sigmoid(f[0]) * f[2], f[1] * sigmoid(f[1]) * f[3]);
+            v[1][j] = pack<T>(f[0], f[1]);
+            v[2][j] = pack<T>(f[2], f[3]);
+          }
+          read_out();
+          if (t == 0) {
+            if (keep) stores_read<0>();
+            else stores_read<S::kBuffers - 1>();
+          }
+          epilogue_bar();
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
-            uint32_t v[3][4];                            // act, gate, up of two groups of columns x two of channels
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float* f = (j & 1 ? hi : lo) + 4 * (i + (j >> 1));
-              v[0][j] = pack<T>(f[0] * sigmoid(f[0]) * f[2], f[1] * sigmoid(f[1]) * f[3]);
-              v[1][j] = pack<T>(f[0], f[1]);
-              v[2][j] = pack<T>(f[2], f[3]);
-            }
             const int row = (i + (lane >> 4)) * 8 + (lane & 7), chunk = quad * 2 + ((lane >> 3) & 1);
-            const uint32_t to = stage_at + row * 128 + ((chunk ^ (row & 7)) << 4);
-            store_turned(to, v[0][0], v[0][1], v[0][2], v[0][3]);
-            if (a.kept) {
-              store_turned(to + 4096, v[1][0], v[1][1], v[1][2], v[1][3]);
-              store_turned(to + 8192, v[2][0], v[2][1], v[2][2], v[2][3]);
-            }
-          }
-          epilogue_bar();
-          for (int o = 0; o < rows_kept; ++o) {
-            uint16_t* out = o == 0 ? a.out : a.kept + (size_t)(o - 1) * a.n_rows * a.I;
+            const uint32_t to = buffer_at + row * 128 + ((chunk ^ (row & 7)) << 4);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int row = (i * 128 + t) >> 3, chunk = t & 7, ch = g.m0 + cta * 64 + chunk * 8;
-              if (c0 + row < g.n && ch < a.I)
-                *reinterpret_cast<uint4*>(out + (size_t)(g.row + c0 + row) * a.I + ch) =
-                    *reinterpret_cast<const uint4*>(staging + o * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
+            for (int o = 0; o < 3; ++o)
+              if (o == 0 || keep) store_turned(to + o * 4096, v[o][2 * i], v[o][2 * i + 1], v[o][2 * i + 2], v[o][2 * i + 3]);
+          }
+          async_fence();
+          epilogue_bar();
+          const int ch = g.m0 + cta * 64;
+          if (whole) {
+            if (t == 0 && ch < a.I) {
+              store_3d(&a.o[0], buffer_at, ch, g.row + c0, 0);
+              if (keep) {
+                store_3d(&a.o[1], buffer_at + 4096, ch, g.row + c0, 0);
+                store_3d(&a.o[1], buffer_at + 8192, ch, g.row + c0, 1);
+              }
+            }
+          } else {
+            for (int o = 0; o < (keep ? 3 : 1); ++o) {
+              uint16_t* out = o == 0 ? a.out : a.kept + (size_t)(o - 1) * a.n_rows * a.I;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int row = (i * 128 + t) >> 3, chunk = t & 7;
+                if (c0 + row < g.n && ch + chunk * 8 < a.I)
+                  *reinterpret_cast<uint4*>(out + (size_t)(g.row + c0 + row) * a.I + ch + chunk * 8) =
+                      *reinterpret_cast<const uint4*>(buffer + o * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
+              }
             }
           }
-          epilogue_bar();
+          if (t == 0) store_commit();
         } else if constexpr (MODE == kGradAct) {
+          // gates and ups lie in two halves of 64 channels, [16 rows x 128 bytes] each; their gradients take their places
+          if (ok) ok = wait(kept_full + at.s, at.turn);
+          const int half = quad >> 1;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int row = (i * 128 + t) >> 4, to = row * 256 + (((t & 15) ^ (row & 7)) << 4);
-            *reinterpret_cast<uint4*>(staging + to) = next_gate[i];
-            *reinterpret_cast<uint4*>(staging + 4096 + to) = next_up[i];
-          }
-          if (c0 + kCols < g.n) fetch(c0 + kCols);
-          epilogue_bar();
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int row = i * 8 + (lane & 7), chunk = quad * 4 + (lane >> 3);
-            const uint32_t at = stage_at + row * 256 + ((chunk ^ (row & 7)) << 4);
+            const int row = i * 8 + (lane & 7), chunk = (quad & 1) * 4 + (lane >> 3);
+            const uint32_t to = buffer_at + half * 2048 + row * 128 + ((chunk ^ (row & 7)) << 4);
             uint32_t gates[4], ups[4], acts[4];
-            load_turned(at, gates);
-            load_turned(at + 4096, ups);
+            load_turned(to, gates);
+            load_turned(to + 4096, ups);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float* f = (j & 2 ? hi : lo) + 4 * i + 2 * (j & 1);
-              const float2 gate = unpack<T>(gates[j]), up = unpack<T>(ups[j]);
+              float2 gate = unpack<T>(gates[j]);
+              const float2 up = unpack<T>(ups[j]);
+              if (!ok) gate.x = gate.y = __uint_as_float(0x7fc00000u);
               const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
               gates[j] = pack<T>(f[0] * up.x * s0 * (1.f + gate.x * (1.f - s0)), f[1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
               ups[j] = pack<T>(f[0] * gate.x * s0, f[1] * gate.y * s1);
               acts[j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
             }
-            store_turned(at, gates[0], gates[1], gates[2], gates[3]);
-            store_turned(at + 4096, ups[0], ups[1], ups[2], ups[3]);
-            store_turned(at + 8192, acts[0], acts[1], acts[2], acts[3]);
+            store_turned(to, gates[0], gates[1], gates[2], gates[3]);
+            store_turned(to + 4096, ups[0], ups[1], ups[2], ups[3]);
+            store_turned(to + 8192, acts[0], acts[1], acts[2], acts[3]);
           }
+          read_out();
+          async_fence();
           epilogue_bar();
+          const int ch = g.m0 + cta * 128;
+          if (whole) {
+            if (t == 0) {
 #pragma unroll
-          for (int o = 0; o < 3; ++o)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int row = (i * 128 + t) >> 4, chunk = t & 15, ch = g.m0 + cta * 128 + chunk * 8;
-              if (c0 + row < g.n && ch < a.I)
-                *reinterpret_cast<uint4*>(a.out + ((size_t)o * a.n_rows + g.row + c0 + row) * a.I + ch) =
-                    *reinterpret_cast<const uint4*>(staging + o * 4096 + row * 256 + ((chunk ^ (row & 7)) << 4));
+              for (int i = 0; i < 6; ++i)
+                if (ch + (i & 1) * 64 < a.I) store_3d(&a.o[0], buffer_at + i * 2048, ch + (i & 1) * 64, g.row + c0, i >> 1);
             }
-          epilogue_bar();
+          } else {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) {
+              const int row = t >> 3, chunk = t & 7, c = ch + (i & 1) * 64 + chunk * 8;
+              if (c0 + row < g.n && c < a.I)
+                *reinterpret_cast<uint4*>(a.out + ((size_t)(i >> 1) * a.n_rows + g.row + c0 + row) * a.I + c) =
+                    *reinterpret_cast<const uint4*>(buffer + i * 2048 + row * 128 + ((chunk ^ (row & 7)) << 4));
+            }
+            epilogue_bar();
+          }
+          if (t == 0) {
+            store_commit();
+            stores_read<1>();                            // the group before this one has left
+            if (groups > 0) mbar_arrive(kept_empty + (int)((groups - 1) & 3));
+          }
+          ++groups;
         } else {
-          // output rows of 128 values: 256 bytes; two buffers, so that one barrier is enough
+          // output rows of 128 values in two halves of [32 rows x 128 bytes]
+          uint32_t v[16];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + (lane & 7), chunk = quad * 4 + (lane >> 3);
-            store_turned(stage_at + buffer * 8192 + row * 256 + ((chunk ^ (row & 7)) << 4), pack<T>(lo[4 * i], lo[4 * i + 1]),
-                         pack<T>(lo[4 * i + 2], lo[4 * i + 3]), pack<T>(hi[4 * i], hi[4 * i + 1]), pack<T>(hi[4 * i + 2], hi[4 * i + 3]));
+            v[4 * i] = pack<T>(lo[4 * i], lo[4 * i + 1]);
+            v[4 * i + 1] = pack<T>(lo[4 * i + 2], lo[4 * i + 3]);
+            v[4 * i + 2] = pack<T>(hi[4 * i], hi[4 * i + 1]);
+            v[4 * i + 3] = pack<T>(hi[4 * i + 2], hi[4 * i + 3]);
           }
+          read_out();
+          if (t == 0) stores_read<S::kBuffers - 1>();
           epilogue_bar();
-          const int chunk = t & 15, m = g.m0 + cta * 128 + chunk * 8;
-          if (m < a.H) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + (lane & 7), chunk = (quad & 1) * 4 + (lane >> 3);
+            store_turned(buffer_at + (quad >> 1) * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+          async_fence();
+          epilogue_bar();
+          const int m = g.m0 + cta * 128;
+          if (whole) {
+            if (t == 0) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                if (m + i * 64 < a.H) {
+                  if constexpr (MODE == kGradBlocks) store_4d(&a.o[0], buffer_at + i * 4096, m + i * 64, g.plane, g.row + c0, g.e);
+                  else store_3d(&a.o[0], buffer_at + i * 4096, m + i * 64, g.row + c0, 0);
+                }
+            }
+          } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int row = (i * 128 + t) >> 4;
-              uint16_t* out = MODE == kGradBlocks ? a.out + (size_t)g.e * a.out_stride + ((size_t)(g.row + c0 + row) * 3 + g.plane) * a.H + m
-                                                  : a.out + (size_t)(g.row + c0 + row) * a.out_stride + m;
-              if (c0 + row < g.n)
-                *reinterpret_cast<uint4*>(out) =
-                    *reinterpret_cast<const uint4*>(staging + buffer * 8192 + row * 256 + ((chunk ^ (row & 7)) << 4));
+              const int row = (i * 128 + t) >> 4, half = (t >> 3) & 1, chunk = t & 7, at_m = m + half * 64 + chunk * 8;
+              if (c0 + row < g.n && at_m < a.H)
+                *reinterpret_cast<uint4*>(a.out + (size_t)(g.row + c0 + row) * a.out_stride + at_m) =
+                    *reinterpret_cast<const uint4*>(buffer + half * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
             }
           }
-          buffer ^= 1;
+          if (t == 0) store_commit();
         }
+        at.next();
       }
       if (g.pieces) ++acc;
     }
+    if (t == 0) stores_done();
   }
   __syncwarp();
   fence_before();
@@ -642,11 +748,11 @@ struct Encoder {
     encode(m, p, 3, dims, strides, box);
   }
   // expert blocks; boxes of 64 columns of one plane of `channels` channels
-  void blocks(CUtensorMap* m, const FfnCall& c, unsigned channels) {
+  void blocks(CUtensorMap* m, const FfnCall& c, const void* p, int64_t block_stride, unsigned channels) {
     const cuuint64_t dims[4] = {(cuuint64_t)c.hidden, 3, (cuuint64_t)c.inter, (cuuint64_t)c.n_experts};
-    const cuuint64_t strides[3] = {(cuuint64_t)c.hidden * 2, (cuuint64_t)c.hidden * 6, (cuuint64_t)c.block_stride * 2};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.hidden * 2, (cuuint64_t)c.hidden * 6, (cuuint64_t)block_stride * 2};
     const cuuint32_t box[4] = {64, 1, channels, 1};
-    encode(m, c.blocks, 4, dims, strides, box);
+    encode(m, p, 4, dims, strides, box);
   }
   // the same with eight channels of a plane, then those of the next, as neighbours: boxes of 64 columns of gate and up of 64 channels
   void blocks_by_eight(CUtensorMap* m, const FfnCall& c) {
@@ -663,12 +769,9 @@ struct Encoder {
 
 template <int MODE, typename T>
 cudaError_t launch_product(const ProductArgs& a, cudaStream_t stream) {
-  constexpr size_t kFixed = 1024 + (size_t)kStages * kStageBytes + kStagingBytes + 256;
-  constexpr size_t kMost = kFixed + (size_t)(3 * REMOE_SORT_MAX_EXPERTS + 1) * 4;
-  const size_t smem = kFixed + (size_t)(3 * a.n_experts + 1) * 4;
-  static_assert(kMost <= 227 * 1024, "shared memory of a CTA");
+  const size_t smem = Shape<MODE>::smem(a.n_experts);
   static std::atomic<bool> ready[kMaxDevices];
-  const cudaError_t e = allow_dynamic_smem(product_kernel<MODE, T>, kMost, ready);
+  const cudaError_t e = allow_dynamic_smem(product_kernel<MODE, T>, Shape<MODE>::smem(REMOE_SORT_MAX_EXPERTS), ready);
   if (e != cudaSuccess) return e;
   // one pair for each pair of SMs, fewer where there are fewer tiles
   const int m = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
@@ -709,13 +812,16 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   a.n_experts = c.n_experts; a.n_rows = c.n_rows; a.H = c.hidden; a.I = c.inter;
   enc.blocks_by_eight(&a.m[0], c);
   enc.n_rows(&a, xs, c.n_rows, c.hidden, xs_stride, 1);
+  enc.matrix(&a.o[0], act, c.n_rows, c.inter, c.inter, 1, Shape<kGateUp>::kCols);
+  if (gate_up) enc.matrix(&a.o[1], gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGateUp>::kCols);
   a.out = static_cast<uint16_t*>(act);
   a.kept = static_cast<uint16_t*>(gate_up);
   if (!enc.ok) return cudaErrorInvalidValue;
   cudaError_t e = launch_product<kGateUp, T>(a, stream);
   if (e != cudaSuccess) return e;
-  enc.blocks(&a.m[0], c, 64);
+  enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 64);
   enc.n_rows(&a, act, c.n_rows, c.inter, c.inter, 1);
+  enc.matrix(&a.o[0], ys, c.n_rows, c.hidden, ys_stride, 1, Shape<kDown>::kCols);
   a.out = static_cast<uint16_t*>(ys);
   a.out_stride = ys_stride;
   if (!enc.ok) return cudaErrorInvalidValue;
@@ -730,17 +836,19 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
   a.n_experts = c.n_experts; a.n_rows = c.n_rows; a.H = c.hidden; a.I = c.inter;
   cudaError_t e = cudaSuccess;
   if (c.n_rows > 0) {
-    enc.blocks(&a.m[0], c, 128);
+    enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 128);
     enc.n_rows(&a, d_ys, c.n_rows, c.hidden, d_ys_stride, 1);
-    a.gate_up = static_cast<const uint16_t*>(gate_up);
+    enc.matrix(&a.gate_up, gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGradAct>::kCols);
+    enc.matrix(&a.o[0], work, c.n_rows, c.inter, c.inter, 3, Shape<kGradAct>::kCols);
     a.out = static_cast<uint16_t*>(work);
     if (!enc.ok) return cudaErrorInvalidValue;
     e = launch_product<kGradAct, T>(a, stream);
     if (e != cudaSuccess) return e;
   }
   if (d_xs && c.n_rows > 0) {
-    enc.blocks(&a.m[0], c, 64);
+    enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 64);
     enc.n_rows(&a, work, c.n_rows, c.inter, c.inter, 2);
+    enc.matrix(&a.o[0], d_xs, c.n_rows, c.hidden, d_xs_stride, 1, Shape<kGradRows>::kCols);
     a.out = static_cast<uint16_t*>(d_xs);
     a.out_stride = d_xs_stride;
     if (!enc.ok) return cudaErrorInvalidValue;
@@ -753,8 +861,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
       enc.matrix(&a.m[1], d_ys, c.n_rows, c.hidden, d_ys_stride, 1, 64);
       enc.matrix(&a.n[0], work, c.n_rows, c.inter, c.inter, 3, 64);
     }
-    a.out = static_cast<uint16_t*>(d_blocks);
-    a.out_stride = d_block_stride;
+    enc.blocks(&a.o[0], c, d_blocks, d_block_stride, Shape<kGradBlocks>::kCols);
     if (!enc.ok) return cudaErrorInvalidValue;
     e = launch_product<kGradBlocks, T>(a, stream);
   }
