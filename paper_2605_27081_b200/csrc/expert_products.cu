@@ -11,13 +11,14 @@
 //   kGradBlocks  m = hidden,  n = channel, k = row:   d W = (d g)^T xs, (d u)^T xs, act^T d_ys, one plane of a block each
 // Operands come through tensor maps straight from where the caller keeps them: K-major tiles (k contiguous) are [128 rows x 64],
 // MN-major ones two [64 x 64] boxes with k as the rows; both are the 128-byte-swizzled images the tensor cores read.
-// Per CTA: warp 0 loads (TMA, a ring of stages of 64 k, 32 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 read the
-// results out of TMEM (two buffers of 256 columns, so that a tile's epilogue runs behind the next tile's products).  With k = row
+// Per CTA: warp 0 loads (TMA, a ring of stages of 64 k, 32 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 and 8-11 read the
+// results out of TMEM (two buffers of 256 columns, a buffer and every other tile for each four, so that a tile's epilogue runs behind the next
+// tiles' products).  With k = row
 // (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
 // written) would enter the sums, so warp 2 stands between the copies and the products and clears it in both operands.
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
 // leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
-// since a copy would run over the next expert's first rows.  kGradAct's kept gates and ups come in the same way they leave, by warp 3.
+// since a copy would run over the next expert's first rows.  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -38,23 +39,24 @@ constexpr int kTile = 256;                               // rows of M and most r
 constexpr int kK = 64;                                   // k of a stage: 128 bytes
 constexpr int kOperandBytes = 128 * 128;                 // a CTA's half of an operand's stage
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kThreads = 256;
+constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;
 constexpr unsigned kPolls = 1u << 18;                    // of a bounded wait
 constexpr int kBoxes = 5;
 // Rows of N in one copy: 16, 32, 64, 96, 128.
 __host__ __device__ constexpr int box_rows(int b) { return b == 0 ? 16 : b == 1 ? 32 : 32 * b; }
 
-// Shared memory: ring, then the epilogue's buffers of kCols columns of the result.
+// Shared memory: ring, then the buffers of the two epilogues, each of kCols columns of the result.
 template <int MODE>
 struct Shape {
   static constexpr int kStages = MODE == kGradAct ? 5 : 6;
   static constexpr int kCols = MODE == kGradAct ? 16 : 32;
-  static constexpr int kBuffer = MODE == kGateUp ? 4096 : MODE == kGradAct ? 12288 : 8192;  // kGateUp: one of three outputs; kGradAct: all three
-  static constexpr int kBuffers = MODE == kGateUp || MODE == kGradAct ? 4 : 2;
+  static constexpr int kBuffer = MODE == kDown || MODE == kGradRows || MODE == kGradBlocks ? 8192 : 12288;    // the others: three outputs
+  static constexpr int kBuffers = MODE == kGradAct ? 2 : 1;
+  static constexpr int kStaging = 2 * kBuffers * kBuffer;
   static constexpr int kBarriers = 3 * kStages + 2 + 2 + 1 + 2 * 4;
-  static constexpr size_t kFixed = 1024 + (size_t)kStages * kStageBytes + kBuffers * kBuffer + 8 * kBarriers + 8;
-  static constexpr size_t smem(int n_experts) { return kFixed + (size_t)(3 * n_experts + 1) * 4; }
+  static constexpr size_t kFixed = 1024 + (size_t)kStages * kStageBytes + kStaging + 8 * kBarriers + 8;
+  static constexpr size_t smem(int n_experts) { return kFixed + (size_t)(2 * n_experts + 2) * 4; }
   static_assert(smem(REMOE_SORT_MAX_EXPERTS) <= 227 * 1024, "shared memory of a CTA");
 };
 
@@ -177,7 +179,7 @@ __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.com
 template <int N> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 __device__ __forceinline__ void async_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void epilogue_bar() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void epilogue_bar(int group) { asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory"); }
 
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) {
@@ -212,49 +214,73 @@ struct Tile {
   }
 };
 
-// The tiles of a launch in the order of experts, dealt to the pairs in turn.  Each role of a CTA walks them by itself.
+// The tiles of a launch in the order of experts, dealt to the pairs in turn: a pair's next tile is as many further as there are pairs.  Each
+// role of a CTA walks them by itself, in steps of mixed digits (no division a tile).  upto [N + 1]: tiles of N of lower experts;
+// first [N + 1]: rows of the experts, ascending.
 template <int MODE>
 struct Walk {
   const ProductArgs& a;
-  const int *first, *upto;                               // shared memory: [N] first row, [N + 1] tiles of N of lower experts
-  const int* count;
-  int m_tiles, n_tiles, t, e;
-  __device__ Walk(const ProductArgs& args, const int* first_, const int* count_, const int* upto_)
-      : a(args), first(first_), upto(upto_), count(count_), t((int)blockIdx.x >> 1), e(0) {
-    const int m = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
-    m_tiles = (m + kTile - 1) / kTile;
+  const int* first;
+  const int* upto;
+  int m_tiles, n_tiles, m, i, j, e, size;                // tile of M, tile of N (j: plane of the block), expert, rows of N in a tile
+  int step_m, step_i, step_j, step_e;
+  __device__ Walk(const ProductArgs& args, const int* first_, const int* upto_) : a(args), first(first_), upto(upto_), e(0), size(0) {
+    const int rows = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
+    const int pairs = (int)gridDim.x >> 1, pair = (int)blockIdx.x >> 1;
+    m_tiles = (rows + kTile - 1) / kTile;
     n_tiles = (a.I + kTile - 1) / kTile;
+    m = pair % m_tiles; i = pair / m_tiles;
+    step_m = pairs % m_tiles; step_i = pairs / m_tiles;
+    j = step_j = step_e = 0;
+    if constexpr (MODE == kGradBlocks) {
+      j = i / n_tiles; i %= n_tiles;
+      e = j / 3; j %= 3;
+      step_j = step_i / n_tiles; step_i %= n_tiles;
+      step_e = step_j / 3; step_j %= 3;
+    }
   }
   __device__ bool next(Tile& g) {
     if constexpr (MODE == kGradBlocks) {
-      const int per = 3 * m_tiles * n_tiles;
-      if ((int64_t)t >= (int64_t)a.n_experts * per) return false;
-      g.e = t / per;
-      int r = t - g.e * per;
-      g.plane = r / (m_tiles * n_tiles);
-      r -= g.plane * m_tiles * n_tiles;
-      const int i = r / m_tiles;
-      g.m0 = (r - i * m_tiles) * kTile;
+      if (e >= a.n_experts) return false;
+      g.e = e;
+      g.plane = j;
+      g.m0 = m * kTile;
       g.row = i * kTile;
       g.n = min(kTile, a.I - g.row);
-      g.first_row = first[g.e];
-      g.count = count[g.e];
+      g.first_row = first[e];
+      g.count = first[e + 1] - g.first_row;
       g.pieces = (g.count + kK - 1) / kK;
+      m += step_m;
+      i += step_i;
+      if (m >= m_tiles) { m -= m_tiles; ++i; }
+      j += step_j;
+      if (i >= n_tiles) { i -= n_tiles; ++j; }
+      e += step_e;
+      if (j >= 3) { j -= 3; ++e; }
     } else {
-      while (e < a.n_experts && t >= upto[e + 1] * m_tiles) ++e;
+      bool moved = size == 0;
+      while (e < a.n_experts && i >= upto[e + 1] - upto[e]) {
+        i -= upto[e + 1] - upto[e];
+        ++e;
+        moved = true;
+      }
       if (e >= a.n_experts) return false;
-      const int local = t - upto[e] * m_tiles, tiles = upto[e + 1] - upto[e];
-      const int i = local / m_tiles;
-      const int size = ((count[e] + tiles - 1) / tiles + 31) / 32 * 32;
+      const int count = first[e + 1] - first[e];
+      if (moved) {                                       // the expert's rows in equal tiles
+        const int tiles = upto[e + 1] - upto[e];
+        size = ((count + tiles - 1) / tiles + 31) / 32 * 32;
+      }
       g.e = e;
-      g.m0 = (local - i * m_tiles) * (MODE == kGateUp ? kTile / 2 : kTile);
+      g.m0 = m * (MODE == kGateUp ? kTile / 2 : kTile);
       g.row = first[e] + i * size;
-      g.n = min(size, count[e] - i * size);
+      g.n = min(size, count - i * size);
       const int k = MODE == kDown || MODE == kGradRows ? a.I : a.H;
       g.pieces = (k + kK - 1) / kK * (MODE == kGradRows ? 2 : 1);
+      m += step_m;
+      i += step_i;
+      if (m >= m_tiles) { m -= m_tiles; ++i; }
     }
     g.half = (g.n + 31) / 32 * 16;
-    t += (int)gridDim.x >> 1;
     return true;
   }
 };
@@ -278,7 +304,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* staging = smem + (size_t)kStages * kStageBytes;
-  uint64_t* full = reinterpret_cast<uint64_t*>(staging + S::kBuffers * S::kBuffer);   // even CTA: both halves of a stage are there
+  uint64_t* full = reinterpret_cast<uint64_t*>(staging + S::kStaging);   // even CTA: both halves of a stage are there
   uint64_t* landed = full + kStages;                     // kRagged: this CTA's copies of a stage have landed
   uint64_t* empty = landed + kStages;                    // a stage has been read
   uint64_t* acc_full = empty + kStages;                  // [2] a result is complete
@@ -288,9 +314,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   uint64_t* kept_empty = kept_full + 4;                  // [4] what replaced them has left
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(kept_empty + 4);
   int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
-  int* first = abort_flag + 1;                           // [N]
-  int* count = first + a.n_experts;                      // [N]
-  int* upto = count + a.n_experts;                       // [N + 1]
+  int* first = abort_flag + 1;                           // [N + 1]
+  int* upto = first + a.n_experts + 1;                   // [N + 1]
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = (int)cluster_rank();
@@ -310,24 +335,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  for (int e = tid; e < a.n_experts; e += kThreads) {
-    const int lo = min(max(__ldg(a.offsets + e), 0), a.n_rows), hi = min(max(__ldg(a.offsets + e + 1), 0), a.n_rows);
-    first[e] = lo;
-    count[e] = max(0, hi - lo);
-  }
+  for (int e = tid; e <= a.n_experts; e += kThreads) first[e] = min(max(__ldg(a.offsets + e), 0), a.n_rows);
   __syncthreads();
-  if (warp == 0) {
-    int sum = 0;
-    for (int e0 = 0; e0 < a.n_experts; e0 += 32) {
-      int v = e0 + lane < a.n_experts ? (count[e0 + lane] + kTile - 1) / kTile : 0;
+  if (warp == 0) {                                       // held to an ascending order; tiles of N, summed up
+    int most = 0, sum = 0;
+    for (int e0 = 0; e0 <= a.n_experts; e0 += 32) {
+      int v = e0 + lane <= a.n_experts ? first[e0 + lane] : 0;
       for (int d = 1; d < 32; d <<= 1) {
         const int w = __shfl_up_sync(0xffffffffu, v, d);
-        if (lane >= d) v += w;
+        if (lane >= d) v = max(v, w);
       }
-      if (e0 + lane < a.n_experts) upto[e0 + lane + 1] = sum + v;
-      sum += __shfl_sync(0xffffffffu, v, 31);
+      v = max(v, most);
+      int before = __shfl_up_sync(0xffffffffu, v, 1);
+      if (lane == 0) before = most;
+      most = __shfl_sync(0xffffffffu, v, 31);
+      int tiles = e0 + lane == 0 ? 0 : (v - before + kTile - 1) / kTile;     // of expert e0 + lane - 1
+      for (int d = 1; d < 32; d <<= 1) {
+        const int w = __shfl_up_sync(0xffffffffu, tiles, d);
+        if (lane >= d) tiles += w;
+      }
+      if (e0 + lane <= a.n_experts) {
+        first[e0 + lane] = v;
+        upto[e0 + lane] = sum + tiles;
+      }
+      sum += __shfl_sync(0xffffffffu, tiles, 31);
     }
-    if (lane == 0) upto[0] = 0;
   }
   fence_before();
   __syncthreads();
@@ -344,7 +376,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 
   auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
 
-  Walk<MODE> walk(a, first, count, upto);
+  Walk<MODE> walk(a, first, upto);
   Tile g;
   if (warp == 0) {
     // ------------------------------------------------------------------------------------------------ copies
@@ -419,7 +451,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       bool ok = true;
       while (!uniform(aborted()) && uniform(walk.next(g))) {
         g.make_uniform();
-        if (g.pieces == 0) continue;
         if (acc >= 2) ok = warp_wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
         if (!ok) break;
         fence_after();
@@ -436,12 +467,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             for (int k = 0; k < kK / 16; ++k)
               mma_pair(d, m_desc + stage + k * kMStep, kDescHi, n_desc + stage + k * kNStep, kDescHi, idesc, (p | k) ? 1u : 0u);
             commit_pair(empty + at.s);
-            if (p + 1 == g.pieces) commit_pair(acc_full + (acc & 1));
           }
           __syncwarp();
           at.next();
         }
         if (!ok) break;
+        if (elect_one()) commit_pair(acc_full + (acc & 1));
+        __syncwarp();
         ++acc;
       }
       if (!ok) {
@@ -449,77 +481,80 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         mbar_wait(drain, 0, kPolls);
       }
     }
-  } else if (warp == 2) {
-    // ------------------------------------------------------------------------------- rows behind an expert's last
+  } else if (warp < 4) {
     if constexpr (kRagged) {
-      Place<kStages> at;
-      bool ok = true;
-      while (ok && !aborted() && walk.next(g)) {
-        const int chunks = g.half > 64 ? 4 : 3;          // of 64 rows of k, two of M and those of N
-        for (int p = 0; p < g.pieces; ++p) {
-          ok = wait(landed + at.s, at.turn);
-          if (!ok) break;
-          const int left = g.count - p * kK;             // the expert's rows from this stage on
-          if (left < kK) {
-            unsigned char* st = smem + (size_t)at.s * kStageBytes;
-            for (int i = lane; i < chunks * (kK - left) * 8; i += 32) {
-              const int line = i >> 3, c = line / (kK - left), r = left + line % (kK - left);
-              *reinterpret_cast<uint4*>(st + c * 8192 + r * 128 + (i & 7) * 16) = make_uint4(0, 0, 0, 0);
-            }
-            async_fence();
-          }
-          __syncwarp();
-          if (lane == 0) {
-            if (left < kK) arrive_release_cluster(in_even_cta(full + at.s));
-            else arrive_at(in_even_cta(full + at.s));
-          }
-          at.next();
-        }
-      }
-    }
-  } else if (warp == 3) {
-    // ------------------------------------------------------------------------------------ kept gates and ups, 16 rows a time
-    if constexpr (MODE == kGradAct) {
-      if (lane == 0) {
-        Place<4> at;
-        int64_t groups = 0;
+      // ----------------------------------------------------------------------------- rows behind an expert's last
+      if (warp == 2) {
+        Place<kStages> at;
         bool ok = true;
         while (ok && !aborted() && walk.next(g)) {
+          const int chunks = g.half > 64 ? 4 : 3;        // of 64 rows of k, two of M and those of N
+          for (int p = 0; p < g.pieces; ++p) {
+            ok = wait(landed + at.s, at.turn);
+            if (!ok) break;
+            const int left = g.count - p * kK;           // the expert's rows from this stage on
+            if (left < kK) {
+              unsigned char* mine = smem + (size_t)at.s * kStageBytes + (lane >> 3) * 8192 + (lane & 7) * 16;   // a row of up to four blocks
+              if ((lane >> 3) < chunks)
+                for (int r = left; r < kK; ++r) *reinterpret_cast<uint4*>(mine + r * 128) = make_uint4(0, 0, 0, 0);
+              async_fence();
+            }
+            __syncwarp();
+            if (lane == 0) {
+              if (left < kK) arrive_release_cluster(in_even_cta(full + at.s));
+              else arrive_at(in_even_cta(full + at.s));
+            }
+            at.next();
+          }
+        }
+      }
+    } else if constexpr (MODE == kGradAct) {
+      // ---------------------------------------------------------- kept gates and ups, 16 rows a time, a warp for each epilogue
+      const int group = warp - 2;
+      if (lane == 0) {
+        Place<2> at;
+        int64_t groups = 0;
+        int tile = 0;
+        bool ok = true;
+        for (; ok && !aborted() && walk.next(g); ++tile) {
+          if ((tile & 1) != group) continue;
           const int ch = g.m0 + cta * 128;
           for (int c0 = 0; c0 < g.n; c0 += kCols) {
-            if (groups >= 4) {
-              ok = wait(kept_empty + at.s, at.turn ^ 1);
+            if (groups >= 2) {
+              ok = wait(kept_empty + 2 * group + at.s, at.turn ^ 1);
               if (!ok) break;
             }
-            const uint32_t to = smem_u32(staging) + at.s * S::kBuffer, bar = smem_u32(kept_full + at.s);
-            mbar_expect_tx(kept_full + at.s, 8192);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load_3d(to + i * 2048, &a.gate_up, ch + (i & 1) * 64, g.row + c0, i >> 1, bar);
+            const uint32_t to = smem_u32(staging) + (2 * group + at.s) * S::kBuffer, bar = smem_u32(kept_full + 2 * group + at.s);
+            mbar_expect_tx(kept_full + 2 * group + at.s, 8192);
+            load_3d(to, &a.gate_up, ch, g.row + c0, 0, bar);
+            load_3d(to + 6144, &a.gate_up, ch + 64, g.row + c0, 0, bar);
             at.next();
             ++groups;
           }
         }
         if (!ok)                                         // copies under way land before the CTA leaves
-          for (int64_t i = groups > 4 ? groups - 4 : 0; i < groups; ++i) wait(kept_full + (int)(i % 4), (uint32_t)(i / 4) & 1);
+          for (int64_t i = groups > 2 ? groups - 2 : 0; i < groups; ++i) wait(kept_full + 2 * group + (int)(i & 1), (uint32_t)(i / 2) & 1);
       }
     }
   } else {
     // ------------------------------------------------------------------------------------------------ results
-    const int quad = warp & 3, t = tid - 128;
+    const int quad = warp & 3, t = tid & 127, group = (warp - 4) >> 2;
+    const bool issuer = quad == 0;                       // one lane of it issues the stores
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     constexpr int kFrag = kCols / 2;
-    int acc = 0;
     int64_t groups = 0;                                  // kGradAct: of columns, so far
     Place<S::kBuffers> at;
+    int third = 0;                                       // kGateUp without kept gates: act alone goes through each third of the buffer in turn
     bool ok = true;
     const bool keep = MODE == kGateUp && a.kept;
-    while (walk.next(g)) {
-      if (g.pieces && ok) {
-        // a whole tile long: more polls for more of k
-        ok = !aborted() && wait(acc_full + (acc & 1), (acc >> 1) & 1, kPolls + (unsigned)min(g.pieces, 1 << 20) * 1024u);
+    const uint32_t col = tmem + lanes + (uint32_t)group * kTile;
+    for (int tile = 0; walk.next(g); ++tile) {
+      if ((tile & 1) != group) continue;
+      if (ok) {
+        // two whole tiles long: more polls for more of k
+        ok = !aborted() && wait(acc_full + group, (tile >> 1) & 1, kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u);
         fence_after();
       }
-      const uint32_t col = tmem + lanes + (uint32_t)(acc & 1) * kTile;
       float lo[kFrag], hi[kFrag];                        // lanes 0-15 and 16-31 of the warp's quarter
       auto fetch = [&](int c0) {
         if (g.pieces && ok) {
@@ -539,13 +574,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         auto read_out = [&]() {                          // registers are free for the next columns, or TMEM for the products
           if (!last) {
             fetch(c0 + kCols);
-          } else if (g.pieces) {
+          } else {
             fence_before();
             __syncwarp();
-            if (lane == 0) arrive_at(in_even_cta(acc_empty + (acc & 1)));
+            if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
           }
         };
-        unsigned char* buffer = staging + (keep ? 0 : at.s * S::kBuffer);
+        unsigned char* buffer = staging + (group * S::kBuffers + at.s) * S::kBuffer;
+        if (MODE == kGateUp && !keep) {
+          buffer += third * 4096;
+          third = third == 2 ? 0 : third + 1;
+        }
         const uint32_t buffer_at = smem_u32(buffer);
         if constexpr (MODE == kGateUp) {
           // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.
@@ -558,11 +597,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             v[2][j] = pack<T>(f[2], f[3]);
           }
           read_out();
-          if (t == 0) {
+          if (issuer && elect_one()) {
             if (keep) stores_read<0>();
-            else stores_read<S::kBuffers - 1>();
+            else stores_read<2>();
           }
-          epilogue_bar();
+          __syncwarp();
+          epilogue_bar(group);
 #pragma unroll
           for (int i = 0; i < 4; i += 2) {
             const int row = (i + (lane >> 4)) * 8 + (lane & 7), chunk = quad * 2 + ((lane >> 3) & 1);
@@ -572,15 +612,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
               if (o == 0 || keep) store_turned(to + o * 4096, v[o][2 * i], v[o][2 * i + 1], v[o][2 * i + 2], v[o][2 * i + 3]);
           }
           async_fence();
-          epilogue_bar();
+          epilogue_bar(group);
           const int ch = g.m0 + cta * 64;
           if (whole) {
-            if (t == 0 && ch < a.I) {
+            if (issuer && ch < a.I && elect_one()) {
               store_3d(&a.o[0], buffer_at, ch, g.row + c0, 0);
-              if (keep) {
-                store_3d(&a.o[1], buffer_at + 4096, ch, g.row + c0, 0);
-                store_3d(&a.o[1], buffer_at + 8192, ch, g.row + c0, 1);
-              }
+              if (keep) store_3d(&a.o[1], buffer_at + 4096, ch, g.row + c0, 0);
             }
           } else {
             for (int o = 0; o < (keep ? 3 : 1); ++o) {
@@ -594,18 +631,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
               }
             }
           }
-          if (t == 0) store_commit();
+          if (issuer && elect_one()) store_commit();
         } else if constexpr (MODE == kGradAct) {
-          // gates and ups lie in two halves of 64 channels, [16 rows x 128 bytes] each; their gradients take their places
-          if (ok) ok = wait(kept_full + at.s, at.turn);
+          // two halves of 64 channels, each [3 planes x 16 rows x 128 bytes]: gates and ups, whose gradients take their places, and act
+          if (ok) ok = wait(kept_full + 2 * group + at.s, at.turn);
           const int half = quad >> 1;
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int row = i * 8 + (lane & 7), chunk = (quad & 1) * 4 + (lane >> 3);
-            const uint32_t to = buffer_at + half * 2048 + row * 128 + ((chunk ^ (row & 7)) << 4);
+            const uint32_t to = buffer_at + half * 6144 + row * 128 + ((chunk ^ (row & 7)) << 4);
             uint32_t gates[4], ups[4], acts[4];
             load_turned(to, gates);
-            load_turned(to + 4096, ups);
+            load_turned(to + 2048, ups);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float* f = (j & 2 ? hi : lo) + 4 * i + 2 * (j & 1);
@@ -618,34 +655,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
               acts[j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
             }
             store_turned(to, gates[0], gates[1], gates[2], gates[3]);
-            store_turned(to + 4096, ups[0], ups[1], ups[2], ups[3]);
-            store_turned(to + 8192, acts[0], acts[1], acts[2], acts[3]);
+            store_turned(to + 2048, ups[0], ups[1], ups[2], ups[3]);
+            store_turned(to + 4096, acts[0], acts[1], acts[2], acts[3]);
           }
           read_out();
           async_fence();
-          epilogue_bar();
+          if (issuer && groups > 0 && elect_one()) {     // what was stored last has left its buffer
+            stores_read<0>();
+            mbar_arrive(kept_empty + 2 * group + (int)((groups - 1) & 1));
+          }
+          __syncwarp();
+          epilogue_bar(group);
           const int ch = g.m0 + cta * 128;
           if (whole) {
-            if (t == 0) {
-#pragma unroll
-              for (int i = 0; i < 6; ++i)
-                if (ch + (i & 1) * 64 < a.I) store_3d(&a.o[0], buffer_at + i * 2048, ch + (i & 1) * 64, g.row + c0, i >> 1);
+            if (issuer && elect_one()) {
+              if (ch < a.I) store_3d(&a.o[0], buffer_at, ch, g.row + c0, 0);
+              if (ch + 64 < a.I) store_3d(&a.o[0], buffer_at + 6144, ch + 64, g.row + c0, 0);
             }
           } else {
 #pragma unroll
             for (int i = 0; i < 6; ++i) {
-              const int row = t >> 3, chunk = t & 7, c = ch + (i & 1) * 64 + chunk * 8;
+              const int row = t >> 3, chunk = t & 7, c = ch + (i / 3) * 64 + chunk * 8;
               if (c0 + row < g.n && c < a.I)
-                *reinterpret_cast<uint4*>(a.out + ((size_t)(i >> 1) * a.n_rows + g.row + c0 + row) * a.I + c) =
+                *reinterpret_cast<uint4*>(a.out + ((size_t)(i % 3) * a.n_rows + g.row + c0 + row) * a.I + c) =
                     *reinterpret_cast<const uint4*>(buffer + i * 2048 + row * 128 + ((chunk ^ (row & 7)) << 4));
             }
-            epilogue_bar();
+            epilogue_bar(group);
           }
-          if (t == 0) {
-            store_commit();
-            stores_read<1>();                            // the group before this one has left
-            if (groups > 0) mbar_arrive(kept_empty + (int)((groups - 1) & 3));
-          }
+          if (issuer && elect_one()) store_commit();
           ++groups;
         } else {
           // output rows of 128 values in two halves of [32 rows x 128 bytes]
@@ -658,18 +695,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             v[4 * i + 3] = pack<T>(hi[4 * i + 2], hi[4 * i + 3]);
           }
           read_out();
-          if (t == 0) stores_read<S::kBuffers - 1>();
-          epilogue_bar();
+          if (issuer && elect_one()) stores_read<0>();
+          __syncwarp();
+          epilogue_bar(group);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int row = i * 8 + (lane & 7), chunk = (quad & 1) * 4 + (lane >> 3);
             store_turned(buffer_at + (quad >> 1) * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
           }
           async_fence();
-          epilogue_bar();
+          epilogue_bar(group);
           const int m = g.m0 + cta * 128;
           if (whole) {
-            if (t == 0) {
+            if (issuer && elect_one()) {
 #pragma unroll
               for (int i = 0; i < 2; ++i)
                 if (m + i * 64 < a.H) {
@@ -686,13 +724,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
                     *reinterpret_cast<const uint4*>(buffer + half * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
             }
           }
-          if (t == 0) store_commit();
+          if (issuer && elect_one()) store_commit();
         }
+        __syncwarp();
         at.next();
       }
-      if (g.pieces) ++acc;
     }
-    if (t == 0) stores_done();
+    if (issuer && elect_one()) stores_done();
   }
   __syncwarp();
   fence_before();
@@ -740,11 +778,11 @@ struct Encoder {
     ok = ok && fn(m, type, rank, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   }
-  // `planes` matrices of n rows, `stride` elements apart; boxes of 64 columns and `box_rows` rows
-  void matrix(CUtensorMap* m, const void* p, int64_t n, int64_t columns, int64_t stride, int planes, unsigned box_rows) {
+  // `planes` matrices of n rows, `stride` elements apart; boxes of 64 columns and `box_rows` rows of `box_planes` of them
+  void matrix(CUtensorMap* m, const void* p, int64_t n, int64_t columns, int64_t stride, int planes, unsigned box_rows, unsigned box_planes = 1) {
     const cuuint64_t dims[3] = {(cuuint64_t)columns, (cuuint64_t)n, (cuuint64_t)planes};
     const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)(n * stride) * 2};
-    const cuuint32_t box[3] = {64, box_rows, 1};
+    const cuuint32_t box[3] = {64, box_rows, box_planes};
     encode(m, p, 3, dims, strides, box);
   }
   // expert blocks; boxes of 64 columns of one plane of `channels` channels
@@ -813,7 +851,7 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   enc.blocks_by_eight(&a.m[0], c);
   enc.n_rows(&a, xs, c.n_rows, c.hidden, xs_stride, 1);
   enc.matrix(&a.o[0], act, c.n_rows, c.inter, c.inter, 1, Shape<kGateUp>::kCols);
-  if (gate_up) enc.matrix(&a.o[1], gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGateUp>::kCols);
+  if (gate_up) enc.matrix(&a.o[1], gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGateUp>::kCols, 2);
   a.out = static_cast<uint16_t*>(act);
   a.kept = static_cast<uint16_t*>(gate_up);
   if (!enc.ok) return cudaErrorInvalidValue;
@@ -838,8 +876,8 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
   if (c.n_rows > 0) {
     enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 128);
     enc.n_rows(&a, d_ys, c.n_rows, c.hidden, d_ys_stride, 1);
-    enc.matrix(&a.gate_up, gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGradAct>::kCols);
-    enc.matrix(&a.o[0], work, c.n_rows, c.inter, c.inter, 3, Shape<kGradAct>::kCols);
+    enc.matrix(&a.gate_up, gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGradAct>::kCols, 2);
+    enc.matrix(&a.o[0], work, c.n_rows, c.inter, c.inter, 3, Shape<kGradAct>::kCols, 3);
     a.out = static_cast<uint16_t*>(work);
     if (!enc.ok) return cudaErrorInvalidValue;
     e = launch_product<kGradAct, T>(a, stream);
