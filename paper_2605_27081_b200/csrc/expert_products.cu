@@ -15,7 +15,7 @@
 // results out of TMEM (two buffers of 256 columns, a buffer and every other tile for each four, so that a tile's epilogue runs behind the next
 // tiles' products).  With k = row
 // (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
-// written) would enter the sums, so warp 2 stands between the copies and the products and clears it in both operands.
+// written) would enter the sums, so warp 2 stands between the copies of such a stage and the products and clears it in both operands.
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
 // leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
 // since a copy would run over the next expert's first rows.  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
@@ -52,8 +52,8 @@ struct Shape {
   static constexpr int kStages = MODE == kGradAct ? 5 : 6;
   static constexpr int kCols = MODE == kGradAct ? 16 : 32;
   static constexpr int kBuffer = MODE == kDown || MODE == kGradRows || MODE == kGradBlocks ? 8192 : 12288;    // the others: three outputs
-  static constexpr int kBuffers = MODE == kGradAct ? 2 : 1;
-  static constexpr int kStaging = 2 * kBuffers * kBuffer;
+  static constexpr int kKept = MODE == kGradAct ? 2 * 8192 : 0;        // kept gates and ups: two groups of columns
+  static constexpr int kStaging = 2 * (kBuffer + kKept);
   static constexpr int kBarriers = 3 * kStages + 2 + 2 + 1 + 2 * 4;
   static constexpr size_t kFixed = 1024 + (size_t)kStages * kStageBytes + kStaging + 8 * kBarriers + 8;
   static constexpr size_t smem(int n_experts) { return kFixed + (size_t)(2 * n_experts + 2) * 4; }
@@ -98,6 +98,9 @@ __device__ __forceinline__ uint32_t in_even_cta(const void* p) {
 }
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_tx_at(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void arrive_release_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -305,13 +308,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   unsigned char* staging = smem + (size_t)kStages * kStageBytes;
   uint64_t* full = reinterpret_cast<uint64_t*>(staging + S::kStaging);   // even CTA: both halves of a stage are there
-  uint64_t* landed = full + kStages;                     // kRagged: this CTA's copies of a stage have landed
+  uint64_t* landed = full + kStages;                     // kRagged: this CTA's copies of a stage that needs clearing have landed
   uint64_t* empty = landed + kStages;                    // a stage has been read
   uint64_t* acc_full = empty + kStages;                  // [2] a result is complete
   uint64_t* acc_empty = acc_full + 2;                    // [2] even CTA: it has been read out by both
   uint64_t* drain = acc_empty + 2;
   uint64_t* kept_full = drain + 1;                       // [4] kGradAct: kept gates and ups are there
-  uint64_t* kept_empty = kept_full + 4;                  // [4] what replaced them has left
+  uint64_t* kept_empty = kept_full + 4;                  // [4] they have been read by four warps
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(kept_empty + 4);
   int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
   int* first = abort_flag + 1;                           // [N + 1]
@@ -328,7 +331,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     }
     for (int b = 0; b < 2; ++b) { mbar_init(acc_full + b, 1); mbar_init(acc_empty + b, 8); }
     mbar_init(drain, 1);
-    for (int b = 0; b < 4; ++b) { mbar_init(kept_full + b, 1); mbar_init(kept_empty + b, 1); }
+    for (int b = 0; b < 4; ++b) { mbar_init(kept_full + b, 1); mbar_init(kept_empty + b, 4); }
     mbar_fence_init();
   }
   if (warp == 2) {
@@ -383,7 +386,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     Place<kStages> at;
     int64_t stages = 0;                                  // issued
     bool ok = true;
-    const uint32_t ring = uniform((int)smem_u32(smem)), bars = uniform((int)(kRagged ? smem_u32(landed) : in_even_cta(full)));
+    const uint32_t ring = uniform((int)smem_u32(smem)), bars = uniform((int)in_even_cta(full)), own_bars = uniform((int)smem_u32(landed));
     while (ok && !uniform(aborted()) && uniform(walk.next(g))) {
       g.make_uniform();
       int box = 0;
@@ -398,9 +401,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           if (!ok) break;
         }
         if (elect_one()) {
-          if constexpr (kRagged) mbar_expect_tx(landed + at.s, bytes);
-          else if (cta == 0) mbar_expect_tx(full + at.s, 2 * bytes);
-          const uint32_t m_dst = ring + at.s * kStageBytes, n_dst = m_dst + kOperandBytes, bar = bars + at.s * 8;
+          // kRagged: each CTA's copies or, where it has to clear what follows the rows, its warp 2 arrive for its half
+          const bool clear = kRagged && (p + 1) * kK > g.count;
+          if constexpr (kRagged) {
+            if (clear) mbar_expect_tx(landed + at.s, bytes);
+            else expect_tx_at(bars + at.s * 8, bytes);
+          } else if (cta == 0) {
+            mbar_expect_tx(full + at.s, 2 * bytes);
+          }
+          const uint32_t m_dst = ring + at.s * kStageBytes, n_dst = m_dst + kOperandBytes, bar = (clear ? own_bars : bars) + at.s * 8;
           if constexpr (MODE == kGateUp) {
             load_5d(m_dst, &a.m[0], p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
             load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
@@ -434,7 +443,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       const int s = (int)(i % kStages);
       const uint32_t turn = (uint32_t)(i / kStages) & 1;
       if (ok) wait(empty + s, turn);
-      else wait((kRagged ? landed : full) + s, turn);
+      else wait(full + s, turn);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------------------------------------ products
@@ -459,7 +468,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           ok = warp_wait(full + at.s, at.turn);
           if (!ok) break;
           // (what warp 2 of either CTA has cleared)
-          if (kRagged && p + 1 == g.pieces) asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          if (kRagged && (p + 1) * kK > g.count) asm volatile("fence.acq_rel.cluster;" ::: "memory");
           fence_after();
           if (elect_one()) {
             const uint32_t stage = (uint32_t)(at.s * kStageBytes) >> 4;
@@ -485,27 +494,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     if constexpr (kRagged) {
       // ----------------------------------------------------------------------------- rows behind an expert's last
       if (warp == 2) {
-        Place<kStages> at;
+        int at = 0;                                      // stage of a tile's first piece
+        uint32_t turns = 0;                              // parity of each stage's next landing
         bool ok = true;
         while (ok && !aborted() && walk.next(g)) {
-          const int chunks = g.half > 64 ? 4 : 3;        // of 64 rows of k, two of M and those of N
-          for (int p = 0; p < g.pieces; ++p) {
-            ok = wait(landed + at.s, at.turn);
-            if (!ok) break;
-            const int left = g.count - p * kK;           // the expert's rows from this stage on
-            if (left < kK) {
-              unsigned char* mine = smem + (size_t)at.s * kStageBytes + (lane >> 3) * 8192 + (lane & 7) * 16;   // a row of up to four blocks
-              if ((lane >> 3) < chunks)
-                for (int r = left; r < kK; ++r) *reinterpret_cast<uint4*>(mine + r * 128) = make_uint4(0, 0, 0, 0);
-              async_fence();
-            }
-            __syncwarp();
-            if (lane == 0) {
-              if (left < kK) arrive_release_cluster(in_even_cta(full + at.s));
-              else arrive_at(in_even_cta(full + at.s));
-            }
-            at.next();
+          const int s = (at + max(g.pieces, 1) - 1) % kStages, left = g.count - (g.pieces - 1) * kK;
+          at = (at + g.pieces) % kStages;
+          if (g.pieces == 0 || left == kK) continue;
+          ok = wait(landed + s, (turns >> s) & 1);
+          if (!ok) break;
+          turns ^= 1u << s;
+          // a row of the blocks of 64 rows a time, two of M and those of N
+          unsigned char* mine = smem + (size_t)s * kStageBytes + (lane >> 3) * 8192 + (lane & 7) * 16;
+          if ((lane >> 3) < (g.half > 64 ? 4 : 3)) {
+#pragma unroll 4
+            for (int r = left; r < kK; ++r) *reinterpret_cast<uint4*>(mine + r * 128) = make_uint4(0, 0, 0, 0);
           }
+          async_fence();
+          __syncwarp();
+          if (lane == 0) arrive_release_cluster(in_even_cta(full + s));
         }
       }
     } else if constexpr (MODE == kGradAct) {
@@ -524,10 +531,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
               ok = wait(kept_empty + 2 * group + at.s, at.turn ^ 1);
               if (!ok) break;
             }
-            const uint32_t to = smem_u32(staging) + (2 * group + at.s) * S::kBuffer, bar = smem_u32(kept_full + 2 * group + at.s);
+            const uint32_t to = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192, bar = smem_u32(kept_full + 2 * group + at.s);
             mbar_expect_tx(kept_full + 2 * group + at.s, 8192);
             load_3d(to, &a.gate_up, ch, g.row + c0, 0, bar);
-            load_3d(to + 6144, &a.gate_up, ch + 64, g.row + c0, 0, bar);
+            load_3d(to + 4096, &a.gate_up, ch + 64, g.row + c0, 0, bar);
             at.next();
             ++groups;
           }
@@ -542,8 +549,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     const bool issuer = quad == 0;                       // one lane of it issues the stores
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
     constexpr int kFrag = kCols / 2;
-    int64_t groups = 0;                                  // kGradAct: of columns, so far
-    Place<S::kBuffers> at;
+    Place<2> at;                                         // kGradAct: of the kept gates and ups
     int third = 0;                                       // kGateUp without kept gates: act alone goes through each third of the buffer in turn
     bool ok = true;
     const bool keep = MODE == kGateUp && a.kept;
@@ -580,7 +586,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
           }
         };
-        unsigned char* buffer = staging + (group * S::kBuffers + at.s) * S::kBuffer;
+        unsigned char* buffer = staging + group * S::kBuffer;
         if (MODE == kGateUp && !keep) {
           buffer += third * 4096;
           third = third == 2 ? 0 : third + 1;
@@ -633,38 +639,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           }
           if (issuer && elect_one()) store_commit();
         } else if constexpr (MODE == kGradAct) {
-          // two halves of 64 channels, each [3 planes x 16 rows x 128 bytes]: gates and ups, whose gradients take their places, and act
+          // two halves of 64 channels: [2 planes x 16 rows x 128 bytes] of gates and ups, [3 planes x ...] of what leaves
           if (ok) ok = wait(kept_full + 2 * group + at.s, at.turn);
-          const int half = quad >> 1;
+          const uint32_t in_half = ((quad & 1) * 4 + (lane >> 3)) ^ (lane & 7);      // 16 bytes of a row
+          const uint32_t kept_at = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192 + (quad >> 1) * 4096 + (lane & 7) * 128 + (in_half << 4);
+          uint32_t gates[2][4], ups[2][4], acts[2][4];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const int row = i * 8 + (lane & 7), chunk = (quad & 1) * 4 + (lane >> 3);
-            const uint32_t to = buffer_at + half * 6144 + row * 128 + ((chunk ^ (row & 7)) << 4);
-            uint32_t gates[4], ups[4], acts[4];
-            load_turned(to, gates);
-            load_turned(to + 2048, ups);
+            load_turned(kept_at + i * 1024, gates[i]);
+            load_turned(kept_at + 2048 + i * 1024, ups[i]);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(kept_empty + 2 * group + at.s);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float* f = (j & 2 ? hi : lo) + 4 * i + 2 * (j & 1);
-              float2 gate = unpack<T>(gates[j]);
-              const float2 up = unpack<T>(ups[j]);
+              float2 gate = unpack<T>(gates[i][j]);
+              const float2 up = unpack<T>(ups[i][j]);
               if (!ok) gate.x = gate.y = __uint_as_float(0x7fc00000u);
               const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
-              gates[j] = pack<T>(f[0] * up.x * s0 * (1.f + gate.x * (1.f - s0)), f[1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
-              ups[j] = pack<T>(f[0] * gate.x * s0, f[1] * gate.y * s1);
-              acts[j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
+              gates[i][j] = pack<T>(f[0] * up.x * s0 * (1.f + gate.x * (1.f - s0)), f[1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
+              ups[i][j] = pack<T>(f[0] * gate.x * s0, f[1] * gate.y * s1);
+              acts[i][j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
             }
-            store_turned(to, gates[0], gates[1], gates[2], gates[3]);
-            store_turned(to + 2048, ups[0], ups[1], ups[2], ups[3]);
-            store_turned(to + 4096, acts[0], acts[1], acts[2], acts[3]);
           }
           read_out();
-          async_fence();
-          if (issuer && groups > 0 && elect_one()) {     // what was stored last has left its buffer
-            stores_read<0>();
-            mbar_arrive(kept_empty + 2 * group + (int)((groups - 1) & 1));
-          }
+          if (issuer && elect_one()) stores_read<0>();
           __syncwarp();
+          epilogue_bar(group);
+          const uint32_t to = buffer_at + (quad >> 1) * 6144 + (lane & 7) * 128 + (in_half << 4);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            store_turned(to + i * 1024, gates[i][0], gates[i][1], gates[i][2], gates[i][3]);
+            store_turned(to + i * 1024 + 2048, ups[i][0], ups[i][1], ups[i][2], ups[i][3]);
+            store_turned(to + i * 1024 + 4096, acts[i][0], acts[i][1], acts[i][2], acts[i][3]);
+          }
+          async_fence();
           epilogue_bar(group);
           const int ch = g.m0 + cta * 128;
           if (whole) {
@@ -683,7 +695,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             epilogue_bar(group);
           }
           if (issuer && elect_one()) store_commit();
-          ++groups;
         } else {
           // output rows of 128 values in two halves of [32 rows x 128 bytes]
           uint32_t v[16];
