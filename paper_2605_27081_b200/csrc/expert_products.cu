@@ -102,9 +102,6 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {
 __device__ __forceinline__ void expect_tx_at(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void arrive_release_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-}
 // Loads of this CTA's own shared memory; completion is counted on a barrier of either CTA of the pair.
 __device__ __forceinline__ void load_5d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4, uint32_t bar) {
   asm volatile(
@@ -467,8 +464,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         for (int p = 0; p < g.pieces; ++p) {
           ok = warp_wait(full + at.s, at.turn);
           if (!ok) break;
-          // (what warp 2 of either CTA has cleared)
-          if (kRagged && (p + 1) * kK > g.count) asm volatile("fence.acq_rel.cluster;" ::: "memory");
           fence_after();
           if (elect_one()) {
             const uint32_t stage = (uint32_t)(at.s * kStageBytes) >> 4;
@@ -510,9 +505,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll 4
             for (int r = left; r < kK; ++r) *reinterpret_cast<uint4*>(mine + r * 128) = make_uint4(0, 0, 0, 0);
           }
+          // The zeros are read by the tensor cores alone (the async proxy), from the shared memory they were written to: the proxy fence
+          // of every lane, then the arrival, puts them before the products.  (Fences at cluster scope on both sides cost 1500 and 1700
+          // cycles a tile of 7000.)
           async_fence();
           __syncwarp();
-          if (lane == 0) arrive_release_cluster(in_even_cta(full + s));
+          if (lane == 0) arrive_at(in_even_cta(full + s));
         }
       }
     } else if constexpr (MODE == kGradAct) {
