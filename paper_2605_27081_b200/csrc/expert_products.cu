@@ -8,7 +8,7 @@
 //   kDown        m = hidden,  n = row, k = channel:                           ys = act W_down
 //   kGradAct     m = channel, n = row, k = hidden:    d act = d_ys W_down^T;  d g, d u, act by the derivative of silu(g) u
 //   kGradRows    m = hidden,  n = row, k = channel of d g, then of d u:       d_xs = d_g W_gate + d_u W_up
-//   kGradBlocks  m = hidden,  n = channel, k = row:   d W = (d g)^T xs, (d u)^T xs, act^T d_ys, one plane of a block each
+//   kGradBlocks  m = channel, n = hidden, k = row:    d W = (d g)^T xs, (d u)^T xs, act^T d_ys, one plane of a block each
 // Operands come through tensor maps straight from where the caller keeps them: K-major tiles (k contiguous) are [128 rows x 64],
 // MN-major ones two [64 x 64] boxes with k as the rows; both are the 128-byte-swizzled images the tensor cores read.
 // Per CTA: warp 0 loads (TMA, a ring of stages of 64 k, 32 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 and 8-11 read the
@@ -18,7 +18,9 @@
 // written) would enter the sums, so warp 2 stands between the copies of such a stage and the products and clears it in both operands.
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
 // leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
-// since a copy would run over the next expert's first rows.  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
+// since a copy would run over the next expert's first rows.  kGradBlocks has the rows of its output as lanes: a thread's 32 columns are 64
+// bytes of one row and leave straight from the registers.  (Through shared memory, with m = hidden, the same took 7 instead of 4 thousand
+// cycles a tile; TMA stores queue behind the loads.)  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -51,7 +53,7 @@ template <int MODE>
 struct Shape {
   static constexpr int kStages = MODE == kGradAct ? 5 : 6;
   static constexpr int kCols = MODE == kGradAct ? 16 : 32;
-  static constexpr int kBuffer = MODE == kDown || MODE == kGradRows || MODE == kGradBlocks ? 8192 : 12288;    // the others: three outputs
+  static constexpr int kBuffer = MODE == kGradBlocks ? 0 : MODE == kDown || MODE == kGradRows ? 8192 : 12288;  // the others: three outputs
   static constexpr int kKept = MODE == kGradAct ? 2 * 8192 : 0;        // kept gates and ups: two groups of columns
   static constexpr int kStaging = 2 * (kBuffer + kKept);
   static constexpr int kBarriers = 3 * kStages + 2 + 2 + 1 + 2 * 4;
@@ -61,15 +63,16 @@ struct Shape {
 };
 
 struct ProductArgs {
-  CUtensorMap m[2];                                      // M: blocks; kGradBlocks: xs, d_ys
-  CUtensorMap n[kBoxes];                                 // N: boxes of box_rows; kGradBlocks: n[0], boxes of 64
+  CUtensorMap m;                                         // M: blocks; kGradBlocks: d g, d u, act
+  CUtensorMap n[kBoxes];                                 // N: boxes of box_rows; kGradBlocks: xs, d_ys, boxes of 64
   const int* offsets;
   int n_experts, n_rows, H, I;
   CUtensorMap gate_up;                                   // kGradAct: [2, n_rows, I], boxes of 16 rows
   CUtensorMap o[2];                                      // outputs (kGateUp: act, the kept gates and ups), boxes of kCols rows
   uint16_t* out;                                         // rows or blocks; kGateUp, kGradAct: [.., n_rows, I]
   uint16_t* kept;                                        // kGateUp: [2, n_rows, I] or null
-  int64_t out_stride;                                    // elements between rows (blocks)
+  int64_t out_stride, block_stride;                      // elements between rows, between blocks
+  bool wide;                                             // kGradBlocks: rows are 32-byte aligned
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -156,6 +159,23 @@ __device__ __forceinline__ void tmem_fragments(uint32_t taddr, float (&v)[8]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
 }
+// 32 consecutive fp32 columns of this thread's lane.  The caller waits.
+__device__ __forceinline__ void tmem_columns(uint32_t taddr, float (&v)[32]) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+        "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+        "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void store_32_bytes(void* p, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
+               "r"(v[6]), "r"(v[7])
+               : "memory");
+}
 // Four 8 x 8 matrices of 16-bit values between fragments and shared memory, turned over: a lane gives the address of row
 // (lane % 8) of matrix (lane / 8), a row being the fragment's column.
 __device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
@@ -170,10 +190,6 @@ __device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
 // Stores of shared memory as boxes of rows; what lies outside the tensor is left out.
 __device__ __forceinline__ void store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
-}
-__device__ __forceinline__ void store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
-  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-               : "memory");
 }
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
@@ -202,7 +218,7 @@ __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f +
 
 // One tile of a pair.
 struct Tile {
-  int e = 0, row = 0, n = 0;                                         // expert; first row (kGradBlocks: channel) and number of them
+  int e = 0, row = 0, n = 0;                             // expert; first row (kGradBlocks: column of hidden) and number of them
   int half = 0;                                          // rows of N in each CTA, a multiple of 16
   int m0 = 0;                                            // first row of M (kGateUp: channel)
   int plane = 0;                                         // kGradBlocks: plane of the block
@@ -222,7 +238,7 @@ struct Walk {
   const ProductArgs& a;
   const int* first;
   const int* upto;
-  int m_tiles, n_tiles, m, i, j, e, size;                // tile of M, tile of N (j: plane of the block), expert, rows of N in a tile
+  int m_tiles, n_tiles, m, i, j, e, size;                // tile of M, tile of N, expert, rows of N in a tile; kGradBlocks: of N, of M, plane
   int step_m, step_i, step_j, step_e;
   __device__ Walk(const ProductArgs& args, const int* first_, const int* upto_) : a(args), first(first_), upto(upto_), e(0), size(0) {
     const int rows = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
@@ -244,9 +260,9 @@ struct Walk {
       if (e >= a.n_experts) return false;
       g.e = e;
       g.plane = j;
-      g.m0 = m * kTile;
-      g.row = i * kTile;
-      g.n = min(kTile, a.I - g.row);
+      g.m0 = i * kTile;
+      g.row = m * kTile;
+      g.n = min(kTile, a.H - g.row);
       g.first_row = first[e];
       g.count = first[e + 1] - g.first_row;
       g.pieces = (g.count + kK - 1) / kK;
@@ -387,10 +403,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     while (ok && !uniform(aborted()) && uniform(walk.next(g))) {
       g.make_uniform();
       int box = 0;
-      if constexpr (kRagged) box = g.half > 64 ? 2 : 1;  // copies of 64 channels
+      if constexpr (kRagged) box = g.half > 64 ? 2 : 1;  // copies of 64 columns
       else while (box_rows(box) < g.half) ++box;
       const uint32_t bytes = kOperandBytes + (kRagged ? box * 8192u : box_rows(box) * 128u);
-      const CUtensorMap* n_map = kRagged ? &a.n[0] : &a.n[box];
+      const CUtensorMap* n_map = kRagged ? &a.n[g.plane == 2] : &a.n[box];
       const int n_row = g.row + cta * g.half;
       for (int p = 0; p < g.pieces; ++p) {
         if (stages >= kStages) {
@@ -408,25 +424,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           }
           const uint32_t m_dst = ring + at.s * kStageBytes, n_dst = m_dst + kOperandBytes, bar = (clear ? own_bars : bars) + at.s * 8;
           if constexpr (MODE == kGateUp) {
-            load_5d(m_dst, &a.m[0], p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
+            load_5d(m_dst, &a.m, p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
             load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
           } else if constexpr (MODE == kGradAct) {
-            load_4d(m_dst, &a.m[0], p * kK, 2, g.m0 + cta * 128, g.e, bar);
+            load_4d(m_dst, &a.m, p * kK, 2, g.m0 + cta * 128, g.e, bar);
             load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
           } else if constexpr (MODE == kDown || MODE == kGradRows) {
             const int per = MODE == kDown ? g.pieces : g.pieces / 2;
             const int j = p >= per, k0 = (p - j * per) * kK;
             const int plane = MODE == kDown ? 2 : j;
-            load_4d(m_dst, &a.m[0], g.m0 + cta * 128, plane, k0, g.e, bar);
-            load_4d(m_dst + 8192, &a.m[0], g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
+            load_4d(m_dst, &a.m, g.m0 + cta * 128, plane, k0, g.e, bar);
+            load_4d(m_dst + 8192, &a.m, g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
             load_3d(n_dst, n_map, k0, n_row, j, bar);
           } else {
             const int row = g.first_row + p * kK;
-            const CUtensorMap* m = &a.m[g.plane == 2];
-            load_3d(m_dst, m, g.m0 + cta * 128, row, 0, bar);
-            load_3d(m_dst + 8192, m, g.m0 + cta * 128 + 64, row, 0, bar);
-            load_3d(n_dst, n_map, n_row, row, g.plane, bar);
-            if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, g.plane, bar);
+            load_3d(m_dst, &a.m, g.m0 + cta * 128, row, g.plane, bar);
+            load_3d(m_dst + 8192, &a.m, g.m0 + cta * 128 + 64, row, g.plane, bar);
+            load_3d(n_dst, n_map, n_row, row, 0, bar);
+            if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, 0, bar);
           }
         }
         __syncwarp();
@@ -559,6 +574,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         ok = !aborted() && wait(acc_full + group, (tile >> 1) & 1, kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u);
         fence_after();
       }
+      if constexpr (MODE == kGradBlocks) {
+        const int ch = g.m0 + cta * 128 + quad * 32 + lane;
+        const bool there = ch < a.I;
+        uint16_t* out = a.out + (size_t)g.e * a.block_stride + ((size_t)ch * 3 + g.plane) * a.H + g.row;
+        float v[32];
+        const bool some = g.pieces && ok;
+        if (some) tmem_columns(col, v);
+        for (int c0 = 0; c0 < g.n; c0 += 32) {
+          uint32_t packed[16];
+          if (some) {
+            ld_wait();
+#pragma unroll
+            for (int c = 0; c < 16; ++c) packed[c] = pack<T>(v[2 * c], v[2 * c + 1]);
+            if (c0 + 32 < g.n) tmem_columns(col + c0 + 32, v);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) packed[c] = ok ? 0u : 0x7fff7fffu;           // NaN in either type
+          }
+          if (c0 + 32 >= g.n) {                          // read out: the buffer is free for the products
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
+          }
+          if (there) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              if (a.wide && c0 + 16 * c + 16 <= g.n) {
+                store_32_bytes(out + c0 + 16 * c, packed + 8 * c);
+              } else {
+#pragma unroll
+                for (int d = 2 * c; d < 2 * c + 2; ++d)
+                  if (c0 + 8 * d < g.n)
+                    *reinterpret_cast<uint4*>(out + c0 + 8 * d) = make_uint4(packed[4 * d], packed[4 * d + 1], packed[4 * d + 2], packed[4 * d + 3]);
+              }
+          }
+        }
+        continue;
+      }
       float lo[kFrag], hi[kFrag];                        // lanes 0-15 and 16-31 of the warp's quarter
       auto fetch = [&](int c0) {
         if (g.pieces && ok) {
@@ -574,7 +627,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
           for (int i = 0; i < kFrag; ++i) lo[i] = hi[i] = ok ? 0.f : __uint_as_float(0x7fc00000u);
         }
-        const bool last = c0 + kCols >= g.n, whole = MODE == kGradBlocks || c0 + kCols <= g.n;
+        const bool last = c0 + kCols >= g.n, whole = c0 + kCols <= g.n;
         auto read_out = [&]() {                          // registers are free for the next columns, or TMEM for the products
           if (!last) {
             fetch(c0 + kCols);
@@ -719,18 +772,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             if (issuer && elect_one()) {
 #pragma unroll
               for (int i = 0; i < 2; ++i)
-                if (m + i * 64 < a.H) {
-                  if constexpr (MODE == kGradBlocks) store_4d(&a.o[0], buffer_at + i * 4096, m + i * 64, g.plane, g.row + c0, g.e);
-                  else store_3d(&a.o[0], buffer_at + i * 4096, m + i * 64, g.row + c0, 0);
-                }
+                if (m + i * 64 < a.H) store_3d(&a.o[0], buffer_at + i * 4096, m + i * 64, g.row + c0, 0);
             }
           } else {
+            const int half = (t >> 3) & 1, chunk = t & 7, at_m = m + half * 64 + chunk * 8;
+            uint16_t* out = a.out + at_m;
+            if (at_m < a.H) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int row = (i * 128 + t) >> 4, half = (t >> 3) & 1, chunk = t & 7, at_m = m + half * 64 + chunk * 8;
-              if (c0 + row < g.n && at_m < a.H)
-                *reinterpret_cast<uint4*>(a.out + (size_t)(g.row + c0 + row) * a.out_stride + at_m) =
-                    *reinterpret_cast<const uint4*>(buffer + half * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
+              for (int i = 0; i < 4; ++i) {
+                const int row = (i * 128 + t) >> 4;
+                if (c0 + row < g.n)
+                  *reinterpret_cast<uint4*>(out + (size_t)(g.row + c0 + row) * a.out_stride) =
+                      *reinterpret_cast<const uint4*>(buffer + half * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
+              }
             }
           }
           if (issuer && elect_one()) store_commit();
@@ -857,7 +911,7 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   ProductArgs a{};
   a.offsets = static_cast<const int*>(c.offsets);
   a.n_experts = c.n_experts; a.n_rows = c.n_rows; a.H = c.hidden; a.I = c.inter;
-  enc.blocks_by_eight(&a.m[0], c);
+  enc.blocks_by_eight(&a.m, c);
   enc.n_rows(&a, xs, c.n_rows, c.hidden, xs_stride, 1);
   enc.matrix(&a.o[0], act, c.n_rows, c.inter, c.inter, 1, Shape<kGateUp>::kCols);
   if (gate_up) enc.matrix(&a.o[1], gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGateUp>::kCols, 2);
@@ -866,7 +920,7 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   if (!enc.ok) return cudaErrorInvalidValue;
   cudaError_t e = launch_product<kGateUp, T>(a, stream);
   if (e != cudaSuccess) return e;
-  enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 64);
+  enc.blocks(&a.m, c, c.blocks, c.block_stride, 64);
   enc.n_rows(&a, act, c.n_rows, c.inter, c.inter, 1);
   enc.matrix(&a.o[0], ys, c.n_rows, c.hidden, ys_stride, 1, Shape<kDown>::kCols);
   a.out = static_cast<uint16_t*>(ys);
@@ -883,7 +937,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
   a.n_experts = c.n_experts; a.n_rows = c.n_rows; a.H = c.hidden; a.I = c.inter;
   cudaError_t e = cudaSuccess;
   if (c.n_rows > 0) {
-    enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 128);
+    enc.blocks(&a.m, c, c.blocks, c.block_stride, 128);
     enc.n_rows(&a, d_ys, c.n_rows, c.hidden, d_ys_stride, 1);
     enc.matrix(&a.gate_up, gate_up, c.n_rows, c.inter, c.inter, 2, Shape<kGradAct>::kCols, 2);
     enc.matrix(&a.o[0], work, c.n_rows, c.inter, c.inter, 3, Shape<kGradAct>::kCols, 3);
@@ -893,7 +947,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
     if (e != cudaSuccess) return e;
   }
   if (d_xs && c.n_rows > 0) {
-    enc.blocks(&a.m[0], c, c.blocks, c.block_stride, 64);
+    enc.blocks(&a.m, c, c.blocks, c.block_stride, 64);
     enc.n_rows(&a, work, c.n_rows, c.inter, c.inter, 2);
     enc.matrix(&a.o[0], d_xs, c.n_rows, c.hidden, d_xs_stride, 1, Shape<kGradRows>::kCols);
     a.out = static_cast<uint16_t*>(d_xs);
@@ -904,11 +958,13 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
   }
   if (d_blocks) {
     if (c.n_rows > 0) {                                  // (without rows no map is looked at)
-      enc.matrix(&a.m[0], xs, c.n_rows, c.hidden, xs_stride, 1, 64);
-      enc.matrix(&a.m[1], d_ys, c.n_rows, c.hidden, d_ys_stride, 1, 64);
-      enc.matrix(&a.n[0], work, c.n_rows, c.inter, c.inter, 3, 64);
+      enc.matrix(&a.m, work, c.n_rows, c.inter, c.inter, 3, 64);
+      enc.matrix(&a.n[0], xs, c.n_rows, c.hidden, xs_stride, 1, 64);
+      enc.matrix(&a.n[1], d_ys, c.n_rows, c.hidden, d_ys_stride, 1, 64);
     }
-    enc.blocks(&a.o[0], c, d_blocks, d_block_stride, Shape<kGradBlocks>::kCols);
+    a.out = static_cast<uint16_t*>(d_blocks);
+    a.block_stride = d_block_stride;
+    a.wide = !rows::misaligned(d_blocks, 32) && c.hidden % 16 == 0 && (c.n_experts == 1 || d_block_stride % 16 == 0);
     if (!enc.ok) return cudaErrorInvalidValue;
     e = launch_product<kGradBlocks, T>(a, stream);
   }
