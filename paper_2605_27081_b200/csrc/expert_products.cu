@@ -88,6 +88,10 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
   return yes != 0;
 }
+// Products of one call follow one another by programmatic launch: the next kernel's CTAs come up, and load what does not depend on
+// the kernel before, as soon as SMs are free; dependency_wait() returns when that kernel has completed.
+__device__ __forceinline__ void launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -333,6 +337,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   int* first = abort_flag + 1;                           // [N + 1]
   int* upto = first + a.n_experts + 1;                   // [N + 1]
 
+  launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = (int)cluster_rank();
   if (tid == 0) {
@@ -408,6 +413,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       const uint32_t bytes = kOperandBytes + (kRagged ? box * 8192u : box_rows(box) * 128u);
       const CUtensorMap* n_map = kRagged ? &a.n[g.plane == 2] : &a.n[box];
       const int n_row = g.row + cta * g.half;
+      // the operands of stage p; M comes from the blocks (but for kGradBlocks) and so can be on its way before the kernel in front has ended
+      auto load_m = [&](int p, uint32_t m_dst, uint32_t bar) {
+        if constexpr (MODE == kGateUp) {
+          load_5d(m_dst, &a.m, p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
+        } else if constexpr (MODE == kGradAct) {
+          load_4d(m_dst, &a.m, p * kK, 2, g.m0 + cta * 128, g.e, bar);
+        } else if constexpr (MODE == kDown || MODE == kGradRows) {
+          const int per = MODE == kDown ? g.pieces : g.pieces / 2;
+          const int j = p >= per, k0 = (p - j * per) * kK, plane = MODE == kDown ? 2 : j;
+          load_4d(m_dst, &a.m, g.m0 + cta * 128, plane, k0, g.e, bar);
+          load_4d(m_dst + 8192, &a.m, g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
+        } else {
+          const int row = g.first_row + p * kK;
+          load_3d(m_dst, &a.m, g.m0 + cta * 128, row, g.plane, bar);
+          load_3d(m_dst + 8192, &a.m, g.m0 + cta * 128 + 64, row, g.plane, bar);
+        }
+      };
+      auto load_n = [&](int p, uint32_t n_dst, uint32_t bar) {
+        if constexpr (MODE == kGateUp || MODE == kGradAct) {
+          load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
+        } else if constexpr (MODE == kDown || MODE == kGradRows) {
+          const int per = MODE == kDown ? g.pieces : g.pieces / 2;
+          const int j = p >= per;
+          load_3d(n_dst, n_map, (p - j * per) * kK, n_row, j, bar);
+        } else {
+          const int row = g.first_row + p * kK;
+          load_3d(n_dst, n_map, n_row, row, 0, bar);
+          if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, 0, bar);
+        }
+      };
+      int early = 0;                                     // stages of the CTA's first tile whose M is on its way already
+      if (stages == 0) {
+        if constexpr (MODE == kDown || MODE == kGradRows) {
+          early = min(g.pieces, kStages);
+          if (elect_one())
+            for (int p = 0; p < early; ++p) {
+              if (cta == 0) mbar_expect_tx(full + p, 2 * bytes);
+              load_m(p, ring + p * kStageBytes, bars + p * 8);
+            }
+          __syncwarp();
+        }
+        dependency_wait();
+      }
       for (int p = 0; p < g.pieces; ++p) {
         if (stages >= kStages) {
           ok = warp_wait(empty + at.s, at.turn ^ 1);
@@ -416,33 +464,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         if (elect_one()) {
           // kRagged: each CTA's copies or, where it has to clear what follows the rows, its warp 2 arrive for its half
           const bool clear = kRagged && (p + 1) * kK > g.count;
-          if constexpr (kRagged) {
-            if (clear) mbar_expect_tx(landed + at.s, bytes);
-            else expect_tx_at(bars + at.s * 8, bytes);
-          } else if (cta == 0) {
-            mbar_expect_tx(full + at.s, 2 * bytes);
+          const uint32_t m_dst = ring + at.s * kStageBytes, bar = (clear ? own_bars : bars) + at.s * 8;
+          if (p >= early) {
+            if constexpr (kRagged) {
+              if (clear) mbar_expect_tx(landed + at.s, bytes);
+              else expect_tx_at(bars + at.s * 8, bytes);
+            } else if (cta == 0) {
+              mbar_expect_tx(full + at.s, 2 * bytes);
+            }
+            load_m(p, m_dst, bar);
           }
-          const uint32_t m_dst = ring + at.s * kStageBytes, n_dst = m_dst + kOperandBytes, bar = (clear ? own_bars : bars) + at.s * 8;
-          if constexpr (MODE == kGateUp) {
-            load_5d(m_dst, &a.m, p * kK, 0, 0, (g.m0 + cta * 64) / 8, g.e, bar);
-            load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
-          } else if constexpr (MODE == kGradAct) {
-            load_4d(m_dst, &a.m, p * kK, 2, g.m0 + cta * 128, g.e, bar);
-            load_3d(n_dst, n_map, p * kK, n_row, 0, bar);
-          } else if constexpr (MODE == kDown || MODE == kGradRows) {
-            const int per = MODE == kDown ? g.pieces : g.pieces / 2;
-            const int j = p >= per, k0 = (p - j * per) * kK;
-            const int plane = MODE == kDown ? 2 : j;
-            load_4d(m_dst, &a.m, g.m0 + cta * 128, plane, k0, g.e, bar);
-            load_4d(m_dst + 8192, &a.m, g.m0 + cta * 128 + 64, plane, k0, g.e, bar);
-            load_3d(n_dst, n_map, k0, n_row, j, bar);
-          } else {
-            const int row = g.first_row + p * kK;
-            load_3d(m_dst, &a.m, g.m0 + cta * 128, row, g.plane, bar);
-            load_3d(m_dst + 8192, &a.m, g.m0 + cta * 128 + 64, row, g.plane, bar);
-            load_3d(n_dst, n_map, n_row, row, 0, bar);
-            if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, 0, bar);
-          }
+          load_n(p, m_dst + kOperandBytes, bar);
         }
         __syncwarp();
         at.next();
@@ -795,6 +827,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     }
     if (issuer && elect_one()) stores_done();
   }
+  dependency_wait();                                     // no CTA, tiles or not, ends before the kernel in front
   __syncwarp();
   fence_before();
   __syncthreads();
@@ -869,7 +902,7 @@ struct Encoder {
 };
 
 template <int MODE, typename T>
-cudaError_t launch_product(const ProductArgs& a, cudaStream_t stream) {
+cudaError_t launch_product(const ProductArgs& a, bool follows, cudaStream_t stream) {
   const size_t smem = Shape<MODE>::smem(a.n_experts);
   static std::atomic<bool> ready[kMaxDevices];
   const cudaError_t e = allow_dynamic_smem(product_kernel<MODE, T>, Shape<MODE>::smem(REMOE_SORT_MAX_EXPERTS), ready);
@@ -885,6 +918,11 @@ cudaError_t launch_product(const ProductArgs& a, cudaStream_t stream) {
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = follows ? 1 : 0;                        // a product of this call is in front
   return cudaLaunchKernelEx(&cfg, product_kernel<MODE, T>, a);
 }
 
@@ -918,7 +956,7 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   a.out = static_cast<uint16_t*>(act);
   a.kept = static_cast<uint16_t*>(gate_up);
   if (!enc.ok) return cudaErrorInvalidValue;
-  cudaError_t e = launch_product<kGateUp, T>(a, stream);
+  cudaError_t e = launch_product<kGateUp, T>(a, false, stream);
   if (e != cudaSuccess) return e;
   enc.blocks(&a.m, c, c.blocks, c.block_stride, 64);
   enc.n_rows(&a, act, c.n_rows, c.inter, c.inter, 1);
@@ -926,7 +964,7 @@ cudaError_t forward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_s
   a.out = static_cast<uint16_t*>(ys);
   a.out_stride = ys_stride;
   if (!enc.ok) return cudaErrorInvalidValue;
-  return launch_product<kDown, T>(a, stream);
+  return launch_product<kDown, T>(a, true, stream);
 }
 
 template <typename T>
@@ -943,7 +981,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
     enc.matrix(&a.o[0], work, c.n_rows, c.inter, c.inter, 3, Shape<kGradAct>::kCols, 3);
     a.out = static_cast<uint16_t*>(work);
     if (!enc.ok) return cudaErrorInvalidValue;
-    e = launch_product<kGradAct, T>(a, stream);
+    e = launch_product<kGradAct, T>(a, false, stream);
     if (e != cudaSuccess) return e;
   }
   if (d_xs && c.n_rows > 0) {
@@ -953,7 +991,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
     a.out = static_cast<uint16_t*>(d_xs);
     a.out_stride = d_xs_stride;
     if (!enc.ok) return cudaErrorInvalidValue;
-    e = launch_product<kGradRows, T>(a, stream);
+    e = launch_product<kGradRows, T>(a, true, stream);
     if (e != cudaSuccess) return e;
   }
   if (d_blocks) {
@@ -966,7 +1004,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
     a.block_stride = d_block_stride;
     a.wide = !rows::misaligned(d_blocks, 32) && c.hidden % 16 == 0 && (c.n_experts == 1 || d_block_stride % 16 == 0);
     if (!enc.ok) return cudaErrorInvalidValue;
-    e = launch_product<kGradBlocks, T>(a, stream);
+    e = launch_product<kGradBlocks, T>(a, c.n_rows > 0, stream);
   }
   return e;
 }

@@ -16,8 +16,8 @@ namespace {
 // ------------------------------------------------------------------------------------------------------------ sort
 // Row of selection s = (selections of lower experts) + (earlier selections of its own).  One cluster: every warp takes a run of
 // consecutive selections and counts them by expert (lanes with the same expert find one another with match.any, so a
-// counter has one writer at a time), the counts are summed over the warps and, through distributed shared memory, over
-// the blocks, and a second walk over the same selections hands out the rows.  Integers only, the same order every time.
+// counter has one writer at a time); the counts before a selection within its run are its rank there.  The counts are summed over the warps
+// and, through distributed shared memory, over the blocks, and every rank becomes a row.  Integers only, the same order every time.
 struct SortArgs {
   const int* ids;
   int* rows;
@@ -26,33 +26,62 @@ struct SortArgs {
 };
 
 constexpr int kSortWarps = 32;
+constexpr int kStrips = 8;               // of 32 selections whose loads are under way together
 
+// ONCE: a run is at most kStrips strips, whose experts and ranks stay in registers; longer ones are read a second time.
+template <bool ONCE>
 __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_constant__ SortArgs a) {
   extern __shared__ int sort_smem[];
   const int N = a.n_experts, W = blockDim.x >> 5;
   int* total = sort_smem;                // [N] of this block
-  int* base = total + N;                 // [N] first row of an expert's selections in this block
-  int* every = base + N;                 // [N] of all blocks, then the first row of the expert
+  int* base = total + N;                 // [N] selections in lower blocks, then the first row of an expert's selections in this block
+  int* every = base + N;                 // [N] of all blocks
   int* count = every + N;                // [W][N]
   const cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned below = (1u << lane) - 1;
   const int64_t begin = ((int64_t)rank * W + warp) * a.run;
   const int64_t end = begin + a.run < a.n ? begin + a.run : a.n;
   int* mine = count + warp * N;
 
+  int id[kStrips], at[kStrips];          // expert (-1: none) and rank among the run's selections of it so far
+  auto load = [&](int64_t s0) {
+#pragma unroll
+    for (int i = 0; i < kStrips; ++i) {
+      const int64_t s = s0 + i * 32 + lane;
+      id[i] = s < end ? __ldg(a.ids + s) : -1;
+    }
+  };
+  auto take = [&]() {                    // hands out places from the warp's counters
+    unsigned peers[kStrips];
+#pragma unroll
+    for (int i = 0; i < kStrips; ++i) {
+      if ((unsigned)id[i] >= (unsigned)N) id[i] = -1;
+      peers[i] = __match_any_sync(0xffffffffu, id[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kStrips; ++i) {
+      const int old = id[i] >= 0 ? mine[id[i]] : 0;
+      __syncwarp();
+      if (id[i] >= 0 && !(peers[i] & below)) mine[id[i]] = old + __popc(peers[i]);
+      __syncwarp();
+      at[i] = old + __popc(peers[i] & below);
+    }
+  };
+  load(begin);
   for (int i = threadIdx.x; i < W * N; i += blockDim.x) count[i] = 0;
   __syncthreads();
-  for (int64_t s0 = begin; s0 < end; s0 += 32) {
-    const int id = s0 + lane < end ? __ldg(a.ids + s0 + lane) : -1;
-    const bool valid = (unsigned)id < (unsigned)N;
-    const unsigned peers = __match_any_sync(0xffffffffu, valid ? id : -1);
-    if (valid && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
-    __syncwarp();
-  }
+  take();
+  if constexpr (!ONCE)
+    for (int64_t s0 = begin + 32 * kStrips; s0 < end; s0 += 32 * kStrips) {
+      load(s0);
+      take();
+    }
   __syncthreads();
   for (int e = threadIdx.x; e < N; e += blockDim.x) {
     int sum = 0;
+#pragma unroll 8
     for (int w = 0; w < W; ++w) {
       const int c = count[w * N + e];
       count[w * N + e] = sum;
@@ -63,6 +92,7 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
   cluster.sync();
   for (int e = threadIdx.x; e < N; e += blockDim.x) {
     int before = 0, all = 0;
+#pragma unroll 8
     for (int b = 0; b < blocks; ++b) {
       const int c = *cluster.map_shared_rank(total + e, b);
       before += b < rank ? c : 0;
@@ -71,7 +101,8 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
     base[e] = before;
     every[e] = all;
   }
-  cluster.sync();                        // no block leaves while another reads its counts
+  __syncthreads();
+  cluster.barrier_arrive();              // (no block leaves while another reads its counts)
   if (warp == 0) {                       // running sum over the experts, a piece for each lane
     const int per = (N + 31) / 32, e0 = min(N, lane * per), e1 = min(N, e0 + per);
     int sum = 0;
@@ -83,26 +114,27 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
     }
     int first = upto - sum;
     for (int e = e0; e < e1; ++e) {
-      const int c = every[e];
-      every[e] = first;
+      base[e] += first;
       if (rank == 0) a.offsets[e] = first;
-      first += c;
+      first += every[e];
     }
     if (rank == 0 && lane == 31) a.offsets[N] = upto;
   }
   __syncthreads();
-  for (int64_t s0 = begin; s0 < end; s0 += 32) {
-    const bool there = s0 + lane < end;
-    const int id = there ? __ldg(a.ids + s0 + lane) : -1;
-    const bool valid = (unsigned)id < (unsigned)N;
-    const unsigned peers = __match_any_sync(0xffffffffu, valid ? id : -1);
-    int row = -1;
-    if (valid) row = every[id] + base[id] + mine[id] + __popc(peers & ((1u << lane) - 1));
-    __syncwarp();
-    if (valid && lane == __ffs(peers) - 1) mine[id] += __popc(peers);
-    __syncwarp();
-    if (there) a.rows[s0 + lane] = row;
+  for (int64_t s0 = begin; s0 < end; s0 += 32 * kStrips) {
+    if constexpr (!ONCE) {
+      load(s0);
+      take();                            // (the counters have become the run's first places)
+    }
+#pragma unroll
+    for (int i = 0; i < kStrips; ++i) {
+      const int64_t s = s0 + i * 32 + lane;
+      int row = -1;
+      if (id[i] >= 0) row = base[id[i]] + at[i] + (ONCE ? mine[id[i]] : 0);
+      if (s < end) a.rows[s] = row;
+    }
   }
+  cluster.barrier_wait();
 }
 
 // ------------------------------------------------------------------------------------------- rows out, rows back
@@ -120,6 +152,27 @@ template <> __device__ __forceinline__ float from_float<float>(float v) { return
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// A load under a predicate, zero without it: no branch, so that a group's loads are issued one behind the other.  (With an if around each,
+// the compiler finished one row before it asked for the next: 50 instead of 30 us for the sum of 4096 x 6 rows of 2048 bf16.)
+__device__ __forceinline__ void load_word_if(uint4& w, const void* p, bool yes) {
+  w = make_uint4(0, 0, 0, 0);
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "+r"(w.x), "+r"(w.y), "+r"(w.z), "+r"(w.w)
+               : "l"(p), "r"((int)yes));
+}
+__device__ __forceinline__ void load_word_if(uint2& w, const void* p, bool yes) {
+  w = make_uint2(0, 0);
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %3, 0;\n\t@p ld.global.v2.u32 {%0, %1}, [%2];\n\t}" : "+r"(w.x), "+r"(w.y) : "l"(p), "r"((int)yes));
+}
+__device__ __forceinline__ void load_word_if(unsigned& w, const void* p, bool yes) {
+  w = 0;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(w) : "l"(p), "r"((int)yes));
+}
+__device__ __forceinline__ void load_word_if(unsigned short& w, const void* p, bool yes) {
+  w = 0;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+h"(w) : "l"(p), "r"((int)yes));
+}
+
 // V consecutive elements of a row as one access.
 template <typename T, int V>
 struct Vec {
@@ -130,6 +183,7 @@ struct Vec {
   };
   __device__ __forceinline__ Vec() {}
   __device__ __forceinline__ void load(const T* p) { word = *reinterpret_cast<const W*>(p); }
+  __device__ __forceinline__ void load_if(const T* p, bool yes) { load_word_if(word, p, yes); }
   __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<W*>(p) = word; }
 };
 
@@ -143,7 +197,8 @@ struct RowArgs {
   const int* rows;                       // [tokens, K]
   const float* gates;                    // [tokens, K] or null
   float* d_gates;                        // [tokens, K] or null
-  int K, H, n_rows;
+  int K, H, n_rows, n_tokens;
+  int threads, parts;                    // threads of an item (whole warps), items of a token
 };
 
 constexpr int kGroup = 8;                // rows of a token whose loads are under way together
@@ -173,64 +228,211 @@ __global__ void __launch_bounds__(256) dispatch_kernel(const __grid_constant__ R
   }
 }
 
+// The rows and gates of a token, a lane each (up to 32 of them), loaded an item ahead of their use.
+struct Picks {
+  int row;
+  float gate;
+  __device__ __forceinline__ void load(const RowArgs& a, int64_t t, int k0, int lane) {
+    row = -1;
+    gate = 1.f;
+    if (k0 + lane < a.K) {
+      row = __ldg(a.rows + t * a.K + k0 + lane);
+      if (a.gates) gate = __ldg(a.gates + t * a.K + k0 + lane);
+    }
+  }
+  // Of one selection, for all lanes.  (Looked over here, not where it is loaded, so that nothing waits for the load.)
+  __device__ __forceinline__ int row_of(const RowArgs& a, int k) const {
+    const int r = __shfl_sync(0xffffffffu, row, k);
+    return (unsigned)r < (unsigned)a.n_rows ? r : -1;
+  }
+  __device__ __forceinline__ float gate_of(int k) const { return __shfl_sync(0xffffffffu, gate, k); }
+};
+
+// Adds a token's rows to `sum` in the order of the selections.
 template <typename T, int V>
-__device__ __forceinline__ void combine_piece(const RowArgs& a, int64_t t, int i) {
-  const int* rows = a.rows + t * a.K;
-  const float* gates = a.gates ? a.gates + t * a.K : nullptr;
-  const T* ys = static_cast<const T*>(a.a) + i;
-  float sum[V];
+__device__ __forceinline__ void add_rows(const RowArgs& a, int64_t t, Picks p, int i, bool here, int lane, float (&sum)[V]) {
+  for (int kb = 0; kb < a.K; kb += 32) {
+    if (kb) p.load(a, t, kb, lane);
+    for (int k0 = 0; k0 < 32 && kb + k0 < a.K; k0 += kGroup) {
+      Vec<T, V> v[kGroup];
+      float g[kGroup];
+      int r[kGroup];
 #pragma unroll
-  for (int j = 0; j < V; ++j) sum[j] = 0.f;
-  for (int k0 = 0; k0 < a.K; k0 += kGroup) {
-    Vec<T, V> v[kGroup];
-    float g[kGroup];
-    bool there[kGroup];
+      for (int k = 0; k < kGroup; ++k) {
+        r[k] = p.row_of(a, k0 + k);
+        g[k] = p.gate_of(k0 + k);
+        v[k].load_if(static_cast<const T*>(a.a) + r[k] * a.a_stride + i, r[k] >= 0 && here);
+      }
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k)
+        if (r[k] >= 0) {
+#pragma unroll
+          for (int j = 0; j < V; ++j) sum[j] = fmaf(g[k], to_float(v[k].e[j]), sum[j]);
+        }
+    }
+  }
+}
+
+// An item is a piece of a token's row for a.threads threads (whole warps), V elements each, in float32; the elements behind the last whole V
+// are pieces of one.  Persistent: the next item's rows and gates are on their way while this one's data is.
+template <typename T, int V, bool TAIL>
+__global__ void __launch_bounds__(256, TAIL ? 2 : 3) combine_kernel(const __grid_constant__ RowArgs a) {
+  const int lane = threadIdx.x & 31, body = a.H / V, pieces = body + a.H % V, step = (int)blockDim.x / a.threads;
+  const int64_t items = (int64_t)a.n_tokens * a.parts, stride = (int64_t)gridDim.x * step;
+  int64_t item = (int64_t)blockIdx.x * step + threadIdx.x / a.threads;
+  Picks next;
+  if (item < items) next.load(a, a.parts == 1 ? item : item / a.parts, 0, lane);
+  for (; item < items; item += stride) {
+    const int64_t t = a.parts == 1 ? item : item / a.parts;
+    const int piece = (int)(item - t * a.parts) * a.threads + threadIdx.x % a.threads;
+    const Picks p = next;
+    const bool whole = piece < body, here = piece < pieces;
+    const int i = whole ? piece * V : body * V + piece - body;
+    if (item + stride < items) next.load(a, a.parts == 1 ? item + stride : (item + stride) / a.parts, 0, lane);
+    T* out = static_cast<T*>(a.out) + t * a.out_stride + i;
+    const T* base = a.b ? static_cast<const T*>(a.b) + t * a.b_stride + i : nullptr;
+    if (!TAIL || __any_sync(0xffffffffu, whole)) {
+      float sum[V];
+      Vec<T, V> o;
+      if (base && whole) o.load(base);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] = 0.f;
+      add_rows<T, V>(a, t, p, i, whole, lane, sum);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if (base) sum[j] += to_float(o.e[j]);
+        o.e[j] = from_float<T>(sum[j]);
+      }
+      if (whole) o.store(out);
+    }
+    if (TAIL && __any_sync(0xffffffffu, here && !whole)) {
+      const bool single = here && !whole;
+      float sum[1] = {0.f};
+      const float first = base && single ? to_float(*base) : 0.f;
+      add_rows<T, 1>(a, t, p, i, single, lane, sum);
+      if (single) *out = from_float<T>(base ? sum[0] + first : sum[0]);
+    }
+  }
+}
+
+// The same sum for rows that are whole numbers of accesses of 4 bytes or more: copies to shared memory, kDeep units (up to eight rows of an
+// item's piece, and the base) ahead of the sums.  A thread reads nothing but what it copied, so there is no barrier, and what is under way costs
+// no registers.  Taken where there are more items than fit at once: 4096 x 6 rows of 2048 bf16 take 25.7 us, with the loads in registers, one
+// item at a time, 33; one token 3.7 against 2.7 (of which either has a launch).  Three blocks of 256 threads, two units deep: with two blocks
+// 29.5 us, three deep 29.8.
+constexpr int kDeep = 2;
+constexpr int kCopyThreads = 256;
+
+template <int BYTES>
+__device__ __forceinline__ void copy_if(uint32_t dst, const void* src, bool yes) {
+  if constexpr (BYTES == 16)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst), "l"(src), "r"((int)yes) : "memory");
+  else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %3, 0;\n\t@p cp.async.ca.shared.global [%0], [%1], %2;\n\t}" ::"r"(dst), "l"(src), "n"(BYTES), "r"((int)yes)
+                 : "memory");
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kCopyThreads) combine_copy_kernel(const __grid_constant__ RowArgs a) {
+  using W = typename Word<V * (int)sizeof(T)>::type;
+  extern __shared__ __align__(16) unsigned char copy_smem[];
+  W* mine = reinterpret_cast<W*>(copy_smem) + threadIdx.x;               // [kDeep][kGroup + 1][blockDim.x]
+  const int lane = threadIdx.x & 31, pieces = a.H / V, step = (int)blockDim.x / a.threads, per = (kGroup + 1) * (int)blockDim.x;
+  const int64_t items = (int64_t)a.n_tokens * a.parts, stride = (int64_t)gridDim.x * step;
+  struct Unit {                          // item, first selection
+    int64_t item;
+    int k0;
+    __device__ __forceinline__ void next(const RowArgs& a, int64_t stride) {
+      k0 += kGroup;
+      if (k0 >= a.K) { k0 = 0; item += stride; }
+    }
+    __device__ __forceinline__ int64_t token(const RowArgs& a) const { return a.parts == 1 ? item : item / a.parts; }
+    __device__ __forceinline__ int piece(const RowArgs& a) const {
+      return (int)(a.parts == 1 ? 0 : item % a.parts) * a.threads + (int)threadIdx.x % a.threads;
+    }
+  };
+  Unit now{(int64_t)blockIdx.x * step + threadIdx.x / a.threads, 0}, ahead = now;
+  Picks picks[kDeep + 1];                // of the units from `now` on; the last one's is on its way
+  auto look = [&](Picks& p, const Unit& u) {
+    p.row = -1;
+    p.gate = 1.f;
+    if (u.item < items && lane < kGroup && u.k0 + lane < a.K) {
+      const int64_t at = u.token(a) * a.K + u.k0 + lane;
+      p.row = __ldg(a.rows + at);
+      if (a.gates) p.gate = __ldg(a.gates + at);
+    }
+  };
+  auto send = [&](const Picks& p, const Unit& u, int slot) {
+    const int piece = u.piece(a);
+    const bool here = u.item < items && piece < pieces;
+    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(mine + slot * per);
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) {
-      const int r = k0 + k < a.K ? __ldg(rows + k0 + k) : -1;
-      there[k] = (unsigned)r < (unsigned)a.n_rows;
-      if (there[k]) {
-        v[k].load(ys + r * a.a_stride);
-        g[k] = gates ? __ldg(gates + k0 + k) : 1.f;
-      }
+      const int r = p.row_of(a, k);
+      copy_if<(int)sizeof(W)>(dst + k * blockDim.x * (int)sizeof(W), static_cast<const T*>(a.a) + r * a.a_stride + piece * V, here && r >= 0);
     }
+    if (a.b) copy_if<(int)sizeof(W)>(dst + kGroup * blockDim.x * (int)sizeof(W), static_cast<const T*>(a.b) + u.token(a) * a.b_stride + piece * V, here && u.k0 == 0);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  look(picks[0], ahead);
+#pragma unroll
+  for (int i = 0; i < kDeep - 1; ++i) {
+    const Unit u = ahead;
+    ahead.next(a, stride);
+    look(picks[i + 1], ahead);
+    send(picks[i], u, i);
+  }
+  float sum[V];
+  int slot = 0;
+  while (now.item < items) {
+    const Unit u = ahead;
+    ahead.next(a, stride);
+    look(picks[kDeep], ahead);
+    send(picks[kDeep - 1], u, slot == 0 ? kDeep - 1 : slot - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
+    const W* from = mine + slot * per;
+    if (now.k0 == 0) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] = 0.f;
+    }
+    Vec<T, V> v;
+    const int piece = now.piece(a);
+    const bool here = piece < pieces;
 #pragma unroll
     for (int k = 0; k < kGroup; ++k)
-      if (there[k]) {
+      if (picks[0].row_of(a, k) >= 0) {
+        const float g = picks[0].gate_of(k);
+        v.word = from[k * blockDim.x];
 #pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] = fmaf(g[k], to_float(v[k].e[j]), sum[j]);
+        for (int j = 0; j < V; ++j) sum[j] = fmaf(g, to_float(v.e[j]), sum[j]);
       }
-  }
-  Vec<T, V> o;
-  if (a.b) {
-    o.load(static_cast<const T*>(a.b) + t * a.b_stride + i);
+    if (now.k0 + kGroup >= a.K && here) {
+      const int64_t t = now.token(a);
+      if (a.b) {
+        if (now.k0 == 0) v.word = from[kGroup * blockDim.x];
+        else v.load(static_cast<const T*>(a.b) + t * a.b_stride + piece * V);
 #pragma unroll
-    for (int j = 0; j < V; ++j) sum[j] += to_float(o.e[j]);
-  }
+        for (int j = 0; j < V; ++j) sum[j] += to_float(v.e[j]);
+      }
 #pragma unroll
-  for (int j = 0; j < V; ++j) o.e[j] = from_float<T>(sum[j]);
-  o.store(static_cast<T*>(a.out) + t * a.out_stride + i);
+      for (int j = 0; j < V; ++j) v.e[j] = from_float<T>(sum[j]);
+      v.store(static_cast<T*>(a.out) + t * a.out_stride + piece * V);
+    }
+#pragma unroll
+    for (int i = 0; i < kDeep; ++i) picks[i] = picks[i + 1];
+    now.next(a, stride);
+    slot = slot == kDeep - 1 ? 0 : slot + 1;
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// One block a token; the rows are added in the order of the selections, in float32.
 template <typename T, int V>
-__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ RowArgs a) {
-  const int body = a.H / V;
-  for (int i = threadIdx.x; i < body; i += blockDim.x) combine_piece<T, V>(a, blockIdx.x, i * V);
-  for (int i = body * V + threadIdx.x; i < a.H; i += blockDim.x) combine_piece<T, 1>(a, blockIdx.x, i);
-}
-
-template <typename T, int V>
-__device__ __forceinline__ void combine_backward_piece(const RowArgs& a, int64_t t, int k0, int i, float (&dot)[kGroup]) {
-  const int* rows = a.rows + t * a.K;
+__device__ __forceinline__ void backward_piece(const RowArgs& a, int64_t t, const int (&r)[kGroup], const float (&g)[kGroup], int i, float (&dot)[kGroup]) {
   Vec<T, V> d, v[kGroup];
-  int r[kGroup];
   d.load(static_cast<const T*>(a.b) + t * a.b_stride + i);
+  if (a.d_gates) {
 #pragma unroll
-  for (int k = 0; k < kGroup; ++k) {
-    r[k] = k0 + k < a.K ? __ldg(rows + k0 + k) : -1;
-    if ((unsigned)r[k] >= (unsigned)a.n_rows) r[k] = -1;
-    if (a.d_gates && r[k] >= 0) v[k].load(static_cast<const T*>(a.a) + r[k] * a.a_stride + i);
+    for (int k = 0; k < kGroup; ++k) v[k].load_if(static_cast<const T*>(a.a) + r[k] * a.a_stride + i, r[k] >= 0);
   }
 #pragma unroll
   for (int k = 0; k < kGroup; ++k) {
@@ -240,82 +442,150 @@ __device__ __forceinline__ void combine_backward_piece(const RowArgs& a, int64_t
       for (int j = 0; j < V; ++j) dot[k] = fmaf(to_float(v[k].e[j]), to_float(d.e[j]), dot[k]);
     }
     if (a.out) {
-      const float g = a.gates ? __ldg(a.gates + t * a.K + k0 + k) : 1.f;
       Vec<T, V> o;
 #pragma unroll
-      for (int j = 0; j < V; ++j) o.e[j] = from_float<T>(g * to_float(d.e[j]));
+      for (int j = 0; j < V; ++j) o.e[j] = from_float<T>(g[k] * to_float(d.e[j]));
       o.store(static_cast<T*>(a.out) + r[k] * a.out_stride + i);
     }
   }
 }
 
-// One block a token: the gradient of the sum is read once for up to eight of its rows; each row's scalar product with
-// it is summed over the block in a fixed order.
-template <typename T, int V>
-__global__ void __launch_bounds__(256) combine_backward_kernel(const __grid_constant__ RowArgs a) {
-  __shared__ float part[8][kGroup];
-  const int64_t t = blockIdx.x;
-  const int body = a.H / V, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int k0 = 0; k0 < a.K; k0 += kGroup) {
-    float dot[kGroup];
+// Eight values a lane, summed over the warp: lane l ends with the sum of value (l / 4) of all lanes.
+__device__ __forceinline__ float reduce_eight(float (&x)[kGroup], int lane) {
+  float y[4], z[2];
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) dot[k] = 0.f;
-    for (int i = threadIdx.x; i < body; i += blockDim.x) combine_backward_piece<T, V>(a, t, k0, i * V, dot);
-    for (int i = body * V + threadIdx.x; i < a.H; i += blockDim.x) combine_backward_piece<T, 1>(a, t, k0, i, dot);
-    if (!a.d_gates) continue;
+  for (int k = 0; k < 4; ++k) {
+    const float keep = lane & 16 ? x[k + 4] : x[k], give = lane & 16 ? x[k] : x[k + 4];
+    y[k] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
+  }
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
+  for (int k = 0; k < 2; ++k) {
+    const float keep = lane & 8 ? y[k + 2] : y[k], give = lane & 8 ? y[k] : y[k + 2];
+    z[k] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+  }
+  const float keep = lane & 4 ? z[1] : z[0], give = lane & 4 ? z[0] : z[1];
+  float s = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+  s += __shfl_xor_sync(0xffffffffu, s, 2);
+  return s + __shfl_xor_sync(0xffffffffu, s, 1);
+}
+
+// A token for a.threads threads, one warp (several tokens a block) or the whole block: the gradient of the sum is read once for up to eight of
+// its rows, whose scalar products with it are summed in a fixed order.  Persistent as above.
+template <typename T, int V, bool TAIL>
+__global__ void __launch_bounds__(256, TAIL ? 2 : 3) combine_backward_kernel(const __grid_constant__ RowArgs a) {
+  __shared__ float part[2][8][kGroup];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, body = a.H / V, pieces = body + a.H % V, step = (int)blockDim.x / a.threads;
+  const int64_t stride = (int64_t)gridDim.x * step;
+  const int first = threadIdx.x % a.threads;
+  int64_t t = (int64_t)blockIdx.x * step + threadIdx.x / a.threads;
+  int turn = 0;
+  Picks next;
+  if (t < a.n_tokens) next.load(a, t, 0, lane);
+  for (; t < a.n_tokens; t += stride) {
+    Picks p = next;
+    if (t + stride < a.n_tokens) next.load(a, t + stride, 0, lane);
+    for (int kb = 0; kb < a.K; kb += kGroup) {
+      if (kb && kb % 32 == 0) p.load(a, t, kb, lane);
+      int r[kGroup];
+      float g[kGroup], dot[kGroup];
 #pragma unroll
-      for (int d = 16; d; d >>= 1) dot[k] += __shfl_xor_sync(0xffffffffu, dot[k], d);
-      if (lane == 0) part[warp][k] = dot[k];
+      for (int k = 0; k < kGroup; ++k) {
+        r[k] = p.row_of(a, kb % 32 + k);
+        g[k] = p.gate_of(kb % 32 + k);
+        dot[k] = 0.f;
+      }
+      for (int i = first; i < pieces; i += a.threads) {
+        if (!TAIL || i < body) backward_piece<T, V>(a, t, r, g, i * V, dot);
+        else backward_piece<T, 1>(a, t, r, g, body * V + i - body, dot);
+      }
+      if (!a.d_gates) continue;
+      const float s = reduce_eight(dot, lane);
+      float* d_gates = a.d_gates + t * a.K + kb;
+      if (a.threads == 32) {
+        if (lane % 4 == 0 && kb + lane / 4 < a.K) d_gates[lane / 4] = s;
+        continue;
+      }
+      if (lane % 4 == 0) part[turn][warp][lane / 4] = s;
+      __syncthreads();                   // (two sets of sums: the next one's writers do not have to wait for these readers)
+      if (threadIdx.x < kGroup && kb + threadIdx.x < a.K) {
+        float sum = 0.f;
+        for (int w = 0; w < (int)(blockDim.x >> 5); ++w) sum += part[turn][w][threadIdx.x];
+        d_gates[threadIdx.x] = sum;
+      }
+      turn ^= 1;
     }
-    __syncthreads();
-    if (threadIdx.x < kGroup && k0 + threadIdx.x < a.K) {
-      float sum = 0.f;
-      for (int w = 0; w < (int)(blockDim.x >> 5); ++w) sum += part[w][threadIdx.x];
-      a.d_gates[t * a.K + k0 + threadIdx.x] = sum;
-    }
-    __syncthreads();
   }
 }
 
 enum Op { kDispatch, kCombine, kCombineBackward };
 
+template <Op OP, typename T, int V, bool TAIL>
+cudaError_t launch_rows_as(const RowArgs& args, cudaStream_t stream) {
+  RowArgs a = args;
+  const int pieces = a.H / V + a.H % V;
+  a.threads = pieces >= 256 ? 256 : (pieces + 31) / 32 * 32;
+  a.parts = 1;
+  if constexpr (OP == kDispatch) return rows::launch<dispatch_kernel<T, V>>(a, a.n_tokens, 1, a.threads, 0, stream);
+  if constexpr (OP == kCombine) {
+    a.parts = (pieces + a.threads - 1) / a.threads;
+    const int step = 256 / a.threads;
+    const int64_t blocks = ((int64_t)a.n_tokens * a.parts + step - 1) / step;
+    if constexpr (!TAIL && V * sizeof(T) >= 4) if (blocks > 148 * 3) {
+      constexpr size_t kUnit = (size_t)kDeep * (kGroup + 1) * V * sizeof(T);
+      static std::atomic<bool> ready[kMaxDevices];
+      const cudaError_t e = allow_dynamic_smem(combine_copy_kernel<T, V>, kUnit * kCopyThreads, ready);
+      if (e != cudaSuccess) return e;
+      return rows::launch<combine_copy_kernel<T, V>>(a, 148 * 3, 1, step * a.threads, kUnit * step * a.threads, stream);
+    }
+    return rows::launch<combine_kernel<T, V, TAIL>>(a, std::min<int64_t>(blocks, 148 * (TAIL ? 2 : 3)), 1, step * a.threads, 0, stream);
+  }
+  if constexpr (OP == kCombineBackward) {
+    const int step = a.threads == 32 ? 8 : 1;
+    return rows::launch<combine_backward_kernel<T, V, TAIL>>(a, std::min<int64_t>((a.n_tokens + step - 1) / step, 148 * (TAIL ? 2 : 3)), 1, step * a.threads, 0, stream);
+  }
+}
+
+// TAIL: a row is not a whole number of accesses.
 template <Op OP, typename T, int V>
-cudaError_t launch_rows(const RowArgs& a, int n_tokens, cudaStream_t stream) {
-  const int pieces = (a.H + V - 1) / V;
-  int threads = (pieces + 31) / 32 * 32;
-  if (threads > 256) threads = 256;
-  if constexpr (OP == kDispatch) return rows::launch<dispatch_kernel<T, V>>(a, n_tokens, 1, threads, 0, stream);
-  if constexpr (OP == kCombine) return rows::launch<combine_kernel<T, V>>(a, n_tokens, 1, threads, 0, stream);
-  if constexpr (OP == kCombineBackward) return rows::launch<combine_backward_kernel<T, V>>(a, n_tokens, 1, threads, 0, stream);
+cudaError_t launch_rows(const RowArgs& a, cudaStream_t stream) {
+  if constexpr (V > 1 && OP != kDispatch)
+    if (a.H % V) return launch_rows_as<OP, T, V, true>(a, stream);
+  return launch_rows_as<OP, T, V, false>(a, stream);
 }
 
 template <Op OP>
-int launch_rows(const RowArgs& a, int n_tokens, int32_t dtype, int width, cudaStream_t stream) {
+int launch_rows(const RowArgs& a, int32_t dtype, int width, cudaStream_t stream) {
   cudaError_t e = cudaErrorInvalidValue;
   if (dtype == REMOE_F32) {
     switch (width) {
-      case 16: e = launch_rows<OP, float, 4>(a, n_tokens, stream); break;
-      case 8: e = launch_rows<OP, float, 2>(a, n_tokens, stream); break;
-      case 4: e = launch_rows<OP, float, 1>(a, n_tokens, stream); break;
+      case 16: e = launch_rows<OP, float, 4>(a, stream); break;
+      case 8: e = launch_rows<OP, float, 2>(a, stream); break;
+      case 4: e = launch_rows<OP, float, 1>(a, stream); break;
     }
   } else if (dtype == REMOE_BF16) {
     switch (width) {
-      case 16: e = launch_rows<OP, __nv_bfloat16, 8>(a, n_tokens, stream); break;
-      case 8: e = launch_rows<OP, __nv_bfloat16, 4>(a, n_tokens, stream); break;
-      case 4: e = launch_rows<OP, __nv_bfloat16, 2>(a, n_tokens, stream); break;
-      case 2: e = launch_rows<OP, __nv_bfloat16, 1>(a, n_tokens, stream); break;
+      case 16: e = launch_rows<OP, __nv_bfloat16, 8>(a, stream); break;
+      case 8: e = launch_rows<OP, __nv_bfloat16, 4>(a, stream); break;
+      case 4: e = launch_rows<OP, __nv_bfloat16, 2>(a, stream); break;
+      case 2: e = launch_rows<OP, __nv_bfloat16, 1>(a, stream); break;
     }
   } else {
     switch (width) {
-      case 16: e = launch_rows<OP, __half, 8>(a, n_tokens, stream); break;
-      case 8: e = launch_rows<OP, __half, 4>(a, n_tokens, stream); break;
-      case 4: e = launch_rows<OP, __half, 2>(a, n_tokens, stream); break;
-      case 2: e = launch_rows<OP, __half, 1>(a, n_tokens, stream); break;
+      case 16: e = launch_rows<OP, __half, 8>(a, stream); break;
+      case 8: e = launch_rows<OP, __half, 4>(a, stream); break;
+      case 4: e = launch_rows<OP, __half, 2>(a, stream); break;
+      case 2: e = launch_rows<OP, __half, 1>(a, stream); break;
     }
   }
   return rows::status(e);
+}
+
+template <bool ONCE>
+cudaError_t launch_sort(const SortArgs& a, int blocks, int warps, cudaStream_t stream) {
+  static std::atomic<bool> ready[kMaxDevices];
+  const cudaError_t e = allow_dynamic_smem(sort_kernel<ONCE>, (size_t)(kSortWarps + 3) * REMOE_SORT_MAX_EXPERTS * 4, ready);
+  if (e != cudaSuccess) return e;
+  return rows::launch<sort_kernel<ONCE>>(a, blocks, blocks, warps * 32, (size_t)(warps + 3) * a.n_experts * 4, stream);
 }
 
 int check_rows_call(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const int32_t* rows_dev, int32_t n_rows) {
@@ -341,15 +611,12 @@ extern "C" int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_expe
   SortArgs a{ids_dev, rows_dev, offsets_dev, n_tokens * top_k, n_experts, 0};
   const int strips = (a.n + 31) / 32;
   int blocks = 1;
-  while (blocks < 8 && strips > blocks * kSortWarps * 4) blocks *= 2;
+  while (blocks < 8 && strips > blocks * kSortWarps) blocks *= 2;
   int warps = (strips + blocks - 1) / blocks;
   warps = warps < 4 ? 4 : warps > kSortWarps ? kSortWarps : warps;
   a.run = (int)(((int64_t)strips + warps * blocks - 1) / (warps * blocks)) * 32;
-  static std::atomic<bool> ready[kMaxDevices];
-  const cudaError_t e = allow_dynamic_smem(sort_kernel, (size_t)(kSortWarps + 3) * REMOE_SORT_MAX_EXPERTS * 4, ready);
-  if (e != cudaSuccess) return REMOE_E_CUDA;
-  return rows::status(rows::launch<sort_kernel>(a, blocks, blocks, warps * 32, (size_t)(warps + 3) * n_experts * 4,
-                                                static_cast<cudaStream_t>(cuda_stream)));
+  return rows::status(a.run <= 32 * kStrips ? launch_sort<true>(a, blocks, warps, static_cast<cudaStream_t>(cuda_stream))
+                                            : launch_sort<false>(a, blocks, warps, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 extern "C" int remoe_expert_dispatch(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const void* x_dev, int64_t x_stride,
@@ -362,9 +629,9 @@ extern "C" int remoe_expert_dispatch(int32_t n_tokens, int32_t top_k, int32_t hi
   if (n_tokens == 0 || n_rows == 0) return REMOE_OK;
   rows::PointerDevice device(x_dev);
   if (device.err_code()) return device.err_code();
-  const RowArgs a{x_dev, x_stride, nullptr, 0, xs_dev, xs_stride, rows_dev, nullptr, nullptr, top_k, hidden, n_rows};
+  const RowArgs a{x_dev, x_stride, nullptr, 0, xs_dev, xs_stride, rows_dev, nullptr, nullptr, top_k, hidden, n_rows, n_tokens, 0, 0};
   const int width = std::min(sorted::access_width(x_dev, x_stride, n_tokens, size), sorted::access_width(xs_dev, xs_stride, n_rows, size));
-  return launch_rows<kDispatch>(a, n_tokens, dtype, width, static_cast<cudaStream_t>(cuda_stream));
+  return launch_rows<kDispatch>(a, dtype, width, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int remoe_expert_combine(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, int32_t n_rows, const void* ys_dev,
@@ -381,10 +648,10 @@ extern "C" int remoe_expert_combine(int32_t n_tokens, int32_t top_k, int32_t hid
   if (n_tokens == 0) return REMOE_OK;
   rows::PointerDevice device(out_dev);
   if (device.err_code()) return device.err_code();
-  const RowArgs a{ys_dev, ys_stride, base_dev, base_stride, out_dev, out_stride, rows_dev, gates_dev, nullptr, top_k, hidden, n_rows};
+  const RowArgs a{ys_dev, ys_stride, base_dev, base_stride, out_dev, out_stride, rows_dev, gates_dev, nullptr, top_k, hidden, n_rows, n_tokens, 0, 0};
   int width = std::min(sorted::access_width(ys_dev, ys_stride, n_rows, size), sorted::access_width(out_dev, out_stride, n_tokens, size));
   if (base_dev) width = std::min(width, sorted::access_width(base_dev, base_stride, n_tokens, size));
-  return launch_rows<kCombine>(a, n_tokens, dtype, width, static_cast<cudaStream_t>(cuda_stream));
+  return launch_rows<kCombine>(a, dtype, width, static_cast<cudaStream_t>(cuda_stream));
 }
 
 extern "C" int remoe_expert_combine_backward(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const void* d_out_dev,
@@ -403,9 +670,9 @@ extern "C" int remoe_expert_combine_backward(int32_t n_tokens, int32_t top_k, in
   if (n_tokens == 0) return REMOE_OK;
   rows::PointerDevice device(d_out_dev);
   if (device.err_code()) return device.err_code();
-  const RowArgs a{ys_dev, ys_stride, d_out_dev, d_out_stride, d_ys_dev, d_ys_stride, rows_dev, gates_dev, d_gates_dev, top_k, hidden, n_rows};
+  const RowArgs a{ys_dev, ys_stride, d_out_dev, d_out_stride, d_ys_dev, d_ys_stride, rows_dev, gates_dev, d_gates_dev, top_k, hidden, n_rows, n_tokens, 0, 0};
   int width = sorted::access_width(d_out_dev, d_out_stride, n_tokens, size);
   if (d_gates_dev) width = std::min(width, sorted::access_width(ys_dev, ys_stride, n_rows, size));
   if (d_ys_dev) width = std::min(width, sorted::access_width(d_ys_dev, d_ys_stride, n_rows, size));
-  return launch_rows<kCombineBackward>(a, n_tokens, dtype, width, static_cast<cudaStream_t>(cuda_stream));
+  return launch_rows<kCombineBackward>(a, dtype, width, static_cast<cudaStream_t>(cuda_stream));
 }
