@@ -15,7 +15,8 @@
 // results out of TMEM (two buffers of 256 columns, a buffer and every other tile for each four, so that a tile's epilogue runs behind the next
 // tiles' products).  With k = row
 // (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
-// written) would enter the sums, so warp 2 stands between the copies of such a stage and the products and clears it in both operands.
+// written) would enter the sums, so warp 2 stands between the copies of such a stage and the products and clears it in both operands, up to the
+// sixteen rows of an instruction.
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
 // leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
 // since a copy would run over the next expert's first rows.  kGradBlocks has the rows of its output as lanes: a thread's 32 columns are 64
@@ -463,7 +464,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         }
         if (elect_one()) {
           // kRagged: each CTA's copies or, where it has to clear what follows the rows, its warp 2 arrive for its half
-          const bool clear = kRagged && (p + 1) * kK > g.count;
+          const bool clear = kRagged && p + 1 == g.pieces && g.count % 16;
           const uint32_t m_dst = ring + at.s * kStageBytes, bar = (clear ? own_bars : bars) + at.s * 8;
           if (p >= early) {
             if constexpr (kRagged) {
@@ -516,7 +517,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             const uint32_t stage = (uint32_t)(at.s * kStageBytes) >> 4;
 #pragma unroll
             for (int k = 0; k < kK / 16; ++k)
-              mma_pair(d, m_desc + stage + k * kMStep, kDescHi, n_desc + stage + k * kNStep, kDescHi, idesc, (p | k) ? 1u : 0u);
+              if (!kRagged || p * kK + k * 16 < g.count)           // (sixteen rows that are not the expert's add nothing)
+                mma_pair(d, m_desc + stage + k * kMStep, kDescHi, n_desc + stage + k * kNStep, kDescHi, idesc, (p | k) ? 1u : 0u);
             commit_pair(empty + at.s);
           }
           __syncwarp();
@@ -542,7 +544,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         while (ok && !aborted() && walk.next(g)) {
           const int s = (at + max(g.pieces, 1) - 1) % kStages, left = g.count - (g.pieces - 1) * kK;
           at = (at + g.pieces) % kStages;
-          if (g.pieces == 0 || left == kK) continue;
+          if (left % 16 == 0) continue;
           ok = wait(landed + s, (turns >> s) & 1);
           if (!ok) break;
           turns ^= 1u << s;
@@ -550,7 +552,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           unsigned char* mine = smem + (size_t)s * kStageBytes + (lane >> 3) * 8192 + (lane & 7) * 16;
           if ((lane >> 3) < (g.half > 64 ? 4 : 3)) {
 #pragma unroll 4
-            for (int r = left; r < kK; ++r) *reinterpret_cast<uint4*>(mine + r * 128) = make_uint4(0, 0, 0, 0);
+            for (int r = left; r < (left + 15) / 16 * 16; ++r) *reinterpret_cast<uint4*>(mine + r * 128) = make_uint4(0, 0, 0, 0);
           }
           // The zeros are read by the tensor cores alone (the async proxy), from the shared memory they were written to: the proxy fence
           // of every lane, then the arrival, puts them before the products.  (Fences at cluster scope on both sides cost 1500 and 1700

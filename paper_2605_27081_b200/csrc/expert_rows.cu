@@ -15,7 +15,7 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------------------ sort
 // Row of selection s = (selections of lower experts) + (earlier selections of its own).  One cluster: every warp takes a run of
-// consecutive selections and counts them by expert (lanes with the same expert find one another with match.any, so a
+// consecutive selections and counts them by expert (lanes with the same expert find one another by a vote for each bit of the id, so a
 // counter has one writer at a time); the counts before a selection within its run are its rank there.  The counts are summed over the warps
 // and, through distributed shared memory, over the blocks, and every rank becomes a row.  Integers only, the same order every time.
 struct SortArgs {
@@ -41,6 +41,7 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
   const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned below = (1u << lane) - 1;
+  const int bits = 32 - __clz(N - 1);
   const int64_t begin = ((int64_t)rank * W + warp) * a.run;
   const int64_t end = begin + a.run < a.n ? begin + a.run : a.n;
   int* mine = count + warp * N;
@@ -58,7 +59,15 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
 #pragma unroll
     for (int i = 0; i < kStrips; ++i) {
       if ((unsigned)id[i] >= (unsigned)N) id[i] = -1;
-      peers[i] = __match_any_sync(0xffffffffu, id[i]);
+      peers[i] = __ballot_sync(0xffffffffu, id[i] >= 0);
+    }
+    for (int b = 0; b < bits; ++b) {
+#pragma unroll
+      for (int i = 0; i < kStrips; ++i) {
+        const bool set = (id[i] >> b) & 1;
+        const unsigned with = __ballot_sync(0xffffffffu, set);
+        peers[i] &= set ? with : ~with;
+      }
     }
 #pragma unroll
     for (int i = 0; i < kStrips; ++i) {
