@@ -451,6 +451,7 @@ int remoe_distill_topk_backward(int32_t n_rows, int32_t vocab, int32_t dtype, co
  *   given), CUDA.
  */
 #define REMOE_SORT_MAX_EXPERTS 1024
+#define REMOE_EXPERT_MAX_HIDDEN 16777216
 
 /*
  * The rows of the selections, in the order (expert, token, rank).
@@ -463,8 +464,8 @@ int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_experts, const 
                       int32_t* offsets_dev, void* cuda_stream);
 
 /*
- * Rows out: xs[rows[t, k]] = x[t].  dtype REMOE_F32, REMOE_BF16 or REMOE_F16 (bits are copied), any width and alignment (16-byte aligned
- * rows are fastest).  Rows outside [0, n_rows) are left out; every row occurs at most once in `rows`.  Its gradient is remoe_expert_combine
+ * Rows out: xs[rows[t, k]] = x[t].  dtype REMOE_F32, REMOE_BF16 or REMOE_F16 (bits are copied), any alignment (16-byte aligned rows
+ * are fastest), hidden <= REMOE_EXPERT_MAX_HIDDEN.  Rows outside [0, n_rows) are left out; every row occurs at most once in `rows`.  Its gradient is remoe_expert_combine
  * of the rows' gradients with gates NULL.
  */
 int remoe_expert_dispatch(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const void* x_dev, int64_t x_stride,

@@ -388,6 +388,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   cluster_sync_all();
   fence_after();
   const uint32_t tmem = *tmem_slot;
+  Walk<MODE> walk(a, first, upto);
+  Tile g;
   // After a wait that ran out a role stops, and the others of its CTA with their next tile (or their own next wait).
   auto aborted = [&]() { return *(volatile int*)abort_flag != 0; };
   auto wait = [&](uint64_t* bar, uint32_t parity, unsigned polls = kPolls) {
@@ -397,9 +399,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   };
 
   auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
+  // for a wait of up to two tiles: more polls for more of k
+  auto long_wait = [&]() { return kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u; };
 
-  Walk<MODE> walk(a, first, upto);
-  Tile g;
+  if (warp != 0) dependency_wait();                      // (the kernel in front may run for longer than a bounded wait)
   if (warp == 0) {
     // ------------------------------------------------------------------------------------------------ copies
     Place<kStages> at;
@@ -545,7 +548,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           const int s = (at + max(g.pieces, 1) - 1) % kStages, left = g.count - (g.pieces - 1) * kK;
           at = (at + g.pieces) % kStages;
           if (left % 16 == 0) continue;
-          ok = wait(landed + s, (turns >> s) & 1);
+          ok = wait(landed + s, (turns >> s) & 1, long_wait());
           if (!ok) break;
           turns ^= 1u << s;
           // a row of the blocks of 64 rows a time, two of M and those of N
@@ -575,7 +578,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           const int ch = g.m0 + cta * 128;
           for (int c0 = 0; c0 < g.n; c0 += kCols) {
             if (groups >= 2) {
-              ok = wait(kept_empty + 2 * group + at.s, at.turn ^ 1);
+              ok = wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait());
               if (!ok) break;
             }
             const uint32_t to = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192, bar = smem_u32(kept_full + 2 * group + at.s);
@@ -604,8 +607,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     for (int tile = 0; walk.next(g); ++tile) {
       if ((tile & 1) != group) continue;
       if (ok) {
-        // two whole tiles long: more polls for more of k
-        ok = !aborted() && wait(acc_full + group, (tile >> 1) & 1, kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u);
+        ok = !aborted() && wait(acc_full + group, (tile >> 1) & 1, long_wait());
         fence_after();
       }
       if constexpr (MODE == kGradBlocks) {

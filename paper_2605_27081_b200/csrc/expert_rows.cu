@@ -601,7 +601,7 @@ int check_rows_call(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dty
   if (n_tokens < 0 || top_k < 1 || hidden < 1 || n_rows < 0 || (!rows_dev && n_tokens > 0) || rows::misaligned(rows_dev, 4)) return REMOE_E_ARG;
   if (dtype == REMOE_FP8_E4M3 || dtype == REMOE_INT4_G32) return REMOE_E_UNSUPPORTED;
   if (!rows::element_size(dtype)) return REMOE_E_ARG;
-  if ((int64_t)n_tokens * top_k > 0x7fffffff) return REMOE_E_UNSUPPORTED;
+  if ((int64_t)n_tokens * top_k > 0x7fffffff || hidden > REMOE_EXPERT_MAX_HIDDEN) return REMOE_E_UNSUPPORTED;
   return REMOE_OK;
 }
 

@@ -67,7 +67,7 @@ def test_bad_sort(kw, code):
 @pytest.mark.parametrize("kw,code", [
     (dict(n_tokens=-1), ARG), (dict(top_k=0), ARG), (dict(hidden=0), ARG), (dict(n_rows=-1), ARG), (dict(rows=N), ARG), (dict(rows=BUF + 2), ARG),
     (dict(dtype=rb.REMOE_FP8_E4M3), UNSUPPORTED), (dict(dtype=rb.REMOE_INT4_G32), UNSUPPORTED), (dict(dtype=5), ARG), (dict(dtype=-1), ARG),
-    (dict(n_tokens=1 << 28, top_k=8), UNSUPPORTED)])
+    (dict(n_tokens=1 << 28, top_k=8), UNSUPPORTED), (dict(hidden=rb.REMOE_EXPERT_MAX_HIDDEN + 1), UNSUPPORTED)])
 def test_bad_rows(call, kw, code):
     assert call(**kw) == code
 
@@ -128,5 +128,5 @@ def test_header_and_binding_name_the_same_limits():
     import os
     import re
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "remoe.h")).read()
-    for name in ("REMOE_SORT_MAX_EXPERTS", "REMOE_FFN_MAX_WIDTH"):
+    for name in ("REMOE_SORT_MAX_EXPERTS", "REMOE_EXPERT_MAX_HIDDEN", "REMOE_FFN_MAX_WIDTH"):
         assert int(re.search(rf"#define {name} (\d+)", text).group(1)) == getattr(rb, name)
