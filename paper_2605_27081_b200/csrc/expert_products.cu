@@ -149,20 +149,11 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-// 16 lanes x 32 (16) fp32 columns of TMEM as 8 x 8 fragments: for the columns 8 i .. 8 i + 7 the thread holds, of lane T / 4, the columns
-// 2 (T % 4) and the next in v[4 i], v[4 i + 1], and of lane T / 4 + 8 the same in v[4 i + 2], v[4 i + 3].  The caller waits.
-__device__ __forceinline__ void tmem_fragments(uint32_t taddr, float (&v)[16]) {
+// 16 lanes x 8 fp32 columns of TMEM as two 8 x 8 fragments: the thread holds, of lane T / 4, the columns 2 (T % 4) and the next in v[0],
+// v[1], and of lane T / 4 + 8 the same in v[2], v[3].  The caller waits.
+__device__ __forceinline__ void tmem_fragments(uint32_t taddr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-               : "r"(taddr));
-}
-__device__ __forceinline__ void tmem_fragments(uint32_t taddr, float (&v)[8]) {
-  uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-               : "r"(taddr));
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
 }
 // 32 consecutive fp32 columns of this thread's lane.  The caller waits.
 __device__ __forceinline__ void tmem_columns(uint32_t taddr, float (&v)[32]) {
@@ -185,6 +176,9 @@ __device__ __forceinline__ void store_32_bytes(void* p, const uint32_t* v) {
 // (lane % 8) of matrix (lane / 8), a row being the fragment's column.
 __device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
+}
+__device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1) {       // two matrices, addresses from lanes 0-15
+  asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(addr), "r"(r0), "r"(r1) : "memory");
 }
 __device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -236,14 +230,14 @@ struct Tile {
 };
 
 // The tiles of a launch in the order of experts, dealt to the pairs in turn: a pair's next tile is as many further as there are pairs.  Each
-// role of a CTA walks them by itself, in steps of mixed digits (no division a tile).  upto [N + 1]: tiles of N of lower experts;
-// first [N + 1]: rows of the experts, ascending.
+// role of a CTA walks them by itself, a whole warp together, in steps of mixed digits (no division a tile).  upto [N + 1]: tiles of N of lower
+// experts; first [N + 1]: rows of the experts, ascending.
 template <int MODE>
 struct Walk {
   const ProductArgs& a;
   const int* first;
   const int* upto;
-  int m_tiles, n_tiles, m, i, j, e, size;                // tile of M, tile of N, expert, rows of N in a tile; kGradBlocks: of N, of M, plane
+  int m_tiles, n_tiles, m, i, j, e, size;                // tile of M, tile of N of all experts, expert, rows of N in a tile; kGradBlocks: of N, of M, plane
   int step_m, step_i, step_j, step_e;
   __device__ Walk(const ProductArgs& args, const int* first_, const int* upto_) : a(args), first(first_), upto(upto_), e(0), size(0) {
     const int rows = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
@@ -279,22 +273,24 @@ struct Walk {
       e += step_e;
       if (j >= 3) { j -= 3; ++e; }
     } else {
+      if (i >= upto[a.n_experts]) return false;
       bool moved = size == 0;
-      while (e < a.n_experts && i >= upto[e + 1] - upto[e]) {
-        i -= upto[e + 1] - upto[e];
-        ++e;
-        moved = true;
+      for (int lane = threadIdx.x & 31;;) {              // past the experts whose tiles end before this one, up to 32 a look
+        const int x = e + 1 + lane;
+        const unsigned behind = __ballot_sync(0xffffffffu, x <= a.n_experts && upto[x] <= i);
+        e += __popc(behind);
+        moved |= behind != 0;
+        if (behind != 0xffffffffu) break;
       }
-      if (e >= a.n_experts) return false;
-      const int count = first[e + 1] - first[e];
+      const int count = first[e + 1] - first[e], before = upto[e];
       if (moved) {                                       // the expert's rows in equal tiles
-        const int tiles = upto[e + 1] - upto[e];
-        size = ((count + tiles - 1) / tiles + 31) / 32 * 32;
+        const int tiles = upto[e + 1] - before;
+        size = ((tiles == 1 ? count : (count + tiles - 1) / tiles) + 31) / 32 * 32;
       }
       g.e = e;
       g.m0 = m * (MODE == kGateUp ? kTile / 2 : kTile);
-      g.row = first[e] + i * size;
-      g.n = min(size, count - i * size);
+      g.row = first[e] + (i - before) * size;
+      g.n = min(size, count - (i - before) * size);
       const int k = MODE == kDown || MODE == kGradRows ? a.I : a.H;
       g.pieces = (k + kK - 1) / kK * (MODE == kGradRows ? 2 : 1);
       m += step_m;
@@ -357,31 +353,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  for (int e = tid; e <= a.n_experts; e += kThreads) first[e] = min(max(__ldg(a.offsets + e), 0), a.n_rows);
-  __syncthreads();
-  if (warp == 0) {                                       // held to an ascending order; tiles of N, summed up
-    int most = 0, sum = 0;
-    for (int e0 = 0; e0 <= a.n_experts; e0 += 32) {
-      int v = e0 + lane <= a.n_experts ? first[e0 + lane] : 0;
-      for (int d = 1; d < 32; d <<= 1) {
-        const int w = __shfl_up_sync(0xffffffffu, v, d);
-        if (lane >= d) v = max(v, w);
+  // Rows of the experts, held to the range and an ascending order, and their tiles of N, summed up.
+  bool ascending = true;
+  for (int e = tid; e <= a.n_experts; e += kThreads) {
+    const int v = min(max(__ldg(a.offsets + e), 0), a.n_rows), before = e ? min(max(__ldg(a.offsets + e - 1), 0), a.n_rows) : 0;
+    first[e] = v;
+    upto[e] = e ? (v - before + kTile - 1) / kTile : 0;
+    ascending &= v >= before;
+  }
+  if (!__syncthreads_and(ascending)) {
+    if (tid == 0)
+      for (int e = 1; e <= a.n_experts; ++e) {
+        first[e] = max(first[e], first[e - 1]);
+        upto[e] = (first[e] - first[e - 1] + kTile - 1) / kTile;
       }
-      v = max(v, most);
-      int before = __shfl_up_sync(0xffffffffu, v, 1);
-      if (lane == 0) before = most;
-      most = __shfl_sync(0xffffffffu, v, 31);
-      int tiles = e0 + lane == 0 ? 0 : (v - before + kTile - 1) / kTile;     // of expert e0 + lane - 1
-      for (int d = 1; d < 32; d <<= 1) {
-        const int w = __shfl_up_sync(0xffffffffu, tiles, d);
-        if (lane >= d) tiles += w;
-      }
-      if (e0 + lane <= a.n_experts) {
-        first[e0 + lane] = v;
-        upto[e0 + lane] = sum + tiles;
-      }
-      sum += __shfl_sync(0xffffffffu, tiles, 31);
+    __syncthreads();
+  }
+  if (warp == 0) {
+    // a piece of the list for each lane
+    const int per = (a.n_experts + 32) / 32, e0 = min(lane * per, a.n_experts + 1), e1 = min(e0 + per, a.n_experts + 1);
+    int sum = 0;
+    for (int e = e0; e < e1; ++e) sum += upto[e];
+    int before = sum;
+    for (int d = 1; d < 32; d <<= 1) {
+      const int w = __shfl_up_sync(0xffffffffu, before, d);
+      if (lane >= d) before += w;
     }
+    before -= sum;
+    for (int e = e0; e < e1; ++e) upto[e] = before += upto[e];
   }
   fence_before();
   __syncthreads();
@@ -544,11 +543,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         int at = 0;                                      // stage of a tile's first piece
         uint32_t turns = 0;                              // parity of each stage's next landing
         bool ok = true;
-        while (ok && !aborted() && walk.next(g)) {
+        while (ok && !uniform(aborted()) && walk.next(g)) {
           const int s = (at + max(g.pieces, 1) - 1) % kStages, left = g.count - (g.pieces - 1) * kK;
           at = (at + g.pieces) % kStages;
           if (left % 16 == 0) continue;
-          ok = wait(landed + s, (turns >> s) & 1, long_wait());
+          ok = __all_sync(0xffffffffu, wait(landed + s, (turns >> s) & 1, long_wait()));
           if (!ok) break;
           turns ^= 1u << s;
           // a row of the blocks of 64 rows a time, two of M and those of N
@@ -568,37 +567,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     } else if constexpr (MODE == kGradAct) {
       // ---------------------------------------------------------- kept gates and ups, 16 rows a time, a warp for each epilogue
       const int group = warp - 2;
-      if (lane == 0) {
-        Place<2> at;
-        int64_t groups = 0;
-        int tile = 0;
-        bool ok = true;
-        for (; ok && !aborted() && walk.next(g); ++tile) {
-          if ((tile & 1) != group) continue;
-          const int ch = g.m0 + cta * 128;
-          for (int c0 = 0; c0 < g.n; c0 += kCols) {
-            if (groups >= 2) {
-              ok = wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait());
-              if (!ok) break;
-            }
+      Place<2> at;
+      int64_t groups = 0;
+      bool ok = true;
+      for (int tile = 0; ok && !uniform(aborted()) && walk.next(g); ++tile) {
+        if ((tile & 1) != group) continue;
+        const int ch = g.m0 + cta * 128;
+        for (int c0 = 0; c0 < g.n; c0 += kCols) {
+          if (groups >= 2) {
+            ok = __all_sync(0xffffffffu, wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait()));
+            if (!ok) break;
+          }
+          if (elect_one()) {
             const uint32_t to = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192, bar = smem_u32(kept_full + 2 * group + at.s);
             mbar_expect_tx(kept_full + 2 * group + at.s, 8192);
             load_3d(to, &a.gate_up, ch, g.row + c0, 0, bar);
             load_3d(to + 4096, &a.gate_up, ch + 64, g.row + c0, 0, bar);
-            at.next();
-            ++groups;
           }
+          __syncwarp();
+          at.next();
+          ++groups;
         }
-        if (!ok)                                         // copies under way land before the CTA leaves
-          for (int64_t i = groups > 2 ? groups - 2 : 0; i < groups; ++i) wait(kept_full + 2 * group + (int)(i & 1), (uint32_t)(i / 2) & 1);
       }
+      if (!ok)                                           // copies under way land before the CTA leaves
+        for (int64_t i = groups > 2 ? groups - 2 : 0; i < groups; ++i) wait(kept_full + 2 * group + (int)(i & 1), (uint32_t)(i / 2) & 1);
     }
   } else {
     // ------------------------------------------------------------------------------------------------ results
     const int quad = warp & 3, t = tid & 127, group = (warp - 4) >> 2;
     const bool issuer = quad == 0;                       // one lane of it issues the stores
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    constexpr int kFrag = kCols / 2;
     Place<2> at;                                         // kGradAct: of the kept gates and ups
     int third = 0;                                       // kGateUp without kept gates: act alone goes through each third of the buffer in turn
     bool ok = true;
@@ -648,64 +646,99 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         }
         continue;
       }
-      float lo[kFrag], hi[kFrag];                        // lanes 0-15 and 16-31 of the warp's quarter
-      auto fetch = [&](int c0) {
-        if (g.pieces && ok) {
-          tmem_fragments(col + c0, lo);
-          tmem_fragments(col + c0 + (16u << 16), hi);
+      // Eight columns a time, in a loop that is not unrolled (a tile of few rows runs its code once, from cold instruction caches: unrolled over
+      // 32 columns this took 4.5 us of one token's 18), the next eight on their way meanwhile; kCols of them leave together.
+      const bool some = g.pieces && ok;
+      float f[8];                                        // fragments of lanes 0-15 and 16-31 of the warp's quarter
+      auto fetch = [&](int c) {
+        if (some) {
+          tmem_fragments(col + c, f);
+          tmem_fragments(col + c + (16u << 16), f + 4);
         }
       };
       fetch(0);
+#pragma unroll 1
       for (int c0 = 0; c0 < g.n; c0 += kCols) {
-        if (g.pieces && ok) {
-          ld_wait();
-        } else {
-#pragma unroll
-          for (int i = 0; i < kFrag; ++i) lo[i] = hi[i] = ok ? 0.f : __uint_as_float(0x7fc00000u);
-        }
-        const bool last = c0 + kCols >= g.n, whole = c0 + kCols <= g.n;
-        auto read_out = [&]() {                          // registers are free for the next columns, or TMEM for the products
-          if (!last) {
-            fetch(c0 + kCols);
-          } else {
-            fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
-          }
-        };
+        const bool whole = c0 + kCols <= g.n;
         unsigned char* buffer = staging + group * S::kBuffer;
         if (MODE == kGateUp && !keep) {
           buffer += third * 4096;
           third = third == 2 ? 0 : third + 1;
         }
         const uint32_t buffer_at = smem_u32(buffer);
-        if constexpr (MODE == kGateUp) {
-          // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.
-          uint32_t v[3][8];                              // act, gate, up: groups of eight columns x two of channels
+        if (MODE == kGradAct && ok) ok = wait(kept_full + 2 * group + at.s, at.turn);
+#pragma unroll 1
+        for (int c = c0; c < min(c0 + kCols, g.n); c += 8) {
+          float v[8];
+          if (some) ld_wait();
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float* f = (j & 1 ? hi : lo) + 4 * (j >> 1);
-            v[0][j] = pack<T>(f[0] * sigmoid(f[0]) * f[2], f[1] * sigmoid(f[1]) * f[3]);
-            v[1][j] = pack<T>(f[0], f[1]);
-            v[2][j] = pack<T>(f[2], f[3]);
+          for (int i = 0; i < 8; ++i) v[i] = some ? f[i] : ok ? 0.f : __uint_as_float(0x7fc00000u);
+          if (c + 8 < g.n) {
+            fetch(c + 8);
+          } else {                                       // read out: the buffer is free for the products
+            fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
           }
-          read_out();
-          if (issuer && elect_one()) {
-            if (keep) stores_read<0>();
-            else stores_read<2>();
-          }
-          __syncwarp();
-          epilogue_bar(group);
-#pragma unroll
-          for (int i = 0; i < 4; i += 2) {
-            const int row = (i + (lane >> 4)) * 8 + (lane & 7), chunk = quad * 2 + ((lane >> 3) & 1);
+          auto free_buffer = [&]() {                     // before the first eight columns are written
+            if (c != c0) return;
+            if (issuer && elect_one()) {
+              if (MODE == kGateUp && !keep) stores_read<2>();
+              else stores_read<0>();
+            }
+            __syncwarp();
+            epilogue_bar(group);
+          };
+          const int row = c - c0 + (lane & 7);           // of the matrices that this lane addresses
+          if constexpr (MODE == kGateUp) {
+            // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.
+            const uint32_t act0 = pack<T>(v[0] * sigmoid(v[0]) * v[2], v[1] * sigmoid(v[1]) * v[3]);
+            const uint32_t act1 = pack<T>(v[4] * sigmoid(v[4]) * v[6], v[5] * sigmoid(v[5]) * v[7]);
+            free_buffer();
+            const int chunk = quad * 2 + ((lane >> 3) & 1);
             const uint32_t to = buffer_at + row * 128 + ((chunk ^ (row & 7)) << 4);
+            store_turned(to, act0, act1);
+            if (keep) {
+              store_turned(to + 4096, pack<T>(v[0], v[1]), pack<T>(v[4], v[5]));
+              store_turned(to + 8192, pack<T>(v[2], v[3]), pack<T>(v[6], v[7]));
+            }
+          } else if constexpr (MODE == kGradAct) {
+            // two halves of 64 channels: [2 planes x 16 rows x 128 bytes] of gates and ups, [3 planes x ...] of what leaves
+            const uint32_t in_row = row * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (row & 7)) << 4);
+            const uint32_t kept_at = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192 + (quad >> 1) * 4096 + in_row;
+            uint32_t gates[4], ups[4], acts[4];
+            load_turned(kept_at, gates);
+            load_turned(kept_at + 2048, ups);
 #pragma unroll
-            for (int o = 0; o < 3; ++o)
-              if (o == 0 || keep) store_turned(to + o * 4096, v[o][2 * i], v[o][2 * i + 1], v[o][2 * i + 2], v[o][2 * i + 3]);
+            for (int j = 0; j < 4; ++j) {
+              float2 gate = unpack<T>(gates[j]);
+              const float2 up = unpack<T>(ups[j]);
+              if (!ok) gate.x = gate.y = __uint_as_float(0x7fc00000u);
+              const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
+              gates[j] = pack<T>(v[2 * j] * up.x * s0 * (1.f + gate.x * (1.f - s0)), v[2 * j + 1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
+              ups[j] = pack<T>(v[2 * j] * gate.x * s0, v[2 * j + 1] * gate.y * s1);
+              acts[j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
+            }
+            free_buffer();
+            const uint32_t to = buffer_at + (quad >> 1) * 6144 + in_row;
+            store_turned(to, gates[0], gates[1], gates[2], gates[3]);
+            store_turned(to + 2048, ups[0], ups[1], ups[2], ups[3]);
+            store_turned(to + 4096, acts[0], acts[1], acts[2], acts[3]);
+          } else {
+            // output rows of 128 values in two halves of [32 rows x 128 bytes]
+            const uint32_t v0 = pack<T>(v[0], v[1]), v1 = pack<T>(v[2], v[3]), v2 = pack<T>(v[4], v[5]), v3 = pack<T>(v[6], v[7]);
+            free_buffer();
+            const int chunk = (quad & 1) * 4 + (lane >> 3);
+            store_turned(buffer_at + (quad >> 1) * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4), v0, v1, v2, v3);
           }
-          async_fence();
-          epilogue_bar(group);
+        }
+        if constexpr (MODE == kGradAct) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(kept_empty + 2 * group + at.s);
+        }
+        async_fence();
+        epilogue_bar(group);
+        if constexpr (MODE == kGateUp) {
           const int ch = g.m0 + cta * 64;
           if (whole) {
             if (issuer && ch < a.I && elect_one()) {
@@ -713,58 +746,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
               if (keep) store_3d(&a.o[1], buffer_at + 4096, ch, g.row + c0, 0);
             }
           } else {
+#pragma unroll 1
             for (int o = 0; o < (keep ? 3 : 1); ++o) {
               uint16_t* out = o == 0 ? a.out : a.kept + (size_t)(o - 1) * a.n_rows * a.I;
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int row = (i * 128 + t) >> 3, chunk = t & 7;
+#pragma unroll 1
+              for (int row = t >> 3, chunk = t & 7; row < kCols; row += 16)
                 if (c0 + row < g.n && ch + chunk * 8 < a.I)
                   *reinterpret_cast<uint4*>(out + (size_t)(g.row + c0 + row) * a.I + ch + chunk * 8) =
                       *reinterpret_cast<const uint4*>(buffer + o * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
-              }
             }
           }
-          if (issuer && elect_one()) store_commit();
         } else if constexpr (MODE == kGradAct) {
-          // two halves of 64 channels: [2 planes x 16 rows x 128 bytes] of gates and ups, [3 planes x ...] of what leaves
-          if (ok) ok = wait(kept_full + 2 * group + at.s, at.turn);
-          const uint32_t in_half = ((quad & 1) * 4 + (lane >> 3)) ^ (lane & 7);      // 16 bytes of a row
-          const uint32_t kept_at = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192 + (quad >> 1) * 4096 + (lane & 7) * 128 + (in_half << 4);
-          uint32_t gates[2][4], ups[2][4], acts[2][4];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            load_turned(kept_at + i * 1024, gates[i]);
-            load_turned(kept_at + 2048 + i * 1024, ups[i]);
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(kept_empty + 2 * group + at.s);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float* f = (j & 2 ? hi : lo) + 4 * i + 2 * (j & 1);
-              float2 gate = unpack<T>(gates[i][j]);
-              const float2 up = unpack<T>(ups[i][j]);
-              if (!ok) gate.x = gate.y = __uint_as_float(0x7fc00000u);
-              const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
-              gates[i][j] = pack<T>(f[0] * up.x * s0 * (1.f + gate.x * (1.f - s0)), f[1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
-              ups[i][j] = pack<T>(f[0] * gate.x * s0, f[1] * gate.y * s1);
-              acts[i][j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
-            }
-          }
-          read_out();
-          if (issuer && elect_one()) stores_read<0>();
-          __syncwarp();
-          epilogue_bar(group);
-          const uint32_t to = buffer_at + (quad >> 1) * 6144 + (lane & 7) * 128 + (in_half << 4);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            store_turned(to + i * 1024, gates[i][0], gates[i][1], gates[i][2], gates[i][3]);
-            store_turned(to + i * 1024 + 2048, ups[i][0], ups[i][1], ups[i][2], ups[i][3]);
-            store_turned(to + i * 1024 + 4096, acts[i][0], acts[i][1], acts[i][2], acts[i][3]);
-          }
-          async_fence();
-          epilogue_bar(group);
           const int ch = g.m0 + cta * 128;
           if (whole) {
             if (issuer && elect_one()) {
@@ -772,37 +764,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
               if (ch + 64 < a.I) store_3d(&a.o[0], buffer_at + 6144, ch + 64, g.row + c0, 0);
             }
           } else {
-#pragma unroll
+#pragma unroll 1
             for (int i = 0; i < 6; ++i) {
               const int row = t >> 3, chunk = t & 7, c = ch + (i / 3) * 64 + chunk * 8;
               if (c0 + row < g.n && c < a.I)
                 *reinterpret_cast<uint4*>(a.out + ((size_t)(i % 3) * a.n_rows + g.row + c0 + row) * a.I + c) =
                     *reinterpret_cast<const uint4*>(buffer + i * 2048 + row * 128 + ((chunk ^ (row & 7)) << 4));
             }
-            epilogue_bar(group);
           }
-          if (issuer && elect_one()) store_commit();
         } else {
-          // output rows of 128 values in two halves of [32 rows x 128 bytes]
-          uint32_t v[16];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            v[4 * i] = pack<T>(lo[4 * i], lo[4 * i + 1]);
-            v[4 * i + 1] = pack<T>(lo[4 * i + 2], lo[4 * i + 3]);
-            v[4 * i + 2] = pack<T>(hi[4 * i], hi[4 * i + 1]);
-            v[4 * i + 3] = pack<T>(hi[4 * i + 2], hi[4 * i + 3]);
-          }
-          read_out();
-          if (issuer && elect_one()) stores_read<0>();
-          __syncwarp();
-          epilogue_bar(group);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + (lane & 7), chunk = (quad & 1) * 4 + (lane >> 3);
-            store_turned(buffer_at + (quad >> 1) * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4), v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-          }
-          async_fence();
-          epilogue_bar(group);
           const int m = g.m0 + cta * 128;
           if (whole) {
             if (issuer && elect_one()) {
@@ -812,19 +782,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             }
           } else {
             const int half = (t >> 3) & 1, chunk = t & 7, at_m = m + half * 64 + chunk * 8;
-            uint16_t* out = a.out + at_m;
             if (at_m < a.H) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int row = (i * 128 + t) >> 4;
-                if (c0 + row < g.n)
-                  *reinterpret_cast<uint4*>(out + (size_t)(g.row + c0 + row) * a.out_stride) =
-                      *reinterpret_cast<const uint4*>(buffer + half * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
-              }
+#pragma unroll 1
+              for (int row = t >> 4; row < kCols && c0 + row < g.n; row += 8)
+                *reinterpret_cast<uint4*>(a.out + (size_t)(g.row + c0 + row) * a.out_stride + at_m) =
+                    *reinterpret_cast<const uint4*>(buffer + half * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4));
             }
           }
-          if (issuer && elect_one()) store_commit();
         }
+        if (issuer && elect_one()) store_commit();
         __syncwarp();
         at.next();
       }
