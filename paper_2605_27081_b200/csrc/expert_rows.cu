@@ -26,6 +26,7 @@ struct SortArgs {
 };
 
 constexpr int kSortWarps = 32;
+constexpr int kSortBlocks = 16;          // most blocks of the cluster
 constexpr int kStrips = 8;               // of 32 selections whose loads are under way together
 
 // ONCE: a run is at most kStrips strips, whose experts and ranks stay in registers; longer ones are read a second time.
@@ -37,6 +38,7 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
   int* base = total + N;                 // [N] selections in lower blocks, then the first row of an expert's selections in this block
   int* every = base + N;                 // [N] of all blocks
   int* count = every + N;                // [W][N]
+  int* theirs = count + W * N;           // [blocks][N] counts of every block
   const cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), blocks = (int)cluster.num_blocks();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -54,23 +56,37 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
       id[i] = s < end ? __ldg(a.ids + s) : -1;
     }
   };
-  auto take = [&]() {                    // hands out places from the warp's counters
+  auto take = [&](int64_t s0) {          // hands out places from the warp's counters
     unsigned peers[kStrips];
 #pragma unroll
-    for (int i = 0; i < kStrips; ++i) {
+    for (int i = 0; i < kStrips; ++i)
       if ((unsigned)id[i] >= (unsigned)N) id[i] = -1;
-      peers[i] = __ballot_sync(0xffffffffu, id[i] >= 0);
-    }
-    for (int b = 0; b < bits; ++b) {
+    if (s0 + 32 * (kStrips / 2) < end) {  // many strips: their votes between one another
 #pragma unroll
-      for (int i = 0; i < kStrips; ++i) {
-        const bool set = (id[i] >> b) & 1;
-        const unsigned with = __ballot_sync(0xffffffffu, set);
-        peers[i] &= set ? with : ~with;
+      for (int i = 0; i < kStrips; ++i) peers[i] = __ballot_sync(0xffffffffu, id[i] >= 0);
+      for (int b = 0; b < bits; ++b) {
+#pragma unroll
+        for (int i = 0; i < kStrips; ++i) {
+          const bool set = (id[i] >> b) & 1;
+          const unsigned with = __ballot_sync(0xffffffffu, set);
+          peers[i] &= set ? with : ~with;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kStrips / 2; ++i) {
+        if (s0 + i * 32 >= end) break;
+        peers[i] = __ballot_sync(0xffffffffu, id[i] >= 0);
+        for (int b = 0; b < bits; ++b) {
+          const bool set = (id[i] >> b) & 1;
+          const unsigned with = __ballot_sync(0xffffffffu, set);
+          peers[i] &= set ? with : ~with;
+        }
       }
     }
 #pragma unroll
     for (int i = 0; i < kStrips; ++i) {
+      if (s0 + i * 32 >= end) break;
       const int old = id[i] >= 0 ? mine[id[i]] : 0;
       __syncwarp();
       if (id[i] >= 0 && !(peers[i] & below)) mine[id[i]] = old + __popc(peers[i]);
@@ -81,11 +97,11 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
   load(begin);
   for (int i = threadIdx.x; i < W * N; i += blockDim.x) count[i] = 0;
   __syncthreads();
-  take();
+  take(begin);
   if constexpr (!ONCE)
     for (int64_t s0 = begin + 32 * kStrips; s0 < end; s0 += 32 * kStrips) {
       load(s0);
-      take();
+      take(s0);
     }
   __syncthreads();
   for (int e = threadIdx.x; e < N; e += blockDim.x) {
@@ -99,11 +115,14 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
     total[e] = sum;
   }
   cluster.sync();
+  // a thread for each block and expert: one trip to another block's memory, not one behind the other
+  for (int i = threadIdx.x; i < blocks * N; i += blockDim.x) theirs[i] = *cluster.map_shared_rank(total + i % N, i / N);
+  __syncthreads();
+  cluster.barrier_arrive();              // (no block leaves while another reads its counts)
   for (int e = threadIdx.x; e < N; e += blockDim.x) {
     int before = 0, all = 0;
-#pragma unroll 8
     for (int b = 0; b < blocks; ++b) {
-      const int c = *cluster.map_shared_rank(total + e, b);
+      const int c = theirs[b * N + e];
       before += b < rank ? c : 0;
       all += c;
     }
@@ -111,7 +130,6 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
     every[e] = all;
   }
   __syncthreads();
-  cluster.barrier_arrive();              // (no block leaves while another reads its counts)
   if (warp == 0) {                       // running sum over the experts, a piece for each lane
     const int per = (N + 31) / 32, e0 = min(N, lane * per), e1 = min(N, e0 + per);
     int sum = 0;
@@ -133,7 +151,7 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
   for (int64_t s0 = begin; s0 < end; s0 += 32 * kStrips) {
     if constexpr (!ONCE) {
       load(s0);
-      take();                            // (the counters have become the run's first places)
+      take(s0);                          // (the counters have become the run's first places)
     }
 #pragma unroll
     for (int i = 0; i < kStrips; ++i) {
@@ -592,9 +610,13 @@ int launch_rows(const RowArgs& a, int32_t dtype, int width, cudaStream_t stream)
 template <bool ONCE>
 cudaError_t launch_sort(const SortArgs& a, int blocks, int warps, cudaStream_t stream) {
   static std::atomic<bool> ready[kMaxDevices];
-  const cudaError_t e = allow_dynamic_smem(sort_kernel<ONCE>, (size_t)(kSortWarps + 3) * REMOE_SORT_MAX_EXPERTS * 4, ready);
+  if (blocks > 8) {
+    const cudaError_t e = cudaFuncSetAttribute(sort_kernel<ONCE>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
+  const cudaError_t e = allow_dynamic_smem(sort_kernel<ONCE>, (size_t)(kSortWarps + 3 + kSortBlocks) * REMOE_SORT_MAX_EXPERTS * 4, ready);
   if (e != cudaSuccess) return e;
-  return rows::launch<sort_kernel<ONCE>>(a, blocks, blocks, warps * 32, (size_t)(warps + 3) * a.n_experts * 4, stream);
+  return rows::launch<sort_kernel<ONCE>>(a, blocks, blocks, warps * 32, (size_t)(warps + 3 + blocks) * a.n_experts * 4, stream);
 }
 
 int check_rows_call(int32_t n_tokens, int32_t top_k, int32_t hidden, int32_t dtype, const int32_t* rows_dev, int32_t n_rows) {
@@ -620,7 +642,9 @@ extern "C" int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_expe
   SortArgs a{ids_dev, rows_dev, offsets_dev, n_tokens * top_k, n_experts, 0};
   const int strips = (a.n + 31) / 32;
   int blocks = 1;
-  while (blocks < 8 && strips > blocks * kSortWarps) blocks *= 2;
+  // One block for up to 4096 selections (2048: 5.2 us, shared between two blocks 7.8; 8192: 9.5 and, between eight, 8.1), else the most that a
+  // cluster may have, and for more than their registers hold the sixteen that this GPU can give (262144: 41 us with eight, 24 with sixteen).
+  if (strips > kSortWarps * kStrips / 2) blocks = strips > 8 * kSortWarps * kStrips ? kSortBlocks : 8;
   int warps = (strips + blocks - 1) / blocks;
   warps = warps < 4 ? 4 : warps > kSortWarps ? kSortWarps : warps;
   a.run = (int)(((int64_t)strips + warps * blocks - 1) / (warps * blocks)) * 32;
