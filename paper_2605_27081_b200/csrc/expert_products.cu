@@ -20,8 +20,8 @@
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
 // leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
 // since a copy would run over the next expert's first rows.  kGradBlocks has the rows of its output as lanes: a thread's 32 columns are 64
-// bytes of one row and leave straight from the registers.  (Through shared memory, with m = hidden, the same took 7 instead of 4 thousand
-// cycles a tile; TMA stores queue behind the loads.)  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
+// bytes of one row and leave straight from the registers.  (Through shared memory, with m = hidden, the gradient of 64 blocks of 1408 x 2048
+// from 24576 rows took 460 to 467 us instead of 451.)  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -148,7 +148,15 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Waits for the loads from TMEM under way, whose registers pass through so that nothing reads them before.
+template <int N>
+__device__ __forceinline__ void ld_wait(float (&v)[N]) {
+  static_assert(N % 8 == 0, "eight registers a time");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7])::"memory");
+#pragma unroll
+  for (int i = 8; i < N; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7])::"memory");
+}
 // 16 lanes x 8 fp32 columns of TMEM as two 8 x 8 fragments: the thread holds, of lane T / 4, the columns 2 (T % 4) and the next in v[0],
 // v[1], and of lane T / 4 + 8 the same in v[2], v[3].  The caller waits.
 __device__ __forceinline__ void tmem_fragments(uint32_t taddr, float* v) {
@@ -605,7 +613,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     for (int tile = 0; walk.next(g); ++tile) {
       if ((tile & 1) != group) continue;
       if (ok) {
-        ok = !aborted() && wait(acc_full + group, (tile >> 1) & 1, long_wait());
+        ok = __all_sync(0xffffffffu, !aborted() && wait(acc_full + group, (tile >> 1) & 1, long_wait()));
         fence_after();
       }
       if constexpr (MODE == kGradBlocks) {
@@ -618,7 +626,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         for (int c0 = 0; c0 < g.n; c0 += 32) {
           uint32_t packed[16];
           if (some) {
-            ld_wait();
+            ld_wait(v);
 #pragma unroll
             for (int c = 0; c < 16; ++c) packed[c] = pack<T>(v[2 * c], v[2 * c + 1]);
             if (c0 + 32 < g.n) tmem_columns(col + c0 + 32, v);
@@ -666,11 +674,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           third = third == 2 ? 0 : third + 1;
         }
         const uint32_t buffer_at = smem_u32(buffer);
-        if (MODE == kGradAct && ok) ok = wait(kept_full + 2 * group + at.s, at.turn);
+        if (MODE == kGradAct && ok) ok = __all_sync(0xffffffffu, wait(kept_full + 2 * group + at.s, at.turn));
 #pragma unroll 1
         for (int c = c0; c < min(c0 + kCols, g.n); c += 8) {
           float v[8];
-          if (some) ld_wait();
+          if (some) ld_wait(f);
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[i] = some ? f[i] : ok ? 0.f : __uint_as_float(0x7fc00000u);
           if (c + 8 < g.n) {
