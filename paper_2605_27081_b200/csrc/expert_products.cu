@@ -12,9 +12,8 @@
 // Operands come through tensor maps straight from where the caller keeps them: K-major tiles (k contiguous) are [128 rows x 64],
 // MN-major ones two [64 x 64] boxes with k as the rows; both are the 128-byte-swizzled images the tensor cores read.
 // Per CTA: warp 0 loads (TMA, a ring of stages of 64 k, 32 KB), warp 1 of the pair's even CTA issues the products, warps 4-7 and 8-11 read the
-// results out of TMEM (two buffers of 256 columns, a buffer and every other tile for each four, so that a tile's epilogue runs behind the next
-// tiles' products).  With k = row
-// (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
+// results out of TMEM (two buffers of 256 columns, so that a tile's epilogue runs behind the next tile's products; every other group of columns
+// for each four, so that a tile alone is out sooner).  With k = row (kGradBlocks) an expert's last rows end inside a stage; what follows them there (the next expert's rows, or memory that nobody has
 // written) would enter the sums, so warp 2 stands between the copies of such a stage and the products and clears it in both operands, up to the
 // sixteen rows of an instruction.
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
@@ -352,7 +351,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       mbar_init(landed + s, 1);
       mbar_init(empty + s, 1);
     }
-    for (int b = 0; b < 2; ++b) { mbar_init(acc_full + b, 1); mbar_init(acc_empty + b, 8); }
+    for (int b = 0; b < 2; ++b) { mbar_init(acc_full + b, 1); mbar_init(acc_empty + b, 16); }
     mbar_init(drain, 1);
     for (int b = 0; b < 4; ++b) { mbar_init(kept_full + b, 1); mbar_init(kept_empty + b, 4); }
     mbar_fence_init();
@@ -406,7 +405,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   };
 
   auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
-  // for a wait of up to two tiles: more polls for more of k
+  // for a wait of a whole tile: more polls for more of k
   auto long_wait = [&]() { return kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u; };
 
   if (warp != 0) dependency_wait();                      // (the kernel in front may run for longer than a bounded wait)
@@ -578,10 +577,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       Place<2> at;
       int64_t groups = 0;
       bool ok = true;
-      for (int tile = 0; ok && !uniform(aborted()) && walk.next(g); ++tile) {
-        if ((tile & 1) != group) continue;
+      while (ok && !uniform(aborted()) && walk.next(g)) {
         const int ch = g.m0 + cta * 128;
-        for (int c0 = 0; c0 < g.n; c0 += kCols) {
+        for (int c0 = group * kCols; c0 < g.n; c0 += 2 * kCols) {
           if (groups >= 2) {
             ok = __all_sync(0xffffffffu, wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait()));
             if (!ok) break;
@@ -609,36 +607,49 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     int third = 0;                                       // kGateUp without kept gates: act alone goes through each third of the buffer in turn
     bool ok = true;
     const bool keep = MODE == kGateUp && a.kept;
-    const uint32_t col = tmem + lanes + (uint32_t)group * kTile;
     for (int tile = 0; walk.next(g); ++tile) {
-      if ((tile & 1) != group) continue;
+      const int acc = tile & 1, from = group * kCols, by = 2 * kCols;        // columns from, from + by, ..: kCols each
+      const uint32_t col = tmem + lanes + (uint32_t)acc * kTile;
       if (ok) {
-        ok = __all_sync(0xffffffffu, !aborted() && wait(acc_full + group, (tile >> 1) & 1, long_wait()));
+        ok = __all_sync(0xffffffffu, !aborted() && wait(acc_full + acc, (tile >> 1) & 1, long_wait()));
         fence_after();
       }
+      auto read_out = [&]() {                            // the buffer is free for the products, as far as this warp goes
+        fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_at(in_even_cta(acc_empty + acc));
+      };
+      if (from >= g.n) {
+        read_out();
+        continue;
+      }
       if constexpr (MODE == kGradBlocks) {
-        const int ch = g.m0 + cta * 128 + quad * 32 + lane;
+        static_assert(MODE != kGradBlocks || kCols == 32, "columns of one load");
+        const int ch0 = g.m0 + cta * 128 + quad * 32, ch = ch0 + lane;
         const bool there = ch < a.I;
-        uint16_t* out = a.out + (size_t)g.e * a.block_stride + ((size_t)ch * 3 + g.plane) * a.H + g.row;
+        uint16_t* block = a.out + (size_t)g.e * a.block_stride + (size_t)g.plane * a.H + g.row;
+        if (g.pieces == 0 && ok) {                       // an expert without rows: zeros, half of a row's columns a warp and access
+          read_out();
+          const int c = group * 128 + (lane & 15) * 8;
+          for (int r = lane >> 4; r < 32; r += 2)
+            if (ch0 + r < a.I && c < g.n) *reinterpret_cast<uint4*>(block + (size_t)(ch0 + r) * 3 * a.H + c) = make_uint4(0, 0, 0, 0);
+          continue;
+        }
+        uint16_t* out = block + (size_t)ch * 3 * a.H;
         float v[32];
-        const bool some = g.pieces && ok;
-        if (some) tmem_columns(col, v);
-        for (int c0 = 0; c0 < g.n; c0 += 32) {
+        if (ok) tmem_columns(col + from, v);
+        for (int c0 = from; c0 < g.n; c0 += by) {
           uint32_t packed[16];
-          if (some) {
+          if (ok) {
             ld_wait(v);
 #pragma unroll
             for (int c = 0; c < 16; ++c) packed[c] = pack<T>(v[2 * c], v[2 * c + 1]);
-            if (c0 + 32 < g.n) tmem_columns(col + c0 + 32, v);
+            if (c0 + by < g.n) tmem_columns(col + c0 + by, v);
           } else {
 #pragma unroll
-            for (int c = 0; c < 16; ++c) packed[c] = ok ? 0u : 0x7fff7fffu;           // NaN in either type
+            for (int c = 0; c < 16; ++c) packed[c] = 0x7fff7fffu;                      // NaN in either type
           }
-          if (c0 + 32 >= g.n) {                          // read out: the buffer is free for the products
-            fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
-          }
+          if (c0 + by >= g.n) read_out();
           if (there) {
 #pragma unroll
             for (int c = 0; c < 2; ++c)
@@ -656,7 +667,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       }
       // Eight columns a time, in a loop that is not unrolled (a tile of few rows runs its code once, from cold instruction caches: unrolled over
       // 32 columns this took 4.5 us of one token's 18), the next eight on their way meanwhile; kCols of them leave together.
-      const bool some = g.pieces && ok;
+      const bool some = ok;
       float f[8];                                        // fragments of lanes 0-15 and 16-31 of the warp's quarter
       auto fetch = [&](int c) {
         if (some) {
@@ -664,9 +675,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           tmem_fragments(col + c + (16u << 16), f + 4);
         }
       };
-      fetch(0);
+      fetch(from);
 #pragma unroll 1
-      for (int c0 = 0; c0 < g.n; c0 += kCols) {
+      for (int c0 = from; c0 < g.n; c0 += by) {
         const bool whole = c0 + kCols <= g.n;
         unsigned char* buffer = staging + group * S::kBuffer;
         if (MODE == kGateUp && !keep) {
@@ -680,14 +691,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           float v[8];
           if (some) ld_wait(f);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = some ? f[i] : ok ? 0.f : __uint_as_float(0x7fc00000u);
-          if (c + 8 < g.n) {
-            fetch(c + 8);
-          } else {                                       // read out: the buffer is free for the products
-            fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_at(in_even_cta(acc_empty + group));
-          }
+          for (int i = 0; i < 8; ++i) v[i] = some ? f[i] : __uint_as_float(0x7fc00000u);
+          const int next = c + 8 < c0 + kCols ? c + 8 : c0 + by;
+          if (next < g.n) fetch(next);
+          else read_out();
           auto free_buffer = [&]() {                     // before the first eight columns are written
             if (c != c0) return;
             if (issuer && elect_one()) {

@@ -230,20 +230,26 @@ struct RowArgs {
 
 constexpr int kGroup = 8;                // rows of a token whose loads are under way together
 
-// One block a token: its row is read once and written to the places of its selections.
+// One block a token: its row is read once, kUnroll pieces under way together, and written to the places of its selections.
 template <typename T, int V>
 __global__ void __launch_bounds__(256) dispatch_kernel(const __grid_constant__ RowArgs a) {
+  constexpr int kUnroll = 4;
   const int64_t t = blockIdx.x;
   const int* rows = a.rows + t * a.K;
   const T* x = static_cast<const T*>(a.a) + t * a.a_stride;
   T* out = static_cast<T*>(a.out);
   const int body = a.H / V;
-  for (int i = threadIdx.x; i < body; i += blockDim.x) {
-    Vec<T, V> v;
-    v.load(x + i * V);
+  for (int i0 = threadIdx.x; i0 < body; i0 += kUnroll * blockDim.x) {
+    Vec<T, V> v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (i0 + u * (int)blockDim.x < body) v[u].load(x + (i0 + u * (int)blockDim.x) * V);
     for (int k = 0; k < a.K; ++k) {
       const int r = __ldg(rows + k);
-      if ((unsigned)r < (unsigned)a.n_rows) v.store(out + r * a.out_stride + i * V);
+      if ((unsigned)r >= (unsigned)a.n_rows) continue;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u)
+        if (i0 + u * (int)blockDim.x < body) v[u].store(out + r * a.out_stride + (i0 + u * (int)blockDim.x) * V);
     }
   }
   for (int i = body * V + threadIdx.x; i < a.H; i += blockDim.x) {
@@ -254,6 +260,10 @@ __global__ void __launch_bounds__(256) dispatch_kernel(const __grid_constant__ R
     }
   }
 }
+
+// Blocks of 256 threads that lie on an SM together: what a group's rows take in registers decides.
+template <typename T, int V, bool TAIL>
+constexpr int resident_blocks() { return V * sizeof(T) < 8 ? 4 : TAIL ? 2 : 3; }
 
 // The rows and gates of a token, a lane each (up to 32 of them), loaded an item ahead of their use.
 struct Picks {
@@ -303,7 +313,7 @@ __device__ __forceinline__ void add_rows(const RowArgs& a, int64_t t, Picks p, i
 // An item is a piece of a token's row for a.threads threads (whole warps), V elements each, in float32; the elements behind the last whole V
 // are pieces of one.  Persistent: the next item's rows and gates are on their way while this one's data is.
 template <typename T, int V, bool TAIL>
-__global__ void __launch_bounds__(256, TAIL ? 2 : 3) combine_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_kernel(const __grid_constant__ RowArgs a) {
   const int lane = threadIdx.x & 31, body = a.H / V, pieces = body + a.H % V, step = (int)blockDim.x / a.threads;
   const int64_t items = (int64_t)a.n_tokens * a.parts, stride = (int64_t)gridDim.x * step;
   int64_t item = (int64_t)blockIdx.x * step + threadIdx.x / a.threads;
@@ -499,7 +509,7 @@ __device__ __forceinline__ float reduce_eight(float (&x)[kGroup], int lane) {
 // A token for a.threads threads, one warp (several tokens a block) or the whole block: the gradient of the sum is read once for up to eight of
 // its rows, whose scalar products with it are summed in a fixed order.  Persistent as above.
 template <typename T, int V, bool TAIL>
-__global__ void __launch_bounds__(256, TAIL ? 2 : 3) combine_backward_kernel(const __grid_constant__ RowArgs a) {
+__global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_backward_kernel(const __grid_constant__ RowArgs a) {
   __shared__ float part[2][8][kGroup];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, body = a.H / V, pieces = body + a.H % V, step = (int)blockDim.x / a.threads;
   const int64_t stride = (int64_t)gridDim.x * step;
@@ -564,11 +574,11 @@ cudaError_t launch_rows_as(const RowArgs& args, cudaStream_t stream) {
       if (e != cudaSuccess) return e;
       return rows::launch<combine_copy_kernel<T, V>>(a, 148 * 3, 1, step * a.threads, kUnit * step * a.threads, stream);
     }
-    return rows::launch<combine_kernel<T, V, TAIL>>(a, std::min<int64_t>(blocks, 148 * (TAIL ? 2 : 3)), 1, step * a.threads, 0, stream);
+    return rows::launch<combine_kernel<T, V, TAIL>>(a, std::min<int64_t>(blocks, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
   }
   if constexpr (OP == kCombineBackward) {
     const int step = a.threads == 32 ? 8 : 1;
-    return rows::launch<combine_backward_kernel<T, V, TAIL>>(a, std::min<int64_t>((a.n_tokens + step - 1) / step, 148 * (TAIL ? 2 : 3)), 1, step * a.threads, 0, stream);
+    return rows::launch<combine_backward_kernel<T, V, TAIL>>(a, std::min<int64_t>((a.n_tokens + step - 1) / step, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
   }
 }
 
