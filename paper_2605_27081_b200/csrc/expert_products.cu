@@ -156,11 +156,13 @@ __device__ __forceinline__ void ld_wait(float (&v)[N]) {
   for (int i = 8; i < N; i += 8)
     asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7])::"memory");
 }
-// 16 lanes x 8 fp32 columns of TMEM as two 8 x 8 fragments: the thread holds, of lane T / 4, the columns 2 (T % 4) and the next in v[0],
-// v[1], and of lane T / 4 + 8 the same in v[2], v[3].  The caller waits.
+// 16 lanes x 16 fp32 columns of TMEM as 8 x 8 fragments: for the columns 8 i .. 8 i + 7 the thread holds, of lane T / 4, the columns 2 (T % 4) and
+// the next in v[4 i], v[4 i + 1], and of lane T / 4 + 8 the same in v[4 i + 2], v[4 i + 3].  The caller waits.
 __device__ __forceinline__ void tmem_fragments(uint32_t taddr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
-  asm volatile("tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr));
+  asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
 }
 // 32 consecutive fp32 columns of this thread's lane.  The caller waits.
 __device__ __forceinline__ void tmem_columns(uint32_t taddr, float (&v)[32]) {
@@ -183,9 +185,6 @@ __device__ __forceinline__ void store_32_bytes(void* p, const uint32_t* v) {
 // (lane % 8) of matrix (lane / 8), a row being the fragment's column.
 __device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
-}
-__device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1) {       // two matrices, addresses from lanes 0-15
-  asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(addr), "r"(r0), "r"(r1) : "memory");
 }
 __device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -665,14 +664,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         }
         continue;
       }
-      // Eight columns a time, in a loop that is not unrolled (a tile of few rows runs its code once, from cold instruction caches: unrolled over
-      // 32 columns this took 4.5 us of one token's 18), the next eight on their way meanwhile; kCols of them leave together.
+      // Sixteen columns a time, in a loop that is not unrolled (a tile of few rows runs its code once, from cold instruction caches: unrolled over
+      // 32 columns this took 4.5 us of one token's 18), the next sixteen on their way meanwhile; kCols of them leave together.
       const bool some = ok;
-      float f[8];                                        // fragments of lanes 0-15 and 16-31 of the warp's quarter
+      float f[16];                                       // fragments of lanes 0-15 and 16-31 of the warp's quarter
       auto fetch = [&](int c) {
         if (some) {
           tmem_fragments(col + c, f);
-          tmem_fragments(col + c + (16u << 16), f + 4);
+          tmem_fragments(col + c + (16u << 16), f + 8);
         }
       };
       fetch(from);
@@ -687,15 +686,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         const uint32_t buffer_at = smem_u32(buffer);
         if (MODE == kGradAct && ok) ok = __all_sync(0xffffffffu, wait(kept_full + 2 * group + at.s, at.turn));
 #pragma unroll 1
-        for (int c = c0; c < min(c0 + kCols, g.n); c += 8) {
-          float v[8];
+        for (int c = c0; c < min(c0 + kCols, g.n); c += 16) {
+          float v[16];
           if (some) ld_wait(f);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = some ? f[i] : __uint_as_float(0x7fc00000u);
-          const int next = c + 8 < c0 + kCols ? c + 8 : c0 + by;
+          for (int i = 0; i < 16; ++i) v[i] = some ? f[i] : __uint_as_float(0x7fc00000u);
+          const int next = c + 16 < c0 + kCols ? c + 16 : c0 + by;
           if (next < g.n) fetch(next);
           else read_out();
-          auto free_buffer = [&]() {                     // before the first eight columns are written
+          auto free_buffer = [&]() {                     // before the first columns are written
             if (c != c0) return;
             if (issuer && elect_one()) {
               if (MODE == kGateUp && !keep) stores_read<2>();
@@ -704,47 +703,63 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
             __syncwarp();
             epilogue_bar(group);
           };
-          const int row = c - c0 + (lane & 7);           // of the matrices that this lane addresses
           if constexpr (MODE == kGateUp) {
             // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.
-            const uint32_t act0 = pack<T>(v[0] * sigmoid(v[0]) * v[2], v[1] * sigmoid(v[1]) * v[3]);
-            const uint32_t act1 = pack<T>(v[4] * sigmoid(v[4]) * v[6], v[5] * sigmoid(v[5]) * v[7]);
+            uint32_t act[4];                             // two groups of columns x two of channels
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float* w = v + (j & 1) * 8 + (j >> 1) * 4;
+              act[j] = pack<T>(w[0] * sigmoid(w[0]) * w[2], w[1] * sigmoid(w[1]) * w[3]);
+            }
             free_buffer();
-            const int chunk = quad * 2 + ((lane >> 3) & 1);
+            const int row = c - c0 + (lane >> 4) * 8 + (lane & 7), chunk = quad * 2 + ((lane >> 3) & 1);       // that this lane addresses
             const uint32_t to = buffer_at + row * 128 + ((chunk ^ (row & 7)) << 4);
-            store_turned(to, act0, act1);
+            store_turned(to, act[0], act[1], act[2], act[3]);
             if (keep) {
-              store_turned(to + 4096, pack<T>(v[0], v[1]), pack<T>(v[4], v[5]));
-              store_turned(to + 8192, pack<T>(v[2], v[3]), pack<T>(v[6], v[7]));
+              store_turned(to + 4096, pack<T>(v[0], v[1]), pack<T>(v[8], v[9]), pack<T>(v[4], v[5]), pack<T>(v[12], v[13]));
+              store_turned(to + 8192, pack<T>(v[2], v[3]), pack<T>(v[10], v[11]), pack<T>(v[6], v[7]), pack<T>(v[14], v[15]));
             }
           } else if constexpr (MODE == kGradAct) {
             // two halves of 64 channels: [2 planes x 16 rows x 128 bytes] of gates and ups, [3 planes x ...] of what leaves
-            const uint32_t in_row = row * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (row & 7)) << 4);
+            const uint32_t in_row = (lane & 7) * 128 + ((((quad & 1) * 4 + (lane >> 3)) ^ (lane & 7)) << 4);
             const uint32_t kept_at = smem_u32(staging) + 2 * S::kBuffer + (2 * group + at.s) * 8192 + (quad >> 1) * 4096 + in_row;
-            uint32_t gates[4], ups[4], acts[4];
-            load_turned(kept_at, gates);
-            load_turned(kept_at + 2048, ups);
+            uint32_t gates[2][4], ups[2][4], acts[2][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              float2 gate = unpack<T>(gates[j]);
-              const float2 up = unpack<T>(ups[j]);
-              if (!ok) gate.x = gate.y = __uint_as_float(0x7fc00000u);
-              const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
-              gates[j] = pack<T>(v[2 * j] * up.x * s0 * (1.f + gate.x * (1.f - s0)), v[2 * j + 1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
-              ups[j] = pack<T>(v[2 * j] * gate.x * s0, v[2 * j + 1] * gate.y * s1);
-              acts[j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
+            for (int i = 0; i < 2; ++i) {
+              load_turned(kept_at + i * 1024, gates[i]);
+              load_turned(kept_at + i * 1024 + 2048, ups[i]);
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float* w = v + (j >> 1) * 8 + i * 4 + (j & 1) * 2;
+                float2 gate = unpack<T>(gates[i][j]);
+                const float2 up = unpack<T>(ups[i][j]);
+                if (!ok) gate.x = gate.y = __uint_as_float(0x7fc00000u);
+                const float s0 = sigmoid(gate.x), s1 = sigmoid(gate.y);
+                gates[i][j] = pack<T>(w[0] * up.x * s0 * (1.f + gate.x * (1.f - s0)), w[1] * up.y * s1 * (1.f + gate.y * (1.f - s1)));
+                ups[i][j] = pack<T>(w[0] * gate.x * s0, w[1] * gate.y * s1);
+                acts[i][j] = pack<T>(gate.x * s0 * up.x, gate.y * s1 * up.y);
+              }
             free_buffer();
             const uint32_t to = buffer_at + (quad >> 1) * 6144 + in_row;
-            store_turned(to, gates[0], gates[1], gates[2], gates[3]);
-            store_turned(to + 2048, ups[0], ups[1], ups[2], ups[3]);
-            store_turned(to + 4096, acts[0], acts[1], acts[2], acts[3]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              store_turned(to + i * 1024, gates[i][0], gates[i][1], gates[i][2], gates[i][3]);
+              store_turned(to + i * 1024 + 2048, ups[i][0], ups[i][1], ups[i][2], ups[i][3]);
+              store_turned(to + i * 1024 + 4096, acts[i][0], acts[i][1], acts[i][2], acts[i][3]);
+            }
           } else {
             // output rows of 128 values in two halves of [32 rows x 128 bytes]
-            const uint32_t v0 = pack<T>(v[0], v[1]), v1 = pack<T>(v[2], v[3]), v2 = pack<T>(v[4], v[5]), v3 = pack<T>(v[6], v[7]);
+            uint32_t w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = pack<T>(v[2 * j], v[2 * j + 1]);
             free_buffer();
             const int chunk = (quad & 1) * 4 + (lane >> 3);
-            store_turned(buffer_at + (quad >> 1) * 4096 + row * 128 + ((chunk ^ (row & 7)) << 4), v0, v1, v2, v3);
+            const uint32_t to = buffer_at + (quad >> 1) * 4096 + (c - c0 + (lane & 7)) * 128 + ((chunk ^ (lane & 7)) << 4);
+            store_turned(to, w[0], w[1], w[4], w[5]);
+            store_turned(to + 1024, w[2], w[3], w[6], w[7]);
           }
         }
         if constexpr (MODE == kGradAct) {
