@@ -229,23 +229,27 @@ struct Tile {
   int plane = 0;                                         // kGradBlocks: plane of the block
   int first_row = 0, count = 0;                          // kGradBlocks: the expert's rows
   int pieces = 0;                                        // of k
-  __device__ __forceinline__ void make_uniform() {
-    e = uniform(e); row = uniform(row); n = uniform(n); half = uniform(half); m0 = uniform(m0);
-    plane = uniform(plane); first_row = uniform(first_row); count = uniform(count); pieces = uniform(pieces);
-  }
 };
 
 // The tiles of a launch in the order of experts, dealt to the pairs in turn: a pair's next tile is as many further as there are pairs.  Each
-// role of a CTA walks them by itself, a whole warp together, in steps of mixed digits (no division a tile).  upto [N + 1]: tiles of N of lower
-// experts; first [N + 1]: rows of the experts, ascending.
+// role of a CTA walks them by itself, a whole warp together, in steps of mixed digits (no division a tile), with the table of the experts
+// (first [N + 1]: their rows, ascending; upto [N + 1]: tiles of N of lower experts) looked at through a window of 32 entries, one in each lane:
+// shared memory, busy with operands, takes some hundred cycles to answer, and every tile would wait for it several times.
 template <int MODE>
 struct Walk {
   const ProductArgs& a;
   const int* first;
   const int* upto;
-  int m_tiles, n_tiles, m, i, j, e, size;                // tile of M, tile of N of all experts, expert, rows of N in a tile; kGradBlocks: of N, of M, plane
+  int base, row_at, tiles_at;                            // window from expert `base` on: entries first[base + lane], upto[base + lane]
+  int m_tiles, n_tiles, m, i, j, e, total;               // tile of M, tile of N of all experts (of `total`), expert; kGradBlocks: of N, of M, plane
   int step_m, step_i, step_j, step_e;
-  __device__ Walk(const ProductArgs& args, const int* first_, const int* upto_) : a(args), first(first_), upto(upto_), e(0), size(0) {
+  __device__ __forceinline__ void look(int from) {
+    base = from;
+    const int x = min(from + ((int)threadIdx.x & 31), a.n_experts);
+    row_at = first[x];
+    tiles_at = upto[x];
+  }
+  __device__ Walk(const ProductArgs& args, const int* first_, const int* upto_) : a(args), first(first_), upto(upto_), e(0) {
     const int rows = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
     const int pairs = (int)gridDim.x >> 1, pair = (int)blockIdx.x >> 1;
     m_tiles = (rows + kTile - 1) / kTile;
@@ -259,17 +263,20 @@ struct Walk {
       step_j = step_i / n_tiles; step_i %= n_tiles;
       step_e = step_j / 3; step_j %= 3;
     }
+    total = upto[a.n_experts];
+    look(MODE == kGradBlocks ? min(e, a.n_experts) : 0);
   }
   __device__ bool next(Tile& g) {
     if constexpr (MODE == kGradBlocks) {
       if (e >= a.n_experts) return false;
+      if (e > base + 30) look(e);
       g.e = e;
       g.plane = j;
       g.m0 = i * kTile;
       g.row = m * kTile;
       g.n = min(kTile, a.H - g.row);
-      g.first_row = first[e];
-      g.count = first[e + 1] - g.first_row;
+      g.first_row = __shfl_sync(0xffffffffu, row_at, e - base);
+      g.count = __shfl_sync(0xffffffffu, row_at, e - base + 1) - g.first_row;
       g.pieces = (g.count + kK - 1) / kK;
       m += step_m;
       i += step_i;
@@ -279,23 +286,16 @@ struct Walk {
       e += step_e;
       if (j >= 3) { j -= 3; ++e; }
     } else {
-      if (i >= upto[a.n_experts]) return false;
-      bool moved = size == 0;
-      for (int lane = threadIdx.x & 31;;) {              // past the experts whose tiles end before this one, up to 32 a look
-        const int x = e + 1 + lane;
-        const unsigned behind = __ballot_sync(0xffffffffu, x <= a.n_experts && upto[x] <= i);
-        e += __popc(behind);
-        moved |= behind != 0;
-        if (behind != 0xffffffffu) break;
-      }
-      const int count = first[e + 1] - first[e], before = upto[e];
-      if (moved) {                                       // the expert's rows in equal tiles
-        const int tiles = upto[e + 1] - before;
-        size = ((tiles == 1 ? count : (count + tiles - 1) / tiles) + 31) / 32 * 32;
-      }
-      g.e = e;
+      if (i >= total) return false;
+      // the last expert with no more tiles in front of it than this one has: the one with this tile
+      int behind;
+      while ((behind = __popc(__ballot_sync(0xffffffffu, tiles_at <= i))) == 32) look(base + 31);
+      const int at = behind - 1, row = __shfl_sync(0xffffffffu, row_at, at), count = __shfl_sync(0xffffffffu, row_at, at + 1) - row;
+      const int before = __shfl_sync(0xffffffffu, tiles_at, at), tiles = __shfl_sync(0xffffffffu, tiles_at, at + 1) - before;
+      const int size = ((tiles == 1 ? count : (count + tiles - 1) / tiles) + 31) / 32 * 32;       // its rows in equal tiles
+      g.e = base + at;
       g.m0 = m * (MODE == kGateUp ? kTile / 2 : kTile);
-      g.row = first[e] + (i - before) * size;
+      g.row = row + (i - before) * size;
       g.n = min(size, count - (i - before) * size);
       const int k = MODE == kDown || MODE == kGradRows ? a.I : a.H;
       g.pieces = (k + kK - 1) / kK * (MODE == kGradRows ? 2 : 1);
@@ -336,15 +336,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   uint64_t* kept_full = drain + 1;                       // [4] kGradAct: kept gates and ups are there
   uint64_t* kept_empty = kept_full + 4;                  // [4] they have been read by four warps
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(kept_empty + 4);
-  int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
-  int* first = abort_flag + 1;                           // [N + 1]
+  int* first = reinterpret_cast<int*>(tmem_slot + 1);    // [N + 1]
   int* upto = first + a.n_experts + 1;                   // [N + 1]
 
   launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cta = (int)cluster_rank();
   if (tid == 0) {
-    *abort_flag = 0;
     for (int s = 0; s < kStages; ++s) {
       mbar_init(full + s, kRagged ? 2 : 1);
       mbar_init(landed + s, 1);
@@ -395,15 +393,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   const uint32_t tmem = *tmem_slot;
   Walk<MODE> walk(a, first, upto);
   Tile g;
-  // After a wait that ran out a role stops, and the others of its CTA with their next tile (or their own next wait).
-  auto aborted = [&]() { return *(volatile int*)abort_flag != 0; };
-  auto wait = [&](uint64_t* bar, uint32_t parity, unsigned polls = kPolls) {
-    if (mbar_wait(bar, parity, polls)) return true;
-    *(volatile int*)abort_flag = 1;
-    return false;
+  // A wait by a whole warp.  After one that ran out its role stops, whatever waits for that role runs out in its turn, and the results stay NaN.
+  auto warp_wait = [&](uint64_t* bar, uint32_t parity, unsigned polls = kPolls) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, polls)) != 0;
   };
-
-  auto warp_wait = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait(bar, parity)) != 0; };
   // for a wait of a whole tile: more polls for more of k
   auto long_wait = [&]() { return kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u; };
 
@@ -414,8 +407,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     int64_t stages = 0;                                  // issued
     bool ok = true;
     const uint32_t ring = uniform((int)smem_u32(smem)), bars = uniform((int)in_even_cta(full)), own_bars = uniform((int)smem_u32(landed));
-    while (ok && !uniform(aborted()) && uniform(walk.next(g))) {
-      g.make_uniform();
+    while (ok && walk.next(g)) {
       int box = 0;
       if constexpr (kRagged) box = g.half > 64 ? 2 : 1;  // copies of 64 columns
       else while (box_rows(box) < g.half) ++box;
@@ -495,8 +487,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     for (int64_t i = stages > kStages ? stages - kStages : 0; i < stages; ++i) {
       const int s = (int)(i % kStages);
       const uint32_t turn = (uint32_t)(i / kStages) & 1;
-      if (ok) wait(empty + s, turn);
-      else wait(full + s, turn);
+      if (ok) warp_wait(empty + s, turn);
+      else warp_wait(full + s, turn);
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------------------------------------ products
@@ -511,9 +503,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       Place<kStages> at;
       int acc = 0;
       bool ok = true;
-      while (!uniform(aborted()) && uniform(walk.next(g))) {
-        g.make_uniform();
-        if (acc >= 2) ok = warp_wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
+      while (walk.next(g)) {
+          if (acc >= 2) ok = warp_wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
         if (!ok) break;
         fence_after();
         const uint32_t d = d0 + (uint32_t)(acc & 1) * kTile, idesc = kIdesc | ((uint32_t)(2 * g.half) >> 3 << 17);
@@ -549,11 +540,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         int at = 0;                                      // stage of a tile's first piece
         uint32_t turns = 0;                              // parity of each stage's next landing
         bool ok = true;
-        while (ok && !uniform(aborted()) && walk.next(g)) {
+        while (ok && walk.next(g)) {
           const int s = (at + max(g.pieces, 1) - 1) % kStages, left = g.count - (g.pieces - 1) * kK;
           at = (at + g.pieces) % kStages;
           if (left % 16 == 0) continue;
-          ok = __all_sync(0xffffffffu, wait(landed + s, (turns >> s) & 1, long_wait()));
+          ok = warp_wait(landed + s, (turns >> s) & 1, long_wait());
           if (!ok) break;
           turns ^= 1u << s;
           // a row of the blocks of 64 rows a time, two of M and those of N
@@ -576,11 +567,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       Place<2> at;
       int64_t groups = 0;
       bool ok = true;
-      while (ok && !uniform(aborted()) && walk.next(g)) {
+      while (ok && walk.next(g)) {
         const int ch = g.m0 + cta * 128;
         for (int c0 = group * kCols; c0 < g.n; c0 += 2 * kCols) {
           if (groups >= 2) {
-            ok = __all_sync(0xffffffffu, wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait()));
+            ok = warp_wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait());
             if (!ok) break;
           }
           if (elect_one()) {
@@ -595,7 +586,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         }
       }
       if (!ok)                                           // copies under way land before the CTA leaves
-        for (int64_t i = groups > 2 ? groups - 2 : 0; i < groups; ++i) wait(kept_full + 2 * group + (int)(i & 1), (uint32_t)(i / 2) & 1);
+        for (int64_t i = groups > 2 ? groups - 2 : 0; i < groups; ++i) warp_wait(kept_full + 2 * group + (int)(i & 1), (uint32_t)(i / 2) & 1);
     }
   } else {
     // ------------------------------------------------------------------------------------------------ results
@@ -610,7 +601,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       const int acc = tile & 1, from = group * kCols, by = 2 * kCols;        // columns from, from + by, ..: kCols each
       const uint32_t col = tmem + lanes + (uint32_t)acc * kTile;
       if (ok) {
-        ok = __all_sync(0xffffffffu, !aborted() && wait(acc_full + acc, (tile >> 1) & 1, long_wait()));
+        ok = warp_wait(acc_full + acc, (tile >> 1) & 1, long_wait());
         fence_after();
       }
       auto read_out = [&]() {                            // the buffer is free for the products, as far as this warp goes
@@ -684,7 +675,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           third = third == 2 ? 0 : third + 1;
         }
         const uint32_t buffer_at = smem_u32(buffer);
-        if (MODE == kGradAct && ok) ok = __all_sync(0xffffffffu, wait(kept_full + 2 * group + at.s, at.turn));
+        if (MODE == kGradAct && ok) ok = warp_wait(kept_full + 2 * group + at.s, at.turn);
 #pragma unroll 1
         for (int c = c0; c < min(c0 + kCols, g.n); c += 16) {
           float v[16];
