@@ -72,7 +72,6 @@ struct ProductArgs {
   uint16_t* out;                                         // rows or blocks; kGateUp, kGradAct: [.., n_rows, I]
   uint16_t* kept;                                        // kGateUp: [2, n_rows, I] or null
   int64_t out_stride, block_stride;                      // elements between rows, between blocks
-  bool wide;                                             // kGradBlocks: rows are 32-byte aligned
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -598,7 +597,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     bool ok = true;
     const bool keep = MODE == kGateUp && a.kept;
     for (int tile = 0; walk.next(g); ++tile) {
-      const int acc = tile & 1, from = group * kCols, by = 2 * kCols;        // columns from, from + by, ..: kCols each
+      // columns: kCols each from `from` on, every other such group (kGradBlocks: one half of them)
+      const int half_n = (g.n + 63) / 64 * 32;
+      const int acc = tile & 1, from = MODE == kGradBlocks ? group * half_n : group * kCols, by = MODE == kGradBlocks ? kCols : 2 * kCols;
       const uint32_t col = tmem + lanes + (uint32_t)acc * kTile;
       if (ok) {
         ok = warp_wait(acc_full + acc, (tile >> 1) & 1, long_wait());
@@ -615,42 +616,59 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       }
       if constexpr (MODE == kGradBlocks) {
         static_assert(MODE != kGradBlocks || kCols == 32, "columns of one load");
-        const int ch0 = g.m0 + cta * 128 + quad * 32, ch = ch0 + lane;
-        const bool there = ch < a.I;
+        const int ch0 = g.m0 + cta * 128 + quad * 32, ch = ch0 + lane, end = min(g.n, from + half_n);
         uint16_t* block = a.out + (size_t)g.e * a.block_stride + (size_t)g.plane * a.H + g.row;
-        if (g.pieces == 0 && ok) {                       // an expert without rows: zeros, half of a row's columns a warp and access
+        // Rows start on any 16 bytes, and an access of part of a 32-byte sector costs as much as a whole one (and its turn in L2 more): where a row starts in
+        // the middle of a sector, its pieces begin and end 8 columns later.
+        if (g.pieces == 0 && ok) {                       // an expert without rows: zeros, a row's columns of the tile with each access
           read_out();
-          const int c = group * 128 + (lane & 15) * 8;
-          for (int r = lane >> 4; r < 32; r += 2)
-            if (ch0 + r < a.I && c < g.n) *reinterpret_cast<uint4*>(block + (size_t)(ch0 + r) * 3 * a.H + c) = make_uint4(0, 0, 0, 0);
+          const int rows = min(32, a.I - ch0);
+          uint16_t* out = block + (size_t)(ch0 + group) * 3 * a.H;
+#pragma unroll 4
+          for (int r = group; r < rows; r += 2, out += 6 * (size_t)a.H) {
+            const int late = reinterpret_cast<uintptr_t>(out) & 16 ? 8 : 0;
+            const int c = (g.row ? late : 0) + lane * 8, stop = g.row + g.n < a.H ? g.n + late : g.n;
+            if (c < stop) *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+            if (g.row == 0 && lane == 0 && stop > kTile) *reinterpret_cast<uint4*>(out + kTile) = make_uint4(0, 0, 0, 0);
+          }
           continue;
         }
+        const bool there = ch < a.I;
         uint16_t* out = block + (size_t)ch * 3 * a.H;
+        const bool late = reinterpret_cast<uintptr_t>(out) & 16;
+        uint32_t carry[4] = {0, 0, 0, 0};                // the last 8 columns of the piece before, where pieces are late
         float v[32];
         if (ok) tmem_columns(col + from, v);
-        for (int c0 = from; c0 < g.n; c0 += by) {
+        for (int c0 = from; c0 < end; c0 += by) {
           uint32_t packed[16];
           if (ok) {
             ld_wait(v);
 #pragma unroll
             for (int c = 0; c < 16; ++c) packed[c] = pack<T>(v[2 * c], v[2 * c + 1]);
-            if (c0 + by < g.n) tmem_columns(col + c0 + by, v);
+            if (c0 + by < end) tmem_columns(col + c0 + by, v);
           } else {
 #pragma unroll
             for (int c = 0; c < 16; ++c) packed[c] = 0x7fff7fffu;                      // NaN in either type
           }
-          if (c0 + by >= g.n) read_out();
-          if (there) {
+          if (c0 + by >= end) read_out();
+          if (!there) continue;
+          if (c0 + 32 <= end) {
+            uint32_t piece[16];                          // what is stored now: the same columns, or 8 earlier ones
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-              if (a.wide && c0 + 16 * c + 16 <= g.n) {
-                store_32_bytes(out + c0 + 16 * c, packed + 8 * c);
-              } else {
+            for (int c = 0; c < 16; ++c) piece[c] = !late ? packed[c] : c < 4 ? carry[c] : packed[c - 4];
+            uint16_t* to = out + c0 - (late ? 8 : 0);
+            if (late && c0 == from) *reinterpret_cast<uint4*>(to + 8) = make_uint4(piece[4], piece[5], piece[6], piece[7]);
+            else store_32_bytes(to, piece);
+            store_32_bytes(to + 16, piece + 8);
 #pragma unroll
-                for (int d = 2 * c; d < 2 * c + 2; ++d)
-                  if (c0 + 8 * d < g.n)
-                    *reinterpret_cast<uint4*>(out + c0 + 8 * d) = make_uint4(packed[4 * d], packed[4 * d + 1], packed[4 * d + 2], packed[4 * d + 3]);
-              }
+            for (int c = 0; c < 4; ++c) carry[c] = packed[12 + c];
+            if (late && c0 + 32 == end) *reinterpret_cast<uint4*>(to + 32) = make_uint4(carry[0], carry[1], carry[2], carry[3]);
+          } else {                                       // the last columns of a width that is no multiple of 32
+            if (late && c0 != from) *reinterpret_cast<uint4*>(out + c0 - 8) = make_uint4(carry[0], carry[1], carry[2], carry[3]);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+              if (c0 + 8 * d < end)
+                *reinterpret_cast<uint4*>(out + c0 + 8 * d) = make_uint4(packed[4 * d], packed[4 * d + 1], packed[4 * d + 2], packed[4 * d + 3]);
           }
         }
         continue;
@@ -993,7 +1011,6 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
     }
     a.out = static_cast<uint16_t*>(d_blocks);
     a.block_stride = d_block_stride;
-    a.wide = !rows::misaligned(d_blocks, 32) && c.hidden % 16 == 0 && (c.n_experts == 1 || d_block_stride % 16 == 0);
     if (!enc.ok) return cudaErrorInvalidValue;
     e = launch_product<kGradBlocks, T>(a, c.n_rows > 0, stream);
   }
