@@ -21,6 +21,9 @@
 // since a copy would run over the next expert's first rows.  kGradBlocks has the rows of its output as lanes: a thread's 32 columns are 64
 // bytes of one row and leave straight from the registers.  (Through shared memory, with m = hidden, the gradient of 64 blocks of 1408 x 2048
 // from 24576 rows took 460 to 467 us instead of 451.)  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
+// Where a launch has few tiles of a long k (a shared expert, a few rows), up to four pairs, a cluster, take a part of a tile's k each.  When all have
+// ended, each sends the others its sums of their columns, into the rings, which are idle by then, and finishes columns of its own: the order of the
+// sums is the same in every run.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -72,6 +75,7 @@ struct ProductArgs {
   uint16_t* out;                                         // rows or blocks; kGateUp, kGradAct: [.., n_rows, I]
   uint16_t* kept;                                        // kGateUp: [2, n_rows, I] or null
   int64_t out_stride, block_stride;                      // elements between rows, between blocks
+  int parts;                                             // pairs that share a tile's k; more than one: a tile at most for a cluster
 };
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -96,11 +100,14 @@ __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// Address of the even CTA's copy of a shared variable.
-__device__ __forceinline__ uint32_t in_even_cta(const void* p) {
+// Address of a CTA's copy of a shared variable.
+__device__ __forceinline__ uint32_t in_cta(const void* p, int rank) {
   uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(p)));
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
   return r;
+}
+__device__ __forceinline__ void send(uint32_t at, const float* v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
 __device__ __forceinline__ void arrive_at(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -128,7 +135,8 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* map, in
       : "memory");
 }
 // Shared-memory matrix descriptor, 128-byte swizzle (see ffn_batched_tc.cu).
-__device__ __forceinline__ constexpr uint32_t desc_lo(uint32_t addr, uint32_t lbo_bytes) { return (addr >> 4) | (lbo_bytes >> 4 << 16); }
+// (An address within a cluster has the CTA's number in its upper bits, which are none of the descriptor's.)
+__device__ __forceinline__ constexpr uint32_t desc_lo(uint32_t addr, uint32_t lbo_bytes) { return ((addr >> 4) & 0x3fffu) | (lbo_bytes >> 4 << 16); }
 constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);     // eight rows of 128 bytes apart
 __device__ __forceinline__ void mma_pair(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
                                          uint32_t accumulate) {
@@ -138,10 +146,10 @@ __device__ __forceinline__ void mma_pair(uint32_t tmem_d, uint32_t a_lo, uint32_
       "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Arrives on the barrier of both CTAs once every product issued so far by this thread has completed.
-__device__ __forceinline__ void commit_pair(uint64_t* bar) {
+// Arrives on the barrier of both CTAs (of the cluster's, as a mask) once every product issued so far by this thread has completed.
+__device__ __forceinline__ void commit_pair(uint64_t* bar, uint32_t both) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_u32(bar)),
-               "h"((uint16_t)3)
+               "h"((uint16_t)both)
                : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -234,7 +242,7 @@ struct Tile {
 // role of a CTA walks them by itself, a whole warp together, in steps of mixed digits (no division a tile), with the table of the experts
 // (first [N + 1]: their rows, ascending; upto [N + 1]: tiles of N of lower experts) looked at through a window of 32 entries, one in each lane:
 // shared memory, busy with operands, takes some hundred cycles to answer, and every tile would wait for it several times.
-template <int MODE>
+template <int MODE, bool SPLIT>
 struct Walk {
   const ProductArgs& a;
   const int* first;
@@ -250,7 +258,7 @@ struct Walk {
   }
   __device__ Walk(const ProductArgs& args, const int* first_, const int* upto_) : a(args), first(first_), upto(upto_), e(0) {
     const int rows = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
-    const int pairs = (int)gridDim.x >> 1, pair = (int)blockIdx.x >> 1;
+    const int parts = SPLIT ? a.parts : 1, pairs = (int)gridDim.x / (2 * parts), pair = (int)blockIdx.x / (2 * parts);          // (clusters, where pairs share a tile)
     m_tiles = (rows + kTile - 1) / kTile;
     n_tiles = (a.I + kTile - 1) / kTile;
     m = pair % m_tiles; i = pair / m_tiles;
@@ -264,6 +272,13 @@ struct Walk {
     }
     total = upto[a.n_experts];
     look(MODE == kGradBlocks ? min(e, a.n_experts) : 0);
+  }
+  // Back to the first tile, or to none.
+  __device__ __forceinline__ void again(bool none) {
+    const int cluster = (int)blockIdx.x / (2 * a.parts);
+    m = cluster % m_tiles;
+    i = none ? total : cluster / m_tiles;
+    look(0);
   }
   __device__ bool next(Tile& g) {
     if constexpr (MODE == kGradBlocks) {
@@ -307,6 +322,10 @@ struct Walk {
   }
 };
 
+// Turns of sixteen columns that one of `units` groups of four epilogue warps takes for a tile of n columns, `cols` at a time; and the bytes of two groups' turn.
+constexpr int kTurnBytes = 256 * 64;
+__host__ __device__ constexpr int turns(int n, int cols, int units) { return ((n + cols - 1) / cols + units - 1) / units * (cols / 16); }
+
 // A place in a ring and the parity of its present use.
 template <int N>
 struct Place {
@@ -317,8 +336,8 @@ struct Place {
   }
 };
 
-template <int MODE, typename T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
+template <int MODE, bool SPLIT, typename T>
+__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ ProductArgs a) {
   using S = Shape<MODE>;
   constexpr int kStages = S::kStages, kCols = S::kCols;
   constexpr bool kRagged = MODE == kGradBlocks;          // k ends inside a stage
@@ -340,7 +359,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 
   launch_dependents();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int cta = (int)cluster_rank();
+  const int rank = (int)cluster_rank(), cta = rank & 1, part = SPLIT ? rank >> 1 : 0, parts = SPLIT ? a.parts : 1;
+  const uint32_t both = 3u << (2 * part);
+  auto in_even_cta = [&](const void* p) { return in_cta(p, 2 * part); };
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(full + s, kRagged ? 2 : 1);
@@ -390,11 +411,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   cluster_sync_all();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk<MODE> walk(a, first, upto);
+  Walk<MODE, SPLIT> walk(a, first, upto);
   Tile g;
   // A wait by a whole warp.  After one that ran out its role stops, whatever waits for that role runs out in its turn, and the results stay NaN.
   auto warp_wait = [&](uint64_t* bar, uint32_t parity, unsigned polls = kPolls) {
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, polls)) != 0;
+  };
+  // the part of a tile's stages that this pair takes
+  auto stages_of = [&](int& begin, int& end) {
+    const int per = SPLIT ? (g.pieces + parts - 1) / parts : g.pieces;
+    begin = min(part * per, g.pieces);
+    end = min(begin + per, g.pieces);
   };
   // for a wait of a whole tile: more polls for more of k
   auto long_wait = [&]() { return kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u; };
@@ -443,20 +470,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           if (box == 2) load_3d(n_dst + 8192, n_map, n_row + 64, row, 0, bar);
         }
       };
-      int early = 0;                                     // stages of the CTA's first tile whose M is on its way already
+      int begin, end;
+      stages_of(begin, end);
+      int early = begin;                                 // stages of the CTA's first tile before this one have their M on its way already
       if (stages == 0) {
         if constexpr (MODE == kDown || MODE == kGradRows) {
-          early = min(g.pieces, kStages);
+          early = min(end, begin + kStages);
           if (elect_one())
-            for (int p = 0; p < early; ++p) {
-              if (cta == 0) mbar_expect_tx(full + p, 2 * bytes);
-              load_m(p, ring + p * kStageBytes, bars + p * 8);
+            for (int p = begin; p < early; ++p) {
+              if (cta == 0) mbar_expect_tx(full + p - begin, 2 * bytes);
+              load_m(p, ring + (p - begin) * kStageBytes, bars + (p - begin) * 8);
             }
           __syncwarp();
         }
         dependency_wait();
       }
-      for (int p = 0; p < g.pieces; ++p) {
+      for (int p = begin; p < end; ++p) {
         if (stages >= kStages) {
           ok = warp_wait(empty + at.s, at.turn ^ 1);
           if (!ok) break;
@@ -507,7 +536,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
         if (!ok) break;
         fence_after();
         const uint32_t d = d0 + (uint32_t)(acc & 1) * kTile, idesc = kIdesc | ((uint32_t)(2 * g.half) >> 3 << 17);
-        for (int p = 0; p < g.pieces; ++p) {
+        int begin, end;
+        stages_of(begin, end);
+        for (int p = begin; p < end; ++p) {
           ok = warp_wait(full + at.s, at.turn);
           if (!ok) break;
           fence_after();
@@ -516,19 +547,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
 #pragma unroll
             for (int k = 0; k < kK / 16; ++k)
               if (!kRagged || p * kK + k * 16 < g.count)           // (sixteen rows that are not the expert's add nothing)
-                mma_pair(d, m_desc + stage + k * kMStep, kDescHi, n_desc + stage + k * kNStep, kDescHi, idesc, (p | k) ? 1u : 0u);
-            commit_pair(empty + at.s);
+                mma_pair(d, m_desc + stage + k * kMStep, kDescHi, n_desc + stage + k * kNStep, kDescHi, idesc, p > begin || k ? 1u : 0u);
+            commit_pair(empty + at.s, both);
           }
           __syncwarp();
           at.next();
         }
         if (!ok) break;
-        if (elect_one()) commit_pair(acc_full + (acc & 1));
+        if (elect_one()) commit_pair(acc_full + (acc & 1), both);
         __syncwarp();
         ++acc;
       }
       if (!ok) {
-        if (elect_one()) commit_pair(drain);             // let the tensor cores finish before TMEM is freed
+        if (elect_one()) commit_pair(drain, both);       // let the tensor cores finish before TMEM is freed
         mbar_wait(drain, 0, kPolls);
       }
     }
@@ -566,9 +597,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
       Place<2> at;
       int64_t groups = 0;
       bool ok = true;
+      if constexpr (SPLIT) {                             // the two meetings of the epilogues, which take nothing from here before them
+        cluster_sync_all();
+        cluster_sync_all();
+      }
       while (ok && walk.next(g)) {
         const int ch = g.m0 + cta * 128;
-        for (int c0 = group * kCols; c0 < g.n; c0 += 2 * kCols) {
+        for (int c0 = (part + parts * group) * kCols; c0 < g.n; c0 += 2 * parts * kCols) {
           if (groups >= 2) {
             ok = warp_wait(kept_empty + 2 * group + at.s, at.turn ^ 1, long_wait());
             if (!ok) break;
@@ -596,10 +631,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
     int third = 0;                                       // kGateUp without kept gates: act alone goes through each third of the buffer in turn
     bool ok = true;
     const bool keep = MODE == kGateUp && a.kept;
+    // Groups of kCols columns go round the units: the pairs that share the tile, with their first epilogue group and then with their second.  Each pair
+    // sends the others what it has of their columns: 16 columns of a thread as four float4, a place for each of the 256 threads, a slot for each sender.
+    const int unit = part + parts * group, units = 2 * parts;
+    int slot_bytes = 0;
+    if constexpr (SPLIT) {
+      const bool here = walk.next(g);
+      if (here) {
+        slot_bytes = turns(g.n, kCols, units) * kTurnBytes;
+        ok = warp_wait(acc_full, 0, long_wait());
+        fence_after();
+      }
+      cluster_sync_all();                                // all products have ended, no ring is in use
+      for (int d = 1; here && d < parts; ++d) {
+        const int q = part + d < parts ? part + d : part + d - parts;
+        uint32_t to = in_cta(smem, 2 * q + cta) + (parts - 1 - d) * slot_bytes + (tid - 128) * 16;
+        for (int c0 = (q + parts * group) * kCols; c0 < g.n; c0 += units * kCols)
+#pragma unroll 1
+          for (int c = c0; c < min(c0 + kCols, g.n); c += 16, to += kTurnBytes) {
+            float f[16];
+            tmem_fragments(tmem + lanes + c, f);
+            tmem_fragments(tmem + lanes + c + (16u << 16), f + 8);
+            ld_wait(f);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f[i] = ok ? f[i] : __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) send(to + i * 4096, f + 4 * i);
+          }
+      }
+      cluster_sync_all();                                // they have arrived
+      walk.again(!here);
+    }
     for (int tile = 0; walk.next(g); ++tile) {
+      const float4* theirs = reinterpret_cast<const float4*>(smem) + (tid - 128);
       // columns: kCols each from `from` on, every other such group (kGradBlocks: one half of them)
       const int half_n = (g.n + 63) / 64 * 32;
-      const int acc = tile & 1, from = MODE == kGradBlocks ? group * half_n : group * kCols, by = MODE == kGradBlocks ? kCols : 2 * kCols;
+      const int acc = tile & 1, from = MODE == kGradBlocks ? group * half_n : unit * kCols, by = MODE == kGradBlocks ? kCols : units * kCols;
       const uint32_t col = tmem + lanes + (uint32_t)acc * kTile;
       if (ok) {
         ok = warp_wait(acc_full + acc, (tile >> 1) & 1, long_wait());
@@ -700,6 +767,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
           if (some) ld_wait(f);
 #pragma unroll
           for (int i = 0; i < 16; ++i) v[i] = some ? f[i] : __uint_as_float(0x7fc00000u);
+          for (int q = 0; q < parts - 1; ++q) {
+            const float4* from_q = theirs + q * (slot_bytes / 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float4 w = from_q[i * 256];
+              v[4 * i] += w.x; v[4 * i + 1] += w.y; v[4 * i + 2] += w.z; v[4 * i + 3] += w.w;
+            }
+          }
+          theirs += kTurnBytes / 16;
           const int next = c + 16 < c0 + kCols ? c + 16 : c0 + by;
           if (next < g.n) fetch(next);
           else read_out();
@@ -838,6 +914,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) product
   }
   dependency_wait();                                     // no CTA, tiles or not, ends before the kernel in front
   __syncwarp();
+  if (SPLIT && warp < (MODE == kGradAct ? 2 : 4)) {      // the two meetings of the epilogues
+    cluster_sync_all();
+    cluster_sync_all();
+  }
   fence_before();
   __syncthreads();
   cluster_sync_all();
@@ -910,29 +990,57 @@ struct Encoder {
   }
 };
 
+// `clusters` of `parts` pairs each.
+template <int MODE, bool SPLIT, typename T>
+cudaError_t launch_pairs(const ProductArgs& a, int clusters, bool follows, cudaStream_t stream) {
+  static std::atomic<bool> ready[kMaxDevices];
+  const cudaError_t e = allow_dynamic_smem(product_kernel<MODE, SPLIT, T>, Shape<MODE>::smem(REMOE_SORT_MAX_EXPERTS), ready);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(clusters * a.parts * 2));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Shape<MODE>::smem(a.n_experts);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)a.parts * 2;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = follows ? 2 : 1;                        // a product of this call is in front
+  return cudaLaunchKernelEx(&cfg, product_kernel<MODE, SPLIT, T>, a);
+}
+
 template <int MODE, typename T>
 cudaError_t launch_product(const ProductArgs& a, bool follows, cudaStream_t stream) {
-  const size_t smem = Shape<MODE>::smem(a.n_experts);
-  static std::atomic<bool> ready[kMaxDevices];
-  const cudaError_t e = allow_dynamic_smem(product_kernel<MODE, T>, Shape<MODE>::smem(REMOE_SORT_MAX_EXPERTS), ready);
-  if (e != cudaSuccess) return e;
-  // one pair for each pair of SMs, fewer where there are fewer tiles
   const int m = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
   const int64_t m_tiles = (m + kTile - 1) / kTile, i_tiles = (a.I + kTile - 1) / kTile;
-  const int64_t n_tiles = MODE == kGradBlocks ? a.n_experts * 3 * i_tiles : a.n_rows / kTile + std::min(a.n_experts, a.n_rows);
-  const int64_t pairs = std::min<int64_t>(74, m_tiles * n_tiles);
-  if (pairs == 0) return cudaSuccess;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)pairs * 2);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = follows ? 1 : 0;                        // a product of this call is in front
-  return cudaLaunchKernelEx(&cfg, product_kernel<MODE, T>, a);
+  const int64_t n_tiles = MODE == kGradBlocks ? a.n_experts * 3 * i_tiles : (a.n_rows + (kTile - 1) * (int64_t)std::min(a.n_experts, a.n_rows)) / kTile;
+  const int64_t tiles = m_tiles * n_tiles;
+  if (tiles == 0) return cudaSuccess;
+  ProductArgs args = a;
+  args.parts = 1;
+  if constexpr (MODE != kGradBlocks) {
+    using S = Shape<MODE>;
+    // Four pairs for a tile up to 15 tiles, two up to 33: as many clusters as this GPU holds at once, fewer where k is short.  With one, two and four pairs a forward pass of a few
+    // rows took (us, the product's pieces of 64 k and its tiles; the rest of the time is the other product's):
+    //   16 pieces,  8 tiles 13.1 13.2 12.9   32 pieces,  8 tiles 16.2 14.9 13.8   88 pieces,  8 tiles 31.1 23.9 21.7
+    //               16 tiles 13.0 13.5                   15 tiles 25.1 23.6 24.9               15 tiles 41.6 36.5 34.3
+    //               30 tiles 22.0 24.5                   30 tiles 19.2 19.9                    30 tiles 61.6 58.4
+    // With 256 rows a tile the sharing costs more and a piece takes longer: 16 pieces of 8 tiles 22.4, 21.6, 32 pieces 26.9, 24.2.  Both products
+    // shared, 32 rows of one expert of 2048 x 5632 bf16 take 22.9 us instead of 31.4, the gradient of those rows 28.0 instead of 55.2.
+    // A slot for each of the other pairs' results, where the ring was
+    static_assert(turns(kTile, S::kCols, 4) * kTurnBytes <= S::kStages * kStageBytes && 3 * turns(kTile, S::kCols, 8) * kTurnBytes <= S::kStages * kStageBytes);
+    const int k = MODE == kDown || MODE == kGradRows ? a.I : a.H, pieces = (k + kK - 1) / kK * (MODE == kGradRows ? 2 : 1);
+    for (int parts : {4, 2})
+      if (pieces >= 24 && tiles <= (parts == 4 ? std::min(15, pieces * 3 / 8) : std::min(33, pieces * 11 / 16))) {
+        args.parts = parts;
+        return launch_pairs<MODE, true, T>(args, (int)tiles, follows, stream);
+      }
+  }
+  // one pair for each pair of SMs, fewer where there are fewer tiles
+  return launch_pairs<MODE, false, T>(args, (int)std::min<int64_t>(74, tiles), follows, stream);
 }
 
 int check_ffn(const FfnCall& c) {

@@ -304,3 +304,35 @@ def test_ffn_backward(counts, H, I, dtype):
         f = Ffn(counts, H, I, dtype, seed=H + I, pad=pad, behind=behind, block_pad=block_pad, first=first)
         f.forward()
         f.check_backward(rms=f.used * H > 5000)
+
+
+# Few tiles of a long k: two and four pairs of SMs share a tile's k.  Some calls have room for more tiles than the rows turn out to need.
+FEW = [([1], 1544, 1544), ([15], 2048, 1400), ([33], 1536, 760), ([64, 0, 3], 1600, 520), ([129], 264, 5632), ([200], 4104, 264), ([256], 1992, 2056), ([257], 512, 1928),
+       ([2, 90, 31, 128], 1672, 128), ([5, 1], 4096, 3080), ([0, 0], 2048, 1544)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("counts,H,I", FEW)
+def test_ffn_of_few_tiles(counts, H, I, dtype):
+    for pad, behind, block_pad, first in [(0, 0, 0, 0), (8, 5, 64, 3)]:
+        f = Ffn(counts, H, I, dtype, seed=H + I, pad=pad, behind=behind, block_pad=block_pad, first=first)
+        f.check_forward()
+        f.check_backward()
+
+
+def test_ffn_of_few_tiles_captured():
+    f = Ffn([40], 2048, 1544, "bf16", seed=2)
+    f.forward()
+    f.backward()
+    want = f.ys.view.clone(), f.d_xs.view.clone(), f.d_blocks.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ok(rb.remoe_expert_ffn(f.R, f.N, f.H, f.I, f.code, f.xs.view, f.xs.stride, f.offsets, f.blocks, f.block, f.gate_up, f.act, f.ys.view, f.ys.stride, stream()))
+        ok(rb.remoe_expert_ffn_backward(f.R, f.N, f.H, f.I, f.code, f.xs.view, f.xs.stride, f.offsets, f.blocks, f.block, f.gate_up, f.d_ys.view, f.d_ys.stride, f.work,
+                                        f.d_xs.view, f.d_xs.stride, f.d_blocks, f.block, stream()))
+    for _ in range(3):
+        for t in (f.ys.view, f.d_xs.view, f.d_blocks, f.gate_up):
+            t.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((f.ys.view, f.d_xs.view, f.d_blocks), want))
