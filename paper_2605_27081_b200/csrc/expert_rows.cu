@@ -578,7 +578,7 @@ cudaError_t launch_rows_as(const RowArgs& args, cudaStream_t stream) {
   }
   if constexpr (OP == kCombineBackward) {
     const int step = a.threads == 32 ? 8 : 1;
-    return rows::launch<combine_backward_kernel<T, V, TAIL>>(a, std::min<int64_t>((a.n_tokens + step - 1) / step, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
+    return rows::launch<combine_backward_kernel<T, V, TAIL>>(a, std::min<int64_t>(((int64_t)a.n_tokens + step - 1) / step, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
   }
 }
 
@@ -650,7 +650,7 @@ extern "C" int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_expe
   rows::PointerDevice device(offsets_dev);
   if (device.err_code()) return device.err_code();
   SortArgs a{ids_dev, rows_dev, offsets_dev, n_tokens * top_k, n_experts, 0};
-  const int strips = (a.n + 31) / 32;
+  const int strips = (int)(((int64_t)a.n + 31) / 32);
   int blocks = 1;
   // One block for up to 4096 selections (2048: 5.2 us, shared between two blocks 7.8; 8192: 9.5 and, between eight, 8.1), else the most that a
   // cluster may have, and for more than their registers hold the sixteen that this GPU can give (262144: 41 us with eight, 24 with sixteen).

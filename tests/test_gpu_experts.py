@@ -336,3 +336,48 @@ def test_ffn_of_few_tiles_captured():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((f.ys.view, f.d_xs.view, f.d_blocks), want))
+
+
+# ---------------------------------------------------------------------------------------------------- as many selections as a call may have
+
+MOST = 2**31 - 1
+
+
+def test_sort_of_the_most_selections():
+    N, piece = 3, 1 << 27
+    ids = torch.empty(MOST, dtype=torch.int32, device="cuda")
+    rows = torch.full((MOST,), -7, dtype=torch.int32, device="cuda")
+    offsets = torch.full((N + 1,), -7, dtype=torch.int32, device="cuda")
+    for s in range(0, MOST, piece):                 # expert s % 3, but for every eighth, which has none
+        at = torch.arange(s, min(s + piece, MOST), dtype=torch.int64, device="cuda")
+        ids[s:s + piece] = torch.where(at % 8 == 7, -1, at // 8 % N).int()
+    ok(rb.remoe_expert_sort(MOST, 1, N, ids, rows, offsets, stream()))
+    torch.cuda.synchronize()
+    # eights 0, 1, 2, ...: seven selections of expert 0, seven of expert 1, ...; the last eight has no eighth
+    eights = (MOST + 1) // 8
+    counts = [7 * ((eights - e + N - 1) // N) for e in range(N)]
+    first = [0, counts[0], counts[0] + counts[1], sum(counts)]
+    assert offsets.tolist() == first
+    start = torch.tensor(first[:N], device="cuda")
+    for s in range(0, MOST, piece):
+        at = torch.arange(s, min(s + piece, MOST), dtype=torch.int64, device="cuda")
+        want = torch.where(at % 8 == 7, -1, start[at // 8 % N] + at // 8 // N * 7 + at % 8)
+        assert torch.equal(rows[s:s + piece].long(), want)
+
+
+def test_combine_backward_of_the_most_tokens():
+    n_rows, piece = 5, 1 << 27
+    d_out = torch.empty(MOST, 1, dtype=torch.bfloat16, device="cuda")
+    rows = torch.empty(MOST, dtype=torch.int32, device="cuda")
+    ys = torch.tensor([[0.5], [-1.0], [2.0], [3.0], [-0.25]], dtype=torch.bfloat16, device="cuda")
+    d_gates = torch.full((MOST,), 9.0, device="cuda")
+    for s in range(0, MOST, piece):                 # values of a few bits: the products are exact
+        at = torch.arange(s, min(s + piece, MOST), device="cuda")
+        rows[s:s + piece] = (at % 6).int()
+        d_out[s:s + piece, 0] = (at % 17 - 8).bfloat16()
+    ok(rb.remoe_expert_combine_backward(MOST, 1, 1, rb.REMOE_BF16, d_out, 1, n_rows, ys, 1, rows, None, None, 0, d_gates, stream()))
+    torch.cuda.synchronize()
+    value = torch.cat([ys[:, 0].float(), torch.zeros(1, device="cuda")])
+    for s in range(0, MOST, piece):
+        at = torch.arange(s, min(s + piece, MOST), device="cuda")
+        assert torch.equal(d_gates[s:s + piece], value[at % 6] * (at % 17 - 8))
