@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       int acc = 0;
       bool ok = true;
       while (walk.next(g)) {
-          if (acc >= 2) ok = warp_wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
+        if (acc >= 2) ok = warp_wait(acc_empty + (acc & 1), ((acc >> 1) - 1) & 1);
         if (!ok) break;
         fence_after();
         const uint32_t d = d0 + (uint32_t)(acc & 1) * kTile, idesc = kIdesc | ((uint32_t)(2 * g.half) >> 3 << 17);
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         __syncwarp();
         if (lane == 0) arrive_at(in_even_cta(acc_empty + acc));
       };
-      if (from >= g.n) {
+      if (from >= g.n && !(MODE == kGradBlocks && g.pieces == 0 && ok)) {
         read_out();
         continue;
       }

@@ -320,6 +320,15 @@ def test_ffn_of_few_tiles(counts, H, I, dtype):
         f.check_backward()
 
 
+@pytest.mark.parametrize("counts,H,I", [([0, 2], 8, 40), ([0, 3, 0], 264, 72), ([0, 0, 1, 0], 24, 136), ([5, 0], 1304, 264), ([0], 544, 8)])
+def test_experts_without_rows_have_no_gradient(counts, H, I):
+    """The last tile of columns is narrow: 8 to 32 of them."""
+    f = Ffn(counts, H, I, "bf16", seed=3, behind=2, block_pad=8)
+    f.forward()
+    f.check_backward(rms=False)
+    assert not f.d_blocks[[e for e, n in enumerate(counts) if n == 0]].any()
+
+
 def test_ffn_of_few_tiles_captured():
     f = Ffn([40], 2048, 1544, "bf16", seed=2)
     f.forward()
