@@ -18,9 +18,10 @@
 // sixteen rows of an instruction.
 // The epilogue turns its 8 x 8 pieces over on the way through shared memory (TMEM in the layout of matrix fragments, stmatrix.trans) and
 // leaves by TMA stores of 16 or 32 rows x 64 values; only the columns of an expert's last, incomplete group of rows leave by plain stores,
-// since a copy would run over the next expert's first rows.  kGradBlocks has the rows of its output as lanes: a thread's 32 columns are 64
-// bytes of one row and leave straight from the registers.  (Through shared memory, with m = hidden, the gradient of 64 blocks of 1408 x 2048
-// from 24576 rows took 460 to 467 us instead of 451.)  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
+// since a copy would run over the next expert's first rows.  kGradBlocks has the rows of its output as lanes and copies boxes of 16 rows x 64
+// columns, which the tensor map ends at the block's channels and columns, each warp on its own.  (Straight from the registers, 32 bytes of 32 rows a
+// store, the gradient of 64 blocks of 1408 x 2048 from 24576 rows took 435 us instead of 403: as many requests as sectors.  128 bytes of eight rows a
+// store, turned over by shuffles: 3 % slower for it, and 8 % for blocks of few rows.)  kGradAct's kept gates and ups come in the same way, by warps 2 and 3.
 // Where a launch has few tiles of a long k (a shared expert, a few rows), up to four pairs, a cluster, take a part of a tile's k each.  When all have
 // ended, each sends the others its sums of their columns, into the rings, which are idle by then, and finishes columns of its own: the order of the
 // sums is the same in every run.
@@ -56,7 +57,7 @@ template <int MODE>
 struct Shape {
   static constexpr int kStages = MODE == kGradAct ? 5 : 6;
   static constexpr int kCols = MODE == kGradAct ? 16 : 32;
-  static constexpr int kBuffer = MODE == kGradBlocks ? 0 : MODE == kDown || MODE == kGradRows ? 8192 : 12288;  // the others: three outputs
+  static constexpr int kBuffer = MODE == kGradBlocks ? 4 * 2048 : MODE == kDown || MODE == kGradRows ? 8192 : 12288;  // the others: three outputs
   static constexpr int kKept = MODE == kGradAct ? 2 * 8192 : 0;        // kept gates and ups: two groups of columns
   static constexpr int kStaging = 2 * (kBuffer + kKept);
   static constexpr int kBarriers = 3 * kStages + 2 + 2 + 1 + 2 * 4;
@@ -171,11 +172,11 @@ __device__ __forceinline__ void tmem_fragments(uint32_t taddr, float* v) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr));
 }
-// 32 consecutive fp32 columns of this thread's lane.  The caller waits.
-__device__ __forceinline__ void tmem_columns(uint32_t taddr, float (&v)[32]) {
+// The same of 64 columns.
+__device__ __forceinline__ void tmem_fragments_64(uint32_t taddr, float (&v)[32]) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
       "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
         "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
@@ -183,15 +184,14 @@ __device__ __forceinline__ void tmem_columns(uint32_t taddr, float (&v)[32]) {
         "=r"(r[31])
       : "r"(taddr));
 }
-__device__ __forceinline__ void store_32_bytes(void* p, const uint32_t* v) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]),
-               "r"(v[6]), "r"(v[7])
-               : "memory");
-}
 // Four 8 x 8 matrices of 16-bit values between fragments and shared memory, turned over: a lane gives the address of row
 // (lane % 8) of matrix (lane / 8), a row being the fragment's column.
 __device__ __forceinline__ void store_turned(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
   asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
+}
+// The same as they are: the rows are the fragment's.
+__device__ __forceinline__ void store_fragments(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3) : "memory");
 }
 __device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -202,6 +202,10 @@ __device__ __forceinline__ void load_turned(uint32_t addr, uint32_t (&r)[4]) {
 // Stores of shared memory as boxes of rows; what lies outside the tensor is left out.
 __device__ __forceinline__ void store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void store_4d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
 }
 __device__ __forceinline__ void store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
@@ -665,8 +669,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     for (int tile = 0; walk.next(g); ++tile) {
       const float4* theirs = reinterpret_cast<const float4*>(smem) + (tid - 128);
       // columns: kCols each from `from` on, every other such group (kGradBlocks: one half of them)
-      const int half_n = (g.n + 63) / 64 * 32;
-      const int acc = tile & 1, from = MODE == kGradBlocks ? group * half_n : unit * kCols, by = MODE == kGradBlocks ? kCols : units * kCols;
+      const int acc = tile & 1, from = unit * kCols, by = units * kCols;
       const uint32_t col = tmem + lanes + (uint32_t)acc * kTile;
       if (ok) {
         ok = warp_wait(acc_full + acc, (tile >> 1) & 1, long_wait());
@@ -677,20 +680,19 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         __syncwarp();
         if (lane == 0) arrive_at(in_even_cta(acc_empty + acc));
       };
-      if (from >= g.n && !(MODE == kGradBlocks && g.pieces == 0 && ok)) {
+      if (MODE != kGradBlocks && from >= g.n) {
         read_out();
         continue;
       }
       if constexpr (MODE == kGradBlocks) {
-        static_assert(MODE != kGradBlocks || kCols == 32, "columns of one load");
-        const int ch0 = g.m0 + cta * 128 + quad * 32, ch = ch0 + lane, end = min(g.n, from + half_n);
-        uint16_t* block = a.out + (size_t)g.e * a.block_stride + (size_t)g.plane * a.H + g.row;
-        // Rows start on any 16 bytes, and an access of part of a 32-byte sector costs as much as a whole one (and its turn in L2 more): where a row starts in
-        // the middle of a sector, its pieces begin and end 8 columns later.
+        const int ch0 = g.m0 + cta * 128 + quad * 32;
         if (g.pieces == 0 && ok) {                       // an expert without rows: zeros, a row's columns of the tile with each access
           read_out();
           const int rows = min(32, a.I - ch0);
+          uint16_t* block = a.out + (size_t)g.e * a.block_stride + (size_t)g.plane * a.H + g.row;
           uint16_t* out = block + (size_t)(ch0 + group) * 3 * a.H;
+          // Rows start on any 16 bytes, and an access of part of a 32-byte sector costs as much as a whole one: where a row starts in the middle of a
+          // sector, its piece begins and ends 8 columns later.
 #pragma unroll 4
           for (int r = group; r < rows; r += 2, out += 6 * (size_t)a.H) {
             const int late = reinterpret_cast<uintptr_t>(out) & 16 ? 8 : 0;
@@ -700,42 +702,40 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
           }
           continue;
         }
-        const bool there = ch < a.I;
-        uint16_t* out = block + (size_t)ch * 3 * a.H;
-        const bool late = reinterpret_cast<uintptr_t>(out) & 16;
-        uint32_t carry[4] = {0, 0, 0, 0};                // the last 8 columns of the piece before, where pieces are late
+        // sixteen rows of a quarter for each group, 64 columns a time
+        const int row0 = ch0 + 16 * group;
+        if (row0 >= a.I) {
+          read_out();
+          continue;
+        }
+        const uint32_t from16 = col + ((uint32_t)group << 20), buffer = smem_u32(staging) + (warp - 4) * 2048;
         float v[32];
-        if (ok) tmem_columns(col + from, v);
-        for (int c0 = from; c0 < end; c0 += by) {
-          uint32_t packed[16];
+        if (ok) tmem_fragments_64(from16, v);
+#pragma unroll 1
+        for (int c0 = 0; c0 < g.n; c0 += 64) {
+          uint32_t packed[16];                           // of rows T / 4 and T / 4 + 8 in turn
           if (ok) {
             ld_wait(v);
 #pragma unroll
-            for (int c = 0; c < 16; ++c) packed[c] = pack<T>(v[2 * c], v[2 * c + 1]);
-            if (c0 + by < end) tmem_columns(col + c0 + by, v);
+            for (int j = 0; j < 16; ++j) packed[j] = pack<T>(v[2 * j], v[2 * j + 1]);
+            if (c0 + 64 < g.n) tmem_fragments_64(from16 + c0 + 64, v);
           } else {
 #pragma unroll
-            for (int c = 0; c < 16; ++c) packed[c] = 0x7fff7fffu;                      // NaN in either type
+            for (int j = 0; j < 16; ++j) packed[j] = 0x7fff7fffu;                // NaN in either type
           }
-          if (c0 + by >= end) read_out();
-          if (!there) continue;
-          if (c0 + 32 <= end) {
-            uint32_t piece[16];                          // what is stored now: the same columns, or 8 earlier ones
+          if (c0 + 64 >= g.n) read_out();
+          if (lane == 0) stores_read<0>();
+          __syncwarp();
+          const int row = ((lane >> 3) & 1) * 8 + (lane & 7);
 #pragma unroll
-            for (int c = 0; c < 16; ++c) piece[c] = !late ? packed[c] : c < 4 ? carry[c] : packed[c - 4];
-            uint16_t* to = out + c0 - (late ? 8 : 0);
-            if (late && c0 == from) *reinterpret_cast<uint4*>(to + 8) = make_uint4(piece[4], piece[5], piece[6], piece[7]);
-            else store_32_bytes(to, piece);
-            store_32_bytes(to + 16, piece + 8);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) carry[c] = packed[12 + c];
-            if (late && c0 + 32 == end) *reinterpret_cast<uint4*>(to + 32) = make_uint4(carry[0], carry[1], carry[2], carry[3]);
-          } else {                                       // the last columns of a width that is no multiple of 32
-            if (late && c0 != from) *reinterpret_cast<uint4*>(out + c0 - 8) = make_uint4(carry[0], carry[1], carry[2], carry[3]);
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-              if (c0 + 8 * d < end)
-                *reinterpret_cast<uint4*>(out + c0 + 8 * d) = make_uint4(packed[4 * d], packed[4 * d + 1], packed[4 * d + 2], packed[4 * d + 3]);
+          for (int j = 0; j < 4; ++j)
+            store_fragments(buffer + row * 128 + (((2 * j + (lane >> 4)) ^ (row & 7)) << 4), packed[4 * j], packed[4 * j + 1], packed[4 * j + 2],
+                            packed[4 * j + 3]);
+          async_fence();
+          __syncwarp();
+          if (lane == 0) {
+            store_4d(&a.o[0], buffer, g.row + c0, g.plane, row0, g.e);
+            store_commit();
           }
         }
         continue;
@@ -910,7 +910,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         at.next();
       }
     }
-    if (issuer && elect_one()) stores_done();
+    if (MODE == kGradBlocks ? lane == 0 : issuer && elect_one()) stores_done();
   }
   dependency_wait();                                     // no CTA, tiles or not, ends before the kernel in front
   __syncwarp();
@@ -1117,6 +1117,7 @@ cudaError_t backward(const FfnCall& c, Encoder& enc, const void* xs, int64_t xs_
       enc.matrix(&a.n[0], xs, c.n_rows, c.hidden, xs_stride, 1, 64);
       enc.matrix(&a.n[1], d_ys, c.n_rows, c.hidden, d_ys_stride, 1, 64);
     }
+    enc.blocks(&a.o[0], c, d_blocks, d_block_stride, 16);
     a.out = static_cast<uint16_t*>(d_blocks);
     a.block_stride = d_block_stride;
     if (!enc.ok) return cudaErrorInvalidValue;
@@ -1166,6 +1167,7 @@ extern "C" int remoe_expert_ffn_backward(int32_t n_rows, int32_t n_experts, int3
   if (d_blocks_dev && (bad_rows(xs_dev, xs_stride, n_rows, hidden) || rows::misaligned(d_blocks_dev, 16) ||
                        (n_experts > 1 && (d_block_stride < (int64_t)3 * inter * hidden || d_block_stride % 8))))
     return REMOE_E_ARG;
+  if (d_blocks_dev && n_experts > 1 && d_block_stride >= (1LL << 38)) return REMOE_E_UNSUPPORTED;
   if (n_rows == 0 && !d_blocks_dev) return REMOE_OK;
   if (n_experts == 1) c.block_stride = d_block_stride = (int64_t)3 * inter * hidden;
   if (n_rows == 1) xs_stride = d_ys_stride = d_xs_stride = hidden;
