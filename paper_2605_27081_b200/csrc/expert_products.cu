@@ -242,6 +242,10 @@ struct Tile {
   int pieces = 0;                                        // of k
 };
 
+// kGradBlocks: halves of a tile, 128 channels, of a plane.  Those of the gates and the ups lie in one row, so that an odd number of them leaves no half
+// empty (64 blocks of 1408 x 2048: 17 tiles for 18).
+__host__ __device__ constexpr int half_tiles(int channels) { return (channels + 127) / 128; }
+
 // The tiles of a launch in the order of experts, dealt to the pairs in turn: a pair's next tile is as many further as there are pairs.  Each
 // role of a CTA walks them by itself, a whole warp together, in steps of mixed digits (no division a tile), with the table of the experts
 // (first [N + 1]: their rows, ascending; upto [N + 1]: tiles of N of lower experts) looked at through a window of 32 entries, one in each lane:
@@ -252,8 +256,8 @@ struct Walk {
   const int* first;
   const int* upto;
   int base, row_at, tiles_at;                            // window from expert `base` on: entries first[base + lane], upto[base + lane]
-  int m_tiles, n_tiles, m, i, j, e, total;               // tile of M, tile of N of all experts (of `total`), expert; kGradBlocks: of N, of M, plane
-  int step_m, step_i, step_j, step_e;
+  int m_tiles, n_tiles, m, i, e, total;                  // tile of M, tile of N of all experts (of `total`), expert; kGradBlocks: of N, of M of the expert
+  int step_m, step_i, step_e;
   __device__ __forceinline__ void look(int from) {
     base = from;
     const int x = min(from + ((int)threadIdx.x & 31), a.n_experts);
@@ -264,15 +268,14 @@ struct Walk {
     const int rows = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
     const int parts = SPLIT ? a.parts : 1, pairs = (int)gridDim.x / (2 * parts), pair = (int)blockIdx.x / (2 * parts);          // (clusters, where pairs share a tile)
     m_tiles = (rows + kTile - 1) / kTile;
-    n_tiles = (a.I + kTile - 1) / kTile;
+    const int halves = half_tiles(a.I);
+    n_tiles = halves + (halves + 1) / 2;
     m = pair % m_tiles; i = pair / m_tiles;
     step_m = pairs % m_tiles; step_i = pairs / m_tiles;
-    j = step_j = step_e = 0;
+    step_e = 0;
     if constexpr (MODE == kGradBlocks) {
-      j = i / n_tiles; i %= n_tiles;
-      e = j / 3; j %= 3;
-      step_j = step_i / n_tiles; step_i %= n_tiles;
-      step_e = step_j / 3; step_j %= 3;
+      e = i / n_tiles; i %= n_tiles;
+      step_e = step_i / n_tiles; step_i %= n_tiles;
     }
     total = upto[a.n_experts];
     look(MODE == kGradBlocks ? min(e, a.n_experts) : 0);
@@ -289,8 +292,10 @@ struct Walk {
       if (e >= a.n_experts) return false;
       if (e > base + 30) look(e);
       g.e = e;
-      g.plane = j;
-      g.m0 = i * kTile;
+      // half a tile of M for each CTA, of the gates and the ups (the rows of N are the same) or the downs
+      const int halves = half_tiles(a.I), cta = (int)blockIdx.x & 1, at = 2 * (i < halves ? i : i - halves) + cta;
+      g.plane = i >= halves ? 2 : at >= halves;
+      g.m0 = (g.plane == 1 ? at - halves : at) * 128 - cta * 128;
       g.row = m * kTile;
       g.n = min(kTile, a.H - g.row);
       g.first_row = __shfl_sync(0xffffffffu, row_at, e - base);
@@ -299,10 +304,8 @@ struct Walk {
       m += step_m;
       i += step_i;
       if (m >= m_tiles) { m -= m_tiles; ++i; }
-      j += step_j;
-      if (i >= n_tiles) { i -= n_tiles; ++j; }
       e += step_e;
-      if (j >= 3) { j -= 3; ++e; }
+      if (i >= n_tiles) { i -= n_tiles; ++e; }
     } else {
       if (i >= total) return false;
       // the last expert with no more tiles in front of it than this one has: the one with this tile
@@ -1015,8 +1018,8 @@ cudaError_t launch_pairs(const ProductArgs& a, int clusters, bool follows, cudaS
 template <int MODE, typename T>
 cudaError_t launch_product(const ProductArgs& a, bool follows, cudaStream_t stream) {
   const int m = MODE == kGateUp ? 2 * a.I : MODE == kGradAct ? a.I : a.H;
-  const int64_t m_tiles = (m + kTile - 1) / kTile, i_tiles = (a.I + kTile - 1) / kTile;
-  const int64_t n_tiles = MODE == kGradBlocks ? a.n_experts * 3 * i_tiles : (a.n_rows + (kTile - 1) * (int64_t)std::min(a.n_experts, a.n_rows)) / kTile;
+  const int64_t m_tiles = (m + kTile - 1) / kTile, halves = half_tiles(a.I);
+  const int64_t n_tiles = MODE == kGradBlocks ? a.n_experts * (halves + (halves + 1) / 2) : (a.n_rows + (kTile - 1) * (int64_t)std::min(a.n_experts, a.n_rows)) / kTile;
   const int64_t tiles = m_tiles * n_tiles;
   if (tiles == 0) return cudaSuccess;
   ProductArgs args = a;
