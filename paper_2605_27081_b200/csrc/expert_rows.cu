@@ -652,9 +652,10 @@ extern "C" int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_expe
   SortArgs a{ids_dev, rows_dev, offsets_dev, n_tokens * top_k, n_experts, 0};
   const int strips = (int)(((int64_t)a.n + 31) / 32);
   int blocks = 1;
-  // One block for up to 4096 selections (2048: 5.2 us, shared between two blocks 7.8; 8192: 9.5 and, between eight, 8.1), else the most that a
-  // cluster may have, and for more than their registers hold the sixteen that this GPU can give (262144: 41 us with eight, 24 with sixteen).
-  if (strips > kSortWarps * kStrips / 2) blocks = strips > 8 * kSortWarps * kStrips ? kSortBlocks : 8;
+  // One block for up to 4096 selections (2048: 5.2 us, shared between two blocks 7.8; 8192: 9.5 and, between eight, 8.1), else the eight that any
+  // cluster may have, and from 16384 on the sixteen that this GPU can give (8192: 5.8 us with either; 24576: 6.8 with eight, 6.4 with sixteen;
+  // 65536: 9.8 and 8.2; 262144: 41 and 25).
+  if (strips > kSortWarps * kStrips / 2) blocks = strips > 2 * kSortWarps * kStrips ? kSortBlocks : 8;
   int warps = (strips + blocks - 1) / blocks;
   warps = warps < 4 ? 4 : warps > kSortWarps ? kSortWarps : warps;
   a.run = (int)(((int64_t)strips + warps * blocks - 1) / (warps * blocks)) * 32;
