@@ -310,22 +310,41 @@ __device__ __forceinline__ void add_rows(const RowArgs& a, int64_t t, Picks p, i
   }
 }
 
+// Items of the combine, dealt to the groups of threads in turn, in steps of mixed digits (no division an item).
+struct Item {
+  int64_t token, by;
+  int part, part_by;
+  __device__ __forceinline__ Item(const RowArgs& a, int step) {
+    const int64_t first = (int64_t)blockIdx.x * step + threadIdx.x / a.threads;
+    const int stride = (int)gridDim.x * step;
+    token = first / a.parts;
+    part = (int)(first - token * a.parts);
+    by = stride / a.parts;
+    part_by = stride % a.parts;
+  }
+  __device__ __forceinline__ void next(const RowArgs& a) {
+    token += by;
+    part += part_by;
+    if (part >= a.parts) { part -= a.parts; ++token; }
+  }
+};
+
 // An item is a piece of a token's row for a.threads threads (whole warps), V elements each, in float32; the elements behind the last whole V
 // are pieces of one.  Persistent: the next item's rows and gates are on their way while this one's data is.
 template <typename T, int V, bool TAIL>
 __global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_kernel(const __grid_constant__ RowArgs a) {
   const int lane = threadIdx.x & 31, body = a.H / V, pieces = body + a.H % V, step = (int)blockDim.x / a.threads;
-  const int64_t items = (int64_t)a.n_tokens * a.parts, stride = (int64_t)gridDim.x * step;
-  int64_t item = (int64_t)blockIdx.x * step + threadIdx.x / a.threads;
   Picks next;
-  if (item < items) next.load(a, a.parts == 1 ? item : item / a.parts, 0, lane);
-  for (; item < items; item += stride) {
-    const int64_t t = a.parts == 1 ? item : item / a.parts;
-    const int piece = (int)(item - t * a.parts) * a.threads + threadIdx.x % a.threads;
+  Item item(a, step);
+  if (item.token < a.n_tokens) next.load(a, item.token, 0, lane);
+  while (item.token < a.n_tokens) {
+    const int64_t t = item.token;
+    const int piece = item.part * a.threads + (int)threadIdx.x % a.threads;
     const Picks p = next;
     const bool whole = piece < body, here = piece < pieces;
     const int i = whole ? piece * V : body * V + piece - body;
-    if (item + stride < items) next.load(a, a.parts == 1 ? item + stride : (item + stride) / a.parts, 0, lane);
+    item.next(a);
+    if (item.token < a.n_tokens) next.load(a, item.token, 0, lane);
     T* out = static_cast<T*>(a.out) + t * a.out_stride + i;
     const T* base = a.b ? static_cast<const T*>(a.b) + t * a.b_stride + i : nullptr;
     if (!TAIL || __any_sync(0xffffffffu, whole)) {
@@ -352,13 +371,16 @@ __global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_ke
   }
 }
 
-// The same sum for rows that are whole numbers of accesses of 4 bytes or more: copies to shared memory, kDeep units (up to eight rows of an
+// The same sum for rows that are whole numbers of accesses of 4 bytes or more: copies to shared memory, a few units (up to G rows of an
 // item's piece, and the base) ahead of the sums.  A thread reads nothing but what it copied, so there is no barrier, and what is under way costs
-// no registers.  Taken where there are more items than fit at once: 4096 x 6 rows of 2048 bf16 take 25.7 us, with the loads in registers, one
-// item at a time, 33; one token 3.7 against 2.7 (of which either has a launch).  Three blocks of 256 threads, two units deep: with two blocks
-// 29.5 us, three deep 29.8.
-constexpr int kDeep = 2;
+// no registers.  Taken where there are more items than fit at once: 4096 x 6 rows of 2048 bf16 and a base take 24.0 us, with the loads in registers,
+// one item at a time, 33; one token 3.7 against 2.7 (of which either has a launch).  G is the least of 2, 4, 6 and 8 that takes a token's rows at
+// once, since the instructions of a unit are for G rows: 4096 x 4 of them take 16.6 us, in groups of eight 21.4, 4096 x 2 of 4096 24.5 and 40.
+// Units ahead and blocks of an SM by what measured best: for G = 8 one ahead and three blocks (25.7 us for 4096 x 6 then), two blocks 29.5, two
+// ahead 29.8; with accesses of 8 bytes four blocks (4096 x 6 of 1028: 21.1 us; three: 23.3), which for those of 16 are slower (26.4).
+__host__ __device__ constexpr int copy_depth(int group) { return group <= 2 ? 4 : group <= 4 ? 3 : 2; }
 constexpr int kCopyThreads = 256;
+__host__ __device__ constexpr int copy_blocks(int bytes) { return bytes == 16 ? 3 : 4; }         // of an SM, by the width of an access
 
 template <int BYTES>
 __device__ __forceinline__ void copy_if(uint32_t dst, const void* src, bool yes) {
@@ -369,84 +391,83 @@ __device__ __forceinline__ void copy_if(uint32_t dst, const void* src, bool yes)
                  : "memory");
 }
 
-template <typename T, int V>
+template <typename T, int V, int G>
 __global__ void __launch_bounds__(kCopyThreads) combine_copy_kernel(const __grid_constant__ RowArgs a) {
   using W = typename Word<V * (int)sizeof(T)>::type;
   extern __shared__ __align__(16) unsigned char copy_smem[];
-  W* mine = reinterpret_cast<W*>(copy_smem) + threadIdx.x;               // [kDeep][kGroup + 1][blockDim.x]
-  const int lane = threadIdx.x & 31, pieces = a.H / V, step = (int)blockDim.x / a.threads, per = (kGroup + 1) * (int)blockDim.x;
-  const int64_t items = (int64_t)a.n_tokens * a.parts, stride = (int64_t)gridDim.x * step;
-  struct Unit {                          // item, first selection
-    int64_t item;
+  W* mine = reinterpret_cast<W*>(copy_smem) + threadIdx.x;               // [D][group, base][blockDim.x]
+  constexpr int D = copy_depth(G);
+  const int per = (G + (a.b ? 1 : 0)) * (int)blockDim.x;
+  const int lane = threadIdx.x & 31, pieces = a.H / V, step = (int)blockDim.x / a.threads;
+  const int in_item = (int)threadIdx.x % a.threads;
+  Item item(a, step);
+  struct Unit {                          // an item, and the first of its selections
+    Item at;
     int k0;
-    __device__ __forceinline__ void next(const RowArgs& a, int64_t stride) {
-      k0 += kGroup;
-      if (k0 >= a.K) { k0 = 0; item += stride; }
-    }
-    __device__ __forceinline__ int64_t token(const RowArgs& a) const { return a.parts == 1 ? item : item / a.parts; }
-    __device__ __forceinline__ int piece(const RowArgs& a) const {
-      return (int)(a.parts == 1 ? 0 : item % a.parts) * a.threads + (int)threadIdx.x % a.threads;
+    __device__ __forceinline__ void next(const RowArgs& a) {
+      k0 += G;
+      if (k0 >= a.K) { k0 = 0; at.next(a); }
     }
   };
-  Unit now{(int64_t)blockIdx.x * step + threadIdx.x / a.threads, 0}, ahead = now;
-  Picks picks[kDeep + 1];                // of the units from `now` on; the last one's is on its way
+  Unit now{item, 0}, ahead = now;
+  Picks picks[D + 1];                // of the units from `now` on; the last one's is on its way
   auto look = [&](Picks& p, const Unit& u) {
     p.row = -1;
     p.gate = 1.f;
-    if (u.item < items && lane < kGroup && u.k0 + lane < a.K) {
-      const int64_t at = u.token(a) * a.K + u.k0 + lane;
+    if (u.at.token < a.n_tokens && lane < G && u.k0 + lane < a.K) {
+      const int64_t at = u.at.token * a.K + u.k0 + lane;
       p.row = __ldg(a.rows + at);
       if (a.gates) p.gate = __ldg(a.gates + at);
     }
   };
   auto send = [&](const Picks& p, const Unit& u, int slot) {
-    const int piece = u.piece(a);
-    const bool here = u.item < items && piece < pieces;
+    const int piece = u.at.part * a.threads + in_item;
+    const bool here = u.at.token < a.n_tokens && piece < pieces;
     const uint32_t dst = (uint32_t)__cvta_generic_to_shared(mine + slot * per);
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) {
+    for (int k = 0; k < G; ++k) {
       const int r = p.row_of(a, k);
       copy_if<(int)sizeof(W)>(dst + k * blockDim.x * (int)sizeof(W), static_cast<const T*>(a.a) + r * a.a_stride + piece * V, here && r >= 0);
     }
-    if (a.b) copy_if<(int)sizeof(W)>(dst + kGroup * blockDim.x * (int)sizeof(W), static_cast<const T*>(a.b) + u.token(a) * a.b_stride + piece * V, here && u.k0 == 0);
+    if (a.b) copy_if<(int)sizeof(W)>(dst + G * blockDim.x * (int)sizeof(W), static_cast<const T*>(a.b) + u.at.token * a.b_stride + piece * V, here && u.k0 == 0);
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   look(picks[0], ahead);
 #pragma unroll
-  for (int i = 0; i < kDeep - 1; ++i) {
+  for (int i = 0; i < D - 1; ++i) {
     const Unit u = ahead;
-    ahead.next(a, stride);
+    ahead.next(a);
     look(picks[i + 1], ahead);
     send(picks[i], u, i);
   }
   float sum[V];
   int slot = 0;
-  while (now.item < items) {
+  while (now.at.token < a.n_tokens) {
     const Unit u = ahead;
-    ahead.next(a, stride);
-    look(picks[kDeep], ahead);
-    send(picks[kDeep - 1], u, slot == 0 ? kDeep - 1 : slot - 1);
-    asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory");
+    ahead.next(a);
+    look(picks[D], ahead);
+    send(picks[D - 1], u, slot == 0 ? D - 1 : slot - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(D - 1) : "memory");
     const W* from = mine + slot * per;
     if (now.k0 == 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) sum[j] = 0.f;
     }
     Vec<T, V> v;
-    const int piece = now.piece(a);
+    const int piece = now.at.part * a.threads + in_item;
     const bool here = piece < pieces;
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k)
+    for (int k = 0; k < G; ++k)
       if (picks[0].row_of(a, k) >= 0) {
         const float g = picks[0].gate_of(k);
         v.word = from[k * blockDim.x];
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] = fmaf(g, to_float(v.e[j]), sum[j]);
       }
-    if (now.k0 + kGroup >= a.K && here) {
-      const int64_t t = now.token(a);
+    if (now.k0 + G >= a.K && here) {
+      const int64_t t = now.at.token;
       if (a.b) {
-        if (now.k0 == 0) v.word = from[kGroup * blockDim.x];
+        if (now.k0 == 0) v.word = from[G * blockDim.x];
         else v.load(static_cast<const T*>(a.b) + t * a.b_stride + piece * V);
 #pragma unroll
         for (int j = 0; j < V; ++j) sum[j] += to_float(v.e[j]);
@@ -456,9 +477,9 @@ __global__ void __launch_bounds__(kCopyThreads) combine_copy_kernel(const __grid
       v.store(static_cast<T*>(a.out) + t * a.out_stride + piece * V);
     }
 #pragma unroll
-    for (int i = 0; i < kDeep; ++i) picks[i] = picks[i + 1];
-    now.next(a, stride);
-    slot = slot == kDeep - 1 ? 0 : slot + 1;
+    for (int i = 0; i < D; ++i) picks[i] = picks[i + 1];
+    now.next(a);
+    slot = slot == D - 1 ? 0 : slot + 1;
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
@@ -556,6 +577,15 @@ __global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_ba
 
 enum Op { kDispatch, kCombine, kCombineBackward };
 
+template <typename T, int V, int G>
+cudaError_t launch_copies(const RowArgs& a, int threads, cudaStream_t stream) {
+  constexpr size_t kPiece = copy_depth(G) * V * sizeof(T);
+  static std::atomic<bool> ready[kMaxDevices];
+  const cudaError_t e = allow_dynamic_smem(combine_copy_kernel<T, V, G>, kPiece * (G + 1) * kCopyThreads, ready);
+  if (e != cudaSuccess) return e;
+  return rows::launch<combine_copy_kernel<T, V, G>>(a, 148 * copy_blocks(V * sizeof(T)), 1, threads, kPiece * (G + (a.b ? 1 : 0)) * threads, stream);
+}
+
 template <Op OP, typename T, int V, bool TAIL>
 cudaError_t launch_rows_as(const RowArgs& args, cudaStream_t stream) {
   RowArgs a = args;
@@ -565,15 +595,16 @@ cudaError_t launch_rows_as(const RowArgs& args, cudaStream_t stream) {
   if constexpr (OP == kDispatch) return rows::launch<dispatch_kernel<T, V>>(a, a.n_tokens, 1, a.threads, 0, stream);
   if constexpr (OP == kCombine) {
     a.parts = (pieces + a.threads - 1) / a.threads;
+    a.threads = ((pieces + a.parts - 1) / a.parts + 31) / 32 * 32;         // (257 pieces: twice 160 threads)
     const int step = 256 / a.threads;
     const int64_t blocks = ((int64_t)a.n_tokens * a.parts + step - 1) / step;
-    if constexpr (!TAIL && V * sizeof(T) >= 4) if (blocks > 148 * 3) {
-      constexpr size_t kUnit = (size_t)kDeep * (kGroup + 1) * V * sizeof(T);
-      static std::atomic<bool> ready[kMaxDevices];
-      const cudaError_t e = allow_dynamic_smem(combine_copy_kernel<T, V>, kUnit * kCopyThreads, ready);
-      if (e != cudaSuccess) return e;
-      return rows::launch<combine_copy_kernel<T, V>>(a, 148 * 3, 1, step * a.threads, kUnit * step * a.threads, stream);
-    }
+    if constexpr (!TAIL && V * sizeof(T) >= 4)
+      if (blocks > 148 * copy_blocks(V * sizeof(T))) {
+        if (a.K <= 2) return launch_copies<T, V, 2>(a, step * a.threads, stream);
+        if (a.K <= 4) return launch_copies<T, V, 4>(a, step * a.threads, stream);
+        if (a.K <= 6) return launch_copies<T, V, 6>(a, step * a.threads, stream);
+        return launch_copies<T, V, 8>(a, step * a.threads, stream);
+      }
     return rows::launch<combine_kernel<T, V, TAIL>>(a, std::min<int64_t>(blocks, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
   }
   if constexpr (OP == kCombineBackward) {
