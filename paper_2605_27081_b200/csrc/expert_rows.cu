@@ -484,16 +484,16 @@ __global__ void __launch_bounds__(kCopyThreads) combine_copy_kernel(const __grid
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void backward_piece(const RowArgs& a, int64_t t, const int (&r)[kGroup], const float (&g)[kGroup], int i, float (&dot)[kGroup]) {
-  Vec<T, V> d, v[kGroup];
+template <typename T, int V, int G>
+__device__ __forceinline__ void backward_piece(const RowArgs& a, int64_t t, const int (&r)[G], const float (&g)[G], int i, float (&dot)[G]) {
+  Vec<T, V> d, v[G];
   d.load(static_cast<const T*>(a.b) + t * a.b_stride + i);
   if (a.d_gates) {
 #pragma unroll
-    for (int k = 0; k < kGroup; ++k) v[k].load_if(static_cast<const T*>(a.a) + r[k] * a.a_stride + i, r[k] >= 0);
+    for (int k = 0; k < G; ++k) v[k].load_if(static_cast<const T*>(a.a) + r[k] * a.a_stride + i, r[k] >= 0);
   }
 #pragma unroll
-  for (int k = 0; k < kGroup; ++k) {
+  for (int k = 0; k < G; ++k) {
     if (r[k] < 0) continue;
     if (a.d_gates) {
 #pragma unroll
@@ -508,30 +508,36 @@ __device__ __forceinline__ void backward_piece(const RowArgs& a, int64_t t, cons
   }
 }
 
-// Eight values a lane, summed over the warp: lane l ends with the sum of value (l / 4) of all lanes.
-__device__ __forceinline__ float reduce_eight(float (&x)[kGroup], int lane) {
-  float y[4], z[2];
+// Eight or four values a lane, summed over the warp: lane l ends with the sum of value l / (32 / G) of all lanes.
+template <int G>
+__device__ __forceinline__ float reduce_group(float (&x)[G], int lane) {
+  float s = 0.f;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float keep = lane & 16 ? x[k + 4] : x[k], give = lane & 16 ? x[k] : x[k + 4];
-    y[k] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
-  }
+  for (int n = G / 2, by = 16; by; n /= 2, by /= 2) {
+    if (n) {                             // half of the values for each half of the lanes
+      const bool high = lane & by;
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const float keep = lane & 8 ? y[k + 2] : y[k], give = lane & 8 ? y[k] : y[k + 2];
-    z[k] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+      for (int k = 0; k < G / 2; ++k)
+        if (k < n) {
+          const float keep = high ? x[k + n] : x[k], give = high ? x[k] : x[k + n];
+          x[k] = keep + __shfl_xor_sync(0xffffffffu, give, by);
+        }
+      s = x[0];
+    } else {
+      s += __shfl_xor_sync(0xffffffffu, s, by);
+    }
   }
-  const float keep = lane & 4 ? z[1] : z[0], give = lane & 4 ? z[0] : z[1];
-  float s = keep + __shfl_xor_sync(0xffffffffu, give, 4);
-  s += __shfl_xor_sync(0xffffffffu, s, 2);
-  return s + __shfl_xor_sync(0xffffffffu, s, 1);
+  return s;
 }
 
 // A token for a.threads threads, one warp (several tokens a block) or the whole block: the gradient of the sum is read once for up to eight of
 // its rows, whose scalar products with it are summed in a fixed order.  Persistent as above.
-template <typename T, int V, bool TAIL>
-__global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_backward_kernel(const __grid_constant__ RowArgs a) {
-  __shared__ float part[2][8][kGroup];
+template <typename T, int V, bool TAIL, int G>
+constexpr int backward_blocks() { return G == 4 && V * sizeof(T) >= 8 ? 4 : resident_blocks<T, V, TAIL>(); }
+
+template <typename T, int V, bool TAIL, int G>
+__global__ void __launch_bounds__(256, backward_blocks<T, V, TAIL, G>()) combine_backward_kernel(const __grid_constant__ RowArgs a) {
+  __shared__ float part[2][8][G];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, body = a.H / V, pieces = body + a.H % V, step = (int)blockDim.x / a.threads;
   const int64_t stride = (int64_t)gridDim.x * step;
   const int first = threadIdx.x % a.threads;
@@ -542,30 +548,30 @@ __global__ void __launch_bounds__(256, resident_blocks<T, V, TAIL>()) combine_ba
   for (; t < a.n_tokens; t += stride) {
     Picks p = next;
     if (t + stride < a.n_tokens) next.load(a, t + stride, 0, lane);
-    for (int kb = 0; kb < a.K; kb += kGroup) {
+    for (int kb = 0; kb < a.K; kb += G) {
       if (kb && kb % 32 == 0) p.load(a, t, kb, lane);
-      int r[kGroup];
-      float g[kGroup], dot[kGroup];
+      int r[G];
+      float g[G], dot[G];
 #pragma unroll
-      for (int k = 0; k < kGroup; ++k) {
+      for (int k = 0; k < G; ++k) {
         r[k] = p.row_of(a, kb % 32 + k);
         g[k] = p.gate_of(kb % 32 + k);
         dot[k] = 0.f;
       }
       for (int i = first; i < pieces; i += a.threads) {
-        if (!TAIL || i < body) backward_piece<T, V>(a, t, r, g, i * V, dot);
-        else backward_piece<T, 1>(a, t, r, g, body * V + i - body, dot);
+        if (!TAIL || i < body) backward_piece<T, V, G>(a, t, r, g, i * V, dot);
+        else backward_piece<T, 1, G>(a, t, r, g, body * V + i - body, dot);
       }
       if (!a.d_gates) continue;
-      const float s = reduce_eight(dot, lane);
+      const float s = reduce_group<G>(dot, lane);
       float* d_gates = a.d_gates + t * a.K + kb;
       if (a.threads == 32) {
-        if (lane % 4 == 0 && kb + lane / 4 < a.K) d_gates[lane / 4] = s;
+        if (lane % (32 / G) == 0 && kb + lane / (32 / G) < a.K) d_gates[lane / (32 / G)] = s;
         continue;
       }
-      if (lane % 4 == 0) part[turn][warp][lane / 4] = s;
+      if (lane % (32 / G) == 0) part[turn][warp][lane / (32 / G)] = s;
       __syncthreads();                   // (two sets of sums: the next one's writers do not have to wait for these readers)
-      if (threadIdx.x < kGroup && kb + threadIdx.x < a.K) {
+      if (threadIdx.x < G && kb + threadIdx.x < a.K) {
         float sum = 0.f;
         for (int w = 0; w < (int)(blockDim.x >> 5); ++w) sum += part[turn][w][threadIdx.x];
         d_gates[threadIdx.x] = sum;
@@ -608,8 +614,11 @@ cudaError_t launch_rows_as(const RowArgs& args, cudaStream_t stream) {
     return rows::launch<combine_kernel<T, V, TAIL>>(a, std::min<int64_t>(blocks, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
   }
   if constexpr (OP == kCombineBackward) {
-    const int step = a.threads == 32 ? 8 : 1;
-    return rows::launch<combine_backward_kernel<T, V, TAIL>>(a, std::min<int64_t>(((int64_t)a.n_tokens + step - 1) / step, 148 * resident_blocks<T, V, TAIL>()), 1, step * a.threads, 0, stream);
+    const int step = a.threads == 32 ? 8 : 1, threads = step * a.threads;
+    const int64_t blocks = ((int64_t)a.n_tokens + step - 1) / step;
+    if (a.K <= 4)
+      return rows::launch<combine_backward_kernel<T, V, TAIL, 4>>(a, std::min<int64_t>(blocks, 148 * (backward_blocks<T, V, TAIL, 4>() * 256 / threads)), 1, threads, 0, stream);
+    return rows::launch<combine_backward_kernel<T, V, TAIL, 8>>(a, std::min<int64_t>(blocks, 148 * (backward_blocks<T, V, TAIL, 8>() * 256 / threads)), 1, threads, 0, stream);
   }
 }
 
