@@ -671,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     }
     for (int tile = 0; walk.next(g); ++tile) {
       const float4* theirs = reinterpret_cast<const float4*>(smem) + (tid - 128);
-      // columns: kCols each from `from` on, every other such group (kGradBlocks: one half of them)
+      // columns: kCols each from `from` on, every other such group (kGradBlocks: all, of half of the rows)
       const int acc = tile & 1, from = unit * kCols, by = units * kCols;
       const uint32_t col = tmem + lanes + (uint32_t)acc * kTile;
       if (ok) {
