@@ -114,6 +114,13 @@ def test_bad_ffn_backward(kw):
     assert _ffn_backward(**kw) == ARG
 
 
+def test_strides_beyond_a_copy():
+    far = 1 << 38
+    assert _ffn(block_stride=far) == UNSUPPORTED and _ffn_backward(block_stride=far) == UNSUPPORTED
+    assert _ffn_backward(d_block_stride=far) == UNSUPPORTED
+    assert _ffn(xs_stride=far) == ARG and _ffn_backward(d_ys_stride=far) == ARG
+
+
 def test_nothing_to_do_is_fine():
     for call in (_dispatch, _combine, _combine_backward):
         assert call(n_tokens=0) == rb.REMOE_OK

@@ -205,6 +205,19 @@ def test_combine_backward(T, K, N, H, dtype):
         assert torch.equal(ys.view[:used], both[0][:used]) and torch.equal(d_gates, both[1])
 
 
+# More tokens than fit on the card at once: every number of rows a group may have, rows of one and of several parts, whole accesses and ragged ones.
+MANY = [(2000, 1, 8, 64), (1800, 2, 8, 4104), (1500, 3, 9, 2056), (2100, 4, 12, 1028), (900, 5, 12, 1030), (1200, 6, 64, 2048), (800, 7, 16, 520), (700, 8, 16, 2568),
+        (5000, 9, 20, 136), (600, 33, 40, 1032), (1300, 4, 6, 1021)]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("T,K,N,H", MANY)
+def test_rows_of_many_tokens(T, K, N, H, dtype):
+    test_dispatch(T, K, N, H, dtype)
+    test_combine(T, K, N, H, dtype)
+    test_combine_backward(T, K, N, H, dtype)
+
+
 # ---------------------------------------------------------------------------------------------------- the experts' products
 
 class Ffn:
@@ -390,3 +403,28 @@ def test_combine_backward_of_the_most_tokens():
     for s in range(0, MOST, piece):
         at = torch.arange(s, min(s + piece, MOST), device="cuda")
         assert torch.equal(d_gates[s:s + piece], value[at % 6] * (at % 17 - 8))
+
+
+def test_two_streams_at_once():
+    """Calls that share tiles over clusters and calls that do not, next to one another."""
+    calls = [Ffn([40], 2048, 1544, "bf16", seed=4), Ffn([300, 7, 0, 129], 1544, 264, "f16", seed=5), Ffn([3, 1], 4096, 1544, "bf16", seed=6)]
+    want = []
+    for f in calls:
+        f.forward()
+        f.backward()
+        want.append((f.ys.view.clone(), f.d_xs.view.clone(), f.d_blocks.clone()))
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for f in calls:
+            for t in (f.ys.view, f.d_xs.view, f.d_blocks, f.gate_up, f.act, f.work):
+                t.fill_(7.0)
+        torch.cuda.synchronize()
+        for _ in range(8):
+            for f, s in zip(calls, streams):
+                ok(rb.remoe_expert_ffn(f.R, f.N, f.H, f.I, f.code, f.xs.view, f.xs.stride, f.offsets, f.blocks, f.block, f.gate_up, f.act, f.ys.view, f.ys.stride,
+                                       s.cuda_stream))
+                ok(rb.remoe_expert_ffn_backward(f.R, f.N, f.H, f.I, f.code, f.xs.view, f.xs.stride, f.offsets, f.blocks, f.block, f.gate_up, f.d_ys.view,
+                                                f.d_ys.stride, f.work, f.d_xs.view, f.d_xs.stride, f.d_blocks, f.block, s.cuda_stream))
+        torch.cuda.synchronize()
+        for f, w in zip(calls, want):
+            assert all(torch.equal(a, b) for a, b in zip((f.ys.view, f.d_xs.view, f.d_blocks), w))
