@@ -47,7 +47,9 @@ constexpr int kOperandBytes = 128 * 128;                 // a CTA's half of an o
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kThreads = 384;
 constexpr uint32_t kTmemCols = 512;
-constexpr unsigned kPolls = 1u << 18;                    // of a bounded wait
+// Polls of a bounded wait, of 2900 clocks each (measured on a barrier that never completes: 1.5 us, so 0.4 s); and more of them for a wait that may last
+// for whole tiles, by the pieces of 64 k in them: 24 us a piece, which takes 0.3 to 0.8.
+constexpr unsigned kPolls = 1u << 18, kPiecePolls = 16;
 constexpr int kBoxes = 5;
 // Rows of N in one copy: 16, 32, 64, 96, 128.
 __host__ __device__ constexpr int box_rows(int b) { return b == 0 ? 16 : b == 1 ? 32 : 32 * b; }
@@ -430,8 +432,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     begin = min(part * per, g.pieces);
     end = min(begin + per, g.pieces);
   };
-  // for a wait of a whole tile: more polls for more of k
-  auto long_wait = [&]() { return kPolls + (unsigned)min(g.pieces, 1 << 20) * 2048u; };
+  auto polls_for = [](unsigned pieces) { return kPolls + min(pieces, 1u << 27) * kPiecePolls; };
+  auto long_wait = [&]() { return polls_for(g.pieces); };                       // of one tile
 
   if (warp != 0) dependency_wait();                      // (the kernel in front may run for longer than a bounded wait)
   if (warp == 0) {
@@ -576,12 +578,14 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       if (warp == 2) {
         int at = 0;                                      // stage of a tile's first piece
         uint32_t turns = 0;                              // parity of each stage's next landing
+        unsigned passed = 0;                             // pieces of the tiles so far: those with nothing to clear are passed over, and the next wait is for all of them
         bool ok = true;
         while (ok && walk.next(g)) {
           const int s = (at + max(g.pieces, 1) - 1) % kStages, left = g.count - (g.pieces - 1) * kK;
           at = (at + g.pieces) % kStages;
+          passed = min(passed + g.pieces + 1, 1u << 27);
           if (left % 16 == 0) continue;
-          ok = warp_wait(landed + s, (turns >> s) & 1, long_wait());
+          ok = warp_wait(landed + s, (turns >> s) & 1, polls_for(passed));
           if (!ok) break;
           turns ^= 1u << s;
           // a row of the blocks of 64 rows a time, two of M and those of N
