@@ -180,24 +180,26 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
 // A load under a predicate, zero without it: no branch, so that a group's loads are issued one behind the other.  (With an if around each,
-// the compiler finished one row before it asked for the next: 50 instead of 30 us for the sum of 4096 x 6 rows of 2048 bf16.)
+// the compiler finished one row before it asked for the next: 50 instead of 30 us for the sum of 4096 x 6 rows of 2048 bf16.)  It reads memory that the same
+// thread may write afterwards (a gradient over the rows themselves), so it names memory to the compiler, too.
 __device__ __forceinline__ void load_word_if(uint4& w, const void* p, bool yes) {
   w = make_uint4(0, 0, 0, 0);
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
                : "+r"(w.x), "+r"(w.y), "+r"(w.z), "+r"(w.w)
-               : "l"(p), "r"((int)yes));
+               : "l"(p), "r"((int)yes)
+               : "memory");
 }
 __device__ __forceinline__ void load_word_if(uint2& w, const void* p, bool yes) {
   w = make_uint2(0, 0);
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %3, 0;\n\t@p ld.global.v2.u32 {%0, %1}, [%2];\n\t}" : "+r"(w.x), "+r"(w.y) : "l"(p), "r"((int)yes));
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %3, 0;\n\t@p ld.global.v2.u32 {%0, %1}, [%2];\n\t}" : "+r"(w.x), "+r"(w.y) : "l"(p), "r"((int)yes) : "memory");
 }
 __device__ __forceinline__ void load_word_if(unsigned& w, const void* p, bool yes) {
   w = 0;
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(w) : "l"(p), "r"((int)yes));
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u32 %0, [%1];\n\t}" : "+r"(w) : "l"(p), "r"((int)yes) : "memory");
 }
 __device__ __forceinline__ void load_word_if(unsigned short& w, const void* p, bool yes) {
   w = 0;
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+h"(w) : "l"(p), "r"((int)yes));
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u16 %0, [%1];\n\t}" : "+h"(w) : "l"(p), "r"((int)yes) : "memory");
 }
 
 // V consecutive elements of a row as one access.
