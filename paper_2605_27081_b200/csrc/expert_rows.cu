@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kSortWarps * 32) sort_kernel(const __grid_cons
 #pragma unroll
     for (int i = 0; i < kStrips; ++i) {
       const int64_t s = s0 + i * 32 + lane;
-      id[i] = s < end ? __ldg(a.ids + s) : -1;
+      id[i] = s < end ? a.ids[s] : -1;   // (a coherent load: `rows` may be the same memory)
     }
   };
   auto take = [&](int64_t s0) {          // hands out places from the warp's counters
