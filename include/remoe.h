@@ -500,7 +500,8 @@ int remoe_expert_combine_backward(int32_t n_tokens, int32_t top_k, int32_t hidde
  *   blocks      n_experts expert blocks [inter, 3, hidden], block_stride elements apart (>= 3 * inter * hidden)
  *   act         [n_rows, inter]: work space, holds silu(gate) * up of every row afterwards, rounded to dtype, as the second product reads it
  *   gate_up     [2, n_rows, inter] or NULL: the two products, kept for the backward call
- * Strides are multiples of 8 below 2^38, pointers 16-byte aligned.  Values beyond float16's range become infinite, as they do in any float16 tensor.
+ * Strides are multiples of 8 below 2^38 (from there on ARG for those of rows, UNSUPPORTED for those of blocks), n_rows * inter is below 2^38, pointers
+ * are 16-byte aligned.  Values beyond float16's range become infinite, as they do in any float16 tensor.
  * If an internal bounded wait ever runs out, the rows concerned are NaN rather than wrong (here and in the backward call), and the call still returns.
  * Failure-detection tests: with REMOE_FAULT_INJECT=lost_product_copy in the environment at the process's first call of the two, the first of every four
  * calls waits for a copy of an operand that does not come, in each launch, and the third for one of kept gates and ups, both under a short limit.

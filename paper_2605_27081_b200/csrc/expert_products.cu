@@ -1023,7 +1023,7 @@ struct Encoder {
   // `planes` matrices of n rows, `stride` elements apart; boxes of 64 columns and `box_rows` rows of `box_planes` of them
   void matrix(CUtensorMap* m, const void* p, int64_t n, int64_t columns, int64_t stride, int planes, unsigned box_rows, unsigned box_planes = 1) {
     const cuuint64_t dims[3] = {(cuuint64_t)columns, (cuuint64_t)n, (cuuint64_t)planes};
-    const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)(n * stride) * 2};
+    const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)(planes > 1 ? n * stride : stride) * 2};       // (of one plane any that a map takes)
     const cuuint32_t box[3] = {64, box_rows, box_planes};
     encode(m, p, 3, dims, strides, box);
   }

@@ -25,3 +25,18 @@ def test_sort_in_place_of_lists_that_start_anywhere(T, K, N):
         assert torch.equal(mine, want) and torch.equal(again, offsets)
         assert bool((flat[:offset] == -9).all()) and bool((flat[offset + T * K:] == -9).all())
     assert torch.equal(want.cpu(), ref.sort(ids, N)[0])
+
+
+@pytest.mark.parametrize("n_rows", [2, 3, 1 << 20])
+def test_strides_up_to_the_limit(n_rows):
+    """Rows as far apart as the header allows; no expert has any, so that none is touched."""
+    far, H, I, N = (1 << 38) - 8, 64, 24, 3
+    new = lambda *s: torch.full(s, 7.0, dtype=torch.bfloat16, device="cuda")
+    xs, ys, d_ys, d_xs, blocks, d_blocks = new(1, H), new(1, H), new(1, H), new(1, H), new(N, I, 3, H), new(N, I, 3, H)
+    act, gate_up, work = new(n_rows, I), new(2, n_rows, I), new(3, n_rows, I)
+    offsets = torch.zeros(N + 1, dtype=torch.int32, device="cuda")
+    ok(rb.remoe_expert_ffn(n_rows, N, H, I, rb.REMOE_BF16, xs, far, offsets, blocks, 3 * I * H, gate_up, act, ys, far, stream()))
+    ok(rb.remoe_expert_ffn_backward(n_rows, N, H, I, rb.REMOE_BF16, xs, far, offsets, blocks, 3 * I * H, gate_up, d_ys, far, work, d_xs, far, d_blocks, 3 * I * H,
+                                    stream()))
+    torch.cuda.synchronize()
+    assert not d_blocks.any() and all(bool((t == 7).all()) for t in (ys, d_xs, act, gate_up, work))
