@@ -237,7 +237,11 @@ template <> __device__ __forceinline__ float2 unpack<__nv_bfloat16>(uint32_t v) 
 }
 template <> __device__ __forceinline__ float2 unpack<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+// From exp(-|x|), so that the divisor stays between 1 and 2: the fast division gives 0 for one above 2^126, which silu(x) u of x < -87.3 is not for a large u.
+__device__ __forceinline__ float sigmoid(float x) {
+  const float e = __expf(-fabsf(x)), r = __fdividef(1.f, 1.f + e);
+  return x < 0.f ? e * r : r;                            // (NaN: e and r are, too)
+}
 
 // One tile of a pair.
 struct Tile {
