@@ -447,7 +447,7 @@ int remoe_distill_topk_backward(int32_t n_rows, int32_t vocab, int32_t dtype, co
  *   - Matrices have rows `..._stride` elements apart (>= their width); what lies between rows, and rows that belong to no
  *     selection, are left as they were, and what they hold does not matter.  A matrix or list without rows may be NULL.  Outputs do not overlap inputs or one another but where it is said.
  *   - Sums are float32, rounded once where they are stored.  NaN and infinities of a row reach what that row takes part in and nothing else.
- *   Errors: ARG (null or misaligned pointers, sizes, strides, unknown types, host memory), UNSUPPORTED (FP8 or 4-bit rows, sizes beyond the limits
+ *   Errors: ARG (null or misaligned pointers, sizes, strides, unknown types, host memory for any buffer that the call uses), UNSUPPORTED (FP8 or 4-bit rows, sizes beyond the limits
  *   given), CUDA.
  */
 #define REMOE_SORT_MAX_EXPERTS 1024

@@ -973,16 +973,7 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
 
 cudaError_t encoder(EncodeTiledFn* out) {
   static std::atomic<void*> known{nullptr};
-  void* fn = known.load(std::memory_order_acquire);
-  if (!fn) {
-    cudaDriverEntryPointQueryResult found;
-    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
-    if (e != cudaSuccess) return e;
-    if (!fn) return cudaErrorNotSupported;
-    known.store(fn, std::memory_order_release);
-  }
-  *out = reinterpret_cast<EncodeTiledFn>(fn);
-  return cudaSuccess;
+  return sorted::driver_entry("cuTensorMapEncodeTiled", &known, out);
 }
 
 struct FfnCall {
@@ -1202,6 +1193,7 @@ extern "C" int remoe_expert_ffn(int32_t n_rows, int32_t n_experts, int32_t hidde
   if (n_rows == 1) xs_stride = ys_stride = hidden;
   rows::PointerDevice device(blocks_dev);
   if (device.err_code()) return device.err_code();
+  if (const int host = sorted::check_device_memory({xs_dev, offsets_dev, gate_up_dev, act_dev, ys_dev})) return host;
   Encoder enc{nullptr, dtype == REMOE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, true};
   if (encoder(&enc.fn) != cudaSuccess) return REMOE_E_CUDA;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
@@ -1230,6 +1222,9 @@ extern "C" int remoe_expert_ffn_backward(int32_t n_rows, int32_t n_experts, int3
   if (n_rows == 1) xs_stride = d_ys_stride = d_xs_stride = hidden;
   rows::PointerDevice device(blocks_dev);
   if (device.err_code()) return device.err_code();
+  if (const int host = n_rows > 0 ? sorted::check_device_memory({offsets_dev, d_blocks_dev, d_blocks_dev ? xs_dev : nullptr, gate_up_dev, d_ys_dev, work_dev, d_xs_dev})
+                                  : sorted::check_device_memory({offsets_dev, d_blocks_dev}))
+    return host;
   Encoder enc{nullptr, dtype == REMOE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, true};
   if (encoder(&enc.fn) != cudaSuccess) return REMOE_E_CUDA;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);

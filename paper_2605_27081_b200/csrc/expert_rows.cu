@@ -691,6 +691,7 @@ extern "C" int remoe_expert_sort(int32_t n_tokens, int32_t top_k, int32_t n_expe
   if (n_experts > REMOE_SORT_MAX_EXPERTS || (int64_t)n_tokens * top_k > 0x7fffffff) return REMOE_E_UNSUPPORTED;
   rows::PointerDevice device(offsets_dev);
   if (device.err_code()) return device.err_code();
+  if (const int host = n_tokens > 0 ? sorted::check_device_memory({ids_dev, rows_dev}) : REMOE_OK) return host;
   SortArgs a{ids_dev, rows_dev, offsets_dev, n_tokens * top_k, n_experts, 0};
   const int strips = (int)(((int64_t)a.n + 31) / 32);
   int blocks = 1;
@@ -715,6 +716,7 @@ extern "C" int remoe_expert_dispatch(int32_t n_tokens, int32_t top_k, int32_t hi
   if (n_tokens == 0 || n_rows == 0) return REMOE_OK;
   rows::PointerDevice device(x_dev);
   if (device.err_code()) return device.err_code();
+  if (const int host = sorted::check_device_memory({rows_dev, xs_dev})) return host;
   const RowArgs a{x_dev, x_stride, nullptr, 0, xs_dev, xs_stride, rows_dev, nullptr, nullptr, top_k, hidden, n_rows, n_tokens, 0, 0};
   const int width = std::min(sorted::access_width(x_dev, x_stride, n_tokens, size), sorted::access_width(xs_dev, xs_stride, n_rows, size));
   return launch_rows<kDispatch>(a, dtype, width, static_cast<cudaStream_t>(cuda_stream));
@@ -734,6 +736,7 @@ extern "C" int remoe_expert_combine(int32_t n_tokens, int32_t top_k, int32_t hid
   if (n_tokens == 0) return REMOE_OK;
   rows::PointerDevice device(out_dev);
   if (device.err_code()) return device.err_code();
+  if (const int host = sorted::check_device_memory({n_rows > 0 ? ys_dev : nullptr, rows_dev, gates_dev, base_dev == out_dev ? nullptr : base_dev})) return host;
   const RowArgs a{ys_dev, ys_stride, base_dev, base_stride, out_dev, out_stride, rows_dev, gates_dev, nullptr, top_k, hidden, n_rows, n_tokens, 0, 0};
   int width = std::min(sorted::access_width(ys_dev, ys_stride, n_rows, size), sorted::access_width(out_dev, out_stride, n_tokens, size));
   if (base_dev) width = std::min(width, sorted::access_width(base_dev, base_stride, n_tokens, size));
@@ -756,6 +759,7 @@ extern "C" int remoe_expert_combine_backward(int32_t n_tokens, int32_t top_k, in
   if (n_tokens == 0) return REMOE_OK;
   rows::PointerDevice device(d_out_dev);
   if (device.err_code()) return device.err_code();
+  if (const int host = sorted::check_device_memory({n_rows > 0 && d_gates_dev ? ys_dev : nullptr, rows_dev, gates_dev, n_rows > 0 ? d_ys_dev : nullptr, d_gates_dev})) return host;
   const RowArgs a{ys_dev, ys_stride, d_out_dev, d_out_stride, d_ys_dev, d_ys_stride, rows_dev, gates_dev, d_gates_dev, top_k, hidden, n_rows, n_tokens, 0, 0};
   int width = sorted::access_width(d_out_dev, d_out_stride, n_tokens, size);
   if (d_gates_dev) width = std::min(width, sorted::access_width(ys_dev, ys_stride, n_rows, size));
