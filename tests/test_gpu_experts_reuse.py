@@ -4,7 +4,8 @@ import torch
 
 from paper_2605_27081_b200 import binding as rb
 import expert_ref as ref
-from test_gpu_experts import ok, route, run_sort, stream
+from test_gpu_experts import NAN, ok, route, run_sort, stream
+from test_gpu_experts_layer import Layer
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +41,70 @@ def test_strides_up_to_the_limit(n_rows):
                                     stream()))
     torch.cuda.synchronize()
     assert not d_blocks.any() and all(bool((t == 7).all()) for t in (ys, d_xs, act, gate_up, work))
+
+
+def poison(m):
+    """Whatever a layer's calls write: NaN in matrices, -7 in lists."""
+    for t in (m.ln_gates, m.d_gates, m.xs, m.ys, m.d_ys, m.d_xs, m.act, m.gate_up, m.work, m.out, m.d_x, m.d_blocks):
+        t.fill_(NAN)
+    for t in (m.ids, m.rows, m.offsets):
+        t.fill_(-7)
+
+
+def results(m):
+    return m.outputs() + [t.clone() for t in (m.ids, m.rows, m.offsets, m.ln_gates)]
+
+
+def test_two_streams_at_once_over_overwritten_buffers():
+    layers = [Layer(500, 6, 20, 512, 264, seed=3, skew=1.0), Layer(300, 2, 3, 1024, 136, "f16", seed=4, drop=0.1)]
+    want = []
+    for m in layers:
+        m.run(), m.back()
+        torch.cuda.synchronize()
+        want.append(results(m))
+        assert not any(bool(torch.isnan(t).any()) for t in want[-1])
+    streams = [torch.cuda.Stream() for _ in layers]
+    for _ in range(5):
+        for m in layers:
+            poison(m)
+        torch.cuda.synchronize()
+        for m, s in zip(layers, streams):
+            with torch.cuda.stream(s):
+                m.run(), m.back()
+        torch.cuda.synchronize()
+        for m, w in zip(layers, want):
+            assert all(torch.equal(a, b) for a, b in zip(results(m), w))
+
+
+def test_two_graphs_at_once_over_overwritten_buffers():
+    layers = [Layer(200, 4, 12, 256, 136, seed=1), Layer(90, 2, 5, 328, 72, "f16", seed=2, drop=0.2)]
+    graphs, gates = [], []
+    for m in layers:
+        m.run(), m.back()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            m.run(), m.back()
+        graphs.append(g)
+        gates.append(m.gates)                            # the graph's own
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for seed in (7, 8):
+        want = []
+        for m in layers:
+            g = torch.Generator(device="cuda").manual_seed(seed)
+            for t in (m.x, m.base, m.d_out, m.logits):
+                t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+            m.run(), m.back()
+            torch.cuda.synchronize()
+            want.append(results(m))
+        for _ in range(3):
+            for m, g in zip(layers, gates):
+                poison(m)
+                g.fill_(NAN)
+            torch.cuda.synchronize()
+            for g, s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+            torch.cuda.synchronize()
+            for m, w in zip(layers, want):
+                assert all(torch.equal(a, b) for a, b in zip(results(m), w))
