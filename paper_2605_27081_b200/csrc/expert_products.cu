@@ -93,7 +93,7 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 }
 // One lane of a converged warp.  The roles that issue copies and products run with whole warps and take a lane only around the instructions
 // themselves: their operands then lie in uniform registers, as the instructions want them.  (With the loop itself in one lane an
-// MMA took 67 cycles to issue and a commit 150, more than the 512 that a stage's products run for.)
+// MMA took 67 cycles to issue and a commit 150: for a stage of 128 k, as it was then, more than the 512 that its eight products run for.)
 __device__ __forceinline__ bool elect_one() {
   uint32_t yes;
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
@@ -826,7 +826,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             epilogue_bar(group);
           };
           if constexpr (MODE == kGateUp) {
-            // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.
+            // rows of M are eight gates, then the ups of the same channels: a thread holds both.  Output rows of 64 channels, 128 bytes.  act is rounded
+            // to 16 bits here, since the next product takes such operands (as d g, d u and a are below): one rounding more than the formula's own.
             uint32_t act[4];                             // two groups of columns x two of channels
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
