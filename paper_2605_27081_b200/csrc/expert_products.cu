@@ -1013,8 +1013,13 @@ struct Encoder {
   bool ok;
   void encode(CUtensorMap* m, const void* p, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
     const cuuint32_t step[5] = {1, 1, 1, 1, 1};
-    ok = ok && fn(m, type, rank, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    auto encoded = [&] {
+      return fn(m, type, rank, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    // A thread that has made no call of the runtime's that needs a context has none, and the driver then refuses the first map.
+    int device;
+    ok = ok && (encoded() || (cudaGetDevice(&device) == cudaSuccess && cudaSetDevice(device) == cudaSuccess && encoded()));
   }
   // `planes` matrices of n rows, `stride` elements apart; boxes of 64 columns and `box_rows` rows of `box_planes` of them
   void matrix(CUtensorMap* m, const void* p, int64_t n, int64_t columns, int64_t stride, int planes, unsigned box_rows, unsigned box_planes = 1) {

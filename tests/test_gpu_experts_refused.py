@@ -47,3 +47,19 @@ def test_buffers_that_a_call_does_not_look_at_may_be_anything():
     ok(rb.remoe_expert_ffn_backward(2, 1, 8, 8, BF16, host, 8, d(), d(), 192, d(), d(), 8, d(), d(), 8, None, 0, stream()))
     torch.cuda.synchronize()
     assert not host.any()
+
+
+@pytest.mark.parametrize("name", ["sort", "dispatch", "combine", "combine_backward", "ffn", "ffn_backward"])
+def test_calls_from_a_thread_that_has_not_used_the_gpu(name):
+    import threading
+    call, args, buffers = calls(lambda: torch.zeros(4096, dtype=torch.int32, device="cuda"))[name]
+    host = torch.zeros(4096, dtype=torch.int32).pin_memory()
+    places = [args] + [args[:i] + [host] + args[i + 1:] for i in buffers]
+    torch.cuda.synchronize()
+    got = []
+    for a in places:                                     # a thread for each: the first call that it makes
+        t = threading.Thread(target=lambda: got.append(call(*a, None)))
+        t.start()
+        t.join()
+    torch.cuda.synchronize()
+    assert got == [0] + [rb.REMOE_E_ARG] * len(buffers)
